@@ -324,6 +324,79 @@ int s24_mask_flips(const uint16_t *mask_new, const uint16_t *mask_old, int64_t n
  * fp64 rounding. */
 int s24_l1_norm_gap(const void *W, s24_dtype dt, int64_t r, int64_t q, int64_t ldw, double *gap, void *stream);
 
+/* ---- Attention: the other half of a transformer layer, in training, in reading prompts and in sampling ----
+ *
+ * hq query heads share hkv key-value heads (hq a multiple of hkv): head h reads key-value head h / (hq / hkv).  Sequences are packed one
+ * after the other, without padding: sequence i has the query rows cu_q[i] .. cu_q[i+1] - 1 and the key rows cu_k[i] .. cu_k[i+1] - 1, in
+ * arrays of sequences + 1 offsets that ascend from 0, on the DEVICE (offsets that do not are cut to what lies in the operands; rows of no
+ * sequence are left as they are).  With lq queries and lk keys, query i sees the keys j < lk, and if `causal` of these j <= i + lk - lq: the
+ * queries are the last ones of the keys (a prompt that is read in chunks; lq = lk in training).  A query that sees none gives a row of zeros.
+ * S24_BF16 and S24_F16; S24_F32 returns S24_ERR_UNSUPPORTED.  Scores, row statistics and sums are fp32; the weights P and, backward, dS
+ * are rounded to the storage type as operands of the second products.  Nothing is added in an order that depends on scheduling. */
+
+/* Rows of heads: element (t, h, i) of token t, head h at data + t*token + h*head + i (strides in elements), so that the parts of one
+ * projection's result [tokens][(hq + 2 hkv) d] or of [heads][tokens][d] buffers are taken as they lie.  data 16-byte aligned, both strides
+ * multiples of 8 (S24_ERR_ALIGN), token below 2^23; rows that are written must not overlap (S24_ERR_SHAPE). */
+typedef struct {
+    void *data;
+    int64_t token, head;
+} s24_heads;
+
+/* d: values of a head, a multiple of 16 up to 128 (beyond: S24_ERR_UNSUPPORTED); below 64 and between 64 and 128 it costs what 64 and 128 do.
+ * scale: the factor c > 0 of the scores, 1 / sqrt(d) as a rule. */
+typedef struct {
+    const int32_t *cu_q, *cu_k;   /* device, may be one array */
+    int64_t sequences, tokens_q, tokens_k;
+    int64_t hq, hkv, d;
+    float scale;
+    int causal;
+} s24_attn_shape;
+
+/* O_i = sum_j P_ij v_j, P_ij = exp(c q_i.k_j - lse_i), lse_i = log sum_j exp(c q_i.k_j) over the keys j that query i sees.
+ *   lse [hq][tokens_q] fp32, out, may be NULL (s24_attn_bwd reads it); minus infinity for a query that sees no key */
+int s24_attn_fwd(const s24_attn_shape *shape, const s24_heads *Q, const s24_heads *K, const s24_heads *V, const s24_heads *O, float *lse,
+                 s24_dtype dt, void *stream);
+
+/* Gradients of s24_attn_fwd from its O and lse: with delta_i = dO_i.O_i and dS_ij = P_ij (dO_i.v_j - delta_i),
+ * dQ_i = c sum_j dS_ij k_j,  dK_j = c sum_i dS_ij q_i,  dV_j = sum_i P_ij dO_i, the last two also over the query heads of a
+ * key-value head.  All of dQ, dK, dV is written (zeros where nothing is seen).
+ *   workspace  device, s24_attn_bwd_workspace(shape) bytes, 16-byte aligned; holds nothing between calls */
+int64_t s24_attn_bwd_workspace(const s24_attn_shape *shape);
+int s24_attn_bwd(const s24_attn_shape *shape, const s24_heads *Q, const s24_heads *K, const s24_heads *V, const s24_heads *O, const s24_heads *dO,
+                 const float *lse, const s24_heads *dQ, const s24_heads *dK, const s24_heads *dV, void *workspace, s24_dtype dt, void *stream);
+
+/* Key-value cache in pages of `page` tokens (a power of two from 16 to 65536), hkv heads of d values (a multiple of 16 up to 128).
+ *   bits = 16   K, V  [pages][hkv][page][d] values of the calls' dtype; k_step, v_step not used
+ *   bits = 8    K, V  [pages][hkv][page][d] bytes and k_step, v_step [pages][hkv][page] fp32:  a token's head is s*n with
+ *               s = max(max|x| / 127, 2^-126) rounded to fp32 and n the whole numbers nearest to x / s, ties to even
+ * (The order of the values within a page of V and the form of a byte are the library's own; a page of a head is moved or shared as a whole.)
+ * K, V, k_step, v_step are device memory of the caller, 16-byte aligned.  Sequence i has its positions j in page
+ * table[i][j / page], table [sequences][width] on the device (page numbers that the cache does not have are cut to its last one).
+ * What a page holds past a sequence's end is read by no result. */
+typedef struct {
+    void *K, *V;
+    float *k_step, *v_step;
+    int64_t pages, page, hkv, d;
+    int bits;
+} s24_kv_cache;
+
+/* Writes tokens to the cache: row t of K and V to place places[t] = page number * page + position in the page (device; a negative place, or one
+ * past the cache, is skipped: padding).  Places must differ. */
+int s24_kv_write(const s24_kv_cache *cache, const s24_heads *K, const s24_heads *V, const int64_t *places, int64_t tokens, s24_dtype dt, void *stream);
+
+/* Reads sequences back, packed as s24_attn_fwd takes them: position j of sequence i to row cu[i] + j of K and V, for the cu[i+1] - cu[i]
+ * positions that it has (those beyond width*page are left as they are).  8 bits: s*n rounded to dt. */
+int s24_kv_read(const s24_kv_cache *cache, const int32_t *table, int64_t width, const int32_t *cu, int64_t sequences, int64_t tokens,
+                const s24_heads *K, const s24_heads *V, s24_dtype dt, void *stream);
+
+/* Attention of one new token of each sequence: O[i] = softmax(c Q[i].K) V over the first lengths[i] (device) positions of sequence i, of all of
+ * them, its own included; Q and O have one row a sequence.  Zeros where lengths[i] is 0; lengths beyond width*page are cut.  In an 8-bit cache
+ * the products are binary16, of the whole numbers as they are, of the queries scaled by a power of two, and of the weights times the steps of V.
+ *   workspace  device, s24_attn_decode_workspace(cache, sequences, hq) bytes, 16-byte aligned; holds nothing between calls */
+int64_t s24_attn_decode_workspace(const s24_kv_cache *cache, int64_t sequences, int64_t hq);
+int s24_attn_decode(const s24_kv_cache *cache, const s24_heads *Q, int64_t hq, const int32_t *table, int64_t width, const int32_t *lengths,
+                    int64_t sequences, float scale, const s24_heads *O, void *workspace, int64_t workspace_bytes, s24_dtype dt, void *stream);
+
 /* Instrumentation, not part of the method: registers a DEVICE buffer of two uint64 (8-byte aligned), or
  * NULL to switch the probe off (the default).  While a buffer is registered, workgroup 0 of every
  * large-tile 16-bit GEMM launched by s24_spmm_fwd / s24_spmm_bwd_dx / s24_dense_dw / s24_dense_gemm

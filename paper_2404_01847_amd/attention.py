@@ -1,0 +1,77 @@
+"""Host-side sequencing of the attention calls: the half of a transformer layer that stands beside SparseFFN.
+
+Only call ordering and buffer ownership live here; every arithmetic step is a libs24 kernel.  In training, Attention owns what one layer keeps
+between its passes.  In sampling, PagedKV holds the keys and values of the sequences that are being sampled, in 16 or 8 bits: the tokens of a
+prompt are written to it as they come, each new token attends over it, and whole sequences are read back where the next chunk of a
+prompt attends to the earlier ones.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import binding as s24
+
+
+class Attention:
+    """Buffers and call sequence of one attention layer: hq query heads on hkv key-value heads of d values, up to tokens_q query rows
+    (tokens_k key rows; None: as many) of packed sequences.  dtype: torch.bfloat16 or torch.float16."""
+
+    def __init__(self, hq: int, hkv: int, d: int, tokens_q: int, tokens_k: int | None = None, dtype=torch.bfloat16, device="cuda", causal: bool = True,
+                 scale: float | None = None):
+        self.hq, self.hkv, self.d, self.tokens_q = hq, hkv, d, tokens_q
+        self.tokens_k = tokens_q if tokens_k is None else tokens_k
+        self.causal, self.scale = causal, scale
+        self.dtype, self.device = dtype, device
+        self.O = torch.empty((tokens_q, hq, d), dtype=dtype, device=device)
+        self.lse = torch.empty((hq, tokens_q), dtype=torch.float32, device=device)
+        self.dQ = self.dK = self.dV = self.work = None   # allocated by the first backward pass
+
+    def forward(self, Q, K, V, cu_q, cu_k=None):
+        """O [tokens_q, hq, d].  Q, K, V may be views of one projection's result; cu_q, cu_k: int32 offsets of the sequences."""
+        return s24.attn_fwd(Q, K, V, self.O, self.lse, cu_q, cu_k, self.causal, self.scale)
+
+    def backward(self, Q, K, V, dO, cu_q, cu_k=None):
+        """dQ, dK, dV of the last forward pass, whose operands are given again."""
+        need = s24.attn_bwd_workspace(self.tokens_q, self.tokens_k, self.hq, self.hkv, self.d, cu_q.shape[0] - 1)
+        if self.dQ is None:
+            # the layout of the projection's gradient: dQ, dK and dV are its parts
+            if self.tokens_q == self.tokens_k:
+                self.dQKV = torch.empty((self.tokens_q, self.hq + 2 * self.hkv, self.d), dtype=self.dtype, device=self.device)
+                self.dQ, self.dK, self.dV = self.dQKV[:, :self.hq], self.dQKV[:, self.hq:self.hq + self.hkv], self.dQKV[:, self.hq + self.hkv:]
+            else:
+                self.dQKV = None
+                self.dQ = torch.empty((self.tokens_q, self.hq, self.d), dtype=self.dtype, device=self.device)
+                self.dK, self.dV = (torch.empty((self.tokens_k, self.hkv, self.d), dtype=self.dtype, device=self.device) for _ in range(2))
+        if self.work is None or self.work.numel() < need:
+            self.work = torch.empty(need, dtype=torch.uint8, device=self.device)
+        return s24.attn_bwd(Q, K, V, self.O, dO, self.lse, self.dQ, self.dK, self.dV, self.work, cu_q, cu_k, self.causal, self.scale)
+
+
+class PagedKV:
+    """Keys and values of many sequences in pages of `page` tokens, in 16 bits (the values as they are) or 8 (whole numbers and a step for each token
+    and head).  Which page belongs to whom is the caller's: a table [sequences, pages of the longest] of page numbers."""
+
+    def __init__(self, pages: int, page: int, hkv: int, d: int, dtype=torch.bfloat16, bits: int = 16, device="cuda"):
+        if bits not in (16, 8):
+            raise ValueError(f"a cache of 16 or 8 bits, not {bits}")
+        self.pages, self.page, self.hkv, self.d, self.dtype, self.bits = pages, page, hkv, d, dtype, bits
+        shape = (pages, hkv, page, d)
+        self.K, self.V = (torch.empty(shape, dtype=dtype if bits == 16 else torch.uint8, device=device) for _ in range(2))
+        self.k_step, self.v_step = (torch.empty(shape[:3], dtype=torch.float32, device=device) if bits == 8 else None for _ in range(2))
+        self.work = {}
+
+    def write(self, K, V, places):
+        """Rows of K and V [tokens, hkv, d] to their places: page number * page + position in the page (int64; negative ones are skipped)."""
+        s24.kv_write(self, K, V, places)
+
+    def read(self, table, cu, K, V):
+        """The sequences, one after the other from the offsets cu on, into K and V [tokens, hkv, d]: as Attention.forward takes them."""
+        return s24.kv_read(self, table, cu, K, V)
+
+    def attend(self, Q, table, lengths, O, scale=None):
+        """O [sequences, hq, d]: attention of one new token of each sequence over its first lengths[i] positions."""
+        key = (Q.shape[0], Q.shape[1], torch.cuda.current_stream().cuda_stream)
+        work = self.work.get(key)
+        if work is None:   # one for each stream: calls on two streams may run at the same time
+            work = self.work[key] = torch.empty(s24.attn_decode_workspace(self, Q.shape[0], Q.shape[1]), dtype=torch.uint8, device=self.K.device)
+        return s24.attn_decode(self, Q, table, lengths, O, work, scale)

@@ -60,6 +60,13 @@ _SIGNATURES = {
     "s24_probe_matrix_rate": (_int, [_int, _int, _int, _vp, _vp]),
     "s24_probe_copy": (_int, [_vp, _vp, _i64, _vp]),
     "s24_probe_reciprocal": (_int, [C.c_uint32, _i64, _vp, _vp]),
+    "s24_attn_fwd": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _int, _vp]),
+    "s24_attn_bwd_workspace": (_i64, [_vp]),
+    "s24_attn_bwd": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _int, _vp]),
+    "s24_kv_write": (_int, [_vp, _vp, _vp, _vp, _i64, _int, _vp]),
+    "s24_kv_read": (_int, [_vp, _vp, _i64, _vp, _i64, _i64, _vp, _vp, _int, _vp]),
+    "s24_attn_decode_workspace": (_i64, [_vp, _i64, _i64]),
+    "s24_attn_decode": (_int, [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _f32, _vp, _vp, _i64, _int, _vp]),
 }
 EXPORTS = tuple(_SIGNATURES)
 
@@ -174,7 +181,7 @@ class _CompressProblem(C.Structure):
 def _packer(cls):
     """Packs a structure's fields into bytes.  (A ctypes structure takes a microsecond to fill, three times as long, and a step of a few hundred
     tokens waits for the host: 37.7 -> 33.4 us of it at 256 x 768 x 3072.)"""
-    form = "@" + "".join({_vp: "P", _i64: "q", _f32: "f"}[t] for _, t in cls._fields_)
+    form = "@" + "".join({_vp: "P", _i64: "q", _f32: "f", _int: "i"}[t] for _, t in cls._fields_)
     return struct.Struct(f"{form}{C.sizeof(cls) - struct.calcsize(form)}x").pack
 
 
@@ -459,6 +466,147 @@ def l1_norm_gap(W, gap):
     r, q = W.shape
     _check(lib().s24_l1_norm_gap(_ptr(W), _dt(W), r, q, W.stride(0), _ptr(gap), _stream()), "s24_l1_norm_gap")
     return gap
+
+
+class _Heads(C.Structure):
+    _fields_ = [("data", _vp), ("token", _i64), ("head", _i64)]
+
+
+class _AttnShape(C.Structure):
+    _fields_ = [("cu_q", _vp), ("cu_k", _vp), ("sequences", _i64), ("tokens_q", _i64), ("tokens_k", _i64), ("hq", _i64), ("hkv", _i64), ("d", _i64),
+                ("scale", _f32), ("causal", _int)]
+
+
+class _KVCache(C.Structure):
+    _fields_ = [("K", _vp), ("V", _vp), ("k_step", _vp), ("v_step", _vp), ("pages", _i64), ("page", _i64), ("hkv", _i64), ("d", _i64), ("bits", _int)]
+
+
+_pack_heads, _pack_shape, _pack_cache = _packer(_Heads), _packer(_AttnShape), _packer(_KVCache)
+
+
+def _heads(where, name, x, tokens, heads, d, dtype):
+    """[tokens, heads, d] with any strides along the first two axes."""
+    if tuple(x.shape) != (tokens, heads, d):
+        raise ValueError(f"{where}: {name} must have shape {(tokens, heads, d)}, got {tuple(x.shape)}")
+    if x.dtype is not dtype:
+        raise ValueError(f"{where}: {name} must be {dtype} like the others, got {x.dtype}")
+    token, head, unit = x.stride()
+    if unit != 1:
+        raise ValueError(f"{where}: {name} needs unit stride along its last axis (strides {x.stride()})")
+    return _pack_heads(x.data_ptr(), token if tokens > 1 else 0, head if heads > 1 else 0)
+
+
+def _whole(where, name, x, dtype, *shape):
+    """A contiguous tensor of whole numbers (offsets, lengths, places, tables) or statistics; None in the shape: any size."""
+    if x.dtype is not dtype or not x.is_contiguous() or x.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, x.shape)):
+        raise ValueError(f"{where}: {name} must be a contiguous {dtype} tensor of shape {shape}, got {x.dtype} {tuple(x.shape)}, strides {x.stride()}")
+    return x.data_ptr()
+
+
+def _one_device(where, first, *others):
+    for x in others:
+        if x is not None and x.device != first.device:
+            raise ValueError(f"{where}: the tensors lie on {first.device} and on {x.device}")
+
+
+def _attn_shape(where, Q, K, cu_q, cu_k, causal, scale):
+    if Q.dim() != 3 or K.dim() != 3:
+        raise ValueError(f"{where}: Q and K must have shape [tokens, heads, d], got {tuple(Q.shape)} and {tuple(K.shape)}")
+    tokens_q, hq, d = Q.shape
+    tokens_k, hkv, _ = K.shape
+    cu_k = cu_q if cu_k is None else cu_k
+    pq, pk = _whole(where, "cu_q", cu_q, torch.int32, None), _whole(where, "cu_k", cu_k, torch.int32, cu_q.shape[0])
+    if cu_q.shape[0] == 0:
+        raise ValueError(f"{where}: cu_q needs an offset for each sequence and one more")
+    return _pack_shape(pq, pk, cu_q.shape[0] - 1, tokens_q, tokens_k, hq, hkv, d, d ** -0.5 if scale is None else scale, int(bool(causal)))
+
+
+def attn_fwd(Q, K, V, O, lse, cu_q, cu_k=None, causal=True, scale=None):
+    """Attention over packed sequences.  Q, O [tokens_q, hq, d], K, V [tokens_k, hkv, d], with any strides along the first two axes; lse [hq, tokens_q]
+    float32 or None; cu_q, cu_k: int32 offsets of the sequences (cu_k None: those of the queries); scale None: 1 / sqrt(d)."""
+    where = "s24_attn_fwd"
+    shape = _attn_shape(where, Q, K, cu_q, cu_k, causal, scale)
+    (tq, hq, d), (tk, hkv, _), dtype = Q.shape, K.shape, Q.dtype
+    _one_device(where, Q, K, V, O, lse, cu_q, cu_k)
+    _check(lib().s24_attn_fwd(shape, _heads(where, "Q", Q, tq, hq, d, dtype), _heads(where, "K", K, tk, hkv, d, dtype),
+                              _heads(where, "V", V, tk, hkv, d, dtype), _heads(where, "O", O, tq, hq, d, dtype),
+                              None if lse is None else _whole(where, "lse", lse, torch.float32, hq, tq), _dt(Q), _stream()), where)
+    return O
+
+
+def attn_bwd_workspace(tokens_q, tokens_k, hq, hkv, d, sequences):
+    """Bytes of workspace that attn_bwd needs for so many tokens, heads and sequences."""
+    return lib().s24_attn_bwd_workspace(_pack_shape(0, 0, sequences, tokens_q, tokens_k, hq, hkv, d, 1.0, 1))
+
+
+def attn_bwd(Q, K, V, O, dO, lse, dQ, dK, dV, workspace, cu_q, cu_k=None, causal=True, scale=None):
+    """Gradients dQ, dK, dV of attn_fwd, from its O and lse; workspace: a uint8 tensor of attn_bwd_workspace(...) bytes."""
+    where = "s24_attn_bwd"
+    shape = _attn_shape(where, Q, K, cu_q, cu_k, causal, scale)
+    (tq, hq, d), (tk, hkv, _), dtype = Q.shape, K.shape, Q.dtype
+    _one_device(where, Q, K, V, O, dO, lse, dQ, dK, dV, workspace, cu_q, cu_k)
+    q = [_heads(where, n, x, tq, hq, d, dtype) for n, x in (("Q", Q), ("O", O), ("dO", dO), ("dQ", dQ))]
+    k = [_heads(where, n, x, tk, hkv, d, dtype) for n, x in (("K", K), ("V", V), ("dK", dK), ("dV", dV))]
+    need = lib().s24_attn_bwd_workspace(shape)
+    work = _whole(where, "workspace", workspace, torch.uint8, None)
+    if workspace.numel() < need:
+        raise ValueError(f"{where}: workspace needs {need} bytes, has {workspace.numel()}")
+    _check(lib().s24_attn_bwd(shape, q[0], k[0], k[1], q[1], q[2], _whole(where, "lse", lse, torch.float32, hq, tq), q[3], k[2], k[3], work, _dt(Q),
+                              _stream()), where)
+    return dQ, dK, dV
+
+
+def _kv_cache(where, cache):
+    """cache: an object with the buffers and sizes of a cache (attention.PagedKV)."""
+    K, V, bits = cache.K, cache.V, cache.bits
+    steps = (cache.k_step, cache.v_step) if bits == 8 else ()
+    _dense(where, "K V k_step v_step", K, V, *steps)
+    if K.shape != (cache.pages, cache.hkv, cache.page, cache.d) or V.shape != K.shape or any(s.shape != K.shape[:3] for s in steps):
+        raise ValueError(f"{where}: the cache's buffers must have shape {(cache.pages, cache.hkv, cache.page, cache.d)}")
+    if K.dtype is not V.dtype or K.dtype is not (torch.uint8 if bits == 8 else cache.dtype) or any(s.dtype is not torch.float32 for s in steps):
+        raise ValueError(f"{where}: a cache of {bits} bits holds {torch.uint8 if bits == 8 else cache.dtype} values and float32 steps")
+    _one_device(where, K, V, *steps)
+    return _pack_cache(_ptr(K), _ptr(V), *((_ptr(s) for s in steps) if steps else (0, 0)), cache.pages, cache.page, cache.hkv, cache.d, bits)
+
+
+def kv_write(cache, K, V, places):
+    """Rows of K and V [tokens, hkv, d] to the places (int64: page number * page + position in the page; negative: skipped) of the cache."""
+    where = "s24_kv_write"
+    tokens = K.shape[0]
+    _one_device(where, cache.K, K, V, places)
+    _check(lib().s24_kv_write(_kv_cache(where, cache), _heads(where, "K", K, tokens, cache.hkv, cache.d, cache.dtype),
+                              _heads(where, "V", V, tokens, cache.hkv, cache.d, cache.dtype), _whole(where, "places", places, torch.int64, tokens),
+                              tokens, _dt(K), _stream()), where)
+
+
+def kv_read(cache, table, cu, K, V):
+    """Position j of sequence i, in page table[i, j // page] (int32), to row cu[i] + j of K and V [tokens, hkv, d]."""
+    where = "s24_kv_read"
+    tokens, sequences = K.shape[0], table.shape[0]
+    _one_device(where, cache.K, table, cu, K, V)
+    _check(lib().s24_kv_read(_kv_cache(where, cache), _whole(where, "table", table, torch.int32, None, None), table.shape[1],
+                             _whole(where, "cu", cu, torch.int32, sequences + 1), sequences, tokens, _heads(where, "K", K, tokens, cache.hkv, cache.d, cache.dtype),
+                             _heads(where, "V", V, tokens, cache.hkv, cache.d, cache.dtype), _dt(K), _stream()), where)
+    return K, V
+
+
+def attn_decode_workspace(cache, sequences, hq):
+    """Bytes of workspace that attn_decode needs for so many sequences and query heads."""
+    return lib().s24_attn_decode_workspace(_kv_cache("s24_attn_decode_workspace", cache), sequences, hq)
+
+
+def attn_decode(cache, Q, table, lengths, O, workspace, scale=None):
+    """O[i] = softmax(scale Q[i].K) V over the first lengths[i] (int32) positions of sequence i.  Q, O [sequences, hq, d]; workspace: a uint8 tensor of
+    attn_decode_workspace(...) bytes."""
+    where = "s24_attn_decode"
+    sequences, hq, d = Q.shape
+    _one_device(where, cache.K, Q, table, lengths, O, workspace)
+    _check(lib().s24_attn_decode(_kv_cache(where, cache), _heads(where, "Q", Q, sequences, hq, cache.d, cache.dtype), hq,
+                                 _whole(where, "table", table, torch.int32, sequences, None), table.shape[1],
+                                 _whole(where, "lengths", lengths, torch.int32, sequences), sequences, d ** -0.5 if scale is None else scale,
+                                 _heads(where, "O", O, sequences, hq, cache.d, cache.dtype), _whole(where, "workspace", workspace, torch.uint8, None),
+                                 workspace.numel(), _dt(Q), _stream()), where)
+    return O
 
 
 def set_clock_probe(buf):

@@ -1,0 +1,527 @@
+// The paged key-value cache: tokens written to it (in 8 bits: quantised), sequences read back, and attention of one new token over it.
+//
+// Layout of a page, for one of its key-value heads:  K [page][d], a token's key in one piece;  V [page / E][d][E] with E = 8 tokens for 16-bit
+// values and 16 for 8-bit ones: 16 bytes are E consecutive tokens of one channel.  Both products of the attention of a token are matrix
+// instructions whose contracted axis lies along a lane's 16 bytes: the channels of K, the tokens of V.  So both go from memory to registers in
+// 16-byte loads with nothing in between.
+// 8 bits: x ~ s n with n = -127 .. 127 held as n + 128, s = max(max|x| / 127, 2^-126) in fp32 for each token and head.
+#include "s24_attn.h"
+
+#include <math.h>
+
+namespace s24_kv {
+using namespace s24_attn;
+
+struct Cache {
+    unsigned char *k, *v;
+    float *ks, *vs;   // [pages][hkv][page]
+    int64_t pages;
+    int page, shift, hkv, d;   // page = 1 << shift
+};
+struct Strided { uint16_t *p; int64_t token, head; };
+
+// n nearest to x / s, ties to even, exactly: the estimate is at most one off, and x - n s is exact in fp32 for 16-bit x (a multiple of the last
+// place of s, and no larger than s).
+__device__ __forceinline__ int nearest(float x, float s, float inverse)
+{
+    const float n = rintf(x * inverse), twice = 2.0f * fmaf(-n, s, x);
+    const int i = (int)n, odd = i & 1;
+    return i + (twice > s || (twice == s && odd)) - (twice < -s || (twice == -s && odd));
+}
+
+// ------------------------------------------------------------------ writing
+struct WriteArgs {
+    Cache c;
+    Strided k, v;
+    const int64_t *places;
+    int tokens;
+};
+// A wave takes one token of one head, a lane two channels.
+template <typename T, int BITS>
+__global__ __launch_bounds__(256) void kv_write_kernel(const WriteArgs a)
+{
+    using Num = s24_num<T>;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t item = (int64_t)blockIdx.x * 4 + wave;
+    if (item >= (int64_t)a.tokens * a.c.hkv) return;
+    const int token = (int)(item / a.c.hkv), h = (int)(item - (int64_t)token * a.c.hkv);
+    const int64_t place = a.places[token];
+    if (place < 0 || place >= a.c.pages << a.c.shift) return;
+    const int64_t first = ((place >> a.c.shift) * a.c.hkv + h) << a.c.shift;   // of the page, in tokens of one head
+    const int at = (int)(place & (a.c.page - 1)), i = 2 * lane;
+    const bool live = i < a.c.d;
+    uint32_t xk = 0, xv = 0;
+    if (live) {
+        xk = *reinterpret_cast<const uint32_t *>(a.k.p + token * a.k.token + h * a.k.head + i);
+        xv = *reinterpret_cast<const uint32_t *>(a.v.p + token * a.v.token + h * a.v.head + i);
+    }
+    if (BITS == 16) {
+        if (!live) return;
+        *reinterpret_cast<uint32_t *>(a.c.k + ((first + at) * a.c.d + i) * 2) = xk;
+        uint16_t *v = reinterpret_cast<uint16_t *>(a.c.v) + first * a.c.d + ((int64_t)(at >> 3) * a.c.d + i) * 8 + (at & 7);
+        v[0] = (uint16_t)xv, v[8] = (uint16_t)(xv >> 16);
+    } else {
+        float mk = fmaxf(fabsf(Num::lo(xk)), fabsf(Num::hi(xk))), mv = fmaxf(fabsf(Num::lo(xv)), fabsf(Num::hi(xv)));
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) mk = fmaxf(mk, __shfl_xor(mk, s)), mv = fmaxf(mv, __shfl_xor(mv, s));
+        const float sk = fmaxf(__fdiv_rn(mk, 127.0f), 0x1p-126f), sv = fmaxf(__fdiv_rn(mv, 127.0f), 0x1p-126f);
+        const float ik = 1.0f / sk, iv = 1.0f / sv;
+        if (lane == 0) a.c.ks[first + at] = sk, a.c.vs[first + at] = sv;
+        if (!live) return;
+        *reinterpret_cast<uint16_t *>(a.c.k + (first + at) * a.c.d + i) =
+            (uint16_t)((nearest(Num::lo(xk), sk, ik) + 128) | (nearest(Num::hi(xk), sk, ik) + 128) << 8);
+        unsigned char *v = a.c.v + first * a.c.d + ((int64_t)(at >> 4) * a.c.d + i) * 16 + (at & 15);
+        v[0] = (unsigned char)(nearest(Num::lo(xv), sv, iv) + 128), v[16] = (unsigned char)(nearest(Num::hi(xv), sv, iv) + 128);
+    }
+}
+
+// ------------------------------------------------------------------ reading back
+struct ReadArgs {
+    Cache c;
+    Strided k, v;
+    const int *table, *cu;
+    int64_t width;
+    int sequences, tokens;
+};
+// A page of the table, whatever the table holds one of the cache's
+__device__ __forceinline__ int64_t page_at(const int *table, int64_t width, int sequence, int index, int64_t pages)
+{
+    const int64_t id = (uint32_t)table[sequence * width + index];
+    return id < pages ? id : pages - 1;
+}
+// 64 tokens of a sequence and one head by a workgroup; a thread takes eight channels of a token.
+template <typename T, int BITS>
+__global__ __launch_bounds__(256) void kv_read_kernel(const ReadArgs a)
+{
+    using Num = s24_num<T>;
+    const int lane = threadIdx.x & 63;
+    const int tile = blockIdx.x / a.c.hkv, h = blockIdx.x - tile * a.c.hkv;
+    int sequence, index, count;
+    if (!find_tile(a.cu, a.sequences, a.tokens, 64, tile, lane, sequence, index, count)) return;
+    const Span s = span(a.cu, sequence, a.tokens);
+    const int pieces = a.c.d >> 3;
+    for (int i = threadIdx.x; i < 64 * pieces; i += 256) {
+        const int pos = index * 64 + i / pieces, c = 8 * (i % pieces);
+        if (pos >= s.count || pos >> a.c.shift >= a.width) continue;
+        const int64_t first = (page_at(a.table, a.width, sequence, pos >> a.c.shift, a.c.pages) * a.c.hkv + h) << a.c.shift;
+        const int at = pos & (a.c.page - 1);
+        uint4 xk;
+        uint32_t xv[4];
+        if (BITS == 16) {
+            xk = *reinterpret_cast<const uint4 *>(a.c.k + ((first + at) * a.c.d + c) * 2);
+            const uint16_t *v = reinterpret_cast<const uint16_t *>(a.c.v) + first * a.c.d + ((int64_t)(at >> 3) * a.c.d + c) * 8 + (at & 7);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) xv[j] = v[16 * j] | (uint32_t)v[16 * j + 8] << 16;
+        } else {
+            const float sk = a.c.ks[first + at], sv = a.c.vs[first + at];
+            const uint2 n = *reinterpret_cast<const uint2 *>(a.c.k + (first + at) * a.c.d + c);
+            const unsigned char *v = a.c.v + first * a.c.d + ((int64_t)(at >> 4) * a.c.d + c) * 16 + (at & 15);
+            uint32_t x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t two = (j < 2 ? n.x : n.y) >> (16 * (j & 1));
+                x[j] = Num::pack2((float)((int)(two & 255) - 128) * sk, (float)((int)(two >> 8 & 255) - 128) * sk);
+                xv[j] = Num::pack2((float)((int)v[32 * j] - 128) * sv, (float)((int)v[32 * j + 16] - 128) * sv);
+            }
+            xk = make_uint4(x[0], x[1], x[2], x[3]);
+        }
+        const int64_t t = s.first + pos;
+        *reinterpret_cast<uint4 *>(a.k.p + t * a.k.token + h * a.k.head + c) = xk;
+        *reinterpret_cast<uint4 *>(a.v.p + t * a.v.token + h * a.v.head + c) = make_uint4(xv[0], xv[1], xv[2], xv[3]);
+    }
+}
+
+// ------------------------------------------------------------------ attention of one new token
+struct DecodeArgs {
+    Cache c;
+    Strided q, o;
+    const int *table, *lengths;
+    int64_t width;
+    int sequences, hq, group, blocks, shares;   // blocks: of 16 query heads in a group; shares: of all positions of all sequences
+    float scale;
+    float *part;   // [tile][head of the tile][d + 2]: sums, reference, weight
+};
+__device__ __forceinline__ int length_of(const DecodeArgs &a, int b)
+{
+    const int64_t most = a.width << a.c.shift;
+    return (int)min((int64_t)max(a.lengths[b], 0), most);
+}
+// Positions are shared out evenly: every sequence is cut into tiles of `chunk` positions, chosen so that there are at most `shares` tiles and
+// one for each sequence.
+__device__ __forceinline__ int chunk_of(const DecodeArgs &a, int lane)
+{
+    int64_t total = 0;
+    for (int b = lane; b < a.sequences; b += 64) total += length_of(a, b);
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) total += __shfl_xor(total, s);
+    const int64_t each = (total + a.shares - 1) / a.shares;
+    return (int)min((each + 255) / 256 * 256, (int64_t)0x7FFFFF00);
+}
+// Tile t of the sequences' tiles; `before` those of earlier sequences
+__device__ __forceinline__ bool tile_of(const DecodeArgs &a, int chunk, int t, int lane, int &sequence, int &index, int &count)
+{
+    for (int base = 0; base < a.sequences; base += 64) {
+        const int b = base + lane;
+        const int n = b < a.sequences ? max(1, (length_of(a, b) + chunk - 1) / chunk) : 0;   // an empty sequence has a tile too: it writes zeros
+        int sum = n;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int other = __shfl_up(sum, d);
+            if (lane >= d) sum += other;
+        }
+        const unsigned long long past = __ballot(t < sum);
+        if (past != 0) {
+            const int owner = __ffsll(past) - 1;
+            sequence = __builtin_amdgcn_readfirstlane(base + owner), count = __builtin_amdgcn_readlane(n, owner);
+            index = t - (__builtin_amdgcn_readlane(sum, owner) - count);
+            return true;
+        }
+        t -= __builtin_amdgcn_readlane(sum, 63);
+    }
+    return false;
+}
+
+// Sixteen bytes of the cache as operands of 8 channels (tokens) each
+__device__ __forceinline__ uint4 halves(uint32_t a, uint32_t b)
+{
+    // a byte under the exponent of 1024 is 1024 + byte
+    auto two = [](uint32_t x, uint32_t select) {
+        const f16x2 v = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(x, 0x64646464u, select));
+        return __builtin_bit_cast(uint32_t, v - (f16x2){(_Float16)1152.0f, (_Float16)1152.0f});
+    };
+    return make_uint4(two(a, 0x00050004u), two(a, 0x00070006u), two(b, 0x00050004u), two(b, 0x00070006u));
+}
+
+// A workgroup takes a tile of positions for one key-value head and 16 of its query heads; its four waves take the blocks of 64 positions in turn
+// and add up in LDS at the end.  Of a block, S^T = K Q^T has positions as rows: row 4g + r of tile t is position 16g + 4t + r, so that a lane's
+// weights are those of 16 consecutive positions, which is what it holds of V.
+template <typename T, int D, int BITS>
+__global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
+{
+    using M = typename std::conditional<BITS == 8, s24_half, T>::type;   // the products of an 8-bit cache are binary16: it holds -127 .. 127
+    using Num = s24_num<T>;
+    constexpr int KL = BITS == 8 ? D / 64 : D / 32, VL = BITS == 8 ? 1 : 2;   // 16-byte loads of a key; of a channel's positions
+    __shared__ float sums[4][D][17];
+    __shared__ float refs[4][16], weights[4][16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, g = lane >> 4;
+    const int heads = a.c.hkv * a.blocks, tile = blockIdx.x / heads, which = blockIdx.x - tile * heads;
+    const int h = which / a.blocks, q0 = 16 * (which - h * a.blocks), mine = min(16, a.group - q0);   // of the group's query heads
+    const int chunk = max(256, chunk_of(a, lane));
+    int b, index, count;
+    if (!tile_of(a, chunk, tile, lane, b, index, count)) return;
+    const int length = __builtin_amdgcn_readfirstlane(length_of(a, b)), end = min(length, (index + 1) * chunk);
+
+    // the queries, an operand of 16 columns
+    uint4 q[D / 32];
+    float c = a.scale * kLog2e;
+    {
+        const uint16_t *row = a.q.p + b * a.q.token + (h * a.group + q0 + min(col, mine - 1)) * a.q.head;
+        float most = 0.0f;
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) {
+            const int i = BITS == 8 ? 64 * (k >> 1) + 16 * g + 8 * (k & 1) : 32 * k + 8 * g;
+            q[k] = i < a.c.d && col < mine ? *reinterpret_cast<const uint4 *>(row + i) : make_uint4(0, 0, 0, 0);
+        }
+        if (BITS == 8) {   // scaled by a power of two into what binary16 holds
+            const uint32_t *x = reinterpret_cast<const uint32_t *>(q);
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) most = fmaxf(most, fmaxf(fabsf(Num::lo(x[i])), fabsf(Num::hi(x[i]))));
+            most = column_max(most);
+            const int e = most > 0.0f ? ilogbf(most) : 0;
+            uint32_t y[D / 8];
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) y[i] = pack2<s24_half>(ldexpf(Num::lo(x[i]), -e), ldexpf(Num::hi(x[i]), -e));
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) q[k] = make_uint4(y[4 * k], y[4 * k + 1], y[4 * k + 2], y[4 * k + 3]);
+            c = ldexpf(c, e);
+        }
+    }
+    float m = -1e30f, l = 0.0f, unit = 0.0f;   // unit: 8 bits, what the steps of V are measured in
+    f32x4 o[D / 16];
+#pragma unroll
+    for (int n = 0; n < D / 16; ++n) o[n] = f32x4{};
+    const int64_t token = (int64_t)a.c.d * (BITS / 8);   // bytes of a token of one head
+
+    for (int k0 = index * chunk + 64 * wave; k0 < end; k0 += 256) {
+        // positions 16*(col/4) .. of K and 16*g .. of V: each sixteen lie in one page
+        auto place = [&](int group) {
+            const int pos = min(k0 + 16 * group, (end - 1) & ~15);
+            return ((page_at(a.table, a.width, b, pos >> a.c.shift, a.c.pages) * a.c.hkv + h) << a.c.shift) + (pos & (a.c.page - 1));
+        };
+        const int64_t pk = place(col >> 2), pv = place(g);
+        uint4 fk[4][KL], fv[D / 16][VL];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int k = 0; k < KL; ++k)
+                fk[t][k] = *reinterpret_cast<const uint4 *>(a.c.k + (pk + 4 * t + (col & 3)) * token + 16 * min(4 * k + g, (int)(token >> 4) - 1));
+        float4 sk[4], sv[4];
+        if (BITS == 8) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) sk[t] = *reinterpret_cast<const float4 *>(a.c.ks + pv + 4 * t), sv[t] = *reinterpret_cast<const float4 *>(a.c.vs + pv + 4 * t);
+        }
+#pragma unroll
+        for (int n = 0; n < D / 16; ++n)
+#pragma unroll
+            for (int u = 0; u < VL; ++u)
+                fv[n][u] = *reinterpret_cast<const uint4 *>(a.c.v + pv * token + ((int64_t)u * a.c.d + min(16 * n + col, a.c.d - 1)) * 16);
+
+        f32x4 s[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            s[t] = f32x4{};
+#pragma unroll
+            for (int k = 0; k < KL; ++k) {
+                if constexpr (BITS == 8) {
+                    s[t] = mma<M>(halves(fk[t][k].x, fk[t][k].y), q[2 * k], s[t]);
+                    s[t] = mma<M>(halves(fk[t][k].z, fk[t][k].w), q[2 * k + 1], s[t]);
+                } else
+                    s[t] = mma<M>(fk[t][k], q[k], s[t]);
+            }
+            if (BITS == 8) s[t][0] *= sk[t].x, s[t][1] *= sk[t].y, s[t][2] *= sk[t].z, s[t][3] *= sk[t].w;
+        }
+        if (k0 + 64 > end) {   // what lies past the sequence's end may hold anything
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                float *step = reinterpret_cast<float *>(&sv[t]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const bool in = k0 + 16 * g + 4 * t + r < end;
+                    s[t][r] = in ? s[t][r] : -INFINITY;
+                    if (BITS == 8) step[r] = in ? step[r] : 0.0f;
+                }
+            }
+            if (BITS == 16) {
+#pragma unroll
+                for (int n = 0; n < D / 16; ++n)
+#pragma unroll
+                    for (int u = 0; u < VL; ++u) {
+                        uint32_t *x = reinterpret_cast<uint32_t *>(&fv[n][u]);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int left = end - (k0 + 16 * g + 8 * u + 2 * j);
+                            x[j] = left >= 2 ? x[j] : left == 1 ? x[j] & 0xFFFFu : 0u;
+                        }
+                    }
+            }
+        }
+        float top = s[0][0], step = 0.0f;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) top = fmaxf(top, s[t][r]);
+            if (BITS == 8) step = fmaxf(step, fmaxf(fmaxf(sv[t].x, sv[t].y), fmaxf(sv[t].z, sv[t].w)));
+        }
+        top = column_max(top) * c;
+        if (BITS == 8) step = column_max(step);
+        if (__any(top > m || step > unit)) {
+            const float now = fmaxf(m, top), shrink = __builtin_amdgcn_exp2f(m - now);
+            m = now, l *= shrink;
+            float all = shrink;
+            if (BITS == 8) {
+                const float wide = step > unit ? 2.0f * step : unit;
+                all *= unit / wide, unit = wide;
+            }
+#pragma unroll
+            for (int n = 0; n < D / 16; ++n) o[n] *= all;
+        }
+        const float inverse = BITS == 8 ? 1.0f / unit : 1.0f;
+        uint4 p[2];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                s[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], c, -m));
+                l += s[t][r];
+                if (BITS == 8) s[t][r] *= reinterpret_cast<const float *>(&sv[t])[r] * inverse;
+            }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) p[u] = operand<M>(s[2 * u], s[2 * u + 1]);
+#pragma unroll
+        for (int n = 0; n < D / 16; ++n) {
+            if constexpr (BITS == 8) {
+                o[n] = mma<M>(halves(fv[n][0].x, fv[n][0].y), p[0], o[n]);
+                o[n] = mma<M>(halves(fv[n][0].z, fv[n][0].w), p[1], o[n]);
+            } else {
+                o[n] = mma<M>(fv[n][0], p[0], o[n]);
+                o[n] = mma<M>(fv[n][1], p[1], o[n]);
+            }
+        }
+    }
+    l = column_sum(l);
+    if (g == 0) refs[wave][col] = m, weights[wave][col] = l;
+    const float own = BITS == 8 ? unit : 1.0f;
+#pragma unroll
+    for (int n = 0; n < D / 16; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sums[wave][16 * n + 4 * g + r][col] = o[n][r] * own;
+    __syncthreads();
+    const int d = a.c.d;
+    float *part = a.part + ((int64_t)tile * a.c.hkv * a.group + h * a.group + q0) * (d + 2);
+    for (int i = threadIdx.x; i < mine * (d / 2); i += 256) {
+        const int n = i / (d / 2), e = 2 * (i - n * (d / 2));
+        const float ref = fmaxf(fmaxf(refs[0][n], refs[1][n]), fmaxf(refs[2][n], refs[3][n]));
+        float x = 0.0f, y = 0.0f, w = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float f = __builtin_amdgcn_exp2f(refs[k][n] - ref);
+            x = fmaf(f, sums[k][e][n], x), y = fmaf(f, sums[k][e + 1][n], y), w = fmaf(f, weights[k][n], w);
+        }
+        if (count == 1) {
+            const float inverse = w > 0.0f ? 1.0f / w : 0.0f;
+            *reinterpret_cast<uint32_t *>(a.o.p + b * a.o.token + (h * a.group + q0 + n) * a.o.head + e) = pack2<T>(x * inverse, y * inverse);
+        } else {
+            float *to = part + (int64_t)n * (d + 2);
+            to[e] = x, to[e + 1] = y;
+            if (e == 0) to[d] = ref, to[d + 1] = w;
+        }
+    }
+}
+
+// The parts of a sequence's tiles, added: one wave a query head, a lane two channels
+template <typename T>
+__global__ __launch_bounds__(64) void attn_join_kernel(const DecodeArgs a)
+{
+    const int lane = threadIdx.x, b = blockIdx.x / a.hq, head = blockIdx.x - b * a.hq, d = a.c.d;
+    const int chunk = max(256, chunk_of(a, lane));
+    int before = 0;
+    for (int i = lane; i < b; i += 64) before += max(1, (length_of(a, i) + chunk - 1) / chunk);
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) before += __shfl_xor(before, s);
+    const int count = (length_of(a, b) + chunk - 1) / chunk;
+    if (count <= 1) return;
+    const int64_t step = (int64_t)a.hq * (d + 2);
+    const float *part = a.part + before * step + (int64_t)head * (d + 2);
+    float ref = -1e30f;
+    for (int i = lane; i < count; i += 64) ref = fmaxf(ref, part[i * step + d]);
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) ref = fmaxf(ref, __shfl_xor(ref, s));
+    float x = 0.0f, y = 0.0f, w = 0.0f;
+    const int e = min(2 * lane, d - 2);
+    for (int i = 0; i < count; ++i) {
+        const float *from = part + i * step;
+        const float f = __builtin_amdgcn_exp2f(from[d] - ref);
+        x = fmaf(f, from[e], x), y = fmaf(f, from[e + 1], y), w = fmaf(f, from[d + 1], w);
+    }
+    const float inverse = w > 0.0f ? 1.0f / w : 0.0f;
+    if (2 * lane < d) *reinterpret_cast<uint32_t *>(a.o.p + b * a.o.token + head * a.o.head + e) = pack2<T>(x * inverse, y * inverse);
+}
+
+// ------------------------------------------------------------------ host
+static int check_cache(const s24_kv_cache *c, s24_dtype dt)
+{
+    S24_REQUIRE(c != nullptr, S24_ERR_NULL);
+    S24_REQUIRE(s24_valid_dtype(dt), S24_ERR_DTYPE);
+    S24_REQUIRE(c->bits == 16 || c->bits == 8, S24_ERR_DTYPE);
+    S24_REQUIRE(c->pages >= 0 && c->pages < INT32_MAX && c->hkv > 0 && c->hkv < 65536, S24_ERR_SHAPE);
+    S24_REQUIRE(c->page >= 16 && c->page <= 1 << 16 && (c->page & (c->page - 1)) == 0, S24_ERR_SHAPE);
+    S24_REQUIRE(c->d >= 16 && c->d % 16 == 0, S24_ERR_SHAPE);
+    S24_REQUIRE(dt != S24_F32 && c->d <= 128, S24_ERR_UNSUPPORTED);
+    if (c->pages > 0) S24_REQUIRE(c->K != nullptr && c->V != nullptr && (c->bits == 16 || (c->k_step != nullptr && c->v_step != nullptr)), S24_ERR_NULL);
+    S24_REQUIRE(s24_aligned(c->K, 16) && s24_aligned(c->V, 16) && s24_aligned(c->k_step, 16) && s24_aligned(c->v_step, 16), S24_ERR_ALIGN);
+    return S24_OK;
+}
+static Cache cache_of(const s24_kv_cache *c)
+{
+    return {static_cast<unsigned char *>(c->K), static_cast<unsigned char *>(c->V), c->k_step, c->v_step, c->pages, (int)c->page,
+            __builtin_ctzll((unsigned long long)c->page), (int)c->hkv, (int)c->d};
+}
+static Strided strided(const s24_heads *v) { return {static_cast<uint16_t *>(v->data), v->token, v->head}; }
+
+// Tiles of one head of all sequences: enough for four workgroups a compute unit
+static int64_t shares_of(int64_t heads)
+{
+    const int64_t n = (4 * (int64_t)s24_cu_count() + heads - 1) / heads;
+    return n < 1 ? 1 : n;
+}
+}  // namespace s24_kv
+
+using namespace s24_kv;
+
+extern "C" int s24_kv_write(const s24_kv_cache *cache, const s24_heads *K, const s24_heads *V, const int64_t *places, int64_t tokens, s24_dtype dt,
+                            void *stream)
+{
+    S24_TRY(check_cache(cache, dt));
+    S24_REQUIRE(tokens >= 0 && tokens < INT32_MAX / 2, S24_ERR_SHAPE);
+    S24_TRY(check_rows(K, tokens, cache->hkv, cache->d, false));
+    S24_TRY(check_rows(V, tokens, cache->hkv, cache->d, false));
+    S24_REQUIRE(places != nullptr || tokens == 0, S24_ERR_NULL);
+    S24_REQUIRE(s24_aligned(places, 8), S24_ERR_ALIGN);
+    const int64_t groups = (tokens * cache->hkv + 3) / 4;
+    S24_REQUIRE(groups <= kMostGroups, S24_ERR_SHAPE);
+    if (groups == 0 || cache->pages == 0) return S24_OK;
+    const WriteArgs a{cache_of(cache), strided(K), strided(V), places, (int)tokens};
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const dim3 grid((unsigned)groups), block(256);
+    if (cache->bits == 16) kv_write_kernel<uint16_t, 16><<<grid, block, 0, st>>>(a);   // a copy, whatever the type
+    else if (dt == S24_BF16) kv_write_kernel<uint16_t, 8><<<grid, block, 0, st>>>(a);
+    else kv_write_kernel<s24_half, 8><<<grid, block, 0, st>>>(a);
+    return s24_launch_status();
+}
+
+extern "C" int s24_kv_read(const s24_kv_cache *cache, const int32_t *table, int64_t width, const int32_t *cu, int64_t sequences, int64_t tokens,
+                           const s24_heads *K, const s24_heads *V, s24_dtype dt, void *stream)
+{
+    S24_TRY(check_cache(cache, dt));
+    S24_REQUIRE(tokens >= 0 && tokens < INT32_MAX / 2 && sequences >= 0 && sequences < INT32_MAX / 2 && width >= 0 && width < INT32_MAX, S24_ERR_SHAPE);
+    S24_TRY(check_rows(K, tokens, cache->hkv, cache->d, true));
+    S24_TRY(check_rows(V, tokens, cache->hkv, cache->d, true));
+    S24_REQUIRE(cu != nullptr && (table != nullptr || width == 0 || sequences == 0), S24_ERR_NULL);
+    S24_REQUIRE(s24_aligned(table, 4) && s24_aligned(cu, 4), S24_ERR_ALIGN);
+    const int64_t groups = most_tiles(tokens, sequences, 64) * cache->hkv;
+    S24_REQUIRE(groups <= kMostGroups, S24_ERR_SHAPE);
+    if (groups == 0 || cache->pages == 0 || width == 0) return S24_OK;
+    const ReadArgs a{cache_of(cache), strided(K), strided(V), table, cu, width, (int)sequences, (int)tokens};
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const dim3 grid((unsigned)groups), block(256);
+    if (cache->bits == 16) kv_read_kernel<uint16_t, 16><<<grid, block, 0, st>>>(a);
+    else if (dt == S24_BF16) kv_read_kernel<uint16_t, 8><<<grid, block, 0, st>>>(a);
+    else kv_read_kernel<s24_half, 8><<<grid, block, 0, st>>>(a);
+    return s24_launch_status();
+}
+
+extern "C" int64_t s24_attn_decode_workspace(const s24_kv_cache *cache, int64_t sequences, int64_t hq)
+{
+    if (cache == nullptr || cache->hkv <= 0 || sequences < 0 || hq <= 0 || hq % cache->hkv != 0) return 0;
+    return (shares_of(cache->hkv * ((hq / cache->hkv + 15) / 16)) + sequences) * hq * (cache->d + 2) * 4;
+}
+
+namespace s24_kv {
+template <typename T> static void decode(const DecodeArgs &a, int bits, dim3 grid, hipStream_t st)
+{
+    const dim3 block(256);
+    if (bits == 16) {
+        if (a.c.d <= 64) attn_decode_kernel<T, 64, 16><<<grid, block, 0, st>>>(a);
+        else attn_decode_kernel<T, 128, 16><<<grid, block, 0, st>>>(a);
+    } else {
+        if (a.c.d <= 64) attn_decode_kernel<T, 64, 8><<<grid, block, 0, st>>>(a);
+        else attn_decode_kernel<T, 128, 8><<<grid, block, 0, st>>>(a);
+    }
+    if (a.width << a.c.shift > 256) attn_join_kernel<T><<<dim3((unsigned)(a.sequences * a.hq)), dim3(64), 0, st>>>(a);
+}
+}  // namespace s24_kv
+
+extern "C" int s24_attn_decode(const s24_kv_cache *cache, const s24_heads *Q, int64_t hq, const int32_t *table, int64_t width, const int32_t *lengths,
+                               int64_t sequences, float scale, const s24_heads *O, void *workspace, int64_t workspace_bytes, s24_dtype dt, void *stream)
+{
+    S24_TRY(check_cache(cache, dt));
+    S24_REQUIRE(sequences >= 0 && sequences < INT32_MAX / 2 && width >= 0 && width < INT32_MAX && hq > 0 && hq < 65536 && hq % cache->hkv == 0, S24_ERR_SHAPE);
+    S24_REQUIRE(width * cache->page < INT32_MAX - 256, S24_ERR_SHAPE);
+    S24_REQUIRE(scale > 0.0f && scale <= 3.0e38f, S24_ERR_SHAPE);
+    S24_TRY(check_rows(Q, sequences, hq, cache->d, false));
+    S24_TRY(check_rows(O, sequences, hq, cache->d, true));
+    if (sequences == 0) return S24_OK;
+    S24_REQUIRE(lengths != nullptr && workspace != nullptr && (table != nullptr || width == 0), S24_ERR_NULL);
+    S24_REQUIRE(s24_aligned(table, 4) && s24_aligned(lengths, 4) && s24_aligned(workspace, 16), S24_ERR_ALIGN);
+    S24_REQUIRE(workspace_bytes >= s24_attn_decode_workspace(cache, sequences, hq), S24_ERR_SHAPE);
+    DecodeArgs a{cache_of(cache), strided(Q), strided(O), table, lengths, cache->pages > 0 ? width : 0};
+    a.sequences = (int)sequences, a.hq = (int)hq, a.group = (int)(hq / cache->hkv), a.blocks = (a.group + 15) / 16;
+    const int64_t heads = cache->hkv * a.blocks, shares = shares_of(heads), groups = (shares + sequences) * heads;
+    S24_REQUIRE(groups <= kMostGroups && sequences * hq <= kMostGroups, S24_ERR_SHAPE);
+    a.shares = (int)shares, a.scale = scale, a.part = static_cast<float *>(workspace);
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (dt == S24_BF16) decode<uint16_t>(a, cache->bits, dim3((unsigned)groups), st);
+    else decode<s24_half>(a, cache->bits, dim3((unsigned)groups), st);
+    return s24_launch_status();
+}
