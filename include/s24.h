@@ -363,7 +363,8 @@ int s24_attn_fwd(const s24_attn_shape *shape, const s24_heads *Q, const s24_head
  *   workspace  device, s24_attn_bwd_workspace(shape) bytes, 16-byte aligned; holds nothing between calls */
 int64_t s24_attn_bwd_workspace(const s24_attn_shape *shape);
 int s24_attn_bwd(const s24_attn_shape *shape, const s24_heads *Q, const s24_heads *K, const s24_heads *V, const s24_heads *O, const s24_heads *dO,
-                 const float *lse, const s24_heads *dQ, const s24_heads *dK, const s24_heads *dV, void *workspace, s24_dtype dt, void *stream);
+                 const float *lse, const s24_heads *dQ, const s24_heads *dK, const s24_heads *dV, void *workspace, int64_t workspace_bytes,
+                 s24_dtype dt, void *stream);
 
 /* Key-value cache in pages of `page` tokens (a power of two from 16 to 65536), hkv heads of d values (a multiple of 16 up to 128).
  *   bits = 16   K, V  [pages][hkv][page][d] values of the calls' dtype; k_step, v_step not used

@@ -24,7 +24,8 @@ class Attention:
         self.dtype, self.device = dtype, device
         self.O = torch.empty((tokens_q, hq, d), dtype=dtype, device=device)
         self.lse = torch.empty((hq, tokens_q), dtype=torch.float32, device=device)
-        self.dQ = self.dK = self.dV = self.work = None   # allocated by the first backward pass
+        self.dQ = self.dK = self.dV = None   # allocated by the first backward pass
+        self.work = {}
 
     def forward(self, Q, K, V, cu_q, cu_k=None):
         """O [tokens_q, hq, d].  Q, K, V may be views of one projection's result; cu_q, cu_k: int32 offsets of the sequences."""
@@ -32,7 +33,10 @@ class Attention:
 
     def backward(self, Q, K, V, dO, cu_q, cu_k=None):
         """dQ, dK, dV of the last forward pass, whose operands are given again."""
-        need = s24.attn_bwd_workspace(self.tokens_q, self.tokens_k, self.hq, self.hkv, self.d, cu_q.shape[0] - 1)
+        work = self.work.get(cu_q.shape[0])   # what it takes depends on the number of sequences
+        if work is None:
+            need = s24.attn_bwd_workspace(self.tokens_q, self.tokens_k, self.hq, self.hkv, self.d, cu_q.shape[0] - 1)
+            work = self.work[cu_q.shape[0]] = torch.empty(need, dtype=torch.uint8, device=self.device)
         if self.dQ is None:
             # the layout of the projection's gradient: dQ, dK and dV are its parts
             if self.tokens_q == self.tokens_k:
@@ -42,9 +46,7 @@ class Attention:
                 self.dQKV = None
                 self.dQ = torch.empty((self.tokens_q, self.hq, self.d), dtype=self.dtype, device=self.device)
                 self.dK, self.dV = (torch.empty((self.tokens_k, self.hkv, self.d), dtype=self.dtype, device=self.device) for _ in range(2))
-        if self.work is None or self.work.numel() < need:
-            self.work = torch.empty(need, dtype=torch.uint8, device=self.device)
-        return s24.attn_bwd(Q, K, V, self.O, dO, self.lse, self.dQ, self.dK, self.dV, self.work, cu_q, cu_k, self.causal, self.scale)
+        return s24.attn_bwd(Q, K, V, self.O, dO, self.lse, self.dQ, self.dK, self.dV, work, cu_q, cu_k, self.causal, self.scale)
 
 
 class PagedKV:
@@ -58,20 +60,21 @@ class PagedKV:
         shape = (pages, hkv, page, d)
         self.K, self.V = (torch.empty(shape, dtype=dtype if bits == 16 else torch.uint8, device=device) for _ in range(2))
         self.k_step, self.v_step = (torch.empty(shape[:3], dtype=torch.float32, device=device) if bits == 8 else None for _ in range(2))
+        self.buffers = s24.KVBuffers(self.K, self.V, dtype, self.k_step, self.v_step)
         self.work = {}
 
     def write(self, K, V, places):
         """Rows of K and V [tokens, hkv, d] to their places: page number * page + position in the page (int64; negative ones are skipped)."""
-        s24.kv_write(self, K, V, places)
+        s24.kv_write(self.buffers, K, V, places)
 
     def read(self, table, cu, K, V):
         """The sequences, one after the other from the offsets cu on, into K and V [tokens, hkv, d]: as Attention.forward takes them."""
-        return s24.kv_read(self, table, cu, K, V)
+        return s24.kv_read(self.buffers, table, cu, K, V)
 
     def attend(self, Q, table, lengths, O, scale=None):
         """O [sequences, hq, d]: attention of one new token of each sequence over its first lengths[i] positions."""
-        key = (Q.shape[0], Q.shape[1], torch.cuda.current_stream().cuda_stream)
+        key = (Q.shape[:2], s24._stream())
         work = self.work.get(key)
         if work is None:   # one for each stream: calls on two streams may run at the same time
-            work = self.work[key] = torch.empty(s24.attn_decode_workspace(self, Q.shape[0], Q.shape[1]), dtype=torch.uint8, device=self.K.device)
-        return s24.attn_decode(self, Q, table, lengths, O, work, scale)
+            work = self.work[key] = torch.empty(s24.attn_decode_workspace(self.buffers, Q.shape[0], Q.shape[1]), dtype=torch.uint8, device=self.K.device)
+        return s24.attn_decode(self.buffers, Q, table, lengths, O, work, scale)

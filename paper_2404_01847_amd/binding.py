@@ -62,7 +62,7 @@ _SIGNATURES = {
     "s24_probe_reciprocal": (_int, [C.c_uint32, _i64, _vp, _vp]),
     "s24_attn_fwd": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _int, _vp]),
     "s24_attn_bwd_workspace": (_i64, [_vp]),
-    "s24_attn_bwd": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _int, _vp]),
+    "s24_attn_bwd": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _int, _vp]),
     "s24_kv_write": (_int, [_vp, _vp, _vp, _vp, _i64, _int, _vp]),
     "s24_kv_read": (_int, [_vp, _vp, _i64, _vp, _i64, _i64, _vp, _vp, _int, _vp]),
     "s24_attn_decode_workspace": (_i64, [_vp, _i64, _i64]),
@@ -484,128 +484,137 @@ class _KVCache(C.Structure):
 _pack_heads, _pack_shape, _pack_cache = _packer(_Heads), _packer(_AttnShape), _packer(_KVCache)
 
 
-def _heads(where, name, x, tokens, heads, d, dtype):
-    """[tokens, heads, d] with any strides along the first two axes."""
-    if tuple(x.shape) != (tokens, heads, d):
-        raise ValueError(f"{where}: {name} must have shape {(tokens, heads, d)}, got {tuple(x.shape)}")
+def _refused(where, name, x, dtype, shape, device):
     if x.dtype is not dtype:
-        raise ValueError(f"{where}: {name} must be {dtype} like the others, got {x.dtype}")
+        raise ValueError(f"{where}: {name} must be {dtype}, got {x.dtype}")
+    if x.get_device() != device:
+        raise ValueError(f"{where}: {name} lies on {x.device}, not where the others do")
+    if len(shape) != x.dim() or any(n is not None and n != m for n, m in zip(shape, x.shape)):
+        raise ValueError(f"{where}: {name} must have shape {tuple(shape)}, got {tuple(x.shape)}")
+    raise ValueError(f"{where}: {name} needs unit stride along its last axis, and no gaps if it holds no heads (strides {x.stride()})")
+
+
+def _heads(where, name, x, shape, dtype, device):
+    """[tokens, heads, d] with any strides along the first two axes.  (Of these checks a call makes up to eight, and few tokens wait for the host: they
+    are written for the case that all is well.)"""
+    if x.dtype is not dtype or x.shape != shape or x.get_device() != device:
+        _refused(where, name, x, dtype, shape, device)
     token, head, unit = x.stride()
     if unit != 1:
-        raise ValueError(f"{where}: {name} needs unit stride along its last axis (strides {x.stride()})")
-    return _pack_heads(x.data_ptr(), token if tokens > 1 else 0, head if heads > 1 else 0)
+        _refused(where, name, x, dtype, shape, device)
+    return _pack_heads(x.data_ptr(), token if shape[0] > 1 else 0, head if shape[1] > 1 else 0)
 
 
-def _whole(where, name, x, dtype, *shape):
-    """A contiguous tensor of whole numbers (offsets, lengths, places, tables) or statistics; None in the shape: any size."""
-    if x.dtype is not dtype or not x.is_contiguous() or x.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, x.shape)):
-        raise ValueError(f"{where}: {name} must be a contiguous {dtype} tensor of shape {shape}, got {x.dtype} {tuple(x.shape)}, strides {x.stride()}")
+def _whole(where, name, x, dtype, shape, device):
+    """A contiguous tensor of whole numbers (offsets, lengths, places, tables), statistics or bytes."""
+    if x.dtype is not dtype or x.shape != shape or x.get_device() != device or not x.is_contiguous():
+        _refused(where, name, x, dtype, shape, device)
     return x.data_ptr()
 
 
-def _one_device(where, first, *others):
-    for x in others:
-        if x is not None and x.device != first.device:
-            raise ValueError(f"{where}: the tensors lie on {first.device} and on {x.device}")
-
-
-def _attn_shape(where, Q, K, cu_q, cu_k, causal, scale):
-    if Q.dim() != 3 or K.dim() != 3:
-        raise ValueError(f"{where}: Q and K must have shape [tokens, heads, d], got {tuple(Q.shape)} and {tuple(K.shape)}")
-    tokens_q, hq, d = Q.shape
-    tokens_k, hkv, _ = K.shape
-    cu_k = cu_q if cu_k is None else cu_k
-    pq, pk = _whole(where, "cu_q", cu_q, torch.int32, None), _whole(where, "cu_k", cu_k, torch.int32, cu_q.shape[0])
-    if cu_q.shape[0] == 0:
-        raise ValueError(f"{where}: cu_q needs an offset for each sequence and one more")
-    return _pack_shape(pq, pk, cu_q.shape[0] - 1, tokens_q, tokens_k, hq, hkv, d, d ** -0.5 if scale is None else scale, int(bool(causal)))
+def _attn_operands(where, Q, K, cu_q, cu_k, causal, scale):
+    """(shapes of the rows of queries and of keys, dtype, device, packed s24_attn_shape)"""
+    sq, sk = Q.shape, K.shape
+    if len(sq) != 3 or len(sk) != 3 or sk[2] != sq[2]:
+        raise ValueError(f"{where}: Q and K must have shape [tokens, heads, d] with one d, got {tuple(sq)} and {tuple(sk)}")
+    device, n = Q.get_device(), cu_q.shape
+    pq = _whole(where, "cu_q", cu_q, torch.int32, n, device)
+    if len(n) != 1 or n[0] == 0:
+        raise ValueError(f"{where}: cu_q needs an offset for each sequence and one more, got shape {tuple(n)}")
+    pk = pq if cu_k is None or cu_k is cu_q else _whole(where, "cu_k", cu_k, torch.int32, n, device)
+    return sq, sk, Q.dtype, device, _pack_shape(pq, pk, n[0] - 1, sq[0], sk[0], sq[1], sk[1], sq[2], sq[2] ** -0.5 if scale is None else scale, bool(causal))
 
 
 def attn_fwd(Q, K, V, O, lse, cu_q, cu_k=None, causal=True, scale=None):
     """Attention over packed sequences.  Q, O [tokens_q, hq, d], K, V [tokens_k, hkv, d], with any strides along the first two axes; lse [hq, tokens_q]
     float32 or None; cu_q, cu_k: int32 offsets of the sequences (cu_k None: those of the queries); scale None: 1 / sqrt(d)."""
     where = "s24_attn_fwd"
-    shape = _attn_shape(where, Q, K, cu_q, cu_k, causal, scale)
-    (tq, hq, d), (tk, hkv, _), dtype = Q.shape, K.shape, Q.dtype
-    _one_device(where, Q, K, V, O, lse, cu_q, cu_k)
-    _check(lib().s24_attn_fwd(shape, _heads(where, "Q", Q, tq, hq, d, dtype), _heads(where, "K", K, tk, hkv, d, dtype),
-                              _heads(where, "V", V, tk, hkv, d, dtype), _heads(where, "O", O, tq, hq, d, dtype),
-                              None if lse is None else _whole(where, "lse", lse, torch.float32, hq, tq), _dt(Q), _stream()), where)
+    sq, sk, dtype, device, shape = _attn_operands(where, Q, K, cu_q, cu_k, causal, scale)
+    status = lib().s24_attn_fwd(shape, _heads(where, "Q", Q, sq, dtype, device), _heads(where, "K", K, sk, dtype, device), _heads(where, "V", V, sk, dtype, device),
+                                _heads(where, "O", O, sq, dtype, device),
+                                None if lse is None else _whole(where, "lse", lse, torch.float32, (sq[1], sq[0]), device), _dt(Q), _stream())
+    if status != 0:
+        raise S24Error(status, where)
     return O
 
 
 def attn_bwd_workspace(tokens_q, tokens_k, hq, hkv, d, sequences):
     """Bytes of workspace that attn_bwd needs for so many tokens, heads and sequences."""
-    return lib().s24_attn_bwd_workspace(_pack_shape(0, 0, sequences, tokens_q, tokens_k, hq, hkv, d, 1.0, 1))
+    return lib().s24_attn_bwd_workspace(_pack_shape(0, 0, sequences, tokens_q, tokens_k, hq, hkv, d, 1.0, True))
 
 
 def attn_bwd(Q, K, V, O, dO, lse, dQ, dK, dV, workspace, cu_q, cu_k=None, causal=True, scale=None):
     """Gradients dQ, dK, dV of attn_fwd, from its O and lse; workspace: a uint8 tensor of attn_bwd_workspace(...) bytes."""
     where = "s24_attn_bwd"
-    shape = _attn_shape(where, Q, K, cu_q, cu_k, causal, scale)
-    (tq, hq, d), (tk, hkv, _), dtype = Q.shape, K.shape, Q.dtype
-    _one_device(where, Q, K, V, O, dO, lse, dQ, dK, dV, workspace, cu_q, cu_k)
-    q = [_heads(where, n, x, tq, hq, d, dtype) for n, x in (("Q", Q), ("O", O), ("dO", dO), ("dQ", dQ))]
-    k = [_heads(where, n, x, tk, hkv, d, dtype) for n, x in (("K", K), ("V", V), ("dK", dK), ("dV", dV))]
-    need = lib().s24_attn_bwd_workspace(shape)
-    work = _whole(where, "workspace", workspace, torch.uint8, None)
-    if workspace.numel() < need:
-        raise ValueError(f"{where}: workspace needs {need} bytes, has {workspace.numel()}")
-    _check(lib().s24_attn_bwd(shape, q[0], k[0], k[1], q[1], q[2], _whole(where, "lse", lse, torch.float32, hq, tq), q[3], k[2], k[3], work, _dt(Q),
-                              _stream()), where)
+    sq, sk, dtype, device, shape = _attn_operands(where, Q, K, cu_q, cu_k, causal, scale)
+    status = lib().s24_attn_bwd(shape, _heads(where, "Q", Q, sq, dtype, device), _heads(where, "K", K, sk, dtype, device), _heads(where, "V", V, sk, dtype, device),
+                                _heads(where, "O", O, sq, dtype, device), _heads(where, "dO", dO, sq, dtype, device),
+                                _whole(where, "lse", lse, torch.float32, (sq[1], sq[0]), device), _heads(where, "dQ", dQ, sq, dtype, device),
+                                _heads(where, "dK", dK, sk, dtype, device), _heads(where, "dV", dV, sk, dtype, device),
+                                _whole(where, "workspace", workspace, torch.uint8, workspace.shape, device), workspace.numel(), _dt(Q), _stream())
+    if status != 0:
+        raise S24Error(status, where)
     return dQ, dK, dV
 
 
-def _kv_cache(where, cache):
-    """cache: an object with the buffers and sizes of a cache (attention.PagedKV)."""
-    K, V, bits = cache.K, cache.V, cache.bits
-    steps = (cache.k_step, cache.v_step) if bits == 8 else ()
-    _dense(where, "K V k_step v_step", K, V, *steps)
-    if K.shape != (cache.pages, cache.hkv, cache.page, cache.d) or V.shape != K.shape or any(s.shape != K.shape[:3] for s in steps):
-        raise ValueError(f"{where}: the cache's buffers must have shape {(cache.pages, cache.hkv, cache.page, cache.d)}")
-    if K.dtype is not V.dtype or K.dtype is not (torch.uint8 if bits == 8 else cache.dtype) or any(s.dtype is not torch.float32 for s in steps):
-        raise ValueError(f"{where}: a cache of {bits} bits holds {torch.uint8 if bits == 8 else cache.dtype} values and float32 steps")
-    _one_device(where, K, V, *steps)
-    return _pack_cache(_ptr(K), _ptr(V), *((_ptr(s) for s in steps) if steps else (0, 0)), cache.pages, cache.page, cache.hkv, cache.d, bits)
+class KVBuffers:
+    """The buffers of a cache, checked and packed once for all calls.  K, V [pages, hkv, page, d]: uint8 with k_step, v_step [pages, hkv, page] float32
+    (8 bits), or dtype (16 bits)."""
+
+    def __init__(self, K, V, dtype, k_step=None, v_step=None):
+        where, bits = "KVBuffers", 16 if k_step is None else 8
+        device, stored = K.get_device(), torch.uint8 if bits == 8 else dtype
+        if K.dim() != 4 or dtype not in (torch.bfloat16, torch.float16) or (k_step is None) != (v_step is None):
+            raise ValueError(f"{where}: buffers [pages, hkv, page, d] of a cache of bfloat16 or float16, with both steps or none")
+        for name, x in (("K", K), ("V", V)):
+            _whole(where, name, x, stored, K.shape, device)
+        for name, x in (("k_step", k_step), ("v_step", v_step)) if bits == 8 else ():
+            _whole(where, name, x, torch.float32, K.shape[:3], device)
+        self.buffers, self.dtype, self.device, self.bits = (K, V, k_step, v_step), dtype, device, bits
+        self.pages, self.hkv, self.page, self.d = K.shape
+        self.packed = _pack_cache(_ptr(K), _ptr(V), _ptr(k_step) or 0, _ptr(v_step) or 0, self.pages, self.page, self.hkv, self.d, bits)
 
 
 def kv_write(cache, K, V, places):
-    """Rows of K and V [tokens, hkv, d] to the places (int64: page number * page + position in the page; negative: skipped) of the cache."""
-    where = "s24_kv_write"
+    """Rows of K and V [tokens, hkv, d] to the places (int64: page number * page + position in the page; negative: skipped) of the cache (KVBuffers)."""
+    where, device = "s24_kv_write", cache.device
     tokens = K.shape[0]
-    _one_device(where, cache.K, K, V, places)
-    _check(lib().s24_kv_write(_kv_cache(where, cache), _heads(where, "K", K, tokens, cache.hkv, cache.d, cache.dtype),
-                              _heads(where, "V", V, tokens, cache.hkv, cache.d, cache.dtype), _whole(where, "places", places, torch.int64, tokens),
-                              tokens, _dt(K), _stream()), where)
+    shape = (tokens, cache.hkv, cache.d)
+    status = lib().s24_kv_write(cache.packed, _heads(where, "K", K, shape, cache.dtype, device), _heads(where, "V", V, shape, cache.dtype, device),
+                                _whole(where, "places", places, torch.int64, (tokens,), device), tokens, _dt(K), _stream())
+    if status != 0:
+        raise S24Error(status, where)
 
 
 def kv_read(cache, table, cu, K, V):
     """Position j of sequence i, in page table[i, j // page] (int32), to row cu[i] + j of K and V [tokens, hkv, d]."""
-    where = "s24_kv_read"
-    tokens, sequences = K.shape[0], table.shape[0]
-    _one_device(where, cache.K, table, cu, K, V)
-    _check(lib().s24_kv_read(_kv_cache(where, cache), _whole(where, "table", table, torch.int32, None, None), table.shape[1],
-                             _whole(where, "cu", cu, torch.int32, sequences + 1), sequences, tokens, _heads(where, "K", K, tokens, cache.hkv, cache.d, cache.dtype),
-                             _heads(where, "V", V, tokens, cache.hkv, cache.d, cache.dtype), _dt(K), _stream()), where)
+    where, device, n = "s24_kv_read", cache.device, table.shape
+    shape = (K.shape[0], cache.hkv, cache.d)
+    status = lib().s24_kv_read(cache.packed, _whole(where, "table", table, torch.int32, (n[0], n[-1]), device), n[-1],
+                               _whole(where, "cu", cu, torch.int32, (n[0] + 1,), device), n[0], shape[0], _heads(where, "K", K, shape, cache.dtype, device),
+                               _heads(where, "V", V, shape, cache.dtype, device), _dt(K), _stream())
+    if status != 0:
+        raise S24Error(status, where)
     return K, V
 
 
 def attn_decode_workspace(cache, sequences, hq):
     """Bytes of workspace that attn_decode needs for so many sequences and query heads."""
-    return lib().s24_attn_decode_workspace(_kv_cache("s24_attn_decode_workspace", cache), sequences, hq)
+    return lib().s24_attn_decode_workspace(cache.packed, sequences, hq)
 
 
 def attn_decode(cache, Q, table, lengths, O, workspace, scale=None):
     """O[i] = softmax(scale Q[i].K) V over the first lengths[i] (int32) positions of sequence i.  Q, O [sequences, hq, d]; workspace: a uint8 tensor of
     attn_decode_workspace(...) bytes."""
-    where = "s24_attn_decode"
+    where, device, n = "s24_attn_decode", cache.device, table.shape
     sequences, hq, d = Q.shape
-    _one_device(where, cache.K, Q, table, lengths, O, workspace)
-    _check(lib().s24_attn_decode(_kv_cache(where, cache), _heads(where, "Q", Q, sequences, hq, cache.d, cache.dtype), hq,
-                                 _whole(where, "table", table, torch.int32, sequences, None), table.shape[1],
-                                 _whole(where, "lengths", lengths, torch.int32, sequences), sequences, d ** -0.5 if scale is None else scale,
-                                 _heads(where, "O", O, sequences, hq, cache.d, cache.dtype), _whole(where, "workspace", workspace, torch.uint8, None),
-                                 workspace.numel(), _dt(Q), _stream()), where)
+    shape = (sequences, hq, cache.d)
+    status = lib().s24_attn_decode(cache.packed, _heads(where, "Q", Q, shape, cache.dtype, device), hq, _whole(where, "table", table, torch.int32, (sequences, n[-1]), device),
+                                   n[-1], _whole(where, "lengths", lengths, torch.int32, (sequences,), device), sequences, d ** -0.5 if scale is None else scale,
+                                   _heads(where, "O", O, shape, cache.dtype, device), _whole(where, "workspace", workspace, torch.uint8, workspace.shape, device),
+                                   workspace.numel(), _dt(Q), _stream())
+    if status != 0:
+        raise S24Error(status, where)
     return O
 
 

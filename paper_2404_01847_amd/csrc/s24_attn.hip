@@ -19,7 +19,9 @@ struct Problem {
     Rows q, k, v, o, dO;
     Out out, dq, dk, dv;
     float *lse;            // [hq][tokens_q]
-    float2 *stats;         // [hq][tokens_q], of the backward pass
+    float2 *stats;         // [hq][tokens_q], of the backward pass: what a row's exponents are taken from, and delta
+    float *sums;           // [parts][tokens_k][hkv][2 d]
+    int parts;
     const int *cu_q, *cu_k;
     int sequences, tokens_q, tokens_k, hq, group, d, causal;
     float scale;
@@ -169,55 +171,35 @@ template <typename T> struct Lift;
 template <> struct Lift<uint16_t> { static constexpr float kUp = 32.0f, kDown = 1.0f, kOfP = 0x1p-32f, kOfDs = 0x1p-32f; };
 template <> struct Lift<s24_half> { static constexpr float kUp = 15.0f, kDown = 0x1p-15f, kOfP = 0x1p-15f, kOfDs = 1.0f; };
 
-// stats[h][t]: what the exponents of a row are taken from, and delta = dO.O
-template <typename T>
-__global__ __launch_bounds__(256) void attn_delta_kernel(const Problem a)
-{
-    using Num = s24_num<T>;
-    using L = Lift<T>;
-    const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4;   // 16 lanes a row: its (at most) 16 pieces
-    const int lane = threadIdx.x & 15;
-    if (item >= (int64_t)a.tokens_q * a.hq) return;
-    const int64_t t = item / a.hq;
-    const int h = (int)(item - t * a.hq);
-    float sum = 0.0f;
-    if (8 * lane < a.d) {
-        const uint4 x = *reinterpret_cast<const uint4 *>(a.dO.p + t * a.dO.token + h * a.dO.head + 8 * lane);
-        const uint4 y = *reinterpret_cast<const uint4 *>(a.o.p + t * a.o.token + h * a.o.head + 8 * lane);
-        const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum = fmaf(Num::lo(xs[i]), Num::lo(ys[i]), fmaf(Num::hi(xs[i]), Num::hi(ys[i]), sum));
-    }
-#pragma unroll
-    for (int s = 1; s < 16; s <<= 1) sum += __shfl_xor(sum, s);
-    const int64_t at = h * (int64_t)a.tokens_q + t;
-    if (lane == 0) a.stats[at] = make_float2(fmaf(a.lse[at], kLog2e, -L::kUp), sum * L::kDown);
-}
-
 // dK and dV of 128 keys of a key-value head, four waves of 32: over the query heads of the group and their queries, 32 at a time.
 // S has the queries as rows, so that P and dS are, as they lie, the operands that contract over the queries.
 template <int D> struct Backward {
-    static constexpr int BK = 128, BQ = 32, TILE = BQ * 2 * D, STAGE = 2 * TILE + 8 * BQ;   // queries, gradients, row statistics
+    static constexpr int BK = 128, BQ = 32, TILE = BQ * 2 * D, STAGE = 2 * TILE + 8 * BQ, VALUES = BK * 2 * D;   // a stage: queries, gradients, row statistics
 };
 template <typename T, int D>
-__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_dkv_kernel(const Problem a)
+__global__ __launch_bounds__(256, 2) void attn_dkv_kernel(const Problem a)
 {
     using C = Backward<D>;
     using L = Lift<T>;
-    __shared__ __align__(16) unsigned char stages[2][C::STAGE];
+    __shared__ __align__(16) unsigned char stages[2][C::STAGE], values[C::VALUES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
     const int hkv = a.hq / a.group;
-    const int tile = blockIdx.x / hkv, kv = head_of(blockIdx.x - tile * hkv, hkv);
+    const int units = hkv * a.parts, tile = blockIdx.x / units, unit = head_of(blockIdx.x - tile * units, units), kv = unit / a.parts, part = unit - kv * a.parts;
     int sequence, index, count;
     if (!find_tile(a.cu_k, a.sequences, a.tokens_k, C::BK, tile, lane, sequence, index, count)) return;
     const Span sq = span(a.cu_q, sequence, a.tokens_q), sk = span(a.cu_k, sequence, a.tokens_k);
     const int k0 = index * C::BK, wk0 = k0 + 32 * wave;   // the first keys are seen by the most queries: they go first
     const int ahead = sk.count - sq.count;
     const int first = a.causal ? max(0, k0 - ahead) / C::BQ : 0;                // query tiles
-    const int each = max(0, (sq.count + C::BQ - 1) / C::BQ - first), steps = each * a.group;
+    const int each = max(0, (sq.count + C::BQ - 1) / C::BQ - first);
+    // the steps of all heads of the group, and of them this part's
+    const int64_t all_steps = (int64_t)each * a.group;
+    const int begin = (int)(all_steps * part / a.parts), steps = (int)(all_steps * (part + 1) / a.parts) - begin;
 
-    uint4 fk[2][D / 32], fv[2][D / 32];
+    // The keys' fragments stay in registers, the values' come from LDS: with both, two waves would not fit a SIMD (3.6 ms instead of MEASURE for 8192 tokens,
+    // 64 heads on 8 of 128).
+    uint4 fk[2][D / 32];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const int64_t t = sk.first + min(wk0 + 16 * j + col, sk.count - 1);
@@ -225,7 +207,18 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_dkv_kernel(const Pr
         for (int k = 0; k < D / 32; ++k) {
             const int i = 32 * k + 8 * g;
             fk[j][k] = i < a.d ? *reinterpret_cast<const uint4 *>(a.k.p + t * a.k.token + kv * a.k.head + i) : make_uint4(0, 0, 0, 0);
-            fv[j][k] = i < a.d ? *reinterpret_cast<const uint4 *>(a.v.p + t * a.v.token + kv * a.v.head + i) : make_uint4(0, 0, 0, 0);
+        }
+    }
+    lds_byte *const tv = (lds_byte *)values;
+    {
+        Copy<D, C::BK, 4> cv;
+        cv.init(wave, lane, (int)a.v.token * 2, a.d);
+        cv.offsets(min(sk.count - k0, C::BK));
+        cv.start(a.v.p + (int64_t)(sk.first + k0) * a.v.token + kv * a.v.head, tv);
+        if (a.d < D) {   // past the head's last value: zeros, of which no gradient row makes anything else
+            wait_and_barrier<0>();
+            for (int i = threadIdx.x; i < C::BK * (D / 8); i += 256)
+                if (8 * (i % (D / 8)) >= a.d) lds_store(tv + piece<D>(i / (D / 8), i % (D / 8)), make_uint4(0, 0, 0, 0));
         }
     }
     f32x4 dk[D / 16][2], dv[D / 16][2];
@@ -235,7 +228,8 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_dkv_kernel(const Pr
 
     Copy<D, C::BQ, 4> cq, cdo;
     cq.init(wave, lane, (int)a.q.token * 2, a.d), cdo.init(wave, lane, (int)a.dO.token * 2, a.d);
-    int next_head = kv * a.group, next_tile = first, buffer = 0;
+    int next_head = kv * a.group + (each > 0 ? begin / each : 0), next_tile = first + (each > 0 ? begin % each : 0), buffer = 0;
+    int qt = next_tile;
     auto copy = [&](int stage) {
         const int left = sq.count - next_tile * C::BQ;
         cq.offsets(min(left, C::BQ)), cdo.offsets(min(left, C::BQ));
@@ -247,7 +241,6 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_dkv_kernel(const Pr
         if (++next_tile == first + each) next_tile = first, ++next_head;
     };
     if (steps > 0) copy(0);
-    int qt = first;
     for (int step = 0; step < steps; ++step) {
         wait_and_barrier<0>();
         if (step + 1 < steps) copy(buffer ^ 1);
@@ -260,16 +253,20 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_dkv_kernel(const Pr
 #pragma unroll
         for (int i = 0; i < 2; ++i) s[i][0] = s[i][1] = dp[i][0] = dp[i][1] = f32x4{};
 #pragma unroll
-        for (int k = 0; k < D / 32; ++k)
+        for (int k = 0; k < D / 32; ++k) {
+            uint4 fv[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) fv[j] = rows<D>(tv, 32 * wave + 16 * j, k, lane);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const uint4 x = rows<D>(tq, 16 * i, k, lane), y = rows<D>(tdo, 16 * i, k, lane);
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     s[i][j] = mma<T>(x, fk[j][k], s[i][j]);
-                    dp[i][j] = mma<T>(y, fv[j][k], dp[i][j]);
+                    dp[i][j] = mma<T>(y, fv[j], dp[i][j]);
                 }
             }
+        }
         f32x4 lse[2], delta[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -316,19 +313,52 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_dkv_kernel(const Pr
     for (int j = 0; j < 2; ++j) {
         const int row = wk0 + 16 * j + col;
         if (row >= sk.count) continue;
-        uint16_t *to_k = a.dk.p + (int64_t)(sk.first + row) * a.dk.token + kv * a.dk.head;
-        uint16_t *to_v = a.dv.p + (int64_t)(sk.first + row) * a.dv.token + kv * a.dv.head;
+        const int64_t t = sk.first + row;
+        if (a.parts == 1) {
+            uint16_t *to_k = a.dk.p + t * a.dk.token + kv * a.dk.head, *to_v = a.dv.p + t * a.dv.token + kv * a.dv.head;
 #pragma unroll
-        for (int n = 0; n < D / 16; ++n)
-            if (16 * n < a.d) {
-                const f32x4 x = dk[n][j] * (a.scale * L::kOfDs), y = dv[n][j] * L::kOfP;
-                *reinterpret_cast<uint2 *>(to_k + 16 * n + 4 * g) = make_uint2(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]));
-                *reinterpret_cast<uint2 *>(to_v + 16 * n + 4 * g) = make_uint2(pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3]));
-            }
+            for (int n = 0; n < D / 16; ++n)
+                if (16 * n < a.d) {
+                    const f32x4 x = dk[n][j] * (a.scale * L::kOfDs), y = dv[n][j] * L::kOfP;
+                    *reinterpret_cast<uint2 *>(to_k + 16 * n + 4 * g) = make_uint2(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]));
+                    *reinterpret_cast<uint2 *>(to_v + 16 * n + 4 * g) = make_uint2(pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3]));
+                }
+        } else {
+            float *to = a.sums + ((part * (int64_t)a.tokens_k + t) * hkv + kv) * 2 * a.d;
+#pragma unroll
+            for (int n = 0; n < D / 16; ++n)
+                if (16 * n < a.d) {
+                    *reinterpret_cast<f32x4 *>(to + 16 * n + 4 * g) = dk[n][j] * (a.scale * L::kOfDs);
+                    *reinterpret_cast<f32x4 *>(to + a.d + 16 * n + 4 * g) = dv[n][j] * L::kOfP;
+                }
+        }
     }
 }
 
-// dQ of 128 queries of a head, four waves of 32, over the keys they see, 32 at a time
+// dK and dV of a few keys from the sums of the parts
+constexpr int kJoinRows = 16;
+template <typename T>
+__global__ __launch_bounds__(256) void attn_dkv_join_kernel(const Problem a)
+{
+    constexpr int BK = kJoinRows;
+    const int hkv = a.hq / a.group, tile = blockIdx.x / hkv, kv = blockIdx.x - tile * hkv;
+    int sequence, index, count;
+    if (!find_tile(a.cu_k, a.sequences, a.tokens_k, BK, tile, threadIdx.x & 63, sequence, index, count)) return;
+    const Span sk = span(a.cu_k, sequence, a.tokens_k);
+    const int quads = a.d >> 1, n = min(BK, sk.count - index * BK) * quads;   // of a row of dK and one of dV
+    const int64_t step = (int64_t)a.tokens_k * hkv * 2 * a.d;
+    for (int item = threadIdx.x; item < n; item += 256) {
+        const int row = item / quads, i = 4 * (item - row * quads);
+        const int64_t t = sk.first + index * BK + row;
+        const float *from = a.sums + (t * hkv + kv) * 2 * a.d + i;
+        f32x4 x = *reinterpret_cast<const f32x4 *>(from);
+        for (int p = 1; p < a.parts; ++p) x += *reinterpret_cast<const f32x4 *>(from + p * step);
+        uint16_t *to = i < a.d ? a.dk.p + t * a.dk.token + kv * a.dk.head + i : a.dv.p + t * a.dv.token + kv * a.dv.head + i - a.d;
+        *reinterpret_cast<uint2 *>(to) = make_uint2(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]));
+    }
+}
+
+// dQ of 128 queries of a head, four waves of 32, over the keys they see, 32 at a time.  Runs first: it leaves the row statistics to dK and dV.
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void attn_dq_kernel(const Problem a)
 {
@@ -351,14 +381,21 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(const Problem a)
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const int64_t t = sq.first + min(wq0 + 16 * j + col, sq.count - 1);
-        const float2 of_row = a.stats[(int64_t)head * a.tokens_q + t];
-        lse[j] = of_row.x, delta[j] = of_row.y;
+        const int64_t at = (int64_t)head * a.tokens_q + t;
+        float sum = 0.0f;
 #pragma unroll
         for (int k = 0; k < D / 32; ++k) {
             const int i = 32 * k + 8 * g;
             q[j][k] = i < a.d ? *reinterpret_cast<const uint4 *>(a.q.p + t * a.q.token + head * a.q.head + i) : make_uint4(0, 0, 0, 0);
             dO[j][k] = i < a.d ? *reinterpret_cast<const uint4 *>(a.dO.p + t * a.dO.token + head * a.dO.head + i) : make_uint4(0, 0, 0, 0);
+            const uint4 o = i < a.d ? *reinterpret_cast<const uint4 *>(a.o.p + t * a.o.token + head * a.o.head + i) : make_uint4(0, 0, 0, 0);
+            using Num = s24_num<T>;
+            const uint32_t xs[4] = {o.x, o.y, o.z, o.w}, ys[4] = {dO[j][k].x, dO[j][k].y, dO[j][k].z, dO[j][k].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum = fmaf(Num::lo(xs[e]), Num::lo(ys[e]), fmaf(Num::hi(xs[e]), Num::hi(ys[e]), sum));
         }
+        lse[j] = fmaf(a.lse[at], kLog2e, -L::kUp), delta[j] = column_sum(sum) * L::kDown;
+        if (g == 0 && wq0 + 16 * j + col < sq.count) a.stats[at] = make_float2(lse[j], delta[j]);
     }
     const float c = a.scale * kLog2e;
     f32x4 dq[D / 16][2];
@@ -487,39 +524,56 @@ extern "C" int s24_attn_fwd(const s24_attn_shape *shape, const s24_heads *Q, con
     return s24_launch_status();
 }
 
+namespace s24_attn {
+// Parts in which the queries of a tile of keys are taken.  Two workgroups fit a compute unit, and when causal the first keys' have many times the work of
+// the last ones': fewer than three for each unit are cut up into four or more.  (The sums of a part travel through memory in fp32: with 1.7 rounds, 12 heads of
+// 64 and 8 x 1024 tokens, that costs more than it gives, 81 us to 67.)
+static int64_t parts_of(const s24_attn_shape *s)
+{
+    const int64_t tiles = most_tiles(s->tokens_k, s->sequences, Backward<128>::BK) * s->hkv, units = s24_cu_count();
+    if (tiles == 0 || tiles >= 3 * units) return 1;
+    const int64_t parts = (4 * units + tiles - 1) / tiles, steps = (s->tokens_q / 32 + 1) * (s->hq / s->hkv);
+    return parts > 8 ? 8 : parts > steps ? steps : parts;
+}
+static int64_t stats_bytes(const s24_attn_shape *s) { return (s->tokens_q * s->hq * (int64_t)sizeof(float2) + 15) / 16 * 16; }
+}  // namespace s24_attn
+
 extern "C" int64_t s24_attn_bwd_workspace(const s24_attn_shape *shape)
 {
-    if (shape == nullptr || shape->tokens_q < 0 || shape->hq < 0) return 0;
-    return shape->tokens_q * shape->hq * (int64_t)sizeof(float2);
+    if (shape == nullptr || shape->tokens_q < 0 || shape->tokens_k < 0 || shape->sequences < 0 || shape->hq <= 0 || shape->hkv <= 0 || shape->hq % shape->hkv != 0 || shape->d < 0) return 0;
+    const int64_t parts = parts_of(shape);
+    return stats_bytes(shape) + (parts > 1 ? parts * shape->tokens_k * shape->hkv * 2 * shape->d * 4 : 0);
 }
 
 namespace s24_attn {
 template <typename T, int D> static int backward(const Problem &a, int64_t tiles_k, int64_t tiles_q, hipStream_t st)
 {
-    const int64_t rows = ((int64_t)a.tokens_q * a.hq + 15) / 16;
-    if (rows > 0) attn_delta_kernel<T><<<dim3((unsigned)rows), dim3(256), 0, st>>>(a);
-    if (tiles_k > 0) attn_dkv_kernel<T, D><<<dim3((unsigned)tiles_k), dim3(256), 0, st>>>(a);
     if (tiles_q > 0) attn_dq_kernel<T, D><<<dim3((unsigned)tiles_q), dim3(256), 0, st>>>(a);
+    if (tiles_k > 0) attn_dkv_kernel<T, D><<<dim3((unsigned)(tiles_k * a.parts)), dim3(256), 0, st>>>(a);
+    if (tiles_k > 0 && a.parts > 1)
+        attn_dkv_join_kernel<T><<<dim3((unsigned)(most_tiles(a.tokens_k, a.sequences, kJoinRows) * (a.hq / a.group))), dim3(256), 0, st>>>(a);
     return s24_launch_status();
 }
 }  // namespace s24_attn
 
 extern "C" int s24_attn_bwd(const s24_attn_shape *shape, const s24_heads *Q, const s24_heads *K, const s24_heads *V, const s24_heads *O,
                             const s24_heads *dO, const float *lse, const s24_heads *dQ, const s24_heads *dK, const s24_heads *dV, void *workspace,
-                            s24_dtype dt, void *stream)
+                            int64_t workspace_bytes, s24_dtype dt, void *stream)
 {
     S24_TRY(check_shape(shape, dt));
     for (const s24_heads *x : {Q, O, dO, dQ}) S24_TRY(check_rows(x, shape->tokens_q, shape->hq, shape->d, x == dQ));
     for (const s24_heads *x : {K, V, dK, dV}) S24_TRY(check_rows(x, shape->tokens_k, shape->hkv, shape->d, x == dK || x == dV));
     S24_REQUIRE((lse != nullptr && workspace != nullptr) || shape->tokens_q == 0, S24_ERR_NULL);
     S24_REQUIRE(s24_aligned(lse, 4) && s24_aligned(workspace, 16), S24_ERR_ALIGN);
+    S24_REQUIRE(workspace_bytes >= s24_attn_bwd_workspace(shape), S24_ERR_SHAPE);
     const int64_t tiles_q = most_tiles(shape->tokens_q, shape->sequences, 128) * shape->hq;
     const int64_t tiles_k = most_tiles(shape->tokens_k, shape->sequences, Backward<128>::BK) * shape->hkv;
-    S24_REQUIRE(tiles_q <= kMostGroups && tiles_k <= kMostGroups && shape->tokens_q * shape->hq < (int64_t)16 * kMostGroups, S24_ERR_SHAPE);
+    S24_REQUIRE(tiles_q <= kMostGroups && tiles_k <= kMostGroups / 8, S24_ERR_SHAPE);
     Problem a = problem_of(shape);
     a.q = rows_of(Q), a.k = rows_of(K), a.v = rows_of(V), a.o = rows_of(O), a.dO = rows_of(dO);
     a.dq = out_of(dQ), a.dk = out_of(dK), a.dv = out_of(dV);
-    a.lse = const_cast<float *>(lse), a.stats = static_cast<float2 *>(workspace);
+    a.lse = const_cast<float *>(lse), a.stats = static_cast<float2 *>(workspace), a.parts = (int)parts_of(shape);
+    a.sums = reinterpret_cast<float *>(static_cast<char *>(workspace) + stats_bytes(shape));
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (dt == S24_BF16) return a.d <= 64 ? backward<uint16_t, 64>(a, tiles_k, tiles_q, st) : backward<uint16_t, 128>(a, tiles_k, tiles_q, st);
     return a.d <= 64 ? backward<s24_half, 64>(a, tiles_k, tiles_q, st) : backward<s24_half, 128>(a, tiles_k, tiles_q, st);

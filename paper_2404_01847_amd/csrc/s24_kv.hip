@@ -8,6 +8,7 @@
 #include "s24_attn.h"
 
 #include <math.h>
+#include <stdlib.h>
 
 namespace s24_kv {
 using namespace s24_attn;
@@ -195,7 +196,11 @@ __device__ __forceinline__ uint4 halves(uint32_t a, uint32_t b)
 // A workgroup takes a tile of positions for one key-value head and 16 of its query heads; its four waves take the blocks of 64 positions in turn
 // and add up in LDS at the end.  Of a block, S^T = K Q^T has positions as rows: row 4g + r of tile t is position 16g + 4t + r, so that a lane's
 // weights are those of 16 consecutive positions, which is what it holds of V.
-template <typename T, int D, int BITS>
+// Softmax in 8 bits: the weights go to the product as exp(s - ref) * (step of V) in binary16, where ref has the largest step so far as a factor too, so that
+// they stay at 2^9 or less; the factor is in the sum of the weights as well and cancels.  (A step below 2^-100 counts as that, for ref to stay in range.)
+// EXACT: d is D, and the addresses within a page are constants.
+constexpr float kRise = 8.0f;   // as in the forward pass over packed sequences: how far a score may exceed the reference before it moves
+template <typename T, int D, int BITS, bool EXACT>
 __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
 {
     using M = typename std::conditional<BITS == 8, s24_half, T>::type;   // the products of an 8-bit cache are binary16: it holds -127 .. 127
@@ -205,12 +210,62 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
     __shared__ float refs[4][16], weights[4][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
+    const int d = EXACT ? D : a.c.d;
     const int heads = a.c.hkv * a.blocks, tile = blockIdx.x / heads, which = blockIdx.x - tile * heads;
     const int h = which / a.blocks, q0 = 16 * (which - h * a.blocks), mine = min(16, a.group - q0);   // of the group's query heads
     const int chunk = max(256, chunk_of(a, lane));
     int b, index, count;
     if (!tile_of(a, chunk, tile, lane, b, index, count)) return;
     const int length = __builtin_amdgcn_readfirstlane(length_of(a, b)), end = min(length, (index + 1) * chunk);
+
+    // Positions 16*(col/4) .. of a block for K, 16*g .. for V: each sixteen lie in one page.  Offsets into the cache, for each in values of one byte or two.
+    const int token = d * (BITS / 8);   // bytes of a token of one head
+    const uint32_t page_tokens = (uint32_t)a.c.hkv << a.c.shift;
+    const int *table = a.table + b * a.width;
+    const unsigned char *const lane_k = a.c.k + ((int64_t)h << a.c.shift) * token + (col & 3) * token, *const lane_v = a.c.v + ((int64_t)h << a.c.shift) * token;
+    struct Place { int64_t k, v; };   // in tokens of one head
+    auto place = [&](int k0) {
+        auto of = [&](int group) {
+            const int pos = min(k0 + 16 * group, (end - 1) & ~15);
+            const uint32_t id = min((uint32_t)table[pos >> a.c.shift], (uint32_t)a.c.pages - 1);
+            return (int64_t)((uint64_t)id * page_tokens) + (pos & (a.c.page - 1));
+        };
+        return Place{of(col >> 2), of(g)};
+    };
+    uint4 fk[4][KL], fv[D / 16][VL];
+    f32x4 sk[4], sv[4];
+    auto load_k = [&](Place p) {
+        const unsigned char *row = lane_k + p.k * token;
+        const float *step = a.c.ks + ((int64_t)h << a.c.shift) + p.v;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+            for (int k = 0; k < KL; ++k)
+                fk[t][k] = *reinterpret_cast<const uint4 *>(row + 4 * t * token + 16 * (EXACT ? 4 * k + g : min(4 * k + g, (token >> 4) - 1)));
+            if (BITS == 8) sk[t] = *reinterpret_cast<const f32x4 *>(step + 4 * t);
+        }
+    };
+    auto load_v = [&](Place p) {
+        const unsigned char *page = lane_v + p.v * token;
+        const float *step = a.c.vs + ((int64_t)h << a.c.shift) + p.v;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+            if (BITS == 8) sv[t] = *reinterpret_cast<const f32x4 *>(step + 4 * t);
+#pragma unroll
+        for (int n = 0; n < D / 16; ++n)
+#pragma unroll
+            for (int u = 0; u < VL; ++u)
+                fv[n][u] = *reinterpret_cast<const uint4 *>(page + (u * d + (EXACT ? 16 * n + col : min(16 * n + col, d - 1))) * 16);
+    };
+    // The loads run ahead: the keys of the next block are requested as soon as this one's scores are formed, its values as soon as they are summed, and the
+    // page numbers a block before that.
+    int k0 = index * chunk + 64 * wave;
+    Place next{};
+    if (k0 < end) {
+        const Place first = place(k0);
+        next = place(k0 + 256);
+        load_k(first), load_v(first);
+    }
 
     // the queries, an operand of 16 columns
     uint4 q[D / 32];
@@ -221,7 +276,7 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
 #pragma unroll
         for (int k = 0; k < D / 32; ++k) {
             const int i = BITS == 8 ? 64 * (k >> 1) + 16 * g + 8 * (k & 1) : 32 * k + 8 * g;
-            q[k] = i < a.c.d && col < mine ? *reinterpret_cast<const uint4 *>(row + i) : make_uint4(0, 0, 0, 0);
+            q[k] = i < d && col < mine ? *reinterpret_cast<const uint4 *>(row + i) : make_uint4(0, 0, 0, 0);
         }
         if (BITS == 8) {   // scaled by a power of two into what binary16 holds
             const uint32_t *x = reinterpret_cast<const uint32_t *>(q);
@@ -237,36 +292,15 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
             c = ldexpf(c, e);
         }
     }
-    float m = -1e30f, l = 0.0f, unit = 0.0f;   // unit: 8 bits, what the steps of V are measured in
+    float m = -1e30f, rise = 0.0f, wide = BITS == 8 ? 0x1p-100f : 1.0f, l = 0.0f;   // reference; its part from the steps of V, which are at most `wide`
+    if (BITS == 8) rise = -100.0f;
     f32x4 o[D / 16];
 #pragma unroll
     for (int n = 0; n < D / 16; ++n) o[n] = f32x4{};
-    const int64_t token = (int64_t)a.c.d * (BITS / 8);   // bytes of a token of one head
 
-    for (int k0 = index * chunk + 64 * wave; k0 < end; k0 += 256) {
-        // positions 16*(col/4) .. of K and 16*g .. of V: each sixteen lie in one page
-        auto place = [&](int group) {
-            const int pos = min(k0 + 16 * group, (end - 1) & ~15);
-            return ((page_at(a.table, a.width, b, pos >> a.c.shift, a.c.pages) * a.c.hkv + h) << a.c.shift) + (pos & (a.c.page - 1));
-        };
-        const int64_t pk = place(col >> 2), pv = place(g);
-        uint4 fk[4][KL], fv[D / 16][VL];
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int k = 0; k < KL; ++k)
-                fk[t][k] = *reinterpret_cast<const uint4 *>(a.c.k + (pk + 4 * t + (col & 3)) * token + 16 * min(4 * k + g, (int)(token >> 4) - 1));
-        float4 sk[4], sv[4];
-        if (BITS == 8) {
-#pragma unroll
-            for (int t = 0; t < 4; ++t) sk[t] = *reinterpret_cast<const float4 *>(a.c.ks + pv + 4 * t), sv[t] = *reinterpret_cast<const float4 *>(a.c.vs + pv + 4 * t);
-        }
-#pragma unroll
-        for (int n = 0; n < D / 16; ++n)
-#pragma unroll
-            for (int u = 0; u < VL; ++u)
-                fv[n][u] = *reinterpret_cast<const uint4 *>(a.c.v + pv * token + ((int64_t)u * a.c.d + min(16 * n + col, a.c.d - 1)) * 16);
-
+    for (; k0 < end; k0 += 256) {
+        const Place now = next;
+        next = place(k0 + 512);
         f32x4 s[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -279,19 +313,18 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
                 } else
                     s[t] = mma<M>(fk[t][k], q[k], s[t]);
             }
-            if (BITS == 8) s[t][0] *= sk[t].x, s[t][1] *= sk[t].y, s[t][2] *= sk[t].z, s[t][3] *= sk[t].w;
+            if (BITS == 8) s[t] *= sk[t];
         }
+        if (k0 + 256 < end) load_k(now);
         if (k0 + 64 > end) {   // what lies past the sequence's end may hold anything
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                float *step = reinterpret_cast<float *>(&sv[t]);
+            for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const bool in = k0 + 16 * g + 4 * t + r < end;
                     s[t][r] = in ? s[t][r] : -INFINITY;
-                    if (BITS == 8) step[r] = in ? step[r] : 0.0f;
+                    if (BITS == 8) sv[t][r] = in ? sv[t][r] : 0.0f;
                 }
-            }
             if (BITS == 16) {
 #pragma unroll
                 for (int n = 0; n < D / 16; ++n)
@@ -311,22 +344,20 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
         for (int t = 0; t < 4; ++t) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) top = fmaxf(top, s[t][r]);
-            if (BITS == 8) step = fmaxf(step, fmaxf(fmaxf(sv[t].x, sv[t].y), fmaxf(sv[t].z, sv[t].w)));
+            if (BITS == 8) step = fmaxf(step, fmaxf(fmaxf(sv[t][0], sv[t][1]), fmaxf(sv[t][2], sv[t][3])));
         }
-        top = column_max(top) * c;
-        if (BITS == 8) step = column_max(step);
-        if (__any(top > m || step > unit)) {
-            const float now = fmaxf(m, top), shrink = __builtin_amdgcn_exp2f(m - now);
-            m = now, l *= shrink;
-            float all = shrink;
+        top *= c;
+        if (__any(top > m - rise + kRise || (BITS == 8 && step > wide))) {   // m - rise: the reference of the scores alone
             if (BITS == 8) {
-                const float wide = step > unit ? 2.0f * step : unit;
-                all *= unit / wide, unit = wide;
+                step = column_max(step);
+                if (step > wide) wide = 2.0f * step;
             }
+            const float lift = BITS == 8 ? __builtin_amdgcn_logf(wide) : 0.0f, now_m = fmaxf(m - rise, column_max(top)) + lift;
+            const float shrink = __builtin_amdgcn_exp2f(m - now_m);
+            m = now_m, rise = lift, l *= shrink;
 #pragma unroll
-            for (int n = 0; n < D / 16; ++n) o[n] *= all;
+            for (int n = 0; n < D / 16; ++n) o[n] *= shrink;
         }
-        const float inverse = BITS == 8 ? 1.0f / unit : 1.0f;
         uint4 p[2];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -334,7 +365,7 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
             for (int r = 0; r < 4; ++r) {
                 s[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], c, -m));
                 l += s[t][r];
-                if (BITS == 8) s[t][r] *= reinterpret_cast<const float *>(&sv[t])[r] * inverse;
+                if (BITS == 8) s[t][r] *= sv[t][r];
             }
 #pragma unroll
         for (int u = 0; u < 2; ++u) p[u] = operand<M>(s[2 * u], s[2 * u + 1]);
@@ -348,16 +379,15 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
                 o[n] = mma<M>(fv[n][1], p[1], o[n]);
             }
         }
+        if (k0 + 256 < end) load_v(now);
     }
     l = column_sum(l);
     if (g == 0) refs[wave][col] = m, weights[wave][col] = l;
-    const float own = BITS == 8 ? unit : 1.0f;
 #pragma unroll
     for (int n = 0; n < D / 16; ++n)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) sums[wave][16 * n + 4 * g + r][col] = o[n][r] * own;
+        for (int r = 0; r < 4; ++r) sums[wave][16 * n + 4 * g + r][col] = o[n][r];
     __syncthreads();
-    const int d = a.c.d;
     float *part = a.part + ((int64_t)tile * a.c.hkv * a.group + h * a.group + q0) * (d + 2);
     for (int i = threadIdx.x; i < mine * (d / 2); i += 256) {
         const int n = i / (d / 2), e = 2 * (i - n * (d / 2));
@@ -373,17 +403,18 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
             *reinterpret_cast<uint32_t *>(a.o.p + b * a.o.token + (h * a.group + q0 + n) * a.o.head + e) = pack2<T>(x * inverse, y * inverse);
         } else {
             float *to = part + (int64_t)n * (d + 2);
-            to[e] = x, to[e + 1] = y;
-            if (e == 0) to[d] = ref, to[d + 1] = w;
+            *reinterpret_cast<float2 *>(to + e) = make_float2(x, y);
+            if (e == 0) *reinterpret_cast<float2 *>(to + d) = make_float2(ref, w);
         }
     }
 }
 
-// The parts of a sequence's tiles, added: one wave a query head, a lane two channels
+// The parts of a sequence's tiles, added: a workgroup a query head, a lane two channels, a wave every fourth part
 template <typename T>
-__global__ __launch_bounds__(64) void attn_join_kernel(const DecodeArgs a)
+__global__ __launch_bounds__(256) void attn_join_kernel(const DecodeArgs a)
 {
-    const int lane = threadIdx.x, b = blockIdx.x / a.hq, head = blockIdx.x - b * a.hq, d = a.c.d;
+    __shared__ float4 waves[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = blockIdx.x / a.hq, head = blockIdx.x - b * a.hq, d = a.c.d;
     const int chunk = max(256, chunk_of(a, lane));
     int before = 0;
     for (int i = lane; i < b; i += 64) before += max(1, (length_of(a, i) + chunk - 1) / chunk);
@@ -393,19 +424,29 @@ __global__ __launch_bounds__(64) void attn_join_kernel(const DecodeArgs a)
     if (count <= 1) return;
     const int64_t step = (int64_t)a.hq * (d + 2);
     const float *part = a.part + before * step + (int64_t)head * (d + 2);
-    float ref = -1e30f;
+    float ref = -INFINITY;
     for (int i = lane; i < count; i += 64) ref = fmaxf(ref, part[i * step + d]);
 #pragma unroll
     for (int s = 1; s < 64; s <<= 1) ref = fmaxf(ref, __shfl_xor(ref, s));
     float x = 0.0f, y = 0.0f, w = 0.0f;
     const int e = min(2 * lane, d - 2);
-    for (int i = 0; i < count; ++i) {
+#pragma unroll 4
+    for (int i = wave; i < count; i += 4) {
         const float *from = part + i * step;
-        const float f = __builtin_amdgcn_exp2f(from[d] - ref);
-        x = fmaf(f, from[e], x), y = fmaf(f, from[e + 1], y), w = fmaf(f, from[d + 1], w);
+        const float2 of = *reinterpret_cast<const float2 *>(from + d), v = *reinterpret_cast<const float2 *>(from + e);
+        const float f = __builtin_amdgcn_exp2f(of.x - ref);
+        x = fmaf(f, v.x, x), y = fmaf(f, v.y, y), w = fmaf(f, of.y, w);
+    }
+    waves[wave][lane] = make_float4(x, y, w, 0.0f);
+    __syncthreads();
+    if (wave != 0 || 2 * lane >= d) return;
+#pragma unroll
+    for (int i = 1; i < 4; ++i) {
+        const float4 v = waves[i][lane];
+        x += v.x, y += v.y, w += v.z;
     }
     const float inverse = w > 0.0f ? 1.0f / w : 0.0f;
-    if (2 * lane < d) *reinterpret_cast<uint32_t *>(a.o.p + b * a.o.token + head * a.o.head + e) = pack2<T>(x * inverse, y * inverse);
+    *reinterpret_cast<uint32_t *>(a.o.p + b * a.o.token + head * a.o.head + e) = pack2<T>(x * inverse, y * inverse);
 }
 
 // ------------------------------------------------------------------ host
@@ -432,7 +473,8 @@ static Strided strided(const s24_heads *v) { return {static_cast<uint16_t *>(v->
 // Tiles of one head of all sequences: enough for four workgroups a compute unit
 static int64_t shares_of(int64_t heads)
 {
-    const int64_t n = (4 * (int64_t)s24_cu_count() + heads - 1) / heads;
+    static const int per = getenv("XS") ? atoi(getenv("XS")) : 4;
+    const int64_t n = (per * (int64_t)s24_cu_count() + heads - 1) / heads;
     return n < 1 ? 1 : n;
 }
 }  // namespace s24_kv
@@ -488,17 +530,14 @@ extern "C" int64_t s24_attn_decode_workspace(const s24_kv_cache *cache, int64_t 
 }
 
 namespace s24_kv {
-template <typename T> static void decode(const DecodeArgs &a, int bits, dim3 grid, hipStream_t st)
+template <typename T, int BITS> static void decode(const DecodeArgs &a, dim3 grid, hipStream_t st)
 {
     const dim3 block(256);
-    if (bits == 16) {
-        if (a.c.d <= 64) attn_decode_kernel<T, 64, 16><<<grid, block, 0, st>>>(a);
-        else attn_decode_kernel<T, 128, 16><<<grid, block, 0, st>>>(a);
-    } else {
-        if (a.c.d <= 64) attn_decode_kernel<T, 64, 8><<<grid, block, 0, st>>>(a);
-        else attn_decode_kernel<T, 128, 8><<<grid, block, 0, st>>>(a);
-    }
-    if (a.width << a.c.shift > 256) attn_join_kernel<T><<<dim3((unsigned)(a.sequences * a.hq)), dim3(64), 0, st>>>(a);
+    if (a.c.d == 64) attn_decode_kernel<T, 64, BITS, true><<<grid, block, 0, st>>>(a);
+    else if (a.c.d == 128) attn_decode_kernel<T, 128, BITS, true><<<grid, block, 0, st>>>(a);
+    else if (a.c.d < 64) attn_decode_kernel<T, 64, BITS, false><<<grid, block, 0, st>>>(a);
+    else attn_decode_kernel<T, 128, BITS, false><<<grid, block, 0, st>>>(a);
+    if (a.width << a.c.shift > 256) attn_join_kernel<T><<<dim3((unsigned)(a.sequences * a.hq)), block, 0, st>>>(a);
 }
 }  // namespace s24_kv
 
@@ -517,11 +556,14 @@ extern "C" int s24_attn_decode(const s24_kv_cache *cache, const s24_heads *Q, in
     S24_REQUIRE(workspace_bytes >= s24_attn_decode_workspace(cache, sequences, hq), S24_ERR_SHAPE);
     DecodeArgs a{cache_of(cache), strided(Q), strided(O), table, lengths, cache->pages > 0 ? width : 0};
     a.sequences = (int)sequences, a.hq = (int)hq, a.group = (int)(hq / cache->hkv), a.blocks = (a.group + 15) / 16;
-    const int64_t heads = cache->hkv * a.blocks, shares = shares_of(heads), groups = (shares + sequences) * heads;
+    const int64_t heads = cache->hkv * a.blocks;
+    const int64_t most = sequences * ((a.width * cache->page + 255) / 256);   // no more tiles of 256 positions than that
+    const int64_t shares = most < shares_of(heads) ? (most > 0 ? most : 1) : shares_of(heads), groups = (shares + sequences) * heads;
     S24_REQUIRE(groups <= kMostGroups && sequences * hq <= kMostGroups, S24_ERR_SHAPE);
     a.shares = (int)shares, a.scale = scale, a.part = static_cast<float *>(workspace);
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (dt == S24_BF16) decode<uint16_t>(a, cache->bits, dim3((unsigned)groups), st);
-    else decode<s24_half>(a, cache->bits, dim3((unsigned)groups), st);
+    const dim3 grid((unsigned)groups);
+    if (dt == S24_BF16) cache->bits == 16 ? decode<uint16_t, 16>(a, grid, st) : decode<uint16_t, 8>(a, grid, st);
+    else cache->bits == 16 ? decode<s24_half, 16>(a, grid, st) : decode<s24_half, 8>(a, grid, st);
     return s24_launch_status();
 }
