@@ -391,7 +391,8 @@ int s24_kv_read(const s24_kv_cache *cache, const int32_t *table, int64_t width, 
                 const s24_heads *K, const s24_heads *V, s24_dtype dt, void *stream);
 
 /* Attention of one new token of each sequence: O[i] = softmax(c Q[i].K) V over the first lengths[i] (device) positions of sequence i, of all of
- * them, its own included; Q and O have one row a sequence.  Zeros where lengths[i] is 0; lengths beyond width*page are cut.  In an 8-bit cache
+ * them, its own included; Q and O have one row a sequence.  Zeros where lengths[i] is 0; lengths beyond width*page are cut.  sequences*width*page
+ * below 2^31 (S24_ERR_SHAPE).  In an 8-bit cache
  * the products are binary16, of the whole numbers as they are, of the queries scaled by a power of two, and of the weights times the steps of V.
  *   workspace  device, s24_attn_decode_workspace(cache, sequences, hq) bytes, 16-byte aligned; holds nothing between calls */
 int64_t s24_attn_decode_workspace(const s24_kv_cache *cache, int64_t sequences, int64_t hq);

@@ -117,30 +117,41 @@ __device__ __forceinline__ Span span(const int *cu, int i, int tokens)
     return {a, b - a};
 }
 
-// The sequence that tile t belongs to, and which of its tiles it is, where a sequence of n rows has ceil(n / rows) tiles; false past the last.
-// Every wave looks for itself, 64 sequences at a time.
-__device__ __forceinline__ bool find_tile(const int *cu, int sequences, int tokens, int rows, int t, int lane, int &sequence, int &index, int &count)
+// Sum over this lane and those before it: within rows of 16, then from row to row, in the vector registers
+__device__ __forceinline__ int running_sum(int x)
 {
-    for (int base = 0; base < sequences; base += 64) {
-        const int i = base + lane;
-        const int n = i < sequences ? (span(cu, i, tokens).count + rows - 1) / rows : 0;
-        int sum = n;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int other = __shfl_up(sum, d);
-            if (lane >= d) sum += other;
-        }
+#if defined(__HIP_DEVICE_COMPILE__)
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // the last lane of a row to the next
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // of the first half to the second
+#endif
+    return x;
+}
+// Item t of lists that lie one after the other, `sizes(i)` long for i = 0 .. n - 1: its list, its place in it and the list's length; false past the last.
+// Every wave looks for itself, 64 lists at a time.
+template <typename Sizes> __device__ __forceinline__ bool find_item(int n, int t, int lane, int &list, int &place, int &length, Sizes sizes)
+{
+    for (int base = 0; base < n; base += 64) {
+        const int size = base + lane < n ? sizes(base + lane) : 0, sum = running_sum(size);
         const unsigned long long past = __ballot(t < sum);
         if (past != 0) {
             const int owner = __ffsll(past) - 1;
-            sequence = __builtin_amdgcn_readfirstlane(base + owner);
-            count = __builtin_amdgcn_readlane(n, owner);
-            index = t - (__builtin_amdgcn_readlane(sum, owner) - count);
+            list = __builtin_amdgcn_readfirstlane(base + owner);
+            length = __builtin_amdgcn_readlane(size, owner);
+            place = t - (__builtin_amdgcn_readlane(sum, owner) - length);
             return true;
         }
         t -= __builtin_amdgcn_readlane(sum, 63);
     }
     return false;
+}
+// The sequence that tile t belongs to, and which of its tiles it is, where a sequence of n rows has ceil(n / rows) tiles
+__device__ __forceinline__ bool find_tile(const int *cu, int sequences, int tokens, int rows, int t, int lane, int &sequence, int &index, int &count)
+{
+    return find_item(sequences, t, lane, sequence, index, count, [&](int i) { return (span(cu, i, tokens).count + rows - 1) / rows; });
 }
 
 // Workgroups are dealt round-robin to the eight XCDs: head of the workgroup at place s of a row of `heads`, such that an XCD has neighbouring ones, which

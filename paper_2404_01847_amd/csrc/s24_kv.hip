@@ -138,48 +138,21 @@ struct DecodeArgs {
     Strided q, o;
     const int *table, *lengths;
     int64_t width;
-    int sequences, hq, group, blocks, shares;   // blocks: of 16 query heads in a group; shares: of all positions of all sequences
+    int sequences, hq, group, sixteens, shares;   // sixteens: of query heads in a group; shares: of the positions of all sequences, for each of the heads
     float scale;
-    float *part;   // [tile][head of the tile][d + 2]: sums, reference, weight
+    float *part;   // [2 shares][hq][d + 4]: sums, reference, weight, and two unused
 };
-__device__ __forceinline__ int length_of(const DecodeArgs &a, int b)
+__device__ __forceinline__ int length_of(const DecodeArgs &a, int b) { return min(max(a.lengths[b], 0), (int)(a.width << a.c.shift)); }
+// The sequences' blocks of 64 positions lie one after the other and are shared out evenly, whatever sequences they belong to: share p has blocks p*each ..
+// (p + 1)*each - 1 of them.  A sequence that lies within one share is finished there.  Of others each share leaves the sums of its part: at 2p if the sequence
+// starts no later than the share, at 2p + 1 otherwise (a share has one such part at either end, at most).
+__device__ __forceinline__ int blocks_of(int length) { return (length + 63) >> 6; }
+__device__ __forceinline__ int total_blocks(const DecodeArgs &a, int before, int lane)   // of the sequences before that one
 {
-    const int64_t most = a.width << a.c.shift;
-    return (int)min((int64_t)max(a.lengths[b], 0), most);
-}
-// Positions are shared out evenly: every sequence is cut into tiles of `chunk` positions, chosen so that there are at most `shares` tiles and
-// one for each sequence.
-__device__ __forceinline__ int chunk_of(const DecodeArgs &a, int lane)
-{
-    int64_t total = 0;
-    for (int b = lane; b < a.sequences; b += 64) total += length_of(a, b);
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) total += __shfl_xor(total, s);
-    const int64_t each = (total + a.shares - 1) / a.shares;
-    return (int)min((each + 255) / 256 * 256, (int64_t)0x7FFFFF00);
-}
-// Tile t of the sequences' tiles; `before` those of earlier sequences
-__device__ __forceinline__ bool tile_of(const DecodeArgs &a, int chunk, int t, int lane, int &sequence, int &index, int &count)
-{
-    for (int base = 0; base < a.sequences; base += 64) {
-        const int b = base + lane;
-        const int n = b < a.sequences ? max(1, (length_of(a, b) + chunk - 1) / chunk) : 0;   // an empty sequence has a tile too: it writes zeros
-        int sum = n;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int other = __shfl_up(sum, d);
-            if (lane >= d) sum += other;
-        }
-        const unsigned long long past = __ballot(t < sum);
-        if (past != 0) {
-            const int owner = __ffsll(past) - 1;
-            sequence = __builtin_amdgcn_readfirstlane(base + owner), count = __builtin_amdgcn_readlane(n, owner);
-            index = t - (__builtin_amdgcn_readlane(sum, owner) - count);
-            return true;
-        }
-        t -= __builtin_amdgcn_readlane(sum, 63);
-    }
-    return false;
+    int total = 0;   // below 2^31, as the host has seen to
+    for (int base = 0; base < before; base += 64)
+        total += __builtin_amdgcn_readlane(running_sum(base + lane < before ? blocks_of(length_of(a, base + lane)) : 0), 63);
+    return total;
 }
 
 // Sixteen bytes of the cache as operands of 8 channels (tokens) each
@@ -193,8 +166,8 @@ __device__ __forceinline__ uint4 halves(uint32_t a, uint32_t b)
     return make_uint4(two(a, 0x00050004u), two(a, 0x00070006u), two(b, 0x00050004u), two(b, 0x00070006u));
 }
 
-// A workgroup takes a tile of positions for one key-value head and 16 of its query heads; its four waves take the blocks of 64 positions in turn
-// and add up in LDS at the end.  Of a block, S^T = K Q^T has positions as rows: row 4g + r of tile t is position 16g + 4t + r, so that a lane's
+// A wave takes a tile of positions for one key-value head and 16 of its query heads, in blocks of 64; the four of a workgroup know nothing of each other.
+// Of a block, S^T = K Q^T has positions as rows: row 4g + r of tile t is position 16g + 4t + r, so that a lane's
 // weights are those of 16 consecutive positions, which is what it holds of V.
 // Softmax in 8 bits: the weights go to the product as exp(s - ref) * (step of V) in binary16, where ref has the largest step so far as a factor too, so that
 // they stay at 2^9 or less; the factor is in the sum of the weights as well and cancels.  (A step below 2^-100 counts as that, for ref to stay in range.)
@@ -206,27 +179,40 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
     using M = typename std::conditional<BITS == 8, s24_half, T>::type;   // the products of an 8-bit cache are binary16: it holds -127 .. 127
     using Num = s24_num<T>;
     constexpr int KL = BITS == 8 ? D / 64 : D / 32, VL = BITS == 8 ? 1 : 2;   // 16-byte loads of a key; of a channel's positions
-    __shared__ float sums[4][D][17];
-    __shared__ float refs[4][16], weights[4][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
     const int d = EXACT ? D : a.c.d;
-    const int heads = a.c.hkv * a.blocks, tile = blockIdx.x / heads, which = blockIdx.x - tile * heads;
-    const int h = which / a.blocks, q0 = 16 * (which - h * a.blocks), mine = min(16, a.group - q0);   // of the group's query heads
-    const int chunk = max(256, chunk_of(a, lane));
-    int b, index, count;
-    if (!tile_of(a, chunk, tile, lane, b, index, count)) return;
-    const int length = __builtin_amdgcn_readfirstlane(length_of(a, b)), end = min(length, (index + 1) * chunk);
+    const int heads = a.c.hkv * a.sixteens, item = 4 * blockIdx.x + wave, share = item / heads, which = item - share * heads;
+    const int h = which / a.sixteens, q0 = 16 * (which - h * a.sixteens), mine = min(16, a.group - q0);   // of the group's query heads
+    const int total = total_blocks(a, a.sequences, lane), each = (total + a.shares - 1) / a.shares, begin = share * each;
+    const int steps = min(total - begin, each);
+    if (share >= a.shares || steps <= 0) return;
+    struct Cursor { int b, first, pos, length; };   // a block: its sequence, which has `first` as its first block; the position at which it starts
+    auto advance = [&](Cursor c) {
+        c.pos += 64;
+        if (c.pos < c.length) return c;
+        c.first += blocks_of(c.length), c.pos = 0;
+        do {   // there is one more: only blocks of the share are asked for
+            c.length = __builtin_amdgcn_readfirstlane(length_of(a, ++c.b));
+        } while (c.length == 0);
+        return c;
+    };
+    Cursor now;
+    {
+        int place, count;
+        find_item(a.sequences, begin, lane, now.b, place, count, [&](int i) { return blocks_of(length_of(a, i)); });
+        now.first = begin - place, now.pos = 64 * place, now.length = __builtin_amdgcn_readfirstlane(length_of(a, now.b));
+    }
 
     // Positions 16*(col/4) .. of a block for K, 16*g .. for V: each sixteen lie in one page.  Offsets into the cache, for each in values of one byte or two.
     const int token = d * (BITS / 8);   // bytes of a token of one head
     const uint32_t page_tokens = (uint32_t)a.c.hkv << a.c.shift;
-    const int *table = a.table + b * a.width;
     const unsigned char *const lane_k = a.c.k + ((int64_t)h << a.c.shift) * token + (col & 3) * token, *const lane_v = a.c.v + ((int64_t)h << a.c.shift) * token;
     struct Place { int64_t k, v; };   // in tokens of one head
-    auto place = [&](int k0) {
+    auto place = [&](const Cursor &at) {
+        const int *table = a.table + at.b * a.width;
         auto of = [&](int group) {
-            const int pos = min(k0 + 16 * group, (end - 1) & ~15);
+            const int pos = min(at.pos + 16 * group, (at.length - 1) & ~15);
             const uint32_t id = min((uint32_t)table[pos >> a.c.shift], (uint32_t)a.c.pages - 1);
             return (int64_t)((uint64_t)id * page_tokens) + (pos & (a.c.page - 1));
         };
@@ -257,22 +243,13 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
             for (int u = 0; u < VL; ++u)
                 fv[n][u] = *reinterpret_cast<const uint4 *>(page + (u * d + (EXACT ? 16 * n + col : min(16 * n + col, d - 1))) * 16);
     };
-    // The loads run ahead: the keys of the next block are requested as soon as this one's scores are formed, its values as soon as they are summed, and the
-    // page numbers a block before that.
-    int k0 = index * chunk + 64 * wave;
-    Place next{};
-    if (k0 < end) {
-        const Place first = place(k0);
-        next = place(k0 + 256);
-        load_k(first), load_v(first);
-    }
-
     // the queries, an operand of 16 columns
     uint4 q[D / 32];
-    float c = a.scale * kLog2e;
-    {
+    float c = 0.0f;
+    auto load_q = [&](int b) {
         const uint16_t *row = a.q.p + b * a.q.token + (h * a.group + q0 + min(col, mine - 1)) * a.q.head;
         float most = 0.0f;
+        c = a.scale * kLog2e;
 #pragma unroll
         for (int k = 0; k < D / 32; ++k) {
             const int i = BITS == 8 ? 64 * (k >> 1) + 16 * g + 8 * (k & 1) : 32 * k + 8 * g;
@@ -291,16 +268,30 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
             for (int k = 0; k < D / 32; ++k) q[k] = make_uint4(y[4 * k], y[4 * k + 1], y[4 * k + 2], y[4 * k + 3]);
             c = ldexpf(c, e);
         }
+    };
+    // The loads run ahead: the keys of the next block are requested as soon as this one's scores are formed, its values as soon as they are summed, and the
+    // page numbers a block before that.
+    Cursor ahead = now;
+    Place next{};
+    {
+        const Place first = place(now);
+        if (steps > 1) ahead = advance(now), next = place(ahead);
+        load_k(first), load_v(first);
+        load_q(now.b);
     }
-    float m = -1e30f, rise = 0.0f, wide = BITS == 8 ? 0x1p-100f : 1.0f, l = 0.0f;   // reference; its part from the steps of V, which are at most `wide`
-    if (BITS == 8) rise = -100.0f;
+    float m, rise, wide, l;   // reference; its part from the steps of V, which are at most `wide`; sum of the weights
     f32x4 o[D / 16];
+    auto clear = [&] {
+        m = -1e30f, rise = BITS == 8 ? -100.0f : 0.0f, wide = 0x1p-100f, l = 0.0f;
 #pragma unroll
-    for (int n = 0; n < D / 16; ++n) o[n] = f32x4{};
-
-    for (; k0 < end; k0 += 256) {
-        const Place now = next;
-        next = place(k0 + 512);
+        for (int n = 0; n < D / 16; ++n) o[n] = f32x4{};
+    };
+    clear();
+    for (int i = 0; i < steps; ++i) {
+        const Place coming = next;
+        const Cursor after = ahead;
+        if (i + 2 < steps) ahead = advance(ahead), next = place(ahead);
+        const int k0 = now.pos, end = now.length;
         f32x4 s[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -315,7 +306,7 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
             }
             if (BITS == 8) s[t] *= sk[t];
         }
-        if (k0 + 256 < end) load_k(now);
+        if (i + 1 < steps) load_k(coming);
         if (k0 + 64 > end) {   // what lies past the sequence's end may hold anything
 #pragma unroll
             for (int t = 0; t < 4; ++t)
@@ -379,60 +370,68 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
                 o[n] = mma<M>(fv[n][1], p[1], o[n]);
             }
         }
-        if (k0 + 256 < end) load_v(now);
-    }
-    l = column_sum(l);
-    if (g == 0) refs[wave][col] = m, weights[wave][col] = l;
-#pragma unroll
-    for (int n = 0; n < D / 16; ++n)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) sums[wave][16 * n + 4 * g + r][col] = o[n][r];
-    __syncthreads();
-    float *part = a.part + ((int64_t)tile * a.c.hkv * a.group + h * a.group + q0) * (d + 2);
-    for (int i = threadIdx.x; i < mine * (d / 2); i += 256) {
-        const int n = i / (d / 2), e = 2 * (i - n * (d / 2));
-        const float ref = fmaxf(fmaxf(refs[0][n], refs[1][n]), fmaxf(refs[2][n], refs[3][n]));
-        float x = 0.0f, y = 0.0f, w = 0.0f;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float f = __builtin_amdgcn_exp2f(refs[k][n] - ref);
-            x = fmaf(f, sums[k][e][n], x), y = fmaf(f, sums[k][e + 1][n], y), w = fmaf(f, weights[k][n], w);
+        if (i + 1 < steps) load_v(coming);
+
+        if (k0 + 64 < end && i + 1 < steps) {   // more of this sequence
+            now = after;
+            continue;
         }
-        if (count == 1) {
-            const float inverse = w > 0.0f ? 1.0f / w : 0.0f;
-            *reinterpret_cast<uint32_t *>(a.o.p + b * a.o.token + (h * a.group + q0 + n) * a.o.head + e) = pack2<T>(x * inverse, y * inverse);
+        l = column_sum(l);
+        const int head = h * a.group + q0 + col;
+        if (now.first >= begin && now.first + blocks_of(end) <= begin + each) {
+            const float inverse = l > 0.0f ? 1.0f / l : 0.0f;
+            uint16_t *out = a.o.p + now.b * a.o.token + head * a.o.head;
+            if (col < mine) {
+#pragma unroll
+                for (int n = 0; n < D / 16; ++n)
+                    if (EXACT || 16 * n < d)
+                        *reinterpret_cast<uint2 *>(out + 16 * n + 4 * g) =
+                            make_uint2(pack2<T>(o[n][0] * inverse, o[n][1] * inverse), pack2<T>(o[n][2] * inverse, o[n][3] * inverse));
+            }
         } else {
-            float *to = part + (int64_t)n * (d + 2);
-            *reinterpret_cast<float2 *>(to + e) = make_float2(x, y);
-            if (e == 0) *reinterpret_cast<float2 *>(to + d) = make_float2(ref, w);
+            float *to = a.part + ((int64_t)(2 * share + (now.first > begin)) * a.hq + head) * (d + 4);
+            if (col < mine) {
+#pragma unroll
+                for (int n = 0; n < D / 16; ++n)
+                    if (EXACT || 16 * n < d) *reinterpret_cast<f32x4 *>(to + 16 * n + 4 * g) = o[n];
+                if (g == 0) *reinterpret_cast<float2 *>(to + d) = make_float2(m, l);
+            }
+        }
+        if (i + 1 < steps) {
+            now = after;
+            clear();
+            load_q(now.b);
         }
     }
 }
 
-// The parts of a sequence's tiles, added: a workgroup a query head, a lane two channels, a wave every fourth part
+// The parts of a sequence that lies in more than one share, added: a workgroup a query head, a lane two channels, a wave every fourth part.
+// A sequence of no positions, which no share has, gets its zeros.
 template <typename T>
 __global__ __launch_bounds__(256) void attn_join_kernel(const DecodeArgs a)
 {
     __shared__ float4 waves[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = blockIdx.x / a.hq, head = blockIdx.x - b * a.hq, d = a.c.d;
-    const int chunk = max(256, chunk_of(a, lane));
-    int before = 0;
-    for (int i = lane; i < b; i += 64) before += max(1, (length_of(a, i) + chunk - 1) / chunk);
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) before += __shfl_xor(before, s);
-    const int count = (length_of(a, b) + chunk - 1) / chunk;
-    if (count <= 1) return;
-    const int64_t step = (int64_t)a.hq * (d + 2);
-    const float *part = a.part + before * step + (int64_t)head * (d + 2);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), b = blockIdx.x / a.hq, head = blockIdx.x - b * a.hq, d = a.c.d;
+    const int e = min(2 * lane, d - 2), length = length_of(a, b);
+    uint32_t *out = reinterpret_cast<uint32_t *>(a.o.p + b * a.o.token + head * a.o.head + e);
+    if (length == 0) {
+        if (wave == 0 && 2 * lane < d) *out = 0;
+        return;
+    }
+    const int each = (total_blocks(a, a.sequences, lane) + a.shares - 1) / a.shares, first = total_blocks(a, b, lane), last = first + blocks_of(length) - 1;
+    const int p0 = first / each, count = last / each - p0 + 1;
+    if (count == 1) return;
+    const int64_t step = 2 * (int64_t)a.hq * (d + 4);
+    const float *part = a.part + p0 * step + (int64_t)head * (d + 4);
+    const float *part0 = first > p0 * each ? part + (step >> 1) : part;   // of the first share, where the sequence may start late
     float ref = -INFINITY;
-    for (int i = lane; i < count; i += 64) ref = fmaxf(ref, part[i * step + d]);
+    for (int i = lane; i < count; i += 64) ref = fmaxf(ref, (i == 0 ? part0 : part + i * step)[d]);
 #pragma unroll
     for (int s = 1; s < 64; s <<= 1) ref = fmaxf(ref, __shfl_xor(ref, s));
     float x = 0.0f, y = 0.0f, w = 0.0f;
-    const int e = min(2 * lane, d - 2);
 #pragma unroll 4
     for (int i = wave; i < count; i += 4) {
-        const float *from = part + i * step;
+        const float *from = i == 0 ? part0 : part + i * step;
         const float2 of = *reinterpret_cast<const float2 *>(from + d), v = *reinterpret_cast<const float2 *>(from + e);
         const float f = __builtin_amdgcn_exp2f(of.x - ref);
         x = fmaf(f, v.x, x), y = fmaf(f, v.y, y), w = fmaf(f, of.y, w);
@@ -446,7 +445,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const DecodeArgs a)
         x += v.x, y += v.y, w += v.z;
     }
     const float inverse = w > 0.0f ? 1.0f / w : 0.0f;
-    *reinterpret_cast<uint32_t *>(a.o.p + b * a.o.token + head * a.o.head + e) = pack2<T>(x * inverse, y * inverse);
+    *out = pack2<T>(x * inverse, y * inverse);
 }
 
 // ------------------------------------------------------------------ host
@@ -470,11 +469,11 @@ static Cache cache_of(const s24_kv_cache *c)
 }
 static Strided strided(const s24_heads *v) { return {static_cast<uint16_t *>(v->data), v->token, v->head}; }
 
-// Tiles of one head of all sequences: enough for four workgroups a compute unit
-static int64_t shares_of(int64_t heads)
+// Shares of the positions for each of `heads` products: as many waves as the device holds at a time.
+static int64_t shares_of(int64_t heads, int64_t d)
 {
-    static const int per = getenv("XS") ? atoi(getenv("XS")) : 4;
-    const int64_t n = (per * (int64_t)s24_cu_count() + heads - 1) / heads;
+    static const int x8 = getenv("XS") ? atoi(getenv("XS")) : 8;
+    const int64_t n = ((d <= 64 ? x8 * 3 / 2 : x8) * (int64_t)s24_cu_count()) / heads;
     return n < 1 ? 1 : n;
 }
 }  // namespace s24_kv
@@ -526,7 +525,7 @@ extern "C" int s24_kv_read(const s24_kv_cache *cache, const int32_t *table, int6
 extern "C" int64_t s24_attn_decode_workspace(const s24_kv_cache *cache, int64_t sequences, int64_t hq)
 {
     if (cache == nullptr || cache->hkv <= 0 || sequences < 0 || hq <= 0 || hq % cache->hkv != 0) return 0;
-    return (shares_of(cache->hkv * ((hq / cache->hkv + 15) / 16)) + sequences) * hq * (cache->d + 2) * 4;
+    return 2 * shares_of(cache->hkv * ((hq / cache->hkv + 15) / 16), cache->d) * hq * (cache->d + 4) * 4;
 }
 
 namespace s24_kv {
@@ -537,7 +536,7 @@ template <typename T, int BITS> static void decode(const DecodeArgs &a, dim3 gri
     else if (a.c.d == 128) attn_decode_kernel<T, 128, BITS, true><<<grid, block, 0, st>>>(a);
     else if (a.c.d < 64) attn_decode_kernel<T, 64, BITS, false><<<grid, block, 0, st>>>(a);
     else attn_decode_kernel<T, 128, BITS, false><<<grid, block, 0, st>>>(a);
-    if (a.width << a.c.shift > 256) attn_join_kernel<T><<<dim3((unsigned)(a.sequences * a.hq)), block, 0, st>>>(a);
+    attn_join_kernel<T><<<dim3((unsigned)(a.sequences * a.hq)), block, 0, st>>>(a);
 }
 }  // namespace s24_kv
 
@@ -546,7 +545,7 @@ extern "C" int s24_attn_decode(const s24_kv_cache *cache, const s24_heads *Q, in
 {
     S24_TRY(check_cache(cache, dt));
     S24_REQUIRE(sequences >= 0 && sequences < INT32_MAX / 2 && width >= 0 && width < INT32_MAX && hq > 0 && hq < 65536 && hq % cache->hkv == 0, S24_ERR_SHAPE);
-    S24_REQUIRE(width * cache->page < INT32_MAX - 256, S24_ERR_SHAPE);
+    S24_REQUIRE(width * cache->page <= (int64_t)1 << 30 && sequences * width * cache->page < INT32_MAX, S24_ERR_SHAPE);
     S24_REQUIRE(scale > 0.0f && scale <= 3.0e38f, S24_ERR_SHAPE);
     S24_TRY(check_rows(Q, sequences, hq, cache->d, false));
     S24_TRY(check_rows(O, sequences, hq, cache->d, true));
@@ -555,11 +554,12 @@ extern "C" int s24_attn_decode(const s24_kv_cache *cache, const s24_heads *Q, in
     S24_REQUIRE(s24_aligned(table, 4) && s24_aligned(lengths, 4) && s24_aligned(workspace, 16), S24_ERR_ALIGN);
     S24_REQUIRE(workspace_bytes >= s24_attn_decode_workspace(cache, sequences, hq), S24_ERR_SHAPE);
     DecodeArgs a{cache_of(cache), strided(Q), strided(O), table, lengths, cache->pages > 0 ? width : 0};
-    a.sequences = (int)sequences, a.hq = (int)hq, a.group = (int)(hq / cache->hkv), a.blocks = (a.group + 15) / 16;
-    const int64_t heads = cache->hkv * a.blocks;
-    const int64_t most = sequences * ((a.width * cache->page + 255) / 256);   // no more tiles of 256 positions than that
-    const int64_t shares = most < shares_of(heads) ? (most > 0 ? most : 1) : shares_of(heads), groups = (shares + sequences) * heads;
-    S24_REQUIRE(groups <= kMostGroups && sequences * hq <= kMostGroups, S24_ERR_SHAPE);
+    a.sequences = (int)sequences, a.hq = (int)hq, a.group = (int)(hq / cache->hkv), a.sixteens = (a.group + 15) / 16;
+    const int64_t heads = cache->hkv * a.sixteens;
+    // (No more than there are blocks: for a few short sequences the host knows of fewer.)
+    const int64_t most = sequences * ((a.width * cache->page + 63) / 64), fit = shares_of(heads, cache->d), shares = most < fit ? (most > 0 ? most : 1) : fit;
+    const int64_t groups = (shares * heads + 3) / 4;
+    S24_REQUIRE(sequences * hq <= kMostGroups, S24_ERR_SHAPE);
     a.shares = (int)shares, a.scale = scale, a.part = static_cast<float *>(workspace);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const dim3 grid((unsigned)groups);
