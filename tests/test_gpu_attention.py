@@ -395,3 +395,68 @@ def test_a_prompt_in_chunks_gives_what_the_whole_gives(s24):
     cache.attend(Q[-1:].contiguous(), table, gpu_i32([n]), O)
     assert_within(O, ref["O"][-1:], bound["O"][-1:], "last token")
     assert_within(whole, ref["O"], bound["O"], "whole")
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("d,hkv", [(64, 5), (64, 12), (128, 8), (80, 3), (16, 4)])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_many_tokens_of_sequences_that_start_anywhere(s24, d, hkv, dtype, bits):
+    """Enough tokens for the kernel that takes runs: continued sequences of odd lengths, single tokens, padding between them, tokens out of order; what was
+    in the pages stays."""
+    from paper_2404_01847_amd.attention import PagedKV
+    rng, page = random.Random(d + bits), 32
+    past = [rng.choice([0, 1, 15, 16, 17, 40]) for _ in range(400)]
+    new = [rng.choice([1, 2, 15, 16, 17, 31, 100, 130]) for _ in past]
+    lens = [a + b for a, b in zip(past, new)]
+    counts = [-(-n // page) for n in lens]
+    order = list(range(sum(counts)))
+    rng.shuffle(order)
+    table, places, at = torch.zeros((len(lens), max(counts)), dtype=torch.int32), [], 0
+    for i, k in enumerate(counts):
+        table[i, :k] = torch.tensor(order[at:at + k], dtype=torch.int32)
+        places.append([order[at + j // page] * page + j % page for j in range(lens[i])])
+        at += k
+    cu, n = offsets(lens), sum(lens)
+    K, V = normal((n, hkv, d), dtype, 1), normal((n, hkv, d), dtype, 2)
+    cache = PagedKV(len(order), page, hkv, d, dtype, bits=bits)
+    flat = torch.tensor([p for x in places for p in x], dtype=torch.int64, device="cuda")
+    old = torch.tensor([j < past[i] for i in range(len(lens)) for j in range(lens[i])], device="cuda")
+    cache.write(K[old].contiguous(), V[old].contiguous(), flat[old].contiguous())
+    rows = torch.nonzero(~old)[:, 0]
+    half = len(rows) // 2
+    back = rows[half:half + 1000].flip(0)                       # some of the tokens come in descending order
+    rows = torch.cat([rows[:half], back, rows[half + 1000:]])
+    gaps = torch.full((len(rows) * 2,), -1, dtype=torch.int64, device="cuda")
+    keep = torch.ones(len(gaps), dtype=torch.bool, device="cuda")
+    keep[2 * half - 3000:2 * half] = False                      # padding among them: every second row there
+    index = torch.arange(len(rows), device="cuda")
+    index = index + torch.clamp(index - (half - 500), 0, 1000)
+    K2, V2 = (torch.full((int(index.max()) + 8, hkv, d), 7.0, dtype=dtype, device="cuda") for _ in range(2))
+    to = gaps[:K2.shape[0]].clone()
+    K2[index], V2[index], to[index] = K[rows], V[rows], flat[rows]
+    to[-1] = len(order) * page + 5
+    cache.write(K2, V2, to)
+    Ko, Vo = torch.full_like(K, math.nan), torch.full_like(V, math.nan)
+    cache.read(table.cuda(), gpu_i32(cu), Ko, Vo)
+    for got, x in ((Ko, K), (Vo, V)):
+        assert torch.equal(got.cpu().double(), x.cpu().double() if bits == 16 else held(x, 8).float().to(dtype).double())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_runs_are_quantised_as_single_tokens_are(s24, dtype):
+    """The same values through both kernels of the cache: the same bytes and steps, also for values on and beside ties."""
+    from paper_2404_01847_amd.attention import PagedKV
+    n, hkv, d = 20000, 4, 128
+    x = normal((n, hkv, d), dtype, 1)
+    top = x.abs().amax(2, keepdim=True).float()
+    ties = ((torch.arange(n * hkv * d, device="cuda").view(n, hkv, d) % 127 + 0.5) * top / 127).to(dtype)
+    x[::2, :, 1:] = torch.where(ties[::2, :, 1:].abs() <= top[::2], ties[::2, :, 1:], x[::2, :, 1:])
+    one, two = (PagedKV(n // 16, 16, hkv, d, dtype, bits=8) for _ in range(2))
+    at = torch.arange(n, device="cuda")
+    one.write(x, x, at)
+    for i in range(0, n, 50):
+        two.write(x[i:i + 50], x[i:i + 50], at[i:i + 50])
+    for a, b in zip((one.K, one.V, one.k_step, one.v_step), (two.K, two.V, two.k_step, two.v_step)):
+        assert torch.equal(a, b)
+    want, _ = quantise(x)
+    assert torch.equal(one.K.transpose(1, 2).reshape(n, hkv, d).cpu().double() - 128, want)
