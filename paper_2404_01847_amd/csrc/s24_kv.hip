@@ -8,7 +8,6 @@
 #include "s24_attn.h"
 
 #include <math.h>
-#include <stdlib.h>
 
 namespace s24_kv {
 using namespace s24_attn;
@@ -114,17 +113,19 @@ template <typename T, bool PAIR> __device__ __forceinline__ float step_of(uint4 
     return fmaxf(__fdiv_rn(token_max<PAIR>(most), 127.0f), 0x1p-126f);
 }
 
-// Many tokens: a wave looks at sixteen of them and takes those runs that begin there and lie within sixteen aligned places of a page, one after the other.
-// Of a prompt, whatever place it starts at, that is sixteen tokens to a wave: V then leaves in pieces of 16 bytes.  (Of single tokens of many sequences it is one
-// at a time, which the kernel below does better.)  Bound by memory: MEASURE
+// Many tokens: a wave looks at sixteen of them and takes, of K or of V, those runs that begin there and lie within sixteen aligned places of a page, one after
+// the other.  Of a prompt, whatever place it starts at, that is sixteen tokens to a wave: V then leaves in pieces of 16 bytes.  (Of single tokens of many
+// sequences it is one at a time, which the kernel below does better.)  Bound by memory: MEASURE
 template <typename T, int BITS, bool PAIR>
 __global__ __launch_bounds__(256) void kv_write_runs_kernel(const WriteArgs a)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int units = PAIR ? (a.c.hkv + 1) / 2 : a.c.hkv, item = 4 * blockIdx.x + wave, window = item / units;
-    const Lane<PAIR> at(a.c, item - window * units, lane);
+    const int units = PAIR ? (a.c.hkv + 1) / 2 : a.c.hkv, item = 4 * blockIdx.x + wave, window = (item >> 1) / units;
+    const bool values = item & 1;
+    const Lane<PAIR> at(a.c, (item >> 1) - window * units, lane);
     const int first_token = 16 * window;
     if (first_token >= a.tokens) return;
+    const Strided from = values ? a.v : a.k;
     const int mine = first_token - 1 + lane;   // lanes 0 .. 33: the token before, the window, and as many as a run that begins in it may reach
     const int64_t place = mine >= 0 && mine < a.tokens && lane < 34 ? a.places[mine] : -1;
     const int64_t before = __shfl_up(place, 1);
@@ -137,26 +138,27 @@ __global__ __launch_bounds__(256) void kv_write_runs_kernel(const WriteArgs a)
         if (to < 0 || to >= a.c.pages << a.c.shift) continue;
         const int skip = (int)(to & 15);
         const int64_t base = ((((to >> a.c.shift) * a.c.hkv + at.h) << a.c.shift) + (to & (a.c.page - 1) & ~15));   // of the sixteen, in tokens of one head
-        uint4 xk[4], xv[4];
+        uint4 x[4];
         bool live[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int k = 4 * at.r + i - skip;
             live[i] = at.live && k >= 0 && k < n;
-            xk[i] = xv[i] = make_uint4(0, 0, 0, 0);
-            if (live[i]) {
-                xk[i] = *reinterpret_cast<const uint4 *>(a.k.p + (int64_t)(token + k) * a.k.token + at.h * a.k.head + at.c);
-                xv[i] = *reinterpret_cast<const uint4 *>(a.v.p + (int64_t)(token + k) * a.v.token + at.h * a.v.head + at.c);
-            }
+            x[i] = live[i] ? *reinterpret_cast<const uint4 *>(from.p + (int64_t)(token + k) * from.token + at.h * from.head + at.c) : make_uint4(0, 0, 0, 0);
         }
         if constexpr (BITS == 16) {
+            if (!values) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (live[i]) *reinterpret_cast<uint4 *>(a.c.k + ((base + 4 * at.r + i) * a.c.d + at.c) * 2) = x[i];
+                continue;
+            }
             uint32_t lo[8], hi[8];   // of a channel: tokens 4r, 4r + 1 and 4r + 2, 4r + 3
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (live[i]) *reinterpret_cast<uint4 *>(a.c.k + ((base + 4 * at.r + i) * a.c.d + at.c) * 2) = xk[i];
                 uint32_t w[4];   // channels 2i and 2i + 1 of the four tokens
 #pragma unroll
-                for (int k = 0; k < 4; ++k) w[k] = i == 0 ? xv[k].x : i == 1 ? xv[k].y : i == 2 ? xv[k].z : xv[k].w;
+                for (int k = 0; k < 4; ++k) w[k] = i == 0 ? x[k].x : i == 1 ? x[k].y : i == 2 ? x[k].z : x[k].w;
                 lo[2 * i] = __builtin_amdgcn_perm(w[1], w[0], 0x05040100u), lo[2 * i + 1] = __builtin_amdgcn_perm(w[1], w[0], 0x07060302u);
                 hi[2 * i] = __builtin_amdgcn_perm(w[3], w[2], 0x05040100u), hi[2 * i + 1] = __builtin_amdgcn_perm(w[3], w[2], 0x07060302u);
             }
@@ -170,39 +172,44 @@ __global__ __launch_bounds__(256) void kv_write_runs_kernel(const WriteArgs a)
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
+                    if (live[i]) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (live[i]) v[8 * e + 4 * (at.r & 1) + i] = (uint16_t)((i < 2 ? lo[e] : hi[e]) >> (16 * (i & 1)));
+                        for (int e = 0; e < 8; ++e) v[8 * e + 4 * (at.r & 1) + i] = (uint16_t)((i < 2 ? lo[e] : hi[e]) >> (16 * (i & 1)));
+                    }
             }
         } else {
             uint32_t bytes[4][8];
-            float sk[4], sv[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                sk[i] = step_of<T, PAIR>(xk[i]), sv[i] = step_of<T, PAIR>(xv[i]);
-                uint32_t m[8];
-                eight_numbers<T>(xk[i], sk[i], __builtin_amdgcn_rcpf(sk[i]), m);
-                eight_numbers<T>(xv[i], sv[i], __builtin_amdgcn_rcpf(sv[i]), bytes[i]);
-                if (!live[i]) continue;
-                *reinterpret_cast<uint2 *>(a.c.k + (base + 4 * at.r + i) * a.c.d + at.c) = make_uint2(four_bytes(m[0], m[1], m[2], m[3]), four_bytes(m[4], m[5], m[6], m[7]));
-                if (at.c == 0) a.c.ks[base + 4 * at.r + i] = sk[i], a.c.vs[base + 4 * at.r + i] = sv[i];
+                const float step = step_of<T, PAIR>(x[i]);
+                eight_numbers<T>(x[i], step, __builtin_amdgcn_rcpf(step), bytes[i]);
+                if (live[i] && at.c == 0) (values ? a.c.vs : a.c.ks)[base + 4 * at.r + i] = step;
+            }
+            if (!values) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (live[i])
+                        *reinterpret_cast<uint2 *>(a.c.k + (base + 4 * at.r + i) * a.c.d + at.c) =
+                            make_uint2(four_bytes(bytes[i][0], bytes[i][1], bytes[i][2], bytes[i][3]), four_bytes(bytes[i][4], bytes[i][5], bytes[i][6], bytes[i][7]));
+                continue;
             }
             unsigned char *v = a.c.v + base * a.c.d + at.c * 16;
             if (n == 16) {
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {   // row r gets all sixteen tokens of channel 4*half + r
-                    uint32_t x[4];
+                    uint32_t w[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = four_bytes(bytes[0][4 * half + e], bytes[1][4 * half + e], bytes[2][4 * half + e], bytes[3][4 * half + e]);
-                    transpose_rows(x);
-                    if (at.live) *reinterpret_cast<uint4 *>(v + 16 * (4 * half + at.r)) = make_uint4(x[0], x[1], x[2], x[3]);
+                    for (int e = 0; e < 4; ++e) w[e] = four_bytes(bytes[0][4 * half + e], bytes[1][4 * half + e], bytes[2][4 * half + e], bytes[3][4 * half + e]);
+                    transpose_rows(w);
+                    if (at.live) *reinterpret_cast<uint4 *>(v + 16 * (4 * half + at.r)) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
+                    if (live[i]) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (live[i]) v[16 * e + 4 * at.r + i] = (unsigned char)bytes[i][e];
+                        for (int e = 0; e < 8; ++e) v[16 * e + 4 * at.r + i] = (unsigned char)bytes[i][e];
+                    }
             }
         }
     }
@@ -675,8 +682,7 @@ template <typename T, int BITS> static void read(const ReadArgs &a, dim3 grid, h
 // Shares of the positions for each of `heads` products: as many waves as the device holds at a time.
 static int64_t shares_of(int64_t heads, int64_t d)
 {
-    static const int x8 = getenv("XS") ? atoi(getenv("XS")) : 8;
-    const int64_t n = ((d <= 64 ? x8 * 3 / 2 : x8) * (int64_t)s24_cu_count()) / heads;
+    const int64_t n = (d <= 64 ? 12 : 8) * (int64_t)s24_cu_count() / heads;
     return n < 1 ? 1 : n;
 }
 }  // namespace s24_kv
@@ -695,10 +701,10 @@ extern "C" int s24_kv_write(const s24_kv_cache *cache, const s24_heads *K, const
     if (tokens == 0 || cache->pages == 0) return S24_OK;
     const WriteArgs a{cache_of(cache), strided(K), strided(V), places, (int)tokens};
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    // The runs' kernel where its waves, one for sixteen tokens of a head or two, are enough to fill the device twice.
-    const int64_t units = cache->d <= 64 ? (cache->hkv + 1) / 2 : cache->hkv, waves = (tokens + 15) / 16 * units;
-    static const int xw = getenv("XW") ? atoi(getenv("XW")) : 8;
-    const bool runs = waves >= xw * (int64_t)s24_cu_count();
+    // The runs' kernel from 40 tokens of a head for each compute unit on.  (8 bits, 8 heads of 128, both sides: 1024 tokens 7.9 us by runs, 6.1 one by one; 2048
+    // tokens 7.6 and 9.5; 16384 tokens 24 and 50.  12 heads of 64, 1024 tokens: 7.3 and 7.2.  16 bits, 8 heads of 128, 1024 tokens: 5.3 and 6.3.)
+    const int64_t units = cache->d <= 64 ? (cache->hkv + 1) / 2 : cache->hkv, waves = 2 * ((tokens + 15) / 16) * units;   // of K and of V
+    const bool runs = tokens * cache->hkv >= 40 * (int64_t)s24_cu_count();
     const int64_t groups = runs ? (waves + 3) / 4 : (tokens * cache->hkv + 3) / 4;
     S24_REQUIRE(groups <= kMostGroups, S24_ERR_SHAPE);
     const dim3 grid((unsigned)groups);
