@@ -51,12 +51,13 @@ template <typename T> __device__ __forceinline__ uint4 operand(f32x4 a, f32x4 b)
     return make_uint4(pack2<T>(a[0], a[1]), pack2<T>(a[2], a[3]), pack2<T>(b[0], b[1]), pack2<T>(b[2], b[3]));
 }
 
-// A tile of rows of D 16-bit values in LDS.  It is read in two ways, neither with bank conflicts: 16 rows at one 16-byte piece, and
-// transposed, 8 rows at two neighbouring pieces.  Hence piece c of a row lies at slot c ^ (twice its place among eight, plus one for the other eight).
+// A tile of rows of D 16-bit values in LDS.  It is read in two ways, neither with bank conflicts: 16-byte pieces of 16 rows, of which the LDS takes rows 0-3 and
+// 12-15 of one piece together with rows 4-11 of the next in a cycle, and transposed, 8 rows at two neighbouring pieces.  Hence piece c of a row lies at slot
+// c ^ (twice its place among eight).
 template <int D> __device__ __forceinline__ int swizzle(int row)
 {
     static_assert(D == 64 || D == 128, "rows of half a round of the banks, or of one");
-    return D == 128 ? (row & 7) << 1 | (row >> 3 & 1) : (row >> 1 & 3) << 1 | (row >> 3 & 1);
+    return D == 128 ? (row & 7) << 1 : (row >> 1 & 3) << 1;
 }
 // Byte offset in a tile of piece c of `row`
 template <int D> __device__ __forceinline__ int piece(int row, int c) { return row * 2 * D + ((c ^ swizzle<D>(row)) << 4); }
