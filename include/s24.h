@@ -353,9 +353,11 @@ typedef struct {
 } s24_attn_shape;
 
 /* O_i = sum_j P_ij v_j, P_ij = exp(c q_i.k_j - lse_i), lse_i = log sum_j exp(c q_i.k_j) over the keys j that query i sees.
- *   lse [hq][tokens_q] fp32, out, may be NULL (s24_attn_bwd reads it); minus infinity for a query that sees no key */
+ *   lse [hq][tokens_q] fp32, out, may be NULL (s24_attn_bwd reads it); minus infinity for a query that sees no key
+ *   workspace  device, s24_attn_fwd_workspace(shape) bytes (0 for most shapes: then NULL will do), 16-byte aligned; holds nothing between calls */
+int64_t s24_attn_fwd_workspace(const s24_attn_shape *shape);
 int s24_attn_fwd(const s24_attn_shape *shape, const s24_heads *Q, const s24_heads *K, const s24_heads *V, const s24_heads *O, float *lse,
-                 s24_dtype dt, void *stream);
+                 void *workspace, int64_t workspace_bytes, s24_dtype dt, void *stream);
 
 /* Gradients of s24_attn_fwd from its O and lse: with delta_i = dO_i.O_i and dS_ij = P_ij (dO_i.v_j - delta_i),
  * dQ_i = c sum_j dS_ij k_j,  dK_j = c sum_i dS_ij q_i,  dV_j = sum_i P_ij dO_i, the last two also over the query heads of a

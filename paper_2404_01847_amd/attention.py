@@ -27,16 +27,21 @@ class Attention:
         self.dQ = self.dK = self.dV = None   # allocated by the first backward pass
         self.work = {}
 
+    def _workspace(self, need, cu_q):
+        """What a pass takes depends on the number of sequences."""
+        key = (need, cu_q.shape[0])
+        if key not in self.work:
+            n = need(self.tokens_q, self.tokens_k, self.hq, self.hkv, self.d, cu_q.shape[0] - 1)
+            self.work[key] = torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
+        return self.work[key]
+
     def forward(self, Q, K, V, cu_q, cu_k=None):
         """O [tokens_q, hq, d].  Q, K, V may be views of one projection's result; cu_q, cu_k: int32 offsets of the sequences."""
-        return s24.attn_fwd(Q, K, V, self.O, self.lse, cu_q, cu_k, self.causal, self.scale)
+        return s24.attn_fwd(Q, K, V, self.O, self.lse, self._workspace(s24.attn_fwd_workspace, cu_q), cu_q, cu_k, self.causal, self.scale)
 
     def backward(self, Q, K, V, dO, cu_q, cu_k=None):
         """dQ, dK, dV of the last forward pass, whose operands are given again."""
-        work = self.work.get(cu_q.shape[0])   # what it takes depends on the number of sequences
-        if work is None:
-            need = s24.attn_bwd_workspace(self.tokens_q, self.tokens_k, self.hq, self.hkv, self.d, cu_q.shape[0] - 1)
-            work = self.work[cu_q.shape[0]] = torch.empty(need, dtype=torch.uint8, device=self.device)
+        work = self._workspace(s24.attn_bwd_workspace, cu_q)
         if self.dQ is None:
             # the layout of the projection's gradient: dQ, dK and dV are its parts
             if self.tokens_q == self.tokens_k:

@@ -60,7 +60,8 @@ _SIGNATURES = {
     "s24_probe_matrix_rate": (_int, [_int, _int, _int, _vp, _vp]),
     "s24_probe_copy": (_int, [_vp, _vp, _i64, _vp]),
     "s24_probe_reciprocal": (_int, [C.c_uint32, _i64, _vp, _vp]),
-    "s24_attn_fwd": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _int, _vp]),
+    "s24_attn_fwd_workspace": (_i64, [_vp]),
+    "s24_attn_fwd": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _int, _vp]),
     "s24_attn_bwd_workspace": (_i64, [_vp]),
     "s24_attn_bwd": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _int, _vp]),
     "s24_kv_write": (_int, [_vp, _vp, _vp, _vp, _i64, _int, _vp]),
@@ -525,17 +526,25 @@ def _attn_operands(where, Q, K, cu_q, cu_k, causal, scale):
     return sq, sk, Q.dtype, device, _pack_shape(pq, pk, n[0] - 1, sq[0], sk[0], sq[1], sk[1], sq[2], sq[2] ** -0.5 if scale is None else scale, bool(causal))
 
 
-def attn_fwd(Q, K, V, O, lse, cu_q, cu_k=None, causal=True, scale=None):
+def attn_fwd(Q, K, V, O, lse, workspace, cu_q, cu_k=None, causal=True, scale=None):
     """Attention over packed sequences.  Q, O [tokens_q, hq, d], K, V [tokens_k, hkv, d], with any strides along the first two axes; lse [hq, tokens_q]
-    float32 or None; cu_q, cu_k: int32 offsets of the sequences (cu_k None: those of the queries); scale None: 1 / sqrt(d)."""
+    float32 or None; cu_q, cu_k: int32 offsets of the sequences (cu_k None: those of the queries); scale None: 1 / sqrt(d);
+    workspace: a uint8 tensor of attn_fwd_workspace(...) bytes, None where that is 0."""
     where = "s24_attn_fwd"
     sq, sk, dtype, device, shape = _attn_operands(where, Q, K, cu_q, cu_k, causal, scale)
     status = lib().s24_attn_fwd(shape, _heads(where, "Q", Q, sq, dtype, device), _heads(where, "K", K, sk, dtype, device), _heads(where, "V", V, sk, dtype, device),
                                 _heads(where, "O", O, sq, dtype, device),
-                                None if lse is None else _whole(where, "lse", lse, torch.float32, (sq[1], sq[0]), device), _dt(Q), _stream())
+                                None if lse is None else _whole(where, "lse", lse, torch.float32, (sq[1], sq[0]), device),
+                                *((None, 0) if workspace is None else (_whole(where, "workspace", workspace, torch.uint8, workspace.shape, device), workspace.numel())),
+                                _dt(Q), _stream())
     if status != 0:
         raise S24Error(status, where)
     return O
+
+
+def attn_fwd_workspace(tokens_q, tokens_k, hq, hkv, d, sequences):
+    """Bytes of workspace that attn_fwd needs for so many tokens, heads and sequences."""
+    return lib().s24_attn_fwd_workspace(_pack_shape(0, 0, sequences, tokens_q, tokens_k, hq, hkv, d, 1.0, True))
 
 
 def attn_bwd_workspace(tokens_q, tokens_k, hq, hkv, d, sequences):

@@ -20,41 +20,82 @@ struct Problem {
     Out out, dq, dk, dv;
     float *lse;            // [hq][tokens_q]
     float2 *stats;         // [hq][tokens_q], of the backward pass: what a row's exponents are taken from, and delta
-    float *sums;           // [parts][tokens_k][hkv][2 d]
+    // Where a kernel's workgroups are few, what a tile sums over is cut into parts, whose sums another kernel adds
     int parts;
+    float *sums;           // [parts][tokens][heads][values]
+    float2 *weights;       // [parts][tokens_q][hq], of the forward pass: reference and sum
     const int *cu_q, *cu_k;
     int sequences, tokens_q, tokens_k, hq, group, d, causal;
     float scale;
 };
 
+// For the scheduler: the LDS reads of a product come a step ahead of its matrix instructions, of which there are STEPS times MATRIX, READS for each.  (Left to itself
+// it reads two operands, waits for them, and multiplies: 
+template <int READS, int MATRIX, int STEPS> __device__ __forceinline__ void reads_ahead()
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_sched_group_barrier(0x100, 2 * READS, 0);
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, MATRIX, 0);
+        if (i + 2 < STEPS) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+    }
+#endif
+}
+
+// Which tile, head and part a workgroup has
+struct Unit { int tile, head, part; };
+__device__ __forceinline__ Unit unit_of(int heads, int parts)
+{
+    const int units = heads * parts, tile = blockIdx.x / units, unit = head_of(blockIdx.x - tile * units, units), head = unit / parts;
+    return {tile, head, unit - head * parts};
+}
+// The queries of a workgroup that goes over the keys, and what they see of them
+struct Queries {
+    Span q, k;
+    int q0, ahead;   // first query of the workgroup; query i sees the keys up to i + ahead
+    int seen, wave_seen, wave_all;   // keys that some query of the workgroup may see, that one of the wave may see, that all of them see
+    __device__ __forceinline__ void init(const Problem &a, int sequence, int tile, int rows, int first_of_wave)
+    {
+        q = span(a.cu_q, sequence, a.tokens_q), k = span(a.cu_k, sequence, a.tokens_k);
+        q0 = tile * rows, ahead = k.count - q.count;
+        const int wq0 = q0 + first_of_wave;
+        auto up_to = [&](int i) { return a.causal ? min(k.count, i + 1 + ahead) : k.count; };
+        seen = up_to(min(q0 + rows, q.count) - 1);
+        wave_seen = wq0 < q.count ? up_to(min(wq0 + 32, q.count) - 1) : 0;
+        wave_all = wq0 + 32 > q.count ? 0 : up_to(wq0);
+    }
+};
+
 // ------------------------------------------------------------------ forward
-// Four waves of 32 queries; keys and values in tiles of 64, two of them in LDS: the next one is copied during the work on this one.
+// Keys and values in tiles of 64, two of them in LDS: the next one is copied during the work on this one.  Four waves of 32 queries (KS = 1), or two pairs, of
+// which each wave takes half of a tile's keys (KS = 2): twice the workgroups, each of half the length, for twice the copies.
 template <int D> struct Forward {
-    static constexpr int BQ = 128, BK = 64, TILE = BK * 2 * D;
+    static constexpr int BK = 64, TILE = BK * 2 * D;
 };
 
 // Scores whose maximum grew by less than this (as a power of two) keep the reference they have: P then reaches 2^8, which the 16-bit types hold with
 // the same relative precision, and the sums stay far inside fp32.
 constexpr float kGrowth = 8.0f;
 
-template <typename T, int D>
+template <typename T, int D, int KS>
 __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
 {
     using C = Forward<D>;
+    constexpr int BQ = 128 / KS, KEYS = C::BK / KS, NI = KEYS / 16;   // queries of a workgroup, a wave's keys of a tile
     __shared__ __align__(16) unsigned char lds_k[2][C::TILE], lds_v[2][C::TILE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int col = lane & 15, g = lane >> 4;
-    const int tile = blockIdx.x / a.hq, head = head_of(blockIdx.x - tile * a.hq, a.hq), kv = head / a.group;
+    const int col = lane & 15, g = lane >> 4, qw = KS == 2 ? wave & 1 : wave, first_key = KS == 2 ? KEYS * (wave >> 1) : 0;
+    const Unit unit = unit_of(a.hq, a.parts);
+    const int head = unit.head, kv = head / a.group;
     int sequence, index, count;
-    if (!find_tile(a.cu_q, a.sequences, a.tokens_q, C::BQ, tile, lane, sequence, index, count)) return;
-    const Span sq = span(a.cu_q, sequence, a.tokens_q), sk = span(a.cu_k, sequence, a.tokens_k);
-    const int q0 = (count - 1 - index) * C::BQ;    // the last ones see the most keys: they go first
-    const int ahead = sk.count - sq.count;         // query i sees the keys up to i + ahead
-    const int wq0 = q0 + 32 * wave;                // this wave's queries
-    const int seen = a.causal ? min(sk.count, q0 + C::BQ + ahead) : sk.count;            // keys that some query of the tile may see
-    const int wave_seen = a.causal ? min(sk.count, wq0 + 32 + ahead) : sk.count;         // of the wave
-    const int wave_all = a.causal ? min(sk.count, wq0 + 1 + ahead) : sk.count;           // keys that all its queries see
-    const int tiles = seen > 0 ? (seen + C::BK - 1) / C::BK : 0;
+    if (!find_tile(a.cu_q, a.sequences, a.tokens_q, BQ, unit.tile, lane, sequence, index, count)) return;
+    Queries s_;
+    s_.init(a, sequence, count - 1 - index, BQ, 32 * qw);    // the last ones see the most keys: they go first
+    const Span sq = s_.q, sk = s_.k;
+    const int wq0 = s_.q0 + 32 * qw, ahead = s_.ahead;
+    const int all_tiles = s_.seen > 0 ? (s_.seen + C::BK - 1) / C::BK : 0;
+    const int begin = (int)((int64_t)all_tiles * unit.part / a.parts), tiles = (int)((int64_t)all_tiles * (unit.part + 1) / a.parts);
 
     uint4 q[2][D / 32];
 #pragma unroll
@@ -79,30 +120,31 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
         ck.start(keys + (int64_t)t * C::BK * a.k.token, (lds_byte *)lds_k[t & 1]);
         cv.start(values + (int64_t)t * C::BK * a.v.token, (lds_byte *)lds_v[t & 1]);
     };
-    if (tiles > 0) copy(0);
-    for (int t = 0; t < tiles; ++t) {
+    if (begin < tiles) copy(begin);
+    for (int t = begin; t < tiles; ++t) {
         wait_and_barrier<0>();
         if (t + 1 < tiles) copy(t + 1);
-        const int k0 = t * C::BK;
-        if (k0 >= wave_seen) continue;
+        const int k0 = t * C::BK + first_key;
+        if (k0 >= s_.wave_seen) continue;
         const lds_byte *tk = (const lds_byte *)lds_k[t & 1], *tv = (const lds_byte *)lds_v[t & 1];
-        f32x4 s[4][2];
+        f32x4 s[NI][2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[i][0] = s[i][1] = f32x4{};
+        for (int i = 0; i < NI; ++i) s[i][0] = s[i][1] = f32x4{};
 #pragma unroll
         for (int k = 0; k < D / 32; ++k)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint4 f = rows<D>(tk, 16 * i, k, lane);
+            for (int i = 0; i < NI; ++i) {
+                const uint4 f = rows<D>(tk, first_key + 16 * i, k, lane);
                 s[i][0] = mma<T>(f, q[0][k], s[i][0]);
                 s[i][1] = mma<T>(f, q[1][k], s[i][1]);
             }
-        if (k0 + C::BK > wave_all) {
+        if (D == 128) reads_ahead<NI, 2 * NI, D / 32>();
+        if (k0 + KEYS > s_.wave_all) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int last = a.causal ? min(sk.count - 1, wq0 + 16 * j + col + ahead) : sk.count - 1;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < NI; ++i)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) s[i][j][r] = k0 + 16 * i + 4 * g + r <= last ? s[i][j][r] : -INFINITY;
             }
@@ -112,7 +154,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
         for (int j = 0; j < 2; ++j) {
             top[j] = s[0][j][0];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < NI; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) top[j] = fmaxf(top[j], s[i][j][r]);
             top[j] *= c;
@@ -126,41 +168,109 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
                 for (int n = 0; n < D / 16; ++n) o[n][j] *= shrink;
             }
         }
-        uint4 p[2][2];
+        uint4 p[NI / 2][2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < NI; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     s[i][j][r] = __builtin_amdgcn_exp2f(fmaf(s[i][j][r], c, -m[j]));
                     l[j] += s[i][j][r];
                 }
 #pragma unroll
-            for (int u = 0; u < 2; ++u) p[u][j] = operand<T>(s[2 * u][j], s[2 * u + 1][j]);
+            for (int u = 0; u < NI / 2; ++u) p[u][j] = operand<T>(s[2 * u][j], s[2 * u + 1][j]);
         }
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < NI / 2; ++u)
 #pragma unroll
             for (int n = 0; n < D / 16; ++n) {
-                const uint4 f = columns<D>(tv, 32 * u, n, lane);
+                const uint4 f = columns<D>(tv, first_key + 32 * u, n, lane);
                 o[n][0] = mma<T>(f, p[u][0], o[n][0]);
                 o[n][1] = mma<T>(f, p[u][1], o[n][1]);
             }
+    }
+    if constexpr (KS == 2) {   // the wave of a pair that has the later keys hands its sums over, in LDS that no wave reads any more
+        constexpr int SUMS = D / 16 * 2 * 1024;   // bytes of a wave's
+        static_assert(SUMS + 1024 <= 2 * C::TILE, "the sums must fit");
+        lds_byte *const to = qw == 0 ? (lds_byte *)lds_k : (lds_byte *)lds_v, *const stats = to + SUMS;
+        wait_and_barrier<0>();
+        if (wave >= 2) {
+#pragma unroll
+            for (int n = 0; n < D / 16; ++n)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) lds_store(to + (2 * n + j) * 1024 + 16 * lane, o[n][j]);
+            lds_store(stats + 16 * lane, f32x4{m[0], m[1], l[0], l[1]});
+        }
+        wait_and_barrier<0>();
+        if (wave >= 2) return;
+        const f32x4 other = __builtin_bit_cast(f32x4, lds_load(stats + 16 * lane));
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const float now = fmaxf(m[j], other[j]), mine = __builtin_amdgcn_exp2f(m[j] - now), its = __builtin_amdgcn_exp2f(other[j] - now);
+            m[j] = now, l[j] = l[j] * mine + other[2 + j] * its;
+#pragma unroll
+            for (int n = 0; n < D / 16; ++n) o[n][j] = o[n][j] * mine + __builtin_bit_cast(f32x4, lds_load(to + (2 * n + j) * 1024 + 16 * lane)) * its;
+        }
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const int row = wq0 + 16 * j + col;
         const float sum = column_sum(l[j]), inverse = sum > 0.0f ? 1.0f / sum : 0.0f;
         if (row >= sq.count) continue;
-        uint16_t *out = a.out.p + (int64_t)(sq.first + row) * a.out.token + head * a.out.head;
+        const int64_t token = sq.first + row;
+        if (a.parts == 1) {
+            uint16_t *out = a.out.p + token * a.out.token + head * a.out.head;
 #pragma unroll
-        for (int n = 0; n < D / 16; ++n)
-            if (16 * n < a.d)
-                *reinterpret_cast<uint2 *>(out + 16 * n + 4 * g) =
-                    make_uint2(pack2<T>(o[n][j][0] * inverse, o[n][j][1] * inverse), pack2<T>(o[n][j][2] * inverse, o[n][j][3] * inverse));
-        if (a.lse != nullptr && g == 0)
-            a.lse[(int64_t)head * a.tokens_q + sq.first + row] = sum > 0.0f ? (m[j] + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+            for (int n = 0; n < D / 16; ++n)
+                if (16 * n < a.d)
+                    *reinterpret_cast<uint2 *>(out + 16 * n + 4 * g) =
+                        make_uint2(pack2<T>(o[n][j][0] * inverse, o[n][j][1] * inverse), pack2<T>(o[n][j][2] * inverse, o[n][j][3] * inverse));
+            if (a.lse != nullptr && g == 0) a.lse[(int64_t)head * a.tokens_q + token] = sum > 0.0f ? (m[j] + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+        } else {
+            const int64_t at = (unit.part * (int64_t)a.tokens_q + token) * a.hq + head;
+#pragma unroll
+            for (int n = 0; n < D / 16; ++n)
+                if (16 * n < a.d) *reinterpret_cast<f32x4 *>(a.sums + at * a.d + 16 * n + 4 * g) = o[n][j];
+            if (g == 0) a.weights[at] = make_float2(m[j], sum);
+        }
+    }
+}
+
+// Rows of a join: a workgroup takes a few of a sequence, for one head
+constexpr int kJoinRows = 16;
+struct Joined { int64_t first; int rows, head; };
+__device__ __forceinline__ bool join_rows(const int *cu, int sequences, int tokens, int heads, Joined &j)
+{
+    const int tile = blockIdx.x / heads;
+    int sequence, index, count;
+    if (!find_tile(cu, sequences, tokens, kJoinRows, tile, threadIdx.x & 63, sequence, index, count)) return false;
+    const Span s = span(cu, sequence, tokens);
+    j = {s.first + (int64_t)index * kJoinRows, min(kJoinRows, s.count - index * kJoinRows), (int)(blockIdx.x - tile * heads)};
+    return true;
+}
+// O and lse from the sums of the parts
+template <typename T>
+__global__ __launch_bounds__(256) void attn_fwd_join_kernel(const Problem a)
+{
+    Joined j;
+    if (!join_rows(a.cu_q, a.sequences, a.tokens_q, a.hq, j)) return;
+    const int quads = a.d >> 2;
+    const int64_t step = (int64_t)a.tokens_q * a.hq;
+    for (int item = threadIdx.x; item < j.rows * quads; item += 256) {
+        const int row = item / quads, i = 4 * (item - row * quads);
+        const int64_t t = j.first + row, at = t * a.hq + j.head;
+        float m = -1e30f, l = 0.0f;
+        for (int p = 0; p < a.parts; ++p) m = fmaxf(m, a.weights[at + p * step].x);
+        f32x4 x = {};
+        for (int p = 0; p < a.parts; ++p) {
+            const float2 w = a.weights[at + p * step];
+            const float f = __builtin_amdgcn_exp2f(w.x - m);
+            l = fmaf(w.y, f, l), x += *reinterpret_cast<const f32x4 *>(a.sums + (at + p * step) * a.d + i) * f;
+        }
+        x *= l > 0.0f ? 1.0f / l : 0.0f;
+        *reinterpret_cast<uint2 *>(a.out.p + t * a.out.token + j.head * a.out.head + i) = make_uint2(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]));
+        if (i == 0 && a.lse != nullptr) a.lse[(int64_t)j.head * a.tokens_q + t] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
     }
 }
 
@@ -177,7 +287,7 @@ template <int D> struct Backward {
     static constexpr int BK = 128, BQ = 32, TILE = BQ * 2 * D, STAGE = 2 * TILE + 8 * BQ, VALUES = BK * 2 * D;   // a stage: queries, gradients, row statistics
 };
 template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void attn_dkv_kernel(const Problem a)
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dkv_kernel(const Problem a)
 {
     using C = Backward<D>;
     using L = Lift<T>;
@@ -185,7 +295,8 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(const Problem a)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
     const int hkv = a.hq / a.group;
-    const int units = hkv * a.parts, tile = blockIdx.x / units, unit = head_of(blockIdx.x - tile * units, units), kv = unit / a.parts, part = unit - kv * a.parts;
+    const Unit unit = unit_of(hkv, a.parts);
+    const int tile = unit.tile, kv = unit.head, part = unit.part;
     int sequence, index, count;
     if (!find_tile(a.cu_k, a.sequences, a.tokens_k, C::BK, tile, lane, sequence, index, count)) return;
     const Span sq = span(a.cu_q, sequence, a.tokens_q), sk = span(a.cu_k, sequence, a.tokens_k);
@@ -335,47 +446,45 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(const Problem a)
     }
 }
 
-// dK and dV of a few keys from the sums of the parts
-constexpr int kJoinRows = 16;
+// dK and dV from the sums of the parts
 template <typename T>
 __global__ __launch_bounds__(256) void attn_dkv_join_kernel(const Problem a)
 {
-    constexpr int BK = kJoinRows;
-    const int hkv = a.hq / a.group, tile = blockIdx.x / hkv, kv = blockIdx.x - tile * hkv;
-    int sequence, index, count;
-    if (!find_tile(a.cu_k, a.sequences, a.tokens_k, BK, tile, threadIdx.x & 63, sequence, index, count)) return;
-    const Span sk = span(a.cu_k, sequence, a.tokens_k);
-    const int quads = a.d >> 1, n = min(BK, sk.count - index * BK) * quads;   // of a row of dK and one of dV
+    const int hkv = a.hq / a.group, quads = a.d >> 1;   // of a row of dK and one of dV
+    Joined j;
+    if (!join_rows(a.cu_k, a.sequences, a.tokens_k, hkv, j)) return;
     const int64_t step = (int64_t)a.tokens_k * hkv * 2 * a.d;
-    for (int item = threadIdx.x; item < n; item += 256) {
+    for (int item = threadIdx.x; item < j.rows * quads; item += 256) {
         const int row = item / quads, i = 4 * (item - row * quads);
-        const int64_t t = sk.first + index * BK + row;
-        const float *from = a.sums + (t * hkv + kv) * 2 * a.d + i;
+        const int64_t t = j.first + row;
+        const float *from = a.sums + (t * hkv + j.head) * 2 * a.d + i;
         f32x4 x = *reinterpret_cast<const f32x4 *>(from);
         for (int p = 1; p < a.parts; ++p) x += *reinterpret_cast<const f32x4 *>(from + p * step);
-        uint16_t *to = i < a.d ? a.dk.p + t * a.dk.token + kv * a.dk.head + i : a.dv.p + t * a.dv.token + kv * a.dv.head + i - a.d;
+        uint16_t *to = i < a.d ? a.dk.p + t * a.dk.token + j.head * a.dk.head + i : a.dv.p + t * a.dv.token + j.head * a.dv.head + i - a.d;
         *reinterpret_cast<uint2 *>(to) = make_uint2(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]));
     }
 }
 
-// dQ of 128 queries of a head, four waves of 32, over the keys they see, 32 at a time.  Runs first: it leaves the row statistics to dK and dV.
-template <typename T, int D>
+// dQ, over the keys that a workgroup's queries see, 32 at a time and wave: four waves of 32 queries (KS = 1), or two pairs, of which each wave takes half of a
+// tile's keys (KS = 2).  Runs first: it leaves the row statistics to dK and dV.
+template <typename T, int D, int KS>
 __global__ __launch_bounds__(256, 2) void attn_dq_kernel(const Problem a)
 {
     using L = Lift<T>;
-    constexpr int BQ = 128, BK = 32, TILE = BK * 2 * D;
+    constexpr int BQ = 128 / KS, BK = 32 * KS, TILE = BK * 2 * D;
     __shared__ __align__(16) unsigned char lds_k[2][TILE], lds_v[2][TILE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int col = lane & 15, g = lane >> 4;
-    const int tile = blockIdx.x / a.hq, head = head_of(blockIdx.x - tile * a.hq, a.hq), kv = head / a.group;
+    const int col = lane & 15, g = lane >> 4, qw = KS == 2 ? wave & 1 : wave, first_key = KS == 2 ? 32 * (wave >> 1) : 0;
+    const Unit unit = unit_of(a.hq, a.parts);
+    const int head = unit.head, kv = head / a.group;
     int sequence, index, count;
-    if (!find_tile(a.cu_q, a.sequences, a.tokens_q, BQ, tile, lane, sequence, index, count)) return;
-    const Span sq = span(a.cu_q, sequence, a.tokens_q), sk = span(a.cu_k, sequence, a.tokens_k);
-    const int q0 = (count - 1 - index) * BQ, ahead = sk.count - sq.count, wq0 = q0 + 32 * wave;
-    const int seen = a.causal ? min(sk.count, q0 + BQ + ahead) : sk.count;
-    const int wave_seen = a.causal ? min(sk.count, wq0 + 32 + ahead) : sk.count;
-    const int wave_all = wq0 + 32 > sq.count ? 0 : a.causal ? min(sk.count, wq0 + 1 + ahead) : sk.count;
-    const int tiles = seen > 0 ? (seen + BK - 1) / BK : 0;
+    if (!find_tile(a.cu_q, a.sequences, a.tokens_q, BQ, unit.tile, lane, sequence, index, count)) return;
+    Queries s_;
+    s_.init(a, sequence, count - 1 - index, BQ, 32 * qw);
+    const Span sq = s_.q, sk = s_.k;
+    const int wq0 = s_.q0 + 32 * qw, ahead = s_.ahead;
+    const int all_tiles = s_.seen > 0 ? (s_.seen + BK - 1) / BK : 0;
+    const int begin = (int)((int64_t)all_tiles * unit.part / a.parts), tiles = (int)((int64_t)all_tiles * (unit.part + 1) / a.parts);
     uint4 q[2][D / 32], dO[2][D / 32];
     float lse[2], delta[2];
 #pragma unroll
@@ -395,7 +504,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(const Problem a)
             for (int e = 0; e < 4; ++e) sum = fmaf(Num::lo(xs[e]), Num::lo(ys[e]), fmaf(Num::hi(xs[e]), Num::hi(ys[e]), sum));
         }
         lse[j] = fmaf(a.lse[at], kLog2e, -L::kUp), delta[j] = column_sum(sum) * L::kDown;
-        if (g == 0 && wq0 + 16 * j + col < sq.count) a.stats[at] = make_float2(lse[j], delta[j]);
+        if (g == 0 && wave < 4 / KS && unit.part == 0 && wq0 + 16 * j + col < sq.count) a.stats[at] = make_float2(lse[j], delta[j]);
     }
     const float c = a.scale * kLog2e;
     f32x4 dq[D / 16][2];
@@ -411,12 +520,12 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(const Problem a)
         ck.start(keys + (int64_t)t * BK * a.k.token, (lds_byte *)lds_k[t & 1]);
         cv.start(values + (int64_t)t * BK * a.v.token, (lds_byte *)lds_v[t & 1]);
     };
-    if (tiles > 0) copy(0);
-    for (int t = 0; t < tiles; ++t) {
+    if (begin < tiles) copy(begin);
+    for (int t = begin; t < tiles; ++t) {
         wait_and_barrier<0>();
         if (t + 1 < tiles) copy(t + 1);
-        const int k0 = t * BK;
-        if (k0 >= wave_seen) continue;
+        const int k0 = t * BK + first_key;
+        if (k0 >= s_.wave_seen) continue;
         const lds_byte *tk = (const lds_byte *)lds_k[t & 1], *tv = (const lds_byte *)lds_v[t & 1];
         f32x4 s[2][2], dp[2][2];
 #pragma unroll
@@ -425,7 +534,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(const Problem a)
         for (int k = 0; k < D / 32; ++k)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const uint4 x = rows<D>(tk, 16 * i, k, lane), y = rows<D>(tv, 16 * i, k, lane);
+                const uint4 x = rows<D>(tk, first_key + 16 * i, k, lane), y = rows<D>(tv, first_key + 16 * i, k, lane);
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     s[i][j] = mma<T>(x, q[j][k], s[i][j]);
@@ -441,7 +550,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(const Problem a)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
                     s[i][j][r] = __builtin_amdgcn_exp2f(fmaf(s[i][j][r], c, -lse[j])) * fmaf(dp[i][j][r], L::kDown, -delta[j]);
-            if (k0 + BK > wave_all) {
+            if (k0 + 32 > s_.wave_all) {
                 const int last = query >= sq.count ? -1 : a.causal ? min(sk.count - 1, query + ahead) : sk.count - 1;
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
@@ -452,22 +561,61 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(const Problem a)
         }
 #pragma unroll
         for (int n = 0; n < D / 16; ++n) {
-            const uint4 x = columns<D>(tk, 0, n, lane);
+            const uint4 x = columns<D>(tk, first_key, n, lane);
             dq[n][0] = mma<T>(x, ds[0], dq[n][0]);
             dq[n][1] = mma<T>(x, ds[1], dq[n][1]);
         }
+    }
+    if constexpr (KS == 2) {   // as in the forward pass
+        constexpr int SUMS = D / 16 * 2 * 1024;
+        static_assert(SUMS <= 2 * TILE, "the sums must fit");
+        lds_byte *const to = qw == 0 ? (lds_byte *)lds_k : (lds_byte *)lds_v;
+        wait_and_barrier<0>();
+        if (wave >= 2) {
+#pragma unroll
+            for (int n = 0; n < D / 16; ++n)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) lds_store(to + (2 * n + j) * 1024 + 16 * lane, dq[n][j]);
+        }
+        wait_and_barrier<0>();
+        if (wave >= 2) return;
+#pragma unroll
+        for (int n = 0; n < D / 16; ++n)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) dq[n][j] += __builtin_bit_cast(f32x4, lds_load(to + (2 * n + j) * 1024 + 16 * lane));
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const int row = wq0 + 16 * j + col;
         if (row >= sq.count) continue;
-        uint16_t *out = a.dq.p + (int64_t)(sq.first + row) * a.dq.token + head * a.dq.head;
+        const int64_t token = sq.first + row;
 #pragma unroll
         for (int n = 0; n < D / 16; ++n)
             if (16 * n < a.d) {
                 const f32x4 x = dq[n][j] * (a.scale * L::kOfDs);
-                *reinterpret_cast<uint2 *>(out + 16 * n + 4 * g) = make_uint2(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]));
+                if (a.parts == 1)
+                    *reinterpret_cast<uint2 *>(a.dq.p + token * a.dq.token + head * a.dq.head + 16 * n + 4 * g) = make_uint2(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]));
+                else
+                    *reinterpret_cast<f32x4 *>(a.sums + ((unit.part * (int64_t)a.tokens_q + token) * a.hq + head) * a.d + 16 * n + 4 * g) = x;
             }
+    }
+}
+
+// dQ from the sums of the parts
+template <typename T>
+__global__ __launch_bounds__(256) void attn_dq_join_kernel(const Problem a)
+{
+    Joined j;
+    if (!join_rows(a.cu_q, a.sequences, a.tokens_q, a.hq, j)) return;
+    const int quads = a.d >> 2;
+    const int64_t step = (int64_t)a.tokens_q * a.hq * a.d;
+    for (int item = threadIdx.x; item < j.rows * quads; item += 256) {
+        const int row = item / quads, i = 4 * (item - row * quads);
+        const int64_t t = j.first + row;
+        const float *from = a.sums + (t * a.hq + j.head) * a.d + i;
+        f32x4 x = *reinterpret_cast<const f32x4 *>(from);
+        for (int p = 1; p < a.parts; ++p) x += *reinterpret_cast<const f32x4 *>(from + p * step);
+        *reinterpret_cast<uint2 *>(a.dq.p + t * a.dq.token + j.head * a.dq.head + i) = make_uint2(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]));
     }
 }
 
@@ -498,63 +646,126 @@ static Problem problem_of(const s24_attn_shape *s)
 
 using namespace s24_attn;
 
+namespace s24_attn {
+// How the work of a launch is cut up.  A workgroup's steps follow each other, and when causal the last queries (the first keys) take twice the average: few
+// workgroups, or some with many steps, leave most of the device idle.  Two ways out:
+// narrow   64 queries to a workgroup instead of 128, two waves for each 32.  For twice the copies: below three workgroups of 128 a compute unit.  (Forward, us, wide
+//          and narrow: 1 head of 64, 8192 tokens 125 and 84; 16 heads of 64, 4096 tokens 71 and 57; 20 heads, 4 x 1024 31 and 27; 12 heads, 8 x 1024 31 and 36;
+//          32 heads of 128, 4096 tokens 150 and 189.)
+// parts    of what a tile sums over.  Their sums go through memory in fp32, and another launch adds them: as many as make the estimate below the least.  (1 head of
+//          64, 8192 tokens, forward and backward: 84 and 338 us in one part, 33 and 85 in eight; 8 heads of 128, 40 tokens after 8000: 144 and 38 in eight.)
+struct Plan { int narrow, parts; };
+// Parts for `groups` workgroups with `steps` steps of `us` microseconds each, of which `busy` are taken on average, where a part's sums take `bytes` bytes: what the
+// longest takes, or all of them on the device, and 5 us for the second launch and 5 bytes a picosecond for sums that are written and read.
+static int parts_for(double groups, double steps, double busy, double us, double bytes)
+{
+    int best = 1;
+    double least = 0.0;
+    for (int p = 1; p <= 16; p *= 2) {
+        const double rounds = groups * p * busy / (2.0 * s24_cu_count());
+        const double t = us * steps / p * (rounds > 1.0 ? rounds : 1.0) + (p > 1 ? 5.0 + p * bytes * 2.0 / 5e6 : 0.0);
+        if (p == 1 || t < least) best = p, least = t;
+    }
+    return best;
+}
+// Of a long one among the sequences, whose lengths the host does not know: of several, twice the average
+static double per_sequence(int64_t tokens, const s24_attn_shape *s) { return (double)tokens * (s->sequences > 1 ? 2.0 / (double)s->sequences : 1.0); }
+static Plan plan_queries(const s24_attn_shape *s)
+{
+    const int64_t wide = most_tiles(s->tokens_q, s->sequences, 128) * s->hq;
+    if (wide >= 3 * (int64_t)s24_cu_count()) return {0, 1};
+    const double busy = s->causal && s->tokens_k > 0 ? 1.0 - 0.5 * (s->tokens_q < s->tokens_k ? (double)s->tokens_q / (double)s->tokens_k : 1.0) : 1.0;
+    return {1, parts_for((double)(most_tiles(s->tokens_q, s->sequences, 64) * s->hq), per_sequence(s->tokens_k, s) / 64.0, busy, s->d <= 64 ? 0.66 : 1.1,
+                         (double)s->tokens_q * (double)s->hq * (double)s->d * 4.0)};
+}
+static int plan_keys(const s24_attn_shape *s)
+{
+    return parts_for((double)(most_tiles(s->tokens_k, s->sequences, 128) * s->hkv), per_sequence(s->tokens_q, s) / 32.0 * (double)(s->hq / s->hkv), s->causal ? 0.5 : 1.0,
+                     s->d <= 64 ? 1.0 : 1.3, (double)s->tokens_k * (double)s->hkv * (double)s->d * 8.0);
+}
+static bool sane(const s24_attn_shape *s)
+{
+    return s != nullptr && s->tokens_q >= 0 && s->tokens_k >= 0 && s->sequences >= 0 && s->hq > 0 && s->hkv > 0 && s->hq % s->hkv == 0 && s->d > 0;
+}
+static int64_t stats_bytes(const s24_attn_shape *s) { return (s->tokens_q * s->hq * (int64_t)sizeof(float2) + 15) / 16 * 16; }
+
+template <typename T, int D> static void forward(const Problem &a, bool narrow, dim3 grid, hipStream_t st)
+{
+    if (narrow) attn_fwd_kernel<T, D, 2><<<grid, dim3(256), 0, st>>>(a);
+    else attn_fwd_kernel<T, D, 1><<<grid, dim3(256), 0, st>>>(a);
+}
+template <typename T> static int forward(const Problem &a, bool narrow, dim3 grid, dim3 join, hipStream_t st)
+{
+    if (a.d <= 64) forward<T, 64>(a, narrow, grid, st);
+    else forward<T, 128>(a, narrow, grid, st);
+    if (a.parts > 1) attn_fwd_join_kernel<T><<<join, dim3(256), 0, st>>>(a);
+    return s24_launch_status();
+}
+}  // namespace s24_attn
+
+extern "C" int64_t s24_attn_fwd_workspace(const s24_attn_shape *shape)
+{
+    if (!sane(shape)) return 0;
+    const int64_t parts = plan_queries(shape).parts;
+    return parts > 1 ? parts * (stats_bytes(shape) + shape->tokens_q * shape->hq * shape->d * 4) : 0;
+}
+
 extern "C" int s24_attn_fwd(const s24_attn_shape *shape, const s24_heads *Q, const s24_heads *K, const s24_heads *V, const s24_heads *O, float *lse,
-                            s24_dtype dt, void *stream)
+                            void *workspace, int64_t workspace_bytes, s24_dtype dt, void *stream)
 {
     S24_TRY(check_shape(shape, dt));
     S24_TRY(check_rows(Q, shape->tokens_q, shape->hq, shape->d, false));
     S24_TRY(check_rows(K, shape->tokens_k, shape->hkv, shape->d, false));
     S24_TRY(check_rows(V, shape->tokens_k, shape->hkv, shape->d, false));
     S24_TRY(check_rows(O, shape->tokens_q, shape->hq, shape->d, true));
-    S24_REQUIRE(s24_aligned(lse, 4), S24_ERR_ALIGN);
-    const int64_t groups = most_tiles(shape->tokens_q, shape->sequences, Forward<128>::BQ) * shape->hq;
-    S24_REQUIRE(groups <= kMostGroups, S24_ERR_SHAPE);
+    const int64_t need = s24_attn_fwd_workspace(shape);
+    S24_REQUIRE(workspace != nullptr || need == 0, S24_ERR_NULL);
+    S24_REQUIRE(s24_aligned(lse, 4) && s24_aligned(workspace, 16), S24_ERR_ALIGN);
+    S24_REQUIRE(workspace_bytes >= need, S24_ERR_SHAPE);
+    const Plan plan = plan_queries(shape);
+    const int64_t groups = most_tiles(shape->tokens_q, shape->sequences, plan.narrow ? 64 : 128) * shape->hq * plan.parts;
+    const int64_t join = most_tiles(shape->tokens_q, shape->sequences, kJoinRows) * shape->hq;
+    S24_REQUIRE(groups <= kMostGroups && join <= kMostGroups, S24_ERR_SHAPE);
     if (groups == 0) return S24_OK;
     Problem a = problem_of(shape);
     a.q = rows_of(Q), a.k = rows_of(K), a.v = rows_of(V), a.out = out_of(O), a.lse = lse;
+    a.parts = plan.parts, a.weights = static_cast<float2 *>(workspace);
+    a.sums = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan.parts * stats_bytes(shape));
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const dim3 grid((unsigned)groups), block(256);
-    if (dt == S24_BF16) {
-        if (a.d <= 64) attn_fwd_kernel<uint16_t, 64><<<grid, block, 0, st>>>(a);
-        else attn_fwd_kernel<uint16_t, 128><<<grid, block, 0, st>>>(a);
-    } else {
-        if (a.d <= 64) attn_fwd_kernel<s24_half, 64><<<grid, block, 0, st>>>(a);
-        else attn_fwd_kernel<s24_half, 128><<<grid, block, 0, st>>>(a);
-    }
-    return s24_launch_status();
+    const dim3 grid((unsigned)groups), join_grid((unsigned)join);
+    return dt == S24_BF16 ? forward<uint16_t>(a, plan.narrow, grid, join_grid, st) : forward<s24_half>(a, plan.narrow, grid, join_grid, st);
 }
 
 namespace s24_attn {
-// Parts in which the queries of a tile of keys are taken.  Two workgroups fit a compute unit, and when causal the first keys' have many times the work of
-// the last ones': fewer than three for each unit are cut up into four or more.  (The sums of a part travel through memory in fp32: with 1.7 rounds, 12 heads of
-// 64 and 8 x 1024 tokens, that costs more than it gives, 81 us to 67.)
-static int64_t parts_of(const s24_attn_shape *s)
+template <typename T, int D> static int backward(Problem a, const s24_attn_shape *s, hipStream_t st)
 {
-    const int64_t tiles = most_tiles(s->tokens_k, s->sequences, Backward<128>::BK) * s->hkv, units = s24_cu_count();
-    if (tiles == 0 || tiles >= 3 * units) return 1;
-    const int64_t parts = (4 * units + tiles - 1) / tiles, steps = (s->tokens_q / 32 + 1) * (s->hq / s->hkv);
-    return parts > 8 ? 8 : parts > steps ? steps : parts;
+    const dim3 block(256);
+    const Plan plan = plan_queries(s);
+    const int64_t rows = plan.narrow ? 64 : 128, queries = most_tiles(a.tokens_q, a.sequences, (int)rows) * a.hq, hkv = a.hq / a.group;
+    a.parts = plan.parts;
+    if (queries > 0) {
+        const dim3 grid((unsigned)(queries * a.parts));
+        if (plan.narrow) attn_dq_kernel<T, D, 2><<<grid, block, 0, st>>>(a);
+        else attn_dq_kernel<T, D, 1><<<grid, block, 0, st>>>(a);
+        if (a.parts > 1) attn_dq_join_kernel<T><<<dim3((unsigned)(most_tiles(a.tokens_q, a.sequences, kJoinRows) * a.hq)), block, 0, st>>>(a);
+    }
+    const int64_t keys = most_tiles(a.tokens_k, a.sequences, Backward<D>::BK) * hkv;
+    a.parts = plan_keys(s);
+    if (keys > 0) {
+        attn_dkv_kernel<T, D><<<dim3((unsigned)(keys * a.parts)), block, 0, st>>>(a);
+        if (a.parts > 1) attn_dkv_join_kernel<T><<<dim3((unsigned)(most_tiles(a.tokens_k, a.sequences, kJoinRows) * hkv)), block, 0, st>>>(a);
+    }
+    return s24_launch_status();
 }
-static int64_t stats_bytes(const s24_attn_shape *s) { return (s->tokens_q * s->hq * (int64_t)sizeof(float2) + 15) / 16 * 16; }
 }  // namespace s24_attn
 
 extern "C" int64_t s24_attn_bwd_workspace(const s24_attn_shape *shape)
 {
-    if (shape == nullptr || shape->tokens_q < 0 || shape->tokens_k < 0 || shape->sequences < 0 || shape->hq <= 0 || shape->hkv <= 0 || shape->hq % shape->hkv != 0 || shape->d < 0) return 0;
-    const int64_t parts = parts_of(shape);
-    return stats_bytes(shape) + (parts > 1 ? parts * shape->tokens_k * shape->hkv * 2 * shape->d * 4 : 0);
+    if (!sane(shape)) return 0;
+    const int64_t parts_q = plan_queries(shape).parts, parts_k = plan_keys(shape);
+    const int64_t q = parts_q > 1 ? parts_q * shape->tokens_q * shape->hq : 0, k = parts_k > 1 ? parts_k * shape->tokens_k * shape->hkv * 2 : 0;
+    return stats_bytes(shape) + (q > k ? q : k) * shape->d * 4;   // the sums of dQ are added before those of dK and dV are formed
 }
-
-namespace s24_attn {
-template <typename T, int D> static int backward(const Problem &a, int64_t tiles_k, int64_t tiles_q, hipStream_t st)
-{
-    if (tiles_q > 0) attn_dq_kernel<T, D><<<dim3((unsigned)tiles_q), dim3(256), 0, st>>>(a);
-    if (tiles_k > 0) attn_dkv_kernel<T, D><<<dim3((unsigned)(tiles_k * a.parts)), dim3(256), 0, st>>>(a);
-    if (tiles_k > 0 && a.parts > 1)
-        attn_dkv_join_kernel<T><<<dim3((unsigned)(most_tiles(a.tokens_k, a.sequences, kJoinRows) * (a.hq / a.group))), dim3(256), 0, st>>>(a);
-    return s24_launch_status();
-}
-}  // namespace s24_attn
 
 extern "C" int s24_attn_bwd(const s24_attn_shape *shape, const s24_heads *Q, const s24_heads *K, const s24_heads *V, const s24_heads *O,
                             const s24_heads *dO, const float *lse, const s24_heads *dQ, const s24_heads *dK, const s24_heads *dV, void *workspace,
@@ -566,15 +777,14 @@ extern "C" int s24_attn_bwd(const s24_attn_shape *shape, const s24_heads *Q, con
     S24_REQUIRE((lse != nullptr && workspace != nullptr) || shape->tokens_q == 0, S24_ERR_NULL);
     S24_REQUIRE(s24_aligned(lse, 4) && s24_aligned(workspace, 16), S24_ERR_ALIGN);
     S24_REQUIRE(workspace_bytes >= s24_attn_bwd_workspace(shape), S24_ERR_SHAPE);
-    const int64_t tiles_q = most_tiles(shape->tokens_q, shape->sequences, 128) * shape->hq;
-    const int64_t tiles_k = most_tiles(shape->tokens_k, shape->sequences, Backward<128>::BK) * shape->hkv;
-    S24_REQUIRE(tiles_q <= kMostGroups && tiles_k <= kMostGroups / 8, S24_ERR_SHAPE);
+    // (the largest of the launches: a join of sixteen rows, or sixteen parts of tiles of 64)
+    S24_REQUIRE(most_tiles(shape->tokens_q, shape->sequences, 4) * shape->hq <= kMostGroups && most_tiles(shape->tokens_k, shape->sequences, 4) * shape->hkv <= kMostGroups, S24_ERR_SHAPE);
     Problem a = problem_of(shape);
     a.q = rows_of(Q), a.k = rows_of(K), a.v = rows_of(V), a.o = rows_of(O), a.dO = rows_of(dO);
     a.dq = out_of(dQ), a.dk = out_of(dK), a.dv = out_of(dV);
-    a.lse = const_cast<float *>(lse), a.stats = static_cast<float2 *>(workspace), a.parts = (int)parts_of(shape);
+    a.lse = const_cast<float *>(lse), a.stats = static_cast<float2 *>(workspace);
     a.sums = reinterpret_cast<float *>(static_cast<char *>(workspace) + stats_bytes(shape));
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (dt == S24_BF16) return a.d <= 64 ? backward<uint16_t, 64>(a, tiles_k, tiles_q, st) : backward<uint16_t, 128>(a, tiles_k, tiles_q, st);
-    return a.d <= 64 ? backward<s24_half, 64>(a, tiles_k, tiles_q, st) : backward<s24_half, 128>(a, tiles_k, tiles_q, st);
+    if (dt == S24_BF16) return a.d <= 64 ? backward<uint16_t, 64>(a, shape, st) : backward<uint16_t, 128>(a, shape, st);
+    return a.d <= 64 ? backward<s24_half, 64>(a, shape, st) : backward<s24_half, 128>(a, shape, st);
 }

@@ -46,7 +46,8 @@ def run(s24, lq, lk, hq, hkv, d, dtype, causal=True, scale=None, views="projecti
     dO = normal((tq, hq, d), dtype, seed + 3)
     O, lse = torch.full((tq, hq, d), math.nan, dtype=dtype, device="cuda"), torch.full((hq, tq), math.nan, device="cuda")
     gq, gk = gpu_i32(cq), gpu_i32(ck)
-    s24.attn_fwd(Q, K, V, O, lse, gq, gk, causal, scale)
+    need = s24.attn_fwd_workspace(tq, tk, hq, hkv, d, len(lq))
+    s24.attn_fwd(Q, K, V, O, lse, torch.empty(need, dtype=torch.uint8, device="cuda"), gq, gk, causal, scale)
     ref, bound = packed(Q, K, V, cq, ck, d ** -0.5 if scale is None else scale, causal, dO if backward else None)
     what = f"lq {lq} lk {lk} heads {hq}/{hkv} d {d} {dtype} causal {causal}"
     assert_within(O, ref["O"], bound["O"], f"O, {what}")
@@ -113,7 +114,7 @@ def test_growing_scores(s24):
         Q[:, 0, 0], K[:, 0, 0], K[:, 0, 1], Q[:, 0, 1] = 1.0, (torch.arange(n) * step).to(BF16), (torch.arange(n) * step - (torch.arange(n) * step).to(BF16)).to(BF16), 1.0
         Q, K = Q.cuda(), K.cuda()
         O, lse = torch.empty_like(Q), torch.empty((1, n), device="cuda")
-        s24.attn_fwd(Q, K, V, O, lse, gpu_i32([0, n]), None, True, 1.0)
+        s24.attn_fwd(Q, K, V, O, lse, torch.empty(s24.attn_fwd_workspace(n, n, 1, 1, d, 1), dtype=torch.uint8, device="cuda"), gpu_i32([0, n]), None, True, 1.0)
         ref, bound = packed(Q, K, V, [0, n], [0, n], 1.0, True)
         assert_within(O, ref["O"], bound["O"], "O")
         assert_within(lse, ref["lse"], bound["lse"], "lse")
@@ -132,7 +133,7 @@ def test_other_sequences_do_not_reach_a_result(s24):
         for x in (clean, wide):
             Q, K, V = x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:-1]
             O, lse = torch.zeros((n, hq, d), dtype=BF16, device="cuda"), torch.zeros((hq, n), device="cuda")
-            s24.attn_fwd(Q, K, V, O, lse, gpu_i32(cu))
+            s24.attn_fwd(Q, K, V, O, lse, torch.empty(s24.attn_fwd_workspace(n, n, hq, hkv, d, 3), dtype=torch.uint8, device="cuda"), gpu_i32(cu))
             dO = normal((n, hq, d), BF16, 9)
             if x is wide:
                 dO[:cu[1]], dO[cu[2]:] = bad, bad
@@ -150,7 +151,7 @@ def test_gradients_against_differences(s24):
     cu = offsets(lens)
     x = {n: normal((cu[-1], h, d), F16, i) for i, (n, h) in enumerate((("Q", hq), ("K", hkv), ("V", hkv), ("W", hq)))}
     O, lse = torch.empty_like(x["Q"]), torch.empty((hq, cu[-1]), device="cuda")
-    s24.attn_fwd(x["Q"], x["K"], x["V"], O, lse, gpu_i32(cu))
+    s24.attn_fwd(x["Q"], x["K"], x["V"], O, lse, None, gpu_i32(cu))
     grads = {n: torch.empty_like(x[n]) for n in "QKV"}
     work = torch.empty(s24.attn_bwd_workspace(cu[-1], cu[-1], hq, hkv, d, 2), dtype=torch.uint8, device="cuda")
     s24.attn_bwd(x["Q"], x["K"], x["V"], O, x["W"], lse, grads["Q"], grads["K"], grads["V"], work, gpu_i32(cu))
