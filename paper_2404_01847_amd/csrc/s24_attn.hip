@@ -21,9 +21,12 @@ struct Problem {
     float *lse;            // [hq][tokens_q]
     float2 *stats;         // [hq][tokens_q], of the backward pass: what a row's exponents are taken from, and delta
     // Where a kernel's workgroups are few, what a tile sums over is cut into parts, whose sums another kernel adds
-    int parts;
-    float *sums;           // [parts][tokens][heads][values]
+    struct Cut {
+        int parts;
+        float *sums;       // [parts][tokens][heads][values]
+    } by_query, by_key;    // O or dQ; dK and dV
     float2 *weights;       // [parts][tokens_q][hq], of the forward pass: reference and sum
+    unsigned key_blocks;   // workgroups for dK and dV in a launch that has those for dQ after them
     const int *cu_q, *cu_k;
     int sequences, tokens_q, tokens_k, hq, group, d, causal;
     float scale;
@@ -45,9 +48,9 @@ template <int READS, int MATRIX, int STEPS> __device__ __forceinline__ void read
 
 // Which tile, head and part a workgroup has
 struct Unit { int tile, head, part; };
-__device__ __forceinline__ Unit unit_of(int heads, int parts)
+__device__ __forceinline__ Unit unit_of(unsigned block, int heads, int parts)
 {
-    const int units = heads * parts, tile = blockIdx.x / units, unit = head_of(blockIdx.x - tile * units, units), head = unit / parts;
+    const int units = heads * parts, tile = block / units, unit = head_of(block - tile * units, units), head = unit / parts;
     return {tile, head, unit - head * parts};
 }
 // The queries of a workgroup that goes over the keys, and what they see of them
@@ -86,7 +89,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
     __shared__ __align__(16) unsigned char lds_k[2][C::TILE], lds_v[2][C::TILE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4, qw = KS == 2 ? wave & 1 : wave, first_key = KS == 2 ? KEYS * (wave >> 1) : 0;
-    const Unit unit = unit_of(a.hq, a.parts);
+    const Unit unit = unit_of(blockIdx.x, a.hq, a.by_query.parts);
     const int head = unit.head, kv = head / a.group;
     int sequence, index, count;
     if (!find_tile(a.cu_q, a.sequences, a.tokens_q, BQ, unit.tile, lane, sequence, index, count)) return;
@@ -95,7 +98,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
     const Span sq = s_.q, sk = s_.k;
     const int wq0 = s_.q0 + 32 * qw, ahead = s_.ahead;
     const int all_tiles = s_.seen > 0 ? (s_.seen + C::BK - 1) / C::BK : 0;
-    const int begin = (int)((int64_t)all_tiles * unit.part / a.parts), tiles = (int)((int64_t)all_tiles * (unit.part + 1) / a.parts);
+    const int begin = (int)((int64_t)all_tiles * unit.part / a.by_query.parts), tiles = (int)((int64_t)all_tiles * (unit.part + 1) / a.by_query.parts);
 
     uint4 q[2][D / 32];
 #pragma unroll
@@ -219,7 +222,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
         const float sum = column_sum(l[j]), inverse = sum > 0.0f ? 1.0f / sum : 0.0f;
         if (row >= sq.count) continue;
         const int64_t token = sq.first + row;
-        if (a.parts == 1) {
+        if (a.by_query.parts == 1) {
             uint16_t *out = a.out.p + token * a.out.token + head * a.out.head;
 #pragma unroll
             for (int n = 0; n < D / 16; ++n)
@@ -231,7 +234,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
             const int64_t at = (unit.part * (int64_t)a.tokens_q + token) * a.hq + head;
 #pragma unroll
             for (int n = 0; n < D / 16; ++n)
-                if (16 * n < a.d) *reinterpret_cast<f32x4 *>(a.sums + at * a.d + 16 * n + 4 * g) = o[n][j];
+                if (16 * n < a.d) *reinterpret_cast<f32x4 *>(a.by_query.sums + at * a.d + 16 * n + 4 * g) = o[n][j];
             if (g == 0) a.weights[at] = make_float2(m[j], sum);
         }
     }
@@ -261,12 +264,12 @@ __global__ __launch_bounds__(256) void attn_fwd_join_kernel(const Problem a)
         const int row = item / quads, i = 4 * (item - row * quads);
         const int64_t t = j.first + row, at = t * a.hq + j.head;
         float m = -1e30f, l = 0.0f;
-        for (int p = 0; p < a.parts; ++p) m = fmaxf(m, a.weights[at + p * step].x);
+        for (int p = 0; p < a.by_query.parts; ++p) m = fmaxf(m, a.weights[at + p * step].x);
         f32x4 x = {};
-        for (int p = 0; p < a.parts; ++p) {
+        for (int p = 0; p < a.by_query.parts; ++p) {
             const float2 w = a.weights[at + p * step];
             const float f = __builtin_amdgcn_exp2f(w.x - m);
-            l = fmaf(w.y, f, l), x += *reinterpret_cast<const f32x4 *>(a.sums + (at + p * step) * a.d + i) * f;
+            l = fmaf(w.y, f, l), x += *reinterpret_cast<const f32x4 *>(a.by_query.sums + (at + p * step) * a.d + i) * f;
         }
         x *= l > 0.0f ? 1.0f / l : 0.0f;
         *reinterpret_cast<uint2 *>(a.out.p + t * a.out.token + j.head * a.out.head + i) = make_uint2(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]));
@@ -286,16 +289,15 @@ template <> struct Lift<s24_half> { static constexpr float kUp = 15.0f, kDown = 
 template <int D> struct Backward {
     static constexpr int BK = 128, BQ = 32, TILE = BQ * 2 * D, STAGE = 2 * TILE + 8 * BQ, VALUES = BK * 2 * D;   // a stage: queries, gradients, row statistics
 };
-template <typename T, int D>
-__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dkv_kernel(const Problem a)
+// tv, stages: C::VALUES and two times C::STAGE bytes of LDS
+template <typename T, int D> __device__ __forceinline__ void dkv_tile(const Problem &a, unsigned block, lds_byte *tv, lds_byte *stages)
 {
     using C = Backward<D>;
     using L = Lift<T>;
-    __shared__ __align__(16) unsigned char stages[2][C::STAGE], values[C::VALUES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
     const int hkv = a.hq / a.group;
-    const Unit unit = unit_of(hkv, a.parts);
+    const Unit unit = unit_of(block, hkv, a.by_key.parts);
     const int tile = unit.tile, kv = unit.head, part = unit.part;
     int sequence, index, count;
     if (!find_tile(a.cu_k, a.sequences, a.tokens_k, C::BK, tile, lane, sequence, index, count)) return;
@@ -306,7 +308,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dkv_kernel(const Pr
     const int each = max(0, (sq.count + C::BQ - 1) / C::BQ - first);
     // the steps of all heads of the group, and of them this part's
     const int64_t all_steps = (int64_t)each * a.group;
-    const int begin = (int)(all_steps * part / a.parts), steps = (int)(all_steps * (part + 1) / a.parts) - begin;
+    const int begin = (int)(all_steps * part / a.by_key.parts), steps = (int)(all_steps * (part + 1) / a.by_key.parts) - begin;
 
     // The keys' fragments stay in registers, the values' come from LDS: with both, two waves would not fit a SIMD (3.6 ms instead of MEASURE for 8192 tokens,
     // 64 heads on 8 of 128).
@@ -320,7 +322,6 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dkv_kernel(const Pr
             fk[j][k] = i < a.d ? *reinterpret_cast<const uint4 *>(a.k.p + t * a.k.token + kv * a.k.head + i) : make_uint4(0, 0, 0, 0);
         }
     }
-    lds_byte *const tv = (lds_byte *)values;
     {
         Copy<D, C::BK, 4> cv;
         cv.init(wave, lane, (int)a.v.token * 2, a.d);
@@ -345,7 +346,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dkv_kernel(const Pr
         const int left = sq.count - next_tile * C::BQ;
         cq.offsets(min(left, C::BQ)), cdo.offsets(min(left, C::BQ));
         const int64_t t = sq.first + next_tile * C::BQ;
-        lds_byte *to = (lds_byte *)stages[stage];
+        lds_byte *to = stages + stage * C::STAGE;
         cq.start(a.q.p + t * a.q.token + next_head * a.q.head, to);
         cdo.start(a.dO.p + t * a.dO.token + next_head * a.dO.head, to + C::TILE);
         if (wave == 0) buffer_to_lds<4>(buffer_of(a.stats + ((int64_t)next_head * a.tokens_q + t)), (lds_ptr)(to + 2 * C::TILE), 4u * (uint32_t)min(lane, 2 * left - 2 + (lane & 1)));
@@ -358,8 +359,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dkv_kernel(const Pr
         const int q0 = qt * C::BQ, now = buffer;
         buffer ^= 1;
         if (++qt == first + each) qt = first;
-        if (a.causal && q0 + C::BQ - 1 + ahead < wk0) continue;   // no query of the tile sees a key of the wave
-        const lds_byte *tq = (const lds_byte *)stages[now], *tdo = tq + C::TILE, *stats = tdo + C::TILE;
+        if (wk0 >= sk.count || (a.causal && q0 + C::BQ - 1 + ahead < wk0)) continue;   // no query of the tile sees a key of the wave
+        const lds_byte *tq = stages + now * C::STAGE, *tdo = tq + C::TILE, *stats = tdo + C::TILE;
         f32x4 s[2][2], dp[2][2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) s[i][0] = s[i][1] = dp[i][0] = dp[i][1] = f32x4{};
@@ -378,26 +379,26 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dkv_kernel(const Pr
                 }
             }
         }
-        f32x4 lse[2], delta[2];
+        const bool all = q0 + C::BQ <= sq.count && wk0 + 32 <= sk.count && (!a.causal || wk0 + 31 <= q0 + ahead);
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < 2; ++i) {
+            f32x4 lse, delta;
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 const float4 two = __builtin_bit_cast(float4, lds_load(stats + 8 * (16 * i + 4 * g + 2 * r)));
-                lse[i][2 * r] = two.x, delta[i][2 * r] = two.y, lse[i][2 * r + 1] = two.z, delta[i][2 * r + 1] = two.w;
+                lse[2 * r] = two.x, delta[2 * r] = two.y, lse[2 * r + 1] = two.z, delta[2 * r + 1] = two.w;
             }
-        const bool all = q0 + C::BQ <= sq.count && wk0 + 32 <= sk.count && (!a.causal || wk0 + 31 <= q0 + ahead);
-        uint4 p[2], ds[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    s[i][j][r] = __builtin_amdgcn_exp2f(fmaf(s[i][j][r], c, -lse[i][r]));
-                    dp[i][j][r] = s[i][j][r] * fmaf(dp[i][j][r], L::kDown, -delta[i][r]);
+                    s[i][j][r] = __builtin_amdgcn_exp2f(fmaf(s[i][j][r], c, -lse[r]));
+                    dp[i][j][r] = s[i][j][r] * fmaf(dp[i][j][r], L::kDown, -delta[r]);
                 }
-            if (!all) {   // whatever stands in rows past the last, nothing of it stays
+        }
+        if (!all) {   // whatever stands in rows past the last, nothing of it stays
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
                 const int key = wk0 + 16 * j + col, lo = key >= sk.count ? sq.count : a.causal ? key - ahead : 0;
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
@@ -408,8 +409,10 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dkv_kernel(const Pr
                         s[i][j][r] = visible ? s[i][j][r] : 0.0f, dp[i][j][r] = visible ? dp[i][j][r] : 0.0f;
                     }
             }
-            p[j] = operand<T>(s[0][j], s[1][j]), ds[j] = operand<T>(dp[0][j], dp[1][j]);
         }
+        uint4 p[2], ds[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) p[j] = operand<T>(s[0][j], s[1][j]), ds[j] = operand<T>(dp[0][j], dp[1][j]);
 #pragma unroll
         for (int n = 0; n < D / 16; ++n) {
             const uint4 x = columns<D>(tdo, 0, n, lane), y = columns<D>(tq, 0, n, lane);
@@ -425,7 +428,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dkv_kernel(const Pr
         const int row = wk0 + 16 * j + col;
         if (row >= sk.count) continue;
         const int64_t t = sk.first + row;
-        if (a.parts == 1) {
+        if (a.by_key.parts == 1) {
             uint16_t *to_k = a.dk.p + t * a.dk.token + kv * a.dk.head, *to_v = a.dv.p + t * a.dv.token + kv * a.dv.head;
 #pragma unroll
             for (int n = 0; n < D / 16; ++n)
@@ -435,7 +438,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dkv_kernel(const Pr
                     *reinterpret_cast<uint2 *>(to_v + 16 * n + 4 * g) = make_uint2(pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3]));
                 }
         } else {
-            float *to = a.sums + ((part * (int64_t)a.tokens_k + t) * hkv + kv) * 2 * a.d;
+            float *to = a.by_key.sums + ((part * (int64_t)a.tokens_k + t) * hkv + kv) * 2 * a.d;
 #pragma unroll
             for (int n = 0; n < D / 16; ++n)
                 if (16 * n < a.d) {
@@ -457,25 +460,24 @@ __global__ __launch_bounds__(256) void attn_dkv_join_kernel(const Problem a)
     for (int item = threadIdx.x; item < j.rows * quads; item += 256) {
         const int row = item / quads, i = 4 * (item - row * quads);
         const int64_t t = j.first + row;
-        const float *from = a.sums + (t * hkv + j.head) * 2 * a.d + i;
+        const float *from = a.by_key.sums + (t * hkv + j.head) * 2 * a.d + i;
         f32x4 x = *reinterpret_cast<const f32x4 *>(from);
-        for (int p = 1; p < a.parts; ++p) x += *reinterpret_cast<const f32x4 *>(from + p * step);
+        for (int p = 1; p < a.by_key.parts; ++p) x += *reinterpret_cast<const f32x4 *>(from + p * step);
         uint16_t *to = i < a.d ? a.dk.p + t * a.dk.token + j.head * a.dk.head + i : a.dv.p + t * a.dv.token + j.head * a.dv.head + i - a.d;
         *reinterpret_cast<uint2 *>(to) = make_uint2(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]));
     }
 }
 
 // dQ, over the keys that a workgroup's queries see, 32 at a time and wave: four waves of 32 queries (KS = 1), or two pairs, of which each wave takes half of a
-// tile's keys (KS = 2).  Runs first: it leaves the row statistics to dK and dV.
-template <typename T, int D, int KS>
-__global__ __launch_bounds__(256, 2) void attn_dq_kernel(const Problem a)
+// tile's keys (KS = 2).  STATS: it reads the row statistics; else it forms them, and leaves them to dK and dV.
+// lk, lv: two tiles of LDS each, for keys and values
+template <typename T, int D, int KS, bool STATS> __device__ __forceinline__ void dq_tile(const Problem &a, unsigned block, lds_byte *lk, lds_byte *lv)
 {
     using L = Lift<T>;
     constexpr int BQ = 128 / KS, BK = 32 * KS, TILE = BK * 2 * D;
-    __shared__ __align__(16) unsigned char lds_k[2][TILE], lds_v[2][TILE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4, qw = KS == 2 ? wave & 1 : wave, first_key = KS == 2 ? 32 * (wave >> 1) : 0;
-    const Unit unit = unit_of(a.hq, a.parts);
+    const Unit unit = unit_of(block, a.hq, a.by_query.parts);
     const int head = unit.head, kv = head / a.group;
     int sequence, index, count;
     if (!find_tile(a.cu_q, a.sequences, a.tokens_q, BQ, unit.tile, lane, sequence, index, count)) return;
@@ -484,7 +486,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(const Problem a)
     const Span sq = s_.q, sk = s_.k;
     const int wq0 = s_.q0 + 32 * qw, ahead = s_.ahead;
     const int all_tiles = s_.seen > 0 ? (s_.seen + BK - 1) / BK : 0;
-    const int begin = (int)((int64_t)all_tiles * unit.part / a.parts), tiles = (int)((int64_t)all_tiles * (unit.part + 1) / a.parts);
+    const int begin = (int)((int64_t)all_tiles * unit.part / a.by_query.parts), tiles = (int)((int64_t)all_tiles * (unit.part + 1) / a.by_query.parts);
     uint4 q[2][D / 32], dO[2][D / 32];
     float lse[2], delta[2];
 #pragma unroll
@@ -497,14 +499,20 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(const Problem a)
             const int i = 32 * k + 8 * g;
             q[j][k] = i < a.d ? *reinterpret_cast<const uint4 *>(a.q.p + t * a.q.token + head * a.q.head + i) : make_uint4(0, 0, 0, 0);
             dO[j][k] = i < a.d ? *reinterpret_cast<const uint4 *>(a.dO.p + t * a.dO.token + head * a.dO.head + i) : make_uint4(0, 0, 0, 0);
+            if (STATS) continue;
             const uint4 o = i < a.d ? *reinterpret_cast<const uint4 *>(a.o.p + t * a.o.token + head * a.o.head + i) : make_uint4(0, 0, 0, 0);
             using Num = s24_num<T>;
             const uint32_t xs[4] = {o.x, o.y, o.z, o.w}, ys[4] = {dO[j][k].x, dO[j][k].y, dO[j][k].z, dO[j][k].w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) sum = fmaf(Num::lo(xs[e]), Num::lo(ys[e]), fmaf(Num::hi(xs[e]), Num::hi(ys[e]), sum));
         }
-        lse[j] = fmaf(a.lse[at], kLog2e, -L::kUp), delta[j] = column_sum(sum) * L::kDown;
-        if (g == 0 && wave < 4 / KS && unit.part == 0 && wq0 + 16 * j + col < sq.count) a.stats[at] = make_float2(lse[j], delta[j]);
+        if (STATS) {
+            const float2 of_row = a.stats[at];
+            lse[j] = of_row.x, delta[j] = of_row.y;
+        } else {
+            lse[j] = fmaf(a.lse[at], kLog2e, -L::kUp), delta[j] = column_sum(sum) * L::kDown;
+            if (g == 0 && wave < 4 / KS && unit.part == 0 && wq0 + 16 * j + col < sq.count) a.stats[at] = make_float2(lse[j], delta[j]);
+        }
     }
     const float c = a.scale * kLog2e;
     f32x4 dq[D / 16][2];
@@ -517,8 +525,8 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(const Problem a)
     auto copy = [&](int t) {
         const int left = sk.count - t * BK;
         if (left < BK) ck.offsets(left), cv.offsets(left);
-        ck.start(keys + (int64_t)t * BK * a.k.token, (lds_byte *)lds_k[t & 1]);
-        cv.start(values + (int64_t)t * BK * a.v.token, (lds_byte *)lds_v[t & 1]);
+        ck.start(keys + (int64_t)t * BK * a.k.token, lk + (t & 1) * TILE);
+        cv.start(values + (int64_t)t * BK * a.v.token, lv + (t & 1) * TILE);
     };
     if (begin < tiles) copy(begin);
     for (int t = begin; t < tiles; ++t) {
@@ -526,7 +534,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(const Problem a)
         if (t + 1 < tiles) copy(t + 1);
         const int k0 = t * BK + first_key;
         if (k0 >= s_.wave_seen) continue;
-        const lds_byte *tk = (const lds_byte *)lds_k[t & 1], *tv = (const lds_byte *)lds_v[t & 1];
+        const lds_byte *tk = lk + (t & 1) * TILE, *tv = lv + (t & 1) * TILE;
         f32x4 s[2][2], dp[2][2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) s[i][0] = s[i][1] = dp[i][0] = dp[i][1] = f32x4{};
@@ -569,7 +577,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(const Problem a)
     if constexpr (KS == 2) {   // as in the forward pass
         constexpr int SUMS = D / 16 * 2 * 1024;
         static_assert(SUMS <= 2 * TILE, "the sums must fit");
-        lds_byte *const to = qw == 0 ? (lds_byte *)lds_k : (lds_byte *)lds_v;
+        lds_byte *const to = qw == 0 ? lk : lv;
         wait_and_barrier<0>();
         if (wave >= 2) {
 #pragma unroll
@@ -593,12 +601,63 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(const Problem a)
         for (int n = 0; n < D / 16; ++n)
             if (16 * n < a.d) {
                 const f32x4 x = dq[n][j] * (a.scale * L::kOfDs);
-                if (a.parts == 1)
+                if (a.by_query.parts == 1)
                     *reinterpret_cast<uint2 *>(a.dq.p + token * a.dq.token + head * a.dq.head + 16 * n + 4 * g) = make_uint2(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]));
                 else
-                    *reinterpret_cast<f32x4 *>(a.sums + ((unit.part * (int64_t)a.tokens_q + token) * a.hq + head) * a.d + 16 * n + 4 * g) = x;
+                    *reinterpret_cast<f32x4 *>(a.by_query.sums + ((unit.part * (int64_t)a.tokens_q + token) * a.hq + head) * a.d + 16 * n + 4 * g) = x;
             }
     }
+}
+
+// Large grids: dQ, which runs first and leaves the row statistics; dK and dV
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void attn_dq_kernel(const Problem a)
+{
+    constexpr int TILE = 32 * 2 * D;
+    __shared__ __align__(16) unsigned char lds_k[2 * TILE], lds_v[2 * TILE];
+    dq_tile<T, D, 1, false>(a, blockIdx.x, (lds_byte *)lds_k, (lds_byte *)lds_v);
+}
+template <typename T, int D>
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dkv_kernel(const Problem a)
+{
+    using C = Backward<D>;
+    __shared__ __align__(16) unsigned char values[C::VALUES], stages[2 * C::STAGE];
+    dkv_tile<T, D>(a, blockIdx.x, (lds_byte *)values, (lds_byte *)stages);
+}
+// Small grids: all three in one launch, since neither fills the device to its end; the row statistics are formed before.  (16 heads of 128, 2048 tokens: 123 us
+// in turn, 97 together; 12 heads of 64, 1024 tokens 46 and 36; 32 heads of 128 on 8, 4096 tokens 485 and 480; 12 heads of 64, 8 x 1024 tokens 101 and 103.)
+template <typename T, int D>
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_bwd_kernel(const Problem a)
+{
+    using C = Backward<D>;
+    static_assert(2 * 64 * 2 * D <= C::VALUES && 2 * 64 * 2 * D <= 2 * C::STAGE, "two tiles must fit");
+    __shared__ __align__(16) unsigned char values[C::VALUES], stages[2 * C::STAGE];
+    if (blockIdx.x < a.key_blocks) dkv_tile<T, D>(a, blockIdx.x, (lds_byte *)values, (lds_byte *)stages);
+    else dq_tile<T, D, 2, true>(a, blockIdx.x - a.key_blocks, (lds_byte *)values, (lds_byte *)stages);
+}
+// stats[h][t]: what a row's exponents are taken from, and delta = dO.O; by 16 lanes, one for each of a row's (at most) 16 pieces
+template <typename T>
+__global__ __launch_bounds__(256) void attn_stats_kernel(const Problem a)
+{
+    using Num = s24_num<T>;
+    using L = Lift<T>;
+    const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4;
+    const int lane = threadIdx.x & 15;
+    if (item >= (int64_t)a.tokens_q * a.hq) return;
+    const int64_t t = item / a.hq;
+    const int h = (int)(item - t * a.hq);
+    float sum = 0.0f;
+    if (8 * lane < a.d) {
+        const uint4 x = *reinterpret_cast<const uint4 *>(a.dO.p + t * a.dO.token + h * a.dO.head + 8 * lane);
+        const uint4 y = *reinterpret_cast<const uint4 *>(a.o.p + t * a.o.token + h * a.o.head + 8 * lane);
+        const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum = fmaf(Num::lo(xs[i]), Num::lo(ys[i]), fmaf(Num::hi(xs[i]), Num::hi(ys[i]), sum));
+    }
+#pragma unroll
+    for (int s = 1; s < 16; s <<= 1) sum += __shfl_xor(sum, s);
+    const int64_t at = h * (int64_t)a.tokens_q + t;
+    if (lane == 0) a.stats[at] = make_float2(fmaf(a.lse[at], kLog2e, -L::kUp), sum * L::kDown);
 }
 
 // dQ from the sums of the parts
@@ -612,9 +671,9 @@ __global__ __launch_bounds__(256) void attn_dq_join_kernel(const Problem a)
     for (int item = threadIdx.x; item < j.rows * quads; item += 256) {
         const int row = item / quads, i = 4 * (item - row * quads);
         const int64_t t = j.first + row;
-        const float *from = a.sums + (t * a.hq + j.head) * a.d + i;
+        const float *from = a.by_query.sums + (t * a.hq + j.head) * a.d + i;
         f32x4 x = *reinterpret_cast<const f32x4 *>(from);
-        for (int p = 1; p < a.parts; ++p) x += *reinterpret_cast<const f32x4 *>(from + p * step);
+        for (int p = 1; p < a.by_query.parts; ++p) x += *reinterpret_cast<const f32x4 *>(from + p * step);
         *reinterpret_cast<uint2 *>(a.dq.p + t * a.dq.token + j.head * a.dq.head + i) = make_uint2(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]));
     }
 }
@@ -698,7 +757,7 @@ template <typename T> static int forward(const Problem &a, bool narrow, dim3 gri
 {
     if (a.d <= 64) forward<T, 64>(a, narrow, grid, st);
     else forward<T, 128>(a, narrow, grid, st);
-    if (a.parts > 1) attn_fwd_join_kernel<T><<<join, dim3(256), 0, st>>>(a);
+    if (a.by_query.parts > 1) attn_fwd_join_kernel<T><<<join, dim3(256), 0, st>>>(a);
     return s24_launch_status();
 }
 }  // namespace s24_attn
@@ -729,42 +788,41 @@ extern "C" int s24_attn_fwd(const s24_attn_shape *shape, const s24_heads *Q, con
     if (groups == 0) return S24_OK;
     Problem a = problem_of(shape);
     a.q = rows_of(Q), a.k = rows_of(K), a.v = rows_of(V), a.out = out_of(O), a.lse = lse;
-    a.parts = plan.parts, a.weights = static_cast<float2 *>(workspace);
-    a.sums = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan.parts * stats_bytes(shape));
+    a.weights = static_cast<float2 *>(workspace);
+    a.by_query = {plan.parts, reinterpret_cast<float *>(static_cast<char *>(workspace) + plan.parts * stats_bytes(shape))};
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const dim3 grid((unsigned)groups), join_grid((unsigned)join);
     return dt == S24_BF16 ? forward<uint16_t>(a, plan.narrow, grid, join_grid, st) : forward<s24_half>(a, plan.narrow, grid, join_grid, st);
 }
 
 namespace s24_attn {
-template <typename T, int D> static int backward(Problem a, const s24_attn_shape *s, hipStream_t st)
+template <typename T, int D> static int backward(Problem a, bool narrow, hipStream_t st)
 {
     const dim3 block(256);
-    const Plan plan = plan_queries(s);
-    const int64_t rows = plan.narrow ? 64 : 128, queries = most_tiles(a.tokens_q, a.sequences, (int)rows) * a.hq, hkv = a.hq / a.group;
-    a.parts = plan.parts;
-    if (queries > 0) {
-        const dim3 grid((unsigned)(queries * a.parts));
-        if (plan.narrow) attn_dq_kernel<T, D, 2><<<grid, block, 0, st>>>(a);
-        else attn_dq_kernel<T, D, 1><<<grid, block, 0, st>>>(a);
-        if (a.parts > 1) attn_dq_join_kernel<T><<<dim3((unsigned)(most_tiles(a.tokens_q, a.sequences, kJoinRows) * a.hq)), block, 0, st>>>(a);
+    const int64_t hkv = a.hq / a.group, key_groups = most_tiles(a.tokens_k, a.sequences, 128) * hkv * a.by_key.parts,
+                  query_groups = most_tiles(a.tokens_q, a.sequences, narrow ? 64 : 128) * a.hq * a.by_query.parts;
+    if (narrow && query_groups > 0) {
+        a.key_blocks = (unsigned)((key_groups + 7) / 8 * 8);   // dQ's workgroups meet the XCDs as they would in a launch of their own
+        attn_stats_kernel<T><<<dim3((unsigned)(((int64_t)a.tokens_q * a.hq + 15) / 16)), block, 0, st>>>(a);
+        attn_bwd_kernel<T, D><<<dim3(a.key_blocks + (unsigned)query_groups), block, 0, st>>>(a);
+    } else {
+        if (query_groups > 0) attn_dq_kernel<T, D><<<dim3((unsigned)query_groups), block, 0, st>>>(a);
+        if (key_groups > 0) attn_dkv_kernel<T, D><<<dim3((unsigned)key_groups), block, 0, st>>>(a);
     }
-    const int64_t keys = most_tiles(a.tokens_k, a.sequences, Backward<D>::BK) * hkv;
-    a.parts = plan_keys(s);
-    if (keys > 0) {
-        attn_dkv_kernel<T, D><<<dim3((unsigned)(keys * a.parts)), block, 0, st>>>(a);
-        if (a.parts > 1) attn_dkv_join_kernel<T><<<dim3((unsigned)(most_tiles(a.tokens_k, a.sequences, kJoinRows) * hkv)), block, 0, st>>>(a);
-    }
+    if (query_groups > 0 && a.by_query.parts > 1)
+        attn_dq_join_kernel<T><<<dim3((unsigned)(most_tiles(a.tokens_q, a.sequences, kJoinRows) * a.hq)), block, 0, st>>>(a);
+    if (key_groups > 0 && a.by_key.parts > 1)
+        attn_dkv_join_kernel<T><<<dim3((unsigned)(most_tiles(a.tokens_k, a.sequences, kJoinRows) * hkv)), block, 0, st>>>(a);
     return s24_launch_status();
 }
+static int64_t query_sums(const s24_attn_shape *s, int parts) { return parts > 1 ? parts * s->tokens_q * s->hq * s->d * 4 : 0; }
+static int64_t key_sums(const s24_attn_shape *s, int parts) { return parts > 1 ? parts * s->tokens_k * s->hkv * s->d * 8 : 0; }
 }  // namespace s24_attn
 
 extern "C" int64_t s24_attn_bwd_workspace(const s24_attn_shape *shape)
 {
     if (!sane(shape)) return 0;
-    const int64_t parts_q = plan_queries(shape).parts, parts_k = plan_keys(shape);
-    const int64_t q = parts_q > 1 ? parts_q * shape->tokens_q * shape->hq : 0, k = parts_k > 1 ? parts_k * shape->tokens_k * shape->hkv * 2 : 0;
-    return stats_bytes(shape) + (q > k ? q : k) * shape->d * 4;   // the sums of dQ are added before those of dK and dV are formed
+    return stats_bytes(shape) + query_sums(shape, plan_queries(shape).parts) + key_sums(shape, plan_keys(shape));
 }
 
 extern "C" int s24_attn_bwd(const s24_attn_shape *shape, const s24_heads *Q, const s24_heads *K, const s24_heads *V, const s24_heads *O,
@@ -777,14 +835,17 @@ extern "C" int s24_attn_bwd(const s24_attn_shape *shape, const s24_heads *Q, con
     S24_REQUIRE((lse != nullptr && workspace != nullptr) || shape->tokens_q == 0, S24_ERR_NULL);
     S24_REQUIRE(s24_aligned(lse, 4) && s24_aligned(workspace, 16), S24_ERR_ALIGN);
     S24_REQUIRE(workspace_bytes >= s24_attn_bwd_workspace(shape), S24_ERR_SHAPE);
-    // (the largest of the launches: a join of sixteen rows, or sixteen parts of tiles of 64)
-    S24_REQUIRE(most_tiles(shape->tokens_q, shape->sequences, 4) * shape->hq <= kMostGroups && most_tiles(shape->tokens_k, shape->sequences, 4) * shape->hkv <= kMostGroups, S24_ERR_SHAPE);
+    // (no launch has more workgroups than these: sixteen parts of tiles of 64 or 128, a join or statistics of sixteen rows each)
+    S24_REQUIRE(most_tiles(shape->tokens_q, shape->sequences, 4) * shape->hq <= kMostGroups / 2 && most_tiles(shape->tokens_k, shape->sequences, 4) * shape->hkv <= kMostGroups / 2, S24_ERR_SHAPE);
     Problem a = problem_of(shape);
     a.q = rows_of(Q), a.k = rows_of(K), a.v = rows_of(V), a.o = rows_of(O), a.dO = rows_of(dO);
     a.dq = out_of(dQ), a.dk = out_of(dK), a.dv = out_of(dV);
     a.lse = const_cast<float *>(lse), a.stats = static_cast<float2 *>(workspace);
-    a.sums = reinterpret_cast<float *>(static_cast<char *>(workspace) + stats_bytes(shape));
+    const Plan plan = plan_queries(shape);
+    char *const sums = static_cast<char *>(workspace) + stats_bytes(shape);
+    a.by_query = {plan.parts, reinterpret_cast<float *>(sums)};
+    a.by_key = {plan_keys(shape), reinterpret_cast<float *>(sums + query_sums(shape, plan.parts))};
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (dt == S24_BF16) return a.d <= 64 ? backward<uint16_t, 64>(a, shape, st) : backward<uint16_t, 128>(a, shape, st);
-    return a.d <= 64 ? backward<s24_half, 64>(a, shape, st) : backward<s24_half, 128>(a, shape, st);
+    if (dt == S24_BF16) return a.d <= 64 ? backward<uint16_t, 64>(a, plan.narrow, st) : backward<uint16_t, 128>(a, plan.narrow, st);
+    return a.d <= 64 ? backward<s24_half, 64>(a, plan.narrow, st) : backward<s24_half, 128>(a, plan.narrow, st);
 }
