@@ -331,8 +331,9 @@ int s24_l1_norm_gap(const void *W, s24_dtype dt, int64_t r, int64_t q, int64_t l
  * arrays of sequences + 1 offsets that ascend from 0, on the DEVICE (offsets that do not are cut to what lies in the operands; rows of no
  * sequence are left as they are).  With lq queries and lk keys, query i sees the keys j < lk, and if `causal` of these j <= i + lk - lq: the
  * queries are the last ones of the keys (a prompt that is read in chunks; lq = lk in training).  A query that sees none gives a row of zeros.
- * S24_BF16 and S24_F16; S24_F32 returns S24_ERR_UNSUPPORTED.  Scores, row statistics and sums are fp32; the weights P and, backward, dS
- * are rounded to the storage type as operands of the second products.  Nothing is added in an order that depends on scheduling. */
+ * S24_BF16 and S24_F16; S24_F32 returns S24_ERR_UNSUPPORTED.  Scores, row statistics and sums are fp32; the weights P are rounded to the storage
+ * type as operands of the second products, dS of the backward pass goes into them as two parts (its rounded value and the rounded rest).
+ * Nothing is added in an order that depends on scheduling. */
 
 /* Rows of heads: element (t, h, i) of token t, head h at data + t*token + h*head + i (strides in elements), so that the parts of one
  * projection's result [tokens][(hq + 2 hkv) d] or of [heads][tokens][d] buffers are taken as they lie.  data 16-byte aligned, both strides

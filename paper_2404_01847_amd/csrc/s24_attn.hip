@@ -410,9 +410,9 @@ template <typename T, int D> __device__ __forceinline__ void dkv_tile(const Prob
                     }
             }
         }
-        uint4 p[2], ds[2];
+        uint4 p[2], ds[2], lo[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) p[j] = operand<T>(s[0][j], s[1][j]), ds[j] = operand<T>(dp[0][j], dp[1][j]);
+        for (int j = 0; j < 2; ++j) p[j] = operand<T>(s[0][j], s[1][j]), ds[j] = operand<T>(dp[0][j], dp[1][j]), lo[j] = rest<T>(ds[j], dp[0][j], dp[1][j]);
 #pragma unroll
         for (int n = 0; n < D / 16; ++n) {
             const uint4 x = columns<D>(tdo, 0, n, lane), y = columns<D>(tq, 0, n, lane);
@@ -420,6 +420,7 @@ template <typename T, int D> __device__ __forceinline__ void dkv_tile(const Prob
             for (int j = 0; j < 2; ++j) {
                 dv[n][j] = mma<T>(x, p[j], dv[n][j]);
                 dk[n][j] = mma<T>(y, ds[j], dk[n][j]);
+                dk[n][j] = mma<T>(y, lo[j], dk[n][j]);
             }
         }
     }
@@ -549,7 +550,7 @@ template <typename T, int D, int KS, bool STATS> __device__ __forceinline__ void
                     dp[i][j] = mma<T>(y, dO[j][k], dp[i][j]);
                 }
             }
-        uint4 ds[2];
+        uint4 ds[2], lo[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const int query = wq0 + 16 * j + col;
@@ -565,13 +566,15 @@ template <typename T, int D, int KS, bool STATS> __device__ __forceinline__ void
 #pragma unroll
                     for (int r = 0; r < 4; ++r) s[i][j][r] = k0 + 16 * i + 4 * g + r <= last ? s[i][j][r] : 0.0f;
             }
-            ds[j] = operand<T>(s[0][j], s[1][j]);
+            ds[j] = operand<T>(s[0][j], s[1][j]), lo[j] = rest<T>(ds[j], s[0][j], s[1][j]);
         }
 #pragma unroll
         for (int n = 0; n < D / 16; ++n) {
             const uint4 x = columns<D>(tk, first_key, n, lane);
             dq[n][0] = mma<T>(x, ds[0], dq[n][0]);
             dq[n][1] = mma<T>(x, ds[1], dq[n][1]);
+            dq[n][0] = mma<T>(x, lo[0], dq[n][0]);
+            dq[n][1] = mma<T>(x, lo[1], dq[n][1]);
         }
     }
     if constexpr (KS == 2) {   // as in the forward pass
@@ -835,8 +838,9 @@ extern "C" int s24_attn_bwd(const s24_attn_shape *shape, const s24_heads *Q, con
     S24_REQUIRE((lse != nullptr && workspace != nullptr) || shape->tokens_q == 0, S24_ERR_NULL);
     S24_REQUIRE(s24_aligned(lse, 4) && s24_aligned(workspace, 16), S24_ERR_ALIGN);
     S24_REQUIRE(workspace_bytes >= s24_attn_bwd_workspace(shape), S24_ERR_SHAPE);
-    // (no launch has more workgroups than these: sixteen parts of tiles of 64 or 128, a join or statistics of sixteen rows each)
-    S24_REQUIRE(most_tiles(shape->tokens_q, shape->sequences, 4) * shape->hq <= kMostGroups / 2 && most_tiles(shape->tokens_k, shape->sequences, 4) * shape->hkv <= kMostGroups / 2, S24_ERR_SHAPE);
+    // (a join has the most workgroups of all launches: parts are taken of few tiles only)
+    S24_REQUIRE(most_tiles(shape->tokens_q, shape->sequences, kJoinRows) * shape->hq <= kMostGroups / 2 &&
+                most_tiles(shape->tokens_k, shape->sequences, kJoinRows) * shape->hkv <= kMostGroups / 2, S24_ERR_SHAPE);
     Problem a = problem_of(shape);
     a.q = rows_of(Q), a.k = rows_of(K), a.v = rows_of(V), a.o = rows_of(O), a.dO = rows_of(dO);
     a.dq = out_of(dQ), a.dk = out_of(dK), a.dv = out_of(dV);
