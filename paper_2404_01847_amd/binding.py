@@ -532,11 +532,14 @@ def attn_fwd(Q, K, V, O, lse, workspace, cu_q, cu_k=None, causal=True, scale=Non
     workspace: a uint8 tensor of attn_fwd_workspace(...) bytes, None where that is 0."""
     where = "s24_attn_fwd"
     sq, sk, dtype, device, shape = _attn_operands(where, Q, K, cu_q, cu_k, causal, scale)
-    status = lib().s24_attn_fwd(shape, _heads(where, "Q", Q, sq, dtype, device), _heads(where, "K", K, sk, dtype, device), _heads(where, "V", V, sk, dtype, device),
-                                _heads(where, "O", O, sq, dtype, device),
-                                None if lse is None else _whole(where, "lse", lse, torch.float32, (sq[1], sq[0]), device),
-                                *((None, 0) if workspace is None else (_whole(where, "workspace", workspace, torch.uint8, workspace.shape, device), workspace.numel())),
-                                _dt(Q), _stream())
+    args = (shape, _heads(where, "Q", Q, sq, dtype, device), _heads(where, "K", K, sk, dtype, device), _heads(where, "V", V, sk, dtype, device),
+            _heads(where, "O", O, sq, dtype, device),
+            None if lse is None else _whole(where, "lse", lse, torch.float32, (sq[1], sq[0]), device),
+            *((None, 0) if workspace is None else (_whole(where, "workspace", workspace, torch.uint8, workspace.shape, device), workspace.numel())),
+            _dt(Q))
+    if device < 0:
+        raise ValueError(f"{where}: the tensors must lie on a GPU")
+    status = lib().s24_attn_fwd(*args, _stream())
     if status != 0:
         raise S24Error(status, where)
     return O
@@ -556,11 +559,14 @@ def attn_bwd(Q, K, V, O, dO, lse, dQ, dK, dV, workspace, cu_q, cu_k=None, causal
     """Gradients dQ, dK, dV of attn_fwd, from its O and lse; workspace: a uint8 tensor of attn_bwd_workspace(...) bytes."""
     where = "s24_attn_bwd"
     sq, sk, dtype, device, shape = _attn_operands(where, Q, K, cu_q, cu_k, causal, scale)
-    status = lib().s24_attn_bwd(shape, _heads(where, "Q", Q, sq, dtype, device), _heads(where, "K", K, sk, dtype, device), _heads(where, "V", V, sk, dtype, device),
-                                _heads(where, "O", O, sq, dtype, device), _heads(where, "dO", dO, sq, dtype, device),
-                                _whole(where, "lse", lse, torch.float32, (sq[1], sq[0]), device), _heads(where, "dQ", dQ, sq, dtype, device),
-                                _heads(where, "dK", dK, sk, dtype, device), _heads(where, "dV", dV, sk, dtype, device),
-                                _whole(where, "workspace", workspace, torch.uint8, workspace.shape, device), workspace.numel(), _dt(Q), _stream())
+    args = (shape, _heads(where, "Q", Q, sq, dtype, device), _heads(where, "K", K, sk, dtype, device), _heads(where, "V", V, sk, dtype, device),
+            _heads(where, "O", O, sq, dtype, device), _heads(where, "dO", dO, sq, dtype, device),
+            _whole(where, "lse", lse, torch.float32, (sq[1], sq[0]), device), _heads(where, "dQ", dQ, sq, dtype, device),
+            _heads(where, "dK", dK, sk, dtype, device), _heads(where, "dV", dV, sk, dtype, device),
+            _whole(where, "workspace", workspace, torch.uint8, workspace.shape, device), workspace.numel(), _dt(Q))
+    if device < 0:
+        raise ValueError(f"{where}: the tensors must lie on a GPU")
+    status = lib().s24_attn_bwd(*args, _stream())
     if status != 0:
         raise S24Error(status, where)
     return dQ, dK, dV
@@ -589,8 +595,11 @@ def kv_write(cache, K, V, places):
     where, device = "s24_kv_write", cache.device
     tokens = K.shape[0]
     shape = (tokens, cache.hkv, cache.d)
-    status = lib().s24_kv_write(cache.packed, _heads(where, "K", K, shape, cache.dtype, device), _heads(where, "V", V, shape, cache.dtype, device),
-                                _whole(where, "places", places, torch.int64, (tokens,), device), tokens, _dt(K), _stream())
+    args = (cache.packed, _heads(where, "K", K, shape, cache.dtype, device), _heads(where, "V", V, shape, cache.dtype, device),
+            _whole(where, "places", places, torch.int64, (tokens,), device), tokens, _dt(K))
+    if device < 0:
+        raise ValueError(f"{where}: the tensors must lie on a GPU")
+    status = lib().s24_kv_write(*args, _stream())
     if status != 0:
         raise S24Error(status, where)
 
@@ -599,9 +608,12 @@ def kv_read(cache, table, cu, K, V):
     """Position j of sequence i, in page table[i, j // page] (int32), to row cu[i] + j of K and V [tokens, hkv, d]."""
     where, device, n = "s24_kv_read", cache.device, table.shape
     shape = (K.shape[0], cache.hkv, cache.d)
-    status = lib().s24_kv_read(cache.packed, _whole(where, "table", table, torch.int32, (n[0], n[-1]), device), n[-1],
-                               _whole(where, "cu", cu, torch.int32, (n[0] + 1,), device), n[0], shape[0], _heads(where, "K", K, shape, cache.dtype, device),
-                               _heads(where, "V", V, shape, cache.dtype, device), _dt(K), _stream())
+    args = (cache.packed, _whole(where, "table", table, torch.int32, (n[0], n[-1]), device), n[-1],
+            _whole(where, "cu", cu, torch.int32, (n[0] + 1,), device), n[0], shape[0], _heads(where, "K", K, shape, cache.dtype, device),
+            _heads(where, "V", V, shape, cache.dtype, device), _dt(K))
+    if device < 0:
+        raise ValueError(f"{where}: the tensors must lie on a GPU")
+    status = lib().s24_kv_read(*args, _stream())
     if status != 0:
         raise S24Error(status, where)
     return K, V
@@ -618,10 +630,13 @@ def attn_decode(cache, Q, table, lengths, O, workspace, scale=None):
     where, device, n = "s24_attn_decode", cache.device, table.shape
     sequences, hq, d = Q.shape
     shape = (sequences, hq, cache.d)
-    status = lib().s24_attn_decode(cache.packed, _heads(where, "Q", Q, shape, cache.dtype, device), hq, _whole(where, "table", table, torch.int32, (sequences, n[-1]), device),
-                                   n[-1], _whole(where, "lengths", lengths, torch.int32, (sequences,), device), sequences, d ** -0.5 if scale is None else scale,
-                                   _heads(where, "O", O, shape, cache.dtype, device), _whole(where, "workspace", workspace, torch.uint8, workspace.shape, device),
-                                   workspace.numel(), _dt(Q), _stream())
+    args = (cache.packed, _heads(where, "Q", Q, shape, cache.dtype, device), hq, _whole(where, "table", table, torch.int32, (sequences, n[-1]), device),
+            n[-1], _whole(where, "lengths", lengths, torch.int32, (sequences,), device), sequences, d ** -0.5 if scale is None else scale,
+            _heads(where, "O", O, shape, cache.dtype, device), _whole(where, "workspace", workspace, torch.uint8, workspace.shape, device),
+            workspace.numel(), _dt(Q))
+    if device < 0:
+        raise ValueError(f"{where}: the tensors must lie on a GPU")
+    status = lib().s24_attn_decode(*args, _stream())
     if status != 0:
         raise S24Error(status, where)
     return O

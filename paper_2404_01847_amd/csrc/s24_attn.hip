@@ -804,6 +804,7 @@ template <typename T, int D> static int backward(Problem a, bool narrow, hipStre
     const dim3 block(256);
     const int64_t hkv = a.hq / a.group, key_groups = most_tiles(a.tokens_k, a.sequences, 128) * hkv * a.by_key.parts,
                   query_groups = most_tiles(a.tokens_q, a.sequences, narrow ? 64 : 128) * a.hq * a.by_query.parts;
+    if (query_groups == 0 && key_groups == 0) return S24_OK;
     if (narrow && query_groups > 0) {
         a.key_blocks = (unsigned)((key_groups + 7) / 8 * 8);   // dQ's workgroups meet the XCDs as they would in a launch of their own
         attn_stats_kernel<T><<<dim3((unsigned)(((int64_t)a.tokens_q * a.hq + 15) / 16)), block, 0, st>>>(a);

@@ -461,3 +461,66 @@ def test_runs_are_quantised_as_single_tokens_are(s24, dtype):
         assert torch.equal(a, b)
     want, _ = quantise(x)
     assert torch.equal(one.K.transpose(1, 2).reshape(n, hkv, d).cpu().double() - 128, want)
+
+
+def test_offsets_past_32_bits(s24):
+    """Heads that lie 2^31 values apart, and pages beyond 2^32 bytes."""
+    n, d, gap = 70, 64, 1 << 31
+    flat = torch.empty(gap + n * d, dtype=BF16, device="cuda")
+    apart = lambda: flat.as_strided((n, 2, d), (d, gap, 1))
+    values = [normal((n, 2, d), BF16, i) for i in range(4)]
+    cu, grads = gpu_i32([0, n]), {}
+    for far in (None, 0, 1, 2, 3):
+        x = list(values)
+        if far is not None:
+            apart().copy_(x[far])
+            x[far] = apart()
+        Q, K, V, dO = x
+        O, lse = torch.empty_like(values[0]), torch.empty((2, n), device="cuda")
+        s24.attn_fwd(Q, K, V, O, lse, None, cu)
+        out = [torch.empty_like(values[0]) for _ in range(3)]
+        work = torch.empty(s24.attn_bwd_workspace(n, n, 2, 2, d, 1), dtype=torch.uint8, device="cuda")
+        s24.attn_bwd(Q, K, V, O, dO, lse, *out, work, cu)
+        grads[far] = [O, *out]
+    for far in (0, 1, 2, 3):
+        assert all(torch.equal(a, b) for a, b in zip(grads[None], grads[far]))
+    s24.attn_fwd(*values[:3], apart(), None, None, cu)
+    assert torch.equal(apart(), grads[None][0])
+    del flat
+    from paper_2404_01847_amd.attention import PagedKV
+    for bits, pages in ((16, 70000), (8, 140000)):
+        cache = PagedKV(pages, 64, 8, 64, bits=bits)
+        assert cache.K.numel() * cache.K.element_size() > 1 << 32
+        K, V, Q = (normal((300, 8, 64), BF16, i) for i in range(3))
+        table = (pages - 1 - torch.arange(5, dtype=torch.int32, device="cuda"))[None]
+        at = torch.arange(300, device="cuda")
+        cache.write(K, V, table[0].long()[at // 64] * 64 + at % 64)
+        small, low = PagedKV(5, 64, 8, 64, bits=bits), torch.arange(5, dtype=torch.int32, device="cuda")[None]
+        small.write(K, V, at)
+        outs = []
+        for c, t in ((cache, table), (small, low)):
+            Ko, Vo, O = torch.empty_like(K), torch.empty_like(V), torch.empty_like(Q[:1])
+            c.read(t, gpu_i32([0, 300]), Ko, Vo)
+            c.attend(Q[:1], t, gpu_i32([300]), O)
+            outs.append((Ko, Vo, O))
+        assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
+def test_offsets_and_tables_that_hold_anything_stay_in_the_operands(s24):
+    """Offsets that do not ascend and page numbers that do not exist are cut to what there is: no result is promised, none is touched that is not theirs."""
+    n, hq, hkv, d = 100, 2, 1, 64
+    Q, K, V = normal((n, hq, d), BF16, 1), normal((n, hkv, d), BF16, 2), normal((n, hkv, d), BF16, 3)
+    O, lse = torch.zeros_like(Q), torch.zeros((hq, n), device="cuda")
+    work = torch.empty(max(s24.attn_bwd_workspace(n, n, hq, hkv, d, 3), s24.attn_fwd_workspace(n, n, hq, hkv, d, 3)), dtype=torch.uint8, device="cuda")
+    grads = [torch.zeros_like(x) for x in (Q, K, V)]
+    for bad in ([0, 1 << 30, 50, 100], [-5, 20, -7, 300], [90, 80, 70, 60], [0, 100, 100, 2 ** 31 - 1]):
+        for cq, ck in ((bad, bad), (bad, [0, 30, 60, 100]), ([0, 30, 60, 100], bad)):
+            s24.attn_fwd(Q, K, V, O, lse, work, gpu_i32(cq), gpu_i32(ck))
+            s24.attn_bwd(Q, K, V, O, Q, lse, *grads, work, gpu_i32(cq), gpu_i32(ck))
+    cache, table, K, V = filled(s24, [40, 40], 16, 1, 64, BF16, 16)
+    O = torch.empty_like(Q[:2])
+    table.fill_(-1)
+    cache.attend(Q[:2], table, gpu_i32([40, 1000000]), O)
+    cache.read(table, gpu_i32([30, -4, 200]), K, V)
+    cache.write(K, V, torch.randint(-(1 << 40), 1 << 40, (80,), device="cuda"))
+    torch.cuda.synchronize()
