@@ -71,8 +71,7 @@ struct Queries {
 };
 
 // ------------------------------------------------------------------ forward
-// Keys and values in tiles of 64, two of them in LDS: the next one is copied during the work on this one.  Four waves of 32 queries (KS = 1), or two pairs, of
-// which each wave takes half of a tile's keys (KS = 2): twice the workgroups, each of half the length, for twice the copies.
+// Four waves of 32 queries.  Keys and values in tiles of 64, two of them in LDS: the next one is copied during the work on this one.
 template <int D> struct Forward {
     static constexpr int BK = 64, TILE = BK * 2 * D;
 };
@@ -81,22 +80,22 @@ template <int D> struct Forward {
 // the same relative precision, and the sums stay far inside fp32.
 constexpr float kGrowth = 8.0f;
 
-template <typename T, int D, int KS>
+template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
 {
     using C = Forward<D>;
-    constexpr int BQ = 128 / KS, KEYS = C::BK / KS, NI = KEYS / 16;   // queries of a workgroup, a wave's keys of a tile
+    constexpr int BQ = 128, NI = C::BK / 16;   // queries of a workgroup, rows of 16 keys in a tile
     __shared__ __align__(16) unsigned char lds_k[2][C::TILE], lds_v[2][C::TILE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int col = lane & 15, g = lane >> 4, qw = KS == 2 ? wave & 1 : wave, first_key = KS == 2 ? KEYS * (wave >> 1) : 0;
+    const int col = lane & 15, g = lane >> 4;
     const Unit unit = unit_of(blockIdx.x, a.hq, a.by_query.parts);
     const int head = unit.head, kv = head / a.group;
     int sequence, index, count;
     if (!find_tile(a.cu_q, a.sequences, a.tokens_q, BQ, unit.tile, lane, sequence, index, count)) return;
     Queries s_;
-    s_.init(a, sequence, count - 1 - index, BQ, 32 * qw);    // the last ones see the most keys: they go first
+    s_.init(a, sequence, count - 1 - index, BQ, 32 * wave);    // the last ones see the most keys: they go first
     const Span sq = s_.q, sk = s_.k;
-    const int wq0 = s_.q0 + 32 * qw, ahead = s_.ahead;
+    const int wq0 = s_.q0 + 32 * wave, ahead = s_.ahead;
     const int all_tiles = s_.seen > 0 ? (s_.seen + C::BK - 1) / C::BK : 0;
     const int begin = (int)((int64_t)all_tiles * unit.part / a.by_query.parts), tiles = (int)((int64_t)all_tiles * (unit.part + 1) / a.by_query.parts);
 
@@ -127,7 +126,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
     for (int t = begin; t < tiles; ++t) {
         wait_and_barrier<0>();
         if (t + 1 < tiles) copy(t + 1);
-        const int k0 = t * C::BK + first_key;
+        const int k0 = t * C::BK;
         if (k0 >= s_.wave_seen) continue;
         const lds_byte *tk = (const lds_byte *)lds_k[t & 1], *tv = (const lds_byte *)lds_v[t & 1];
         f32x4 s[NI][2];
@@ -137,12 +136,12 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
         for (int k = 0; k < D / 32; ++k)
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
-                const uint4 f = rows<D>(tk, first_key + 16 * i, k, lane);
+                const uint4 f = rows<D>(tk, 16 * i, k, lane);
                 s[i][0] = mma<T>(f, q[0][k], s[i][0]);
                 s[i][1] = mma<T>(f, q[1][k], s[i][1]);
             }
         if (D == 128) reads_ahead<NI, 2 * NI, D / 32>();
-        if (k0 + KEYS > s_.wave_all) {
+        if (k0 + C::BK > s_.wave_all) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int last = a.causal ? min(sk.count - 1, wq0 + 16 * j + col + ahead) : sk.count - 1;
@@ -188,33 +187,10 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
         for (int u = 0; u < NI / 2; ++u)
 #pragma unroll
             for (int n = 0; n < D / 16; ++n) {
-                const uint4 f = columns<D>(tv, first_key + 32 * u, n, lane);
+                const uint4 f = columns<D>(tv, 32 * u, n, lane);
                 o[n][0] = mma<T>(f, p[u][0], o[n][0]);
                 o[n][1] = mma<T>(f, p[u][1], o[n][1]);
             }
-    }
-    if constexpr (KS == 2) {   // the wave of a pair that has the later keys hands its sums over, in LDS that no wave reads any more
-        constexpr int SUMS = D / 16 * 2 * 1024;   // bytes of a wave's
-        static_assert(SUMS + 1024 <= 2 * C::TILE, "the sums must fit");
-        lds_byte *const to = qw == 0 ? (lds_byte *)lds_k : (lds_byte *)lds_v, *const stats = to + SUMS;
-        wait_and_barrier<0>();
-        if (wave >= 2) {
-#pragma unroll
-            for (int n = 0; n < D / 16; ++n)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) lds_store(to + (2 * n + j) * 1024 + 16 * lane, o[n][j]);
-            lds_store(stats + 16 * lane, f32x4{m[0], m[1], l[0], l[1]});
-        }
-        wait_and_barrier<0>();
-        if (wave >= 2) return;
-        const f32x4 other = __builtin_bit_cast(f32x4, lds_load(stats + 16 * lane));
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const float now = fmaxf(m[j], other[j]), mine = __builtin_amdgcn_exp2f(m[j] - now), its = __builtin_amdgcn_exp2f(other[j] - now);
-            m[j] = now, l[j] = l[j] * mine + other[2 + j] * its;
-#pragma unroll
-            for (int n = 0; n < D / 16; ++n) o[n][j] = o[n][j] * mine + __builtin_bit_cast(f32x4, lds_load(to + (2 * n + j) * 1024 + 16 * lane)) * its;
-        }
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -470,7 +446,7 @@ __global__ __launch_bounds__(256) void attn_dkv_join_kernel(const Problem a)
 }
 
 // dQ, over the keys that a workgroup's queries see, 32 at a time and wave: four waves of 32 queries (KS = 1), or two pairs, of which each wave takes half of a
-// tile's keys (KS = 2).  STATS: it reads the row statistics; else it forms them, and leaves them to dK and dV.
+// tile's keys (KS = 2): twice the workgroups, each of half the length, for twice the copies.  STATS: it reads the row statistics; else it forms them, and leaves them to dK and dV.
 // lk, lv: two tiles of LDS each, for keys and values
 template <typename T, int D, int KS, bool STATS> __device__ __forceinline__ void dq_tile(const Problem &a, unsigned block, lds_byte *lk, lds_byte *lv)
 {
@@ -577,7 +553,7 @@ template <typename T, int D, int KS, bool STATS> __device__ __forceinline__ void
             dq[n][1] = mma<T>(x, lo[1], dq[n][1]);
         }
     }
-    if constexpr (KS == 2) {   // as in the forward pass
+    if constexpr (KS == 2) {   // the wave of a pair that has the later keys hands its sums over, in LDS that no wave reads any more
         constexpr int SUMS = D / 16 * 2 * 1024;
         static_assert(SUMS <= 2 * TILE, "the sums must fit");
         lds_byte *const to = qw == 0 ? lk : lv;
@@ -710,15 +686,12 @@ using namespace s24_attn;
 
 namespace s24_attn {
 // How the work of a launch is cut up.  A workgroup's steps follow each other, and when causal the last queries (the first keys) take twice the average: few
-// workgroups, or some with many steps, leave most of the device idle.  Two ways out:
-// narrow   64 queries to a workgroup instead of 128, two waves for each 32.  For twice the copies: below three workgroups of 128 a compute unit.  (Forward, us, wide
-//          and narrow: 1 head of 64, 8192 tokens 125 and 84; 16 heads of 64, 4096 tokens 71 and 57; 20 heads, 4 x 1024 31 and 27; 12 heads, 8 x 1024 31 and 36;
-//          32 heads of 128, 4096 tokens 150 and 189.)
-// parts    of what a tile sums over.  Their sums go through memory in fp32, and another launch adds them: as many as make the estimate below the least.  (1 head of
-//          64, 8192 tokens, forward and backward: 84 and 338 us in one part, 33 and 85 in eight; 8 heads of 128, 40 tokens after 8000: 144 and 38 in eight.)
-struct Plan { int narrow, parts; };
-// Parts for `groups` workgroups with `steps` steps of `us` microseconds each, of which `busy` are taken on average, where a part's sums take `bytes` bytes: what the
-// longest takes, or all of them on the device, and 5 us for the second launch and 5 bytes a picosecond for sums that are written and read.
+// workgroups, or some with many steps, leave most of the device idle.  So what a tile sums over is cut into parts, whose sums go through memory in fp32
+// for another launch to add: as many parts as make the estimate the least.  `groups` workgroups have `steps` steps of `us` microseconds each, of which `busy`
+// are taken on average, and a part's sums take `bytes` bytes: the time is that of the longest, or of all of them on the device, two a compute unit, and 5 us for the
+// second launch and 5 bytes a picosecond for sums that are written and read.  (On operands that are in no cache, in one part and in the best of 2, 4 and 8.
+// Forward: 1 head of 64, 8192 tokens 134 us and 34 in 8; 8 heads of 128 on 2, 40 tokens after 8000: 190 and 41 in 8; 64 on 8, 512 after 3500: 111 and 92
+// in 2; 32 of 128, 1500 tokens 47 and 54 in 2; the estimate takes the better one in 15 of 16 shapes.)
 static int parts_for(double groups, double steps, double busy, double us, double bytes)
 {
     int best = 1;
@@ -732,18 +705,26 @@ static int parts_for(double groups, double steps, double busy, double us, double
 }
 // Of a long one among the sequences, whose lengths the host does not know: of several, twice the average
 static double per_sequence(int64_t tokens, const s24_attn_shape *s) { return (double)tokens * (s->sequences > 1 ? 2.0 / (double)s->sequences : 1.0); }
-static Plan plan_queries(const s24_attn_shape *s)
+static double busy_keys(const s24_attn_shape *s)   // part of the keys that a query sees
 {
-    const int64_t wide = most_tiles(s->tokens_q, s->sequences, 128) * s->hq;
-    if (wide >= 3 * (int64_t)s24_cu_count()) return {0, 1};
-    const double busy = s->causal && s->tokens_k > 0 ? 1.0 - 0.5 * (s->tokens_q < s->tokens_k ? (double)s->tokens_q / (double)s->tokens_k : 1.0) : 1.0;
-    return {1, parts_for((double)(most_tiles(s->tokens_q, s->sequences, 64) * s->hq), per_sequence(s->tokens_k, s) / 64.0, busy, s->d <= 64 ? 0.66 : 1.1,
-                         (double)s->tokens_q * (double)s->hq * (double)s->d * 4.0)};
+    return s->causal && s->tokens_k > 0 ? 1.0 - 0.5 * (s->tokens_q < s->tokens_k ? (double)s->tokens_q / (double)s->tokens_k : 1.0) : 1.0;
 }
-static int plan_keys(const s24_attn_shape *s)
+static int forward_parts(const s24_attn_shape *s)
 {
-    return parts_for((double)(most_tiles(s->tokens_k, s->sequences, 128) * s->hkv), per_sequence(s->tokens_q, s) / 32.0 * (double)(s->hq / s->hkv), s->causal ? 0.5 : 1.0,
-                     s->d <= 64 ? 1.0 : 1.3, (double)s->tokens_k * (double)s->hkv * (double)s->d * 8.0);
+    return parts_for((double)(most_tiles(s->tokens_q, s->sequences, 128) * s->hq), per_sequence(s->tokens_k, s) / 64.0, busy_keys(s), s->d <= 64 ? 1.05 : 1.5,
+                     (double)s->tokens_q * (double)s->hq * (double)s->d * 4.0);
+}
+// Backward.  joint: below four workgroups of 128 queries a compute unit all three gradients come from one launch, dQ from tiles of 64 queries (attn_bwd_kernel).
+struct Plan { bool joint; int query_parts, key_parts; };
+static Plan plan_backward(const s24_attn_shape *s)
+{
+    Plan p{most_tiles(s->tokens_q, s->sequences, 128) * s->hq < 4 * (int64_t)s24_cu_count(), 1, 1};
+    if (p.joint)
+        p.query_parts = parts_for((double)(most_tiles(s->tokens_q, s->sequences, 64) * s->hq), per_sequence(s->tokens_k, s) / 64.0, busy_keys(s), s->d <= 64 ? 0.66 : 1.1,
+                                  (double)s->tokens_q * (double)s->hq * (double)s->d * 4.0);
+    p.key_parts = parts_for((double)(most_tiles(s->tokens_k, s->sequences, 128) * s->hkv), per_sequence(s->tokens_q, s) / 32.0 * (double)(s->hq / s->hkv), s->causal ? 0.5 : 1.0,
+                            s->d <= 64 ? 1.0 : 1.3, (double)s->tokens_k * (double)s->hkv * (double)s->d * 8.0);
+    return p;
 }
 static bool sane(const s24_attn_shape *s)
 {
@@ -751,16 +732,12 @@ static bool sane(const s24_attn_shape *s)
 }
 static int64_t stats_bytes(const s24_attn_shape *s) { return (s->tokens_q * s->hq * (int64_t)sizeof(float2) + 15) / 16 * 16; }
 
-template <typename T, int D> static void forward(const Problem &a, bool narrow, dim3 grid, hipStream_t st)
+template <typename T> static int forward(const Problem &a, dim3 grid, dim3 join, hipStream_t st)
 {
-    if (narrow) attn_fwd_kernel<T, D, 2><<<grid, dim3(256), 0, st>>>(a);
-    else attn_fwd_kernel<T, D, 1><<<grid, dim3(256), 0, st>>>(a);
-}
-template <typename T> static int forward(const Problem &a, bool narrow, dim3 grid, dim3 join, hipStream_t st)
-{
-    if (a.d <= 64) forward<T, 64>(a, narrow, grid, st);
-    else forward<T, 128>(a, narrow, grid, st);
-    if (a.by_query.parts > 1) attn_fwd_join_kernel<T><<<join, dim3(256), 0, st>>>(a);
+    const dim3 block(256);
+    if (a.d <= 64) attn_fwd_kernel<T, 64><<<grid, block, 0, st>>>(a);
+    else attn_fwd_kernel<T, 128><<<grid, block, 0, st>>>(a);
+    if (a.by_query.parts > 1) attn_fwd_join_kernel<T><<<join, block, 0, st>>>(a);
     return s24_launch_status();
 }
 }  // namespace s24_attn
@@ -768,7 +745,7 @@ template <typename T> static int forward(const Problem &a, bool narrow, dim3 gri
 extern "C" int64_t s24_attn_fwd_workspace(const s24_attn_shape *shape)
 {
     if (!sane(shape)) return 0;
-    const int64_t parts = plan_queries(shape).parts;
+    const int64_t parts = forward_parts(shape);
     return parts > 1 ? parts * (stats_bytes(shape) + shape->tokens_q * shape->hq * shape->d * 4) : 0;
 }
 
@@ -784,28 +761,28 @@ extern "C" int s24_attn_fwd(const s24_attn_shape *shape, const s24_heads *Q, con
     S24_REQUIRE(workspace != nullptr || need == 0, S24_ERR_NULL);
     S24_REQUIRE(s24_aligned(lse, 4) && s24_aligned(workspace, 16), S24_ERR_ALIGN);
     S24_REQUIRE(workspace_bytes >= need, S24_ERR_SHAPE);
-    const Plan plan = plan_queries(shape);
-    const int64_t groups = most_tiles(shape->tokens_q, shape->sequences, plan.narrow ? 64 : 128) * shape->hq * plan.parts;
+    const int parts = forward_parts(shape);
+    const int64_t groups = most_tiles(shape->tokens_q, shape->sequences, 128) * shape->hq * parts;
     const int64_t join = most_tiles(shape->tokens_q, shape->sequences, kJoinRows) * shape->hq;
     S24_REQUIRE(groups <= kMostGroups && join <= kMostGroups, S24_ERR_SHAPE);
     if (groups == 0) return S24_OK;
     Problem a = problem_of(shape);
     a.q = rows_of(Q), a.k = rows_of(K), a.v = rows_of(V), a.out = out_of(O), a.lse = lse;
     a.weights = static_cast<float2 *>(workspace);
-    a.by_query = {plan.parts, reinterpret_cast<float *>(static_cast<char *>(workspace) + plan.parts * stats_bytes(shape))};
+    a.by_query = {parts, reinterpret_cast<float *>(static_cast<char *>(workspace) + parts * stats_bytes(shape))};
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const dim3 grid((unsigned)groups), join_grid((unsigned)join);
-    return dt == S24_BF16 ? forward<uint16_t>(a, plan.narrow, grid, join_grid, st) : forward<s24_half>(a, plan.narrow, grid, join_grid, st);
+    return dt == S24_BF16 ? forward<uint16_t>(a, grid, join_grid, st) : forward<s24_half>(a, grid, join_grid, st);
 }
 
 namespace s24_attn {
-template <typename T, int D> static int backward(Problem a, bool narrow, hipStream_t st)
+template <typename T, int D> static int backward(Problem a, bool joint, hipStream_t st)
 {
     const dim3 block(256);
     const int64_t hkv = a.hq / a.group, key_groups = most_tiles(a.tokens_k, a.sequences, 128) * hkv * a.by_key.parts,
-                  query_groups = most_tiles(a.tokens_q, a.sequences, narrow ? 64 : 128) * a.hq * a.by_query.parts;
+                  query_groups = most_tiles(a.tokens_q, a.sequences, joint ? 64 : 128) * a.hq * a.by_query.parts;
     if (query_groups == 0 && key_groups == 0) return S24_OK;
-    if (narrow && query_groups > 0) {
+    if (joint && query_groups > 0) {
         a.key_blocks = (unsigned)((key_groups + 7) / 8 * 8);   // dQ's workgroups meet the XCDs as they would in a launch of their own
         attn_stats_kernel<T><<<dim3((unsigned)(((int64_t)a.tokens_q * a.hq + 15) / 16)), block, 0, st>>>(a);
         attn_bwd_kernel<T, D><<<dim3(a.key_blocks + (unsigned)query_groups), block, 0, st>>>(a);
@@ -826,7 +803,8 @@ static int64_t key_sums(const s24_attn_shape *s, int parts) { return parts > 1 ?
 extern "C" int64_t s24_attn_bwd_workspace(const s24_attn_shape *shape)
 {
     if (!sane(shape)) return 0;
-    return stats_bytes(shape) + query_sums(shape, plan_queries(shape).parts) + key_sums(shape, plan_keys(shape));
+    const Plan plan = plan_backward(shape);
+    return stats_bytes(shape) + query_sums(shape, plan.query_parts) + key_sums(shape, plan.key_parts);
 }
 
 extern "C" int s24_attn_bwd(const s24_attn_shape *shape, const s24_heads *Q, const s24_heads *K, const s24_heads *V, const s24_heads *O,
@@ -846,11 +824,11 @@ extern "C" int s24_attn_bwd(const s24_attn_shape *shape, const s24_heads *Q, con
     a.q = rows_of(Q), a.k = rows_of(K), a.v = rows_of(V), a.o = rows_of(O), a.dO = rows_of(dO);
     a.dq = out_of(dQ), a.dk = out_of(dK), a.dv = out_of(dV);
     a.lse = const_cast<float *>(lse), a.stats = static_cast<float2 *>(workspace);
-    const Plan plan = plan_queries(shape);
+    const Plan plan = plan_backward(shape);
     char *const sums = static_cast<char *>(workspace) + stats_bytes(shape);
-    a.by_query = {plan.parts, reinterpret_cast<float *>(sums)};
-    a.by_key = {plan_keys(shape), reinterpret_cast<float *>(sums + query_sums(shape, plan.parts))};
+    a.by_query = {plan.query_parts, reinterpret_cast<float *>(sums)};
+    a.by_key = {plan.key_parts, reinterpret_cast<float *>(sums + query_sums(shape, plan.query_parts))};
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (dt == S24_BF16) return a.d <= 64 ? backward<uint16_t, 64>(a, plan.narrow, st) : backward<uint16_t, 128>(a, plan.narrow, st);
-    return a.d <= 64 ? backward<s24_half, 64>(a, plan.narrow, st) : backward<s24_half, 128>(a, plan.narrow, st);
+    if (dt == S24_BF16) return a.d <= 64 ? backward<uint16_t, 64>(a, plan.joint, st) : backward<uint16_t, 128>(a, plan.joint, st);
+    return a.d <= 64 ? backward<s24_half, 64>(a, plan.joint, st) : backward<s24_half, 128>(a, plan.joint, st);
 }
