@@ -333,6 +333,7 @@ int s24_l1_norm_gap(const void *W, s24_dtype dt, int64_t r, int64_t q, int64_t l
  * queries are the last ones of the keys (a prompt that is read in chunks; lq = lk in training).  A query that sees none gives a row of zeros.
  * S24_BF16 and S24_F16; S24_F32 returns S24_ERR_UNSUPPORTED.  Scores, row statistics and sums are fp32; the weights P are rounded to the storage
  * type as operands of the second products, dS of the backward pass goes into them as two parts (its rounded value and the rounded rest).
+ * The scores' size must stay below 2^23, up to which fp32 still holds their fractions' halves; NaN among what a query sees gives NaN.
  * Nothing is added in an order that depends on scheduling. */
 
 /* Rows of heads: element (t, h, i) of token t, head h at data + t*token + h*head + i (strides in elements), so that the parts of one
@@ -372,7 +373,7 @@ int s24_attn_bwd(const s24_attn_shape *shape, const s24_heads *Q, const s24_head
 /* Key-value cache in pages of `page` tokens (a power of two from 16 to 65536), hkv heads of d values (a multiple of 16 up to 128).
  *   bits = 16   K, V  [pages][hkv][page][d] values of the calls' dtype; k_step, v_step not used
  *   bits = 8    K, V  [pages][hkv][page][d] bytes and k_step, v_step [pages][hkv][page] fp32:  a token's head is s*n with
- *               s = max(max|x| / 127, 2^-126) rounded to fp32 and n the whole numbers nearest to x / s, ties to even
+ *               s = max(max|x| / 127, 2^-126) rounded to fp32 and n the whole numbers nearest to x / s, ties to even; s = NaN where an x is NaN or infinite
  * (The order of the values within a page of V and the form of a byte are the library's own; a page of a head is moved or shared as a whole.)
  * K, V, k_step, v_step are device memory of the caller, 16-byte aligned.  Sequence i has its positions j in page
  * table[i][j / page], table [sequences][width] on the device (page numbers that the cache does not have are cut to its last one).

@@ -195,7 +195,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const int row = wq0 + 16 * j + col;
-        const float sum = column_sum(l[j]), inverse = sum > 0.0f ? 1.0f / sum : 0.0f;
+        const float sum = column_sum(l[j]), inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
         if (row >= sq.count) continue;
         const int64_t token = sq.first + row;
         if (a.by_query.parts == 1) {
@@ -205,7 +205,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
                 if (16 * n < a.d)
                     *reinterpret_cast<uint2 *>(out + 16 * n + 4 * g) =
                         make_uint2(pack2<T>(o[n][j][0] * inverse, o[n][j][1] * inverse), pack2<T>(o[n][j][2] * inverse, o[n][j][3] * inverse));
-            if (a.lse != nullptr && g == 0) a.lse[(int64_t)head * a.tokens_q + token] = sum > 0.0f ? (m[j] + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+            if (a.lse != nullptr && g == 0) a.lse[(int64_t)head * a.tokens_q + token] = sum == 0.0f ? -INFINITY : (m[j] + __builtin_amdgcn_logf(sum)) * kLn2;
         } else {
             const int64_t at = (unit.part * (int64_t)a.tokens_q + token) * a.hq + head;
 #pragma unroll
@@ -247,9 +247,9 @@ __global__ __launch_bounds__(256) void attn_fwd_join_kernel(const Problem a)
             const float f = __builtin_amdgcn_exp2f(w.x - m);
             l = fmaf(w.y, f, l), x += *reinterpret_cast<const f32x4 *>(a.by_query.sums + (at + p * step) * a.d + i) * f;
         }
-        x *= l > 0.0f ? 1.0f / l : 0.0f;
+        x *= l == 0.0f ? 0.0f : 1.0f / l;
         *reinterpret_cast<uint2 *>(a.out.p + t * a.out.token + j.head * a.out.head + i) = make_uint2(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]));
-        if (i == 0 && a.lse != nullptr) a.lse[(int64_t)j.head * a.tokens_q + t] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+        if (i == 0 && a.lse != nullptr) a.lse[(int64_t)j.head * a.tokens_q + t] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
     }
 }
 

@@ -47,17 +47,27 @@ template <bool PAIR> struct Lane {
         live = c < cache.d && h < cache.hkv;
     }
 };
+// Magnitudes are compared as the bits that they are, two at a time: what is no number is the largest of all, and stays.
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
 // Largest of the lanes that hold a token of a head
-template <bool PAIR> __device__ __forceinline__ float token_max(float x)
+template <bool PAIR> __device__ __forceinline__ uint32_t token_max(uint32_t x)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    auto with = [&](int y) { return fmaxf(x, __builtin_bit_cast(float, y)); };
-    x = with(__builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0xB1, 0xf, 0xf, true));    // lanes 1 0 3 2 of four
-    x = with(__builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x4E, 0xf, 0xf, true));    // 2 3 0 1
-    x = with(__builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x141, 0xf, 0xf, true));   // eight, the other way round
-    if (!PAIR) x = with(__builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x140, 0xf, 0xf, true));   // sixteen
+    x = larger(x, __builtin_amdgcn_mov_dpp(x, 0xB1, 0xf, 0xf, true));    // lanes 1 0 3 2 of four
+    x = larger(x, __builtin_amdgcn_mov_dpp(x, 0x4E, 0xf, 0xf, true));    // 2 3 0 1
+    x = larger(x, __builtin_amdgcn_mov_dpp(x, 0x141, 0xf, 0xf, true));   // eight, the other way round
+    if (!PAIR) x = larger(x, __builtin_amdgcn_mov_dpp(x, 0x140, 0xf, 0xf, true));   // sixteen
 #endif
     return x;
+}
+// The step of a token whose magnitudes have these two as their largest: NaN if one of them is none or is infinite, so that nothing finite comes of it
+template <typename T> __device__ __forceinline__ float step_for(uint32_t two)
+{
+    const float most = s24_num<T>::lo(max(two & 0xFFFFu, two >> 16));
+    return most < INFINITY ? fmaxf(__fdiv_rn(most, 127.0f), 0x1p-126f) : NAN;
 }
 // Rows of 16 lanes: the odd rows of a and the even rows of b change places / the last two of a and the first two of b
 __device__ __forceinline__ void swap_rows(uint32_t &a, uint32_t &b)
@@ -103,14 +113,10 @@ __device__ __forceinline__ uint32_t four_bytes(uint32_t a, uint32_t b, uint32_t 
 {
     return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
 }
-template <typename T, bool PAIR> __device__ __forceinline__ float step_of(uint4 packed)
+template <typename T, bool PAIR> __device__ __forceinline__ float step_of(uint4 x)
 {
-    using Num = s24_num<T>;
-    const uint32_t w[4] = {packed.x, packed.y, packed.z, packed.w};
-    float most = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) most = fmaxf(most, fmaxf(fabsf(Num::lo(w[i])), fabsf(Num::hi(w[i]))));
-    return fmaxf(__fdiv_rn(token_max<PAIR>(most), 127.0f), 0x1p-126f);
+    const uint32_t sign = 0x7FFF7FFFu;
+    return step_for<T>(token_max<PAIR>(larger(larger(x.x & sign, x.y & sign), larger(x.z & sign, x.w & sign))));
 }
 
 // Many tokens: a wave looks at sixteen of them and takes, of K or of V, those runs that begin there and lie within sixteen aligned places of a page, one after
@@ -240,10 +246,10 @@ __global__ __launch_bounds__(256) void kv_write_kernel(const WriteArgs a)
         uint16_t *v = reinterpret_cast<uint16_t *>(a.c.v) + first * a.c.d + ((int64_t)(at >> 3) * a.c.d + i) * 8 + (at & 7);
         v[0] = (uint16_t)xv, v[8] = (uint16_t)(xv >> 16);
     } else {
-        float mk = fmaxf(fabsf(Num::lo(xk)), fabsf(Num::hi(xk))), mv = fmaxf(fabsf(Num::lo(xv)), fabsf(Num::hi(xv)));
+        uint32_t mk = xk & 0x7FFF7FFFu, mv = xv & 0x7FFF7FFFu;
 #pragma unroll
-        for (int s = 1; s < 64; s <<= 1) mk = fmaxf(mk, __shfl_xor(mk, s)), mv = fmaxf(mv, __shfl_xor(mv, s));
-        const float sk = fmaxf(__fdiv_rn(mk, 127.0f), 0x1p-126f), sv = fmaxf(__fdiv_rn(mv, 127.0f), 0x1p-126f);
+        for (int s = 1; s < 64; s <<= 1) mk = larger(mk, __shfl_xor(mk, s)), mv = larger(mv, __shfl_xor(mv, s));
+        const float sk = step_for<T>(mk), sv = step_for<T>(mv);
         const float ik = __builtin_amdgcn_rcpf(sk), iv = __builtin_amdgcn_rcpf(sv);
         if (lane == 0) a.c.ks[first + at] = sk, a.c.vs[first + at] = sv;
         if (!live) return;
@@ -575,7 +581,7 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
         l = column_sum(l);
         const int head = h * a.group + q0 + col;
         if (now.first >= begin && now.first + blocks_of(end) <= begin + each) {
-            const float inverse = l > 0.0f ? 1.0f / l : 0.0f;
+            const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
             uint16_t *out = a.o.p + now.b * a.o.token + head * a.o.head;
             if (col < mine) {
 #pragma unroll
@@ -640,7 +646,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const DecodeArgs a)
         const float4 v = waves[i][lane];
         x += v.x, y += v.y, w += v.z;
     }
-    const float inverse = w > 0.0f ? 1.0f / w : 0.0f;
+    const float inverse = w == 0.0f ? 0.0f : 1.0f / w;
     *out = pack2<T>(x * inverse, y * inverse);
 }
 

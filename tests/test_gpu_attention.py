@@ -524,3 +524,67 @@ def test_offsets_and_tables_that_hold_anything_stay_in_the_operands(s24):
     cache.read(table, gpu_i32([30, -4, 200]), K, V)
     cache.write(K, V, torch.randint(-(1 << 40), 1 << 40, (80,), device="cuda"))
     torch.cuda.synchronize()
+
+
+# ---------------------------------------------------------------------------------------------------- values that are no numbers, and extreme scores
+@pytest.mark.parametrize("n", [33, 2000])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_the_8_bit_cache_does_not_lose_what_is_no_number(s24, bad, n):
+    """Such a token's head has the step NaN: it reads back as NaN, and its sequence's attention is NaN; others stay."""
+    from paper_2404_01847_amd.attention import PagedKV
+    pages = -(-n // 16)
+    cache = PagedKV(2 * pages, 16, 8, 128, BF16, bits=8)
+    K, V = normal((2 * 16 * pages, 8, 128), BF16, 1), normal((2 * 16 * pages, 8, 128), BF16, 2)
+    K[5, 3, 17] = bad
+    V[9, 6, 100] = bad
+    cache.write(K, V, torch.arange(2 * 16 * pages, device="cuda"))
+    steps_k, steps_v = (t.transpose(1, 2).reshape(-1, 8) for t in (cache.k_step, cache.v_step))
+    assert steps_k.isnan().nonzero().tolist() == [[5, 3]] and steps_v.isnan().nonzero().tolist() == [[9, 6]]
+    table = torch.arange(2 * pages, dtype=torch.int32, device="cuda").view(2, pages)
+    Ko, Vo = torch.empty((2 * n, 8, 128), dtype=BF16, device="cuda"), torch.empty((2 * n, 8, 128), dtype=BF16, device="cuda")
+    cache.read(table, gpu_i32([0, n, 2 * n]), Ko, Vo)
+    assert Ko.isnan().all(2).nonzero().tolist() == [[5, 3]] and int(Ko.isnan().sum()) == 128
+    assert Vo.isnan().all(2).nonzero().tolist() == [[9, 6]] and int(Vo.isnan().sum()) == 128
+    Q = normal((2, 16, 128), BF16, 3)
+    O = torch.zeros_like(Q)
+    cache.attend(Q, table, gpu_i32([n, n]), O)
+    assert O[0, 6:8].isnan().all() and O[0, 12:14].isnan().all() and int(O.isnan().sum()) == 4 * 128
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n,heads", [(70, 2), (3000, 1)])     # in one part, and in several
+def test_what_is_no_number_shows_in_the_statistics_and_gradients(s24, n, heads, d):
+    from paper_2404_01847_amd.attention import Attention
+    cu = gpu_i32([0, n])
+    layer = Attention(heads, heads, d, n, n, BF16)
+    Q, K, V, dO = (normal((n, heads, d), BF16, i) for i in range(4))
+    K[40, 0, 3] = math.nan                                      # queries from 40 on see it
+    layer.forward(Q, K, V, cu)
+    dQ = layer.backward(Q, K, V, dO, cu)[0]
+    assert layer.lse[0, 40:].isnan().all() and layer.lse[0, :32].isfinite().all() and layer.lse[1:].isfinite().all()
+    assert layer.O[40:, 0].isnan().all() and dQ[40:, 0].isnan().all() and layer.O[:, 1:].isfinite().all() and dQ[:, 1:].isfinite().all()
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("sign", [-1, 1])
+def test_equal_scores_of_any_size_weigh_the_same(s24, bits, sign):
+    """All of a row's scores are 2^23 or its negative.  The weights are then one number, which the second product has rounded to its type: 2^-8, or 2^-11 with a
+    token's step, of the weighted sizes; the result's rounding is another 2^-8 of it."""
+    from paper_2404_01847_amd.attention import Attention
+    n, d = 300, 64
+    K, Q = torch.full((n, 1, d), sign * 2.0 ** 9, dtype=BF16, device="cuda"), torch.full((n, 1, d), 2.0 ** 11, dtype=BF16, device="cuda")
+    V = normal((n, 1, d), BF16, 1)
+
+    def bound(mean, size, weights):
+        return 2.0 ** -8 * mean.abs() + (1 + 2.0 ** -8) * (weights + 2.0 ** -13) * size
+    if bits == 16:
+        layer, count = Attention(1, 1, d, n, n, BF16), torch.arange(1, n + 1, device="cuda").view(-1, 1, 1)
+        O = layer.forward(Q, K, V, gpu_i32([0, n]))
+        mean, size = V.double().cumsum(0) / count, V.double().abs().cumsum(0) / count
+        assert ((O.double() - mean).abs() <= bound(mean, size, 2.0 ** -8)).all()
+    cache, table, _, _ = filled(s24, [n], 32, 1, d, BF16, bits)
+    cache.write(K, V, table[0].long().repeat_interleave(32)[:n] * 32 + torch.arange(n, device="cuda") % 32)
+    O = torch.full((1, 1, d), math.nan, dtype=BF16, device="cuda")
+    cache.attend(Q[:1], table, gpu_i32([n]), O)
+    x = held(V, bits).cuda()
+    assert ((O[0].double() - x.mean(0)).abs() <= bound(x.mean(0), x.abs().mean(0), 2.0 ** -11 if bits == 8 else 2.0 ** -8)).all()
