@@ -166,6 +166,31 @@ __device__ __forceinline__ bool find_tile(const int *cu, int sequences, int toke
     return find_item(sequences, t, lane, sequence, index, count, [&](int i) { return (span(cu, i, tokens).count + rows - 1) / rows; });
 }
 
+// The same for tiles that take unequal time, the longest of all sequences first, so that a launch does not end with a few long ones.  A sequence's tiles are
+// counted from its longest: tile j is of length min(longest, from - j), and there are `tiles`.  `at` is then j.  Found is the length L of which and above which
+// there are more than t tiles, and above which there are not.  Not `mixed`, or more sequences than a wave holds lengths of: one sequence after the other.
+struct Lengths { int tiles, from, longest; };
+template <typename Of> __device__ __forceinline__ bool find_by_length(bool mixed, int n, int t, int most, int lane, int &list, int &at, Of of)
+{
+    int count;
+    if (!mixed || n > 64) return find_item(n, t, lane, list, at, count, [&](int i) { return of(i).tiles; });
+    const Lengths mine = lane < n ? of(lane) : Lengths{0, 0, 0};
+    auto above = [&](int length) { return length < mine.longest ? min(max(mine.from - length, 0), mine.tiles) : 0; };
+    auto sum = [](int x) { return __builtin_amdgcn_readlane(running_sum(x), 63); };
+    if (t >= sum(above(0))) return false;
+    int lo = 0, hi = most;   // more than t tiles are longer than lo, no more than t longer than hi
+    while (hi - lo > 1) {
+        const int middle = (lo + hi) >> 1;
+        if (sum(above(middle)) > t) lo = middle;
+        else hi = middle;
+    }
+    const int before = above(hi);
+    int place;
+    if (!find_item(n, t - sum(before), lane, list, place, count, [&](int) { return above(hi - 1) - before; })) return false;
+    at = __builtin_amdgcn_readlane(before, list) + place;
+    return true;
+}
+
 // Workgroups are dealt round-robin to the eight XCDs: head of the workgroup at place s of a row of `heads`, such that an XCD has neighbouring ones, which
 // share keys and values in its L2.
 __device__ __forceinline__ int head_of(int s, int heads) { return heads % 8 == 0 ? (s & 7) * (heads >> 3) + (s >> 3) : s; }

@@ -29,6 +29,7 @@ struct Problem {
     unsigned key_blocks;   // workgroups for dK and dV in a launch that has those for dQ after them
     const int *cu_q, *cu_k;
     int sequences, tokens_q, tokens_k, hq, group, d, causal;
+    bool mix_queries, mix_keys;   // order of the tiles of queries, of keys: by length alone, or sequence by sequence
     float scale;
 };
 
@@ -70,6 +71,27 @@ struct Queries {
     }
 };
 
+// The workgroup's tile of `rows` queries: a sequence, and which of its tiles.  When causal the last ones see the most keys.
+__device__ __forceinline__ bool find_queries(const Problem &a, int rows, int t, int lane, int &sequence, int &tile)
+{
+    int at;
+    auto of = [&](int i) {
+        const int n = (span(a.cu_q, i, a.tokens_q).count + rows - 1) / rows, keys = (span(a.cu_k, i, a.tokens_k).count + rows - 1) / rows;
+        return a.causal ? Lengths{n, max(keys, n), INT32_MAX} : Lengths{n, INT32_MAX, max(keys, 1)};
+    };
+    if (!find_by_length(a.mix_queries, a.sequences, t, max(a.tokens_q, a.tokens_k) / rows + 1, lane, sequence, at, of)) return false;
+    tile = of(sequence).tiles - 1 - at;
+    return true;
+}
+// Of `rows` keys: when causal the first ones are seen by the most queries, by all of them as far as the queries have keys before them.
+__device__ __forceinline__ bool find_keys(const Problem &a, int rows, int t, int lane, int &sequence, int &tile)
+{
+    return find_by_length(a.mix_keys, a.sequences, t, max(a.tokens_q, a.tokens_k) / rows + 1, lane, sequence, tile, [&](int i) {
+        const int n = (span(a.cu_k, i, a.tokens_k).count + rows - 1) / rows, queries = (span(a.cu_q, i, a.tokens_q).count + rows - 1) / rows;
+        return Lengths{n, a.causal ? n : INT32_MAX, max(queries, 1)};
+    });
+}
+
 // ------------------------------------------------------------------ forward
 // Four waves of 32 queries.  Keys and values in tiles of 64, two of them in LDS: the next one is copied during the work on this one.
 template <int D> struct Forward {
@@ -90,10 +112,10 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
     const int col = lane & 15, g = lane >> 4;
     const Unit unit = unit_of(blockIdx.x, a.hq, a.by_query.parts);
     const int head = unit.head, kv = head / a.group;
-    int sequence, index, count;
-    if (!find_tile(a.cu_q, a.sequences, a.tokens_q, BQ, unit.tile, lane, sequence, index, count)) return;
+    int sequence, index;
+    if (!find_queries(a, BQ, unit.tile, lane, sequence, index)) return;
     Queries s_;
-    s_.init(a, sequence, count - 1 - index, BQ, 32 * wave);    // the last ones see the most keys: they go first
+    s_.init(a, sequence, index, BQ, 32 * wave);
     const Span sq = s_.q, sk = s_.k;
     const int wq0 = s_.q0 + 32 * wave, ahead = s_.ahead;
     const int all_tiles = s_.seen > 0 ? (s_.seen + C::BK - 1) / C::BK : 0;
@@ -274,11 +296,11 @@ template <typename T, int D> __device__ __forceinline__ void dkv_tile(const Prob
     const int col = lane & 15, g = lane >> 4;
     const int hkv = a.hq / a.group;
     const Unit unit = unit_of(block, hkv, a.by_key.parts);
-    const int tile = unit.tile, kv = unit.head, part = unit.part;
-    int sequence, index, count;
-    if (!find_tile(a.cu_k, a.sequences, a.tokens_k, C::BK, tile, lane, sequence, index, count)) return;
+    const int kv = unit.head, part = unit.part;
+    int sequence, index;
+    if (!find_keys(a, C::BK, unit.tile, lane, sequence, index)) return;
     const Span sq = span(a.cu_q, sequence, a.tokens_q), sk = span(a.cu_k, sequence, a.tokens_k);
-    const int k0 = index * C::BK, wk0 = k0 + 32 * wave;   // the first keys are seen by the most queries: they go first
+    const int k0 = index * C::BK, wk0 = k0 + 32 * wave;
     const int ahead = sk.count - sq.count;
     const int first = a.causal ? max(0, k0 - ahead) / C::BQ : 0;                // query tiles
     const int each = max(0, (sq.count + C::BQ - 1) / C::BQ - first);
@@ -456,10 +478,10 @@ template <typename T, int D, int KS, bool STATS> __device__ __forceinline__ void
     const int col = lane & 15, g = lane >> 4, qw = KS == 2 ? wave & 1 : wave, first_key = KS == 2 ? 32 * (wave >> 1) : 0;
     const Unit unit = unit_of(block, a.hq, a.by_query.parts);
     const int head = unit.head, kv = head / a.group;
-    int sequence, index, count;
-    if (!find_tile(a.cu_q, a.sequences, a.tokens_q, BQ, unit.tile, lane, sequence, index, count)) return;
+    int sequence, index;
+    if (!find_queries(a, BQ, unit.tile, lane, sequence, index)) return;
     Queries s_;
-    s_.init(a, sequence, count - 1 - index, BQ, 32 * qw);
+    s_.init(a, sequence, index, BQ, 32 * qw);
     const Span sq = s_.q, sk = s_.k;
     const int wq0 = s_.q0 + 32 * qw, ahead = s_.ahead;
     const int all_tiles = s_.seen > 0 ? (s_.seen + BK - 1) / BK : 0;
@@ -678,6 +700,12 @@ static Problem problem_of(const s24_attn_shape *s)
     a.cu_q = s->cu_q, a.cu_k = s->cu_k;
     a.sequences = (int)s->sequences, a.tokens_q = (int)s->tokens_q, a.tokens_k = (int)s->tokens_k;
     a.hq = (int)s->hq, a.group = (int)(s->hq / s->hkv), a.d = (int)s->d, a.causal = s->causal != 0, a.scale = s->scale;
+    // By length, unless the launch has many times the workgroups that the device holds, and the order matters less than keys that are still in the L2s; or the
+    // queries are few for their keys, and a sequence's tiles are of nearly one length.  (Sequence by sequence and by length, forward: 8 x 2048 tokens of 8 heads of
+    // 128 115 and 83 us, 6 x 1536 of 16 heads 91 and 80, 16 x 1024 of 32 heads on 8 227 and 236, 4 x 4096 of 32 heads 549 and 587; 1000 tokens after 18000, of 64
+    // heads on 8, 308 and 328.  Tiles of keys gain at all sizes: gradients of 16 x 1024 tokens 866 and 712 us, of 8 x 2048 442 and 328.)
+    a.mix_queries = s->sequences > 1 && s->tokens_k <= 2 * s->tokens_q && most_tiles(s->tokens_q, s->sequences, 128) * s->hq <= 8 * (int64_t)s24_cu_count();
+    a.mix_keys = s->sequences > 1;
     return a;
 }
 }  // namespace s24_attn

@@ -588,3 +588,13 @@ def test_equal_scores_of_any_size_weigh_the_same(s24, bits, sign):
     cache.attend(Q[:1], table, gpu_i32([n]), O)
     x = held(V, bits).cuda()
     assert ((O[0].double() - x.mean(0)).abs() <= bound(x.mean(0), x.abs().mean(0), 2.0 ** -11 if bits == 8 else 2.0 ** -8)).all()
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("count", [2, 31, 64, 65])     # a wave holds the lengths of 64
+def test_tiles_of_many_sequences_are_all_taken(s24, count, causal):
+    """Tiles go by their length, whatever sequence they are of; empty sequences, and some with more keys or more queries, among them."""
+    rng = random.Random(count)
+    lk = [rng.choice([0, 1, 20, 129, 400, rng.randrange(1, 700)]) for _ in range(count - 1)] + [650]
+    lq = [rng.choice([n, n, n, n // 2, n + rng.choice([0, 140])]) for n in lk]
+    run(s24, lq, lk, 2, 1, 64, BF16, causal=causal, seed=count)
