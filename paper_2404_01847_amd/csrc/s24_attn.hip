@@ -54,32 +54,45 @@ __device__ __forceinline__ Unit unit_of(unsigned block, int heads, int parts)
     const int units = heads * parts, tile = block / units, unit = head_of(block - tile * units, units), head = unit / parts;
     return {tile, head, unit - head * parts};
 }
-// The queries of a workgroup that goes over the keys, and what they see of them
+// The rows of a workgroup that goes over the keys of a key-value head: the queries of the head's whole group, token by token.  So a tile's rows see almost the same
+// keys, and a sequence of few tokens fills a tile with those of several heads.  (512, 446 and 43 tokens after 4700 to 7400, 64 heads on 8 of 128: 309 us with one
+// head to a tile, 245 so; 8192 tokens of one sequence take the same.)
 struct Queries {
     Span q, k;
-    int q0, ahead;   // first query of the workgroup; query i sees the keys up to i + ahead
-    int seen, wave_seen, wave_all;   // keys that some query of the workgroup may see, that one of the wave may see, that all of them see
-    __device__ __forceinline__ void init(const Problem &a, int sequence, int tile, int rows, int first_of_wave)
+    int rows, row0, token0, extra, ahead;   // of the sequence; first one of the workgroup, its token, its place among the token's; token i sees the keys up to i + ahead
+    int seen, wave_seen, wave_all;          // keys that some row of the workgroup may see, that one of the wave may see, that all of them see
+    float inverse;
+    __device__ __forceinline__ void init(const Problem &a, int sequence, int tile, int rows_of_tile, int first_of_wave)
     {
         q = span(a.cu_q, sequence, a.tokens_q), k = span(a.cu_k, sequence, a.tokens_k);
-        q0 = tile * rows, ahead = k.count - q.count;
-        const int wq0 = q0 + first_of_wave;
-        auto up_to = [&](int i) { return a.causal ? min(k.count, i + 1 + ahead) : k.count; };
-        seen = up_to(min(q0 + rows, q.count) - 1);
-        wave_seen = wq0 < q.count ? up_to(min(wq0 + 32, q.count) - 1) : 0;
-        wave_all = wq0 + 32 > q.count ? 0 : up_to(wq0);
+        rows = q.count * a.group, row0 = tile * rows_of_tile, token0 = row0 / a.group, extra = row0 - token0 * a.group, ahead = k.count - q.count;
+        inverse = 1.0f / (float)a.group;
+        const int w0 = row0 + first_of_wave;
+        auto up_to = [&](int row) { return a.causal ? min(k.count, token0 + place_of(row - row0) + 1 + ahead) : k.count; };
+        seen = up_to(min(row0 + rows_of_tile, rows) - 1);
+        wave_seen = w0 < rows ? up_to(min(w0 + 32, rows) - 1) : 0;
+        wave_all = w0 + 32 > rows ? 0 : up_to(w0);
+        seen = __builtin_amdgcn_readfirstlane(seen), wave_seen = __builtin_amdgcn_readfirstlane(wave_seen), wave_all = __builtin_amdgcn_readfirstlane(wave_all);
+    }
+    // Tokens from the workgroup's first one to that of its row i.  (Half a step of the quotient is far more than the product's rounding: i + extra < 2^17.)
+    __device__ __forceinline__ int place_of(int i) const { return (int)(((float)(i + extra) + 0.5f) * inverse); }
+    // Token (of the packed ones), place in the sequence and head of the workgroup's row i; of its last one for those past the sequence
+    struct Row { int64_t token; int at, head; };
+    __device__ __forceinline__ Row row(const Problem &a, int kv, int i) const
+    {
+        const int mine = min(i, rows - 1 - row0), place = place_of(mine);
+        return {q.first + token0 + place, token0 + place, kv * a.group + mine + extra - place * a.group};
     }
 };
-
-// The workgroup's tile of `rows` queries: a sequence, and which of its tiles.  When causal the last ones see the most keys.
+// The workgroup's tile: a sequence, and which of its tiles.  When causal the last ones see the most keys.
 __device__ __forceinline__ bool find_queries(const Problem &a, int rows, int t, int lane, int &sequence, int &tile)
 {
     int at;
     auto of = [&](int i) {
-        const int n = (span(a.cu_q, i, a.tokens_q).count + rows - 1) / rows, keys = (span(a.cu_k, i, a.tokens_k).count + rows - 1) / rows;
+        const int n = (span(a.cu_q, i, a.tokens_q).count * a.group + rows - 1) / rows, keys = (span(a.cu_k, i, a.tokens_k).count * a.group + rows - 1) / rows;
         return a.causal ? Lengths{n, max(keys, n), INT32_MAX} : Lengths{n, INT32_MAX, max(keys, 1)};
     };
-    if (!find_by_length(a.mix_queries, a.sequences, t, max(a.tokens_q, a.tokens_k) / rows + 1, lane, sequence, at, of)) return false;
+    if (!find_by_length(a.mix_queries, a.sequences, t, max(a.tokens_q, a.tokens_k) * a.group / rows + 1, lane, sequence, at, of)) return false;
     tile = of(sequence).tiles - 1 - at;
     return true;
 }
@@ -93,7 +106,7 @@ __device__ __forceinline__ bool find_keys(const Problem &a, int rows, int t, int
 }
 
 // ------------------------------------------------------------------ forward
-// Four waves of 32 queries.  Keys and values in tiles of 64, two of them in LDS: the next one is copied during the work on this one.
+// Four waves of 32 rows.  Keys and values in tiles of 64, two of them in LDS: the next one is copied during the work on this one.
 template <int D> struct Forward {
     static constexpr int BK = 64, TILE = BK * 2 * D;
 };
@@ -106,25 +119,27 @@ template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
 {
     using C = Forward<D>;
-    constexpr int BQ = 128, NI = C::BK / 16;   // queries of a workgroup, rows of 16 keys in a tile
+    constexpr int BQ = 128, NI = C::BK / 16;   // rows of a workgroup, of 16 keys in a tile
     __shared__ __align__(16) unsigned char lds_k[2][C::TILE], lds_v[2][C::TILE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
-    const Unit unit = unit_of(blockIdx.x, a.hq, a.by_query.parts);
-    const int head = unit.head, kv = head / a.group;
+    const Unit unit = unit_of(blockIdx.x, a.hq / a.group, a.by_query.parts);
+    const int kv = unit.head;
     int sequence, index;
     if (!find_queries(a, BQ, unit.tile, lane, sequence, index)) return;
     Queries s_;
     s_.init(a, sequence, index, BQ, 32 * wave);
-    const Span sq = s_.q, sk = s_.k;
-    const int wq0 = s_.q0 + 32 * wave, ahead = s_.ahead;
+    const Span sk = s_.k;
     const int all_tiles = s_.seen > 0 ? (s_.seen + C::BK - 1) / C::BK : 0;
     const int begin = (int)((int64_t)all_tiles * unit.part / a.by_query.parts), tiles = (int)((int64_t)all_tiles * (unit.part + 1) / a.by_query.parts);
 
     uint4 q[2][D / 32];
+    int last[2];   // that a row sees
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const uint16_t *row = a.q.p + (int64_t)(sq.first + min(wq0 + 16 * j + col, sq.count - 1)) * a.q.token + head * a.q.head;
+        const Queries::Row of = s_.row(a, kv, 32 * wave + 16 * j + col);
+        const uint16_t *row = a.q.p + of.token * a.q.token + of.head * a.q.head;
+        last[j] = a.causal ? min(sk.count - 1, of.at + s_.ahead) : sk.count - 1;
 #pragma unroll
         for (int k = 0; k < D / 32; ++k)
             q[j][k] = 32 * k + 8 * g < a.d ? *reinterpret_cast<const uint4 *>(row + 32 * k + 8 * g) : make_uint4(0, 0, 0, 0);
@@ -165,13 +180,11 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
         if (D == 128) reads_ahead<NI, 2 * NI, D / 32>();
         if (k0 + C::BK > s_.wave_all) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int last = a.causal ? min(sk.count - 1, wq0 + 16 * j + col + ahead) : sk.count - 1;
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int i = 0; i < NI; ++i)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) s[i][j][r] = k0 + 16 * i + 4 * g + r <= last ? s[i][j][r] : -INFINITY;
-            }
+                    for (int r = 0; r < 4; ++r) s[i][j][r] = k0 + 16 * i + 4 * g + r <= last[j] ? s[i][j][r] : -INFINITY;
         }
         float top[2];
 #pragma unroll
@@ -216,10 +229,12 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const int row = wq0 + 16 * j + col;
+        const int row = 32 * wave + 16 * j + col;
         const float sum = column_sum(l[j]), inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
-        if (row >= sq.count) continue;
-        const int64_t token = sq.first + row;
+        if (s_.row0 + row >= s_.rows) continue;
+        const Queries::Row of = s_.row(a, kv, row);
+        const int64_t token = of.token;
+        const int head = of.head;
         if (a.by_query.parts == 1) {
             uint16_t *out = a.out.p + token * a.out.token + head * a.out.head;
 #pragma unroll
@@ -476,22 +491,27 @@ template <typename T, int D, int KS, bool STATS> __device__ __forceinline__ void
     constexpr int BQ = 128 / KS, BK = 32 * KS, TILE = BK * 2 * D;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4, qw = KS == 2 ? wave & 1 : wave, first_key = KS == 2 ? 32 * (wave >> 1) : 0;
-    const Unit unit = unit_of(block, a.hq, a.by_query.parts);
-    const int head = unit.head, kv = head / a.group;
+    const Unit unit = unit_of(block, a.hq / a.group, a.by_query.parts);
+    const int kv = unit.head;
     int sequence, index;
     if (!find_queries(a, BQ, unit.tile, lane, sequence, index)) return;
     Queries s_;
     s_.init(a, sequence, index, BQ, 32 * qw);
-    const Span sq = s_.q, sk = s_.k;
-    const int wq0 = s_.q0 + 32 * qw, ahead = s_.ahead;
+    const Span sk = s_.k;
     const int all_tiles = s_.seen > 0 ? (s_.seen + BK - 1) / BK : 0;
     const int begin = (int)((int64_t)all_tiles * unit.part / a.by_query.parts), tiles = (int)((int64_t)all_tiles * (unit.part + 1) / a.by_query.parts);
     uint4 q[2][D / 32], dO[2][D / 32];
     float lse[2], delta[2];
+    int last[2];   // that a row sees
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const int64_t t = sq.first + min(wq0 + 16 * j + col, sq.count - 1);
+        const int of_tile = 32 * qw + 16 * j + col;
+        const bool live = s_.row0 + of_tile < s_.rows;
+        const Queries::Row of = s_.row(a, kv, of_tile);
+        const int64_t t = of.token;
+        const int head = of.head;
         const int64_t at = (int64_t)head * a.tokens_q + t;
+        last[j] = !live ? -1 : a.causal ? min(sk.count - 1, of.at + s_.ahead) : sk.count - 1;
         float sum = 0.0f;
 #pragma unroll
         for (int k = 0; k < D / 32; ++k) {
@@ -510,7 +530,7 @@ template <typename T, int D, int KS, bool STATS> __device__ __forceinline__ void
             lse[j] = of_row.x, delta[j] = of_row.y;
         } else {
             lse[j] = fmaf(a.lse[at], kLog2e, -L::kUp), delta[j] = column_sum(sum) * L::kDown;
-            if (g == 0 && wave < 4 / KS && unit.part == 0 && wq0 + 16 * j + col < sq.count) a.stats[at] = make_float2(lse[j], delta[j]);
+            if (g == 0 && wave < 4 / KS && unit.part == 0 && live) a.stats[at] = make_float2(lse[j], delta[j]);
         }
     }
     const float c = a.scale * kLog2e;
@@ -551,18 +571,16 @@ template <typename T, int D, int KS, bool STATS> __device__ __forceinline__ void
         uint4 ds[2], lo[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int query = wq0 + 16 * j + col;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
                     s[i][j][r] = __builtin_amdgcn_exp2f(fmaf(s[i][j][r], c, -lse[j])) * fmaf(dp[i][j][r], L::kDown, -delta[j]);
             if (k0 + 32 > s_.wave_all) {
-                const int last = query >= sq.count ? -1 : a.causal ? min(sk.count - 1, query + ahead) : sk.count - 1;
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) s[i][j][r] = k0 + 16 * i + 4 * g + r <= last ? s[i][j][r] : 0.0f;
+                    for (int r = 0; r < 4; ++r) s[i][j][r] = k0 + 16 * i + 4 * g + r <= last[j] ? s[i][j][r] : 0.0f;
             }
             ds[j] = operand<T>(s[0][j], s[1][j]), lo[j] = rest<T>(ds[j], s[0][j], s[1][j]);
         }
@@ -595,9 +613,11 @@ template <typename T, int D, int KS, bool STATS> __device__ __forceinline__ void
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const int row = wq0 + 16 * j + col;
-        if (row >= sq.count) continue;
-        const int64_t token = sq.first + row;
+        const int row = 32 * qw + 16 * j + col;
+        if (s_.row0 + row >= s_.rows) continue;
+        const Queries::Row of = s_.row(a, kv, row);
+        const int64_t token = of.token;
+        const int head = of.head;
 #pragma unroll
         for (int n = 0; n < D / 16; ++n)
             if (16 * n < a.d) {
@@ -686,11 +706,17 @@ static int check_shape(const s24_attn_shape *s, s24_dtype dt)
     S24_REQUIRE(s24_valid_dtype(dt), S24_ERR_DTYPE);
     S24_REQUIRE(s->sequences >= 0 && s->tokens_q >= 0 && s->tokens_k >= 0 && s->hq > 0 && s->hkv > 0 && s->hq % s->hkv == 0, S24_ERR_SHAPE);
     S24_REQUIRE(s->sequences < INT32_MAX / 2 && s->tokens_q < INT32_MAX / 2 && s->tokens_k < INT32_MAX / 2 && s->hq < 65536, S24_ERR_SHAPE);
+    S24_REQUIRE((s->tokens_q > s->tokens_k ? s->tokens_q : s->tokens_k) * (s->hq / s->hkv) < INT32_MAX / 2, S24_ERR_SHAPE);
     S24_REQUIRE(s->d >= 16 && s->d % 16 == 0, S24_ERR_SHAPE);
     S24_REQUIRE(s->scale > 0.0f && s->scale <= 3.0e38f, S24_ERR_SHAPE);
     S24_REQUIRE(s24_aligned(s->cu_q, 4) && s24_aligned(s->cu_k, 4), S24_ERR_ALIGN);
     S24_REQUIRE(dt != S24_F32 && s->d <= 128, S24_ERR_UNSUPPORTED);
     return S24_OK;
+}
+// Workgroups (of one part) that go over the keys, for tiles of `rows` rows: the queries of a group of heads
+static int64_t query_groups(const s24_attn_shape *s, int rows)
+{
+    return (s->tokens_q * (s->hq / s->hkv) / rows + (s->tokens_q < s->sequences ? s->tokens_q : s->sequences)) * s->hkv;
 }
 static Rows rows_of(const s24_heads *v) { return {static_cast<const uint16_t *>(v->data), v->token, v->head}; }
 static Out out_of(const s24_heads *v) { return {static_cast<uint16_t *>(v->data), v->token, v->head}; }
@@ -704,7 +730,7 @@ static Problem problem_of(const s24_attn_shape *s)
     // queries are few for their keys, and a sequence's tiles are of nearly one length.  (Sequence by sequence and by length, forward: 8 x 2048 tokens of 8 heads of
     // 128 115 and 83 us, 6 x 1536 of 16 heads 91 and 80, 16 x 1024 of 32 heads on 8 227 and 236, 4 x 4096 of 32 heads 549 and 587; 1000 tokens after 18000, of 64
     // heads on 8, 308 and 328.  Tiles of keys gain at all sizes: gradients of 16 x 1024 tokens 866 and 712 us, of 8 x 2048 442 and 328.)
-    a.mix_queries = s->sequences > 1 && s->tokens_k <= 2 * s->tokens_q && most_tiles(s->tokens_q, s->sequences, 128) * s->hq <= 8 * (int64_t)s24_cu_count();
+    a.mix_queries = s->sequences > 1 && s->tokens_k <= 2 * s->tokens_q && query_groups(s, 128) <= 8 * (int64_t)s24_cu_count();
     a.mix_keys = s->sequences > 1;
     return a;
 }
@@ -739,16 +765,16 @@ static double busy_keys(const s24_attn_shape *s)   // part of the keys that a qu
 }
 static int forward_parts(const s24_attn_shape *s)
 {
-    return parts_for((double)(most_tiles(s->tokens_q, s->sequences, 128) * s->hq), per_sequence(s->tokens_k, s) / 64.0, busy_keys(s), s->d <= 64 ? 1.05 : 1.5,
+    return parts_for((double)query_groups(s, 128), per_sequence(s->tokens_k, s) / 64.0, busy_keys(s), s->d <= 64 ? 1.05 : 1.5,
                      (double)s->tokens_q * (double)s->hq * (double)s->d * 4.0);
 }
 // Backward.  joint: below four workgroups of 128 queries a compute unit all three gradients come from one launch, dQ from tiles of 64 queries (attn_bwd_kernel).
 struct Plan { bool joint; int query_parts, key_parts; };
 static Plan plan_backward(const s24_attn_shape *s)
 {
-    Plan p{most_tiles(s->tokens_q, s->sequences, 128) * s->hq < 4 * (int64_t)s24_cu_count(), 1, 1};
+    Plan p{query_groups(s, 128) < 4 * (int64_t)s24_cu_count(), 1, 1};
     if (p.joint)
-        p.query_parts = parts_for((double)(most_tiles(s->tokens_q, s->sequences, 64) * s->hq), per_sequence(s->tokens_k, s) / 64.0, busy_keys(s), s->d <= 64 ? 0.66 : 1.1,
+        p.query_parts = parts_for((double)query_groups(s, 64), per_sequence(s->tokens_k, s) / 64.0, busy_keys(s), s->d <= 64 ? 0.66 : 1.1,
                                   (double)s->tokens_q * (double)s->hq * (double)s->d * 4.0);
     p.key_parts = parts_for((double)(most_tiles(s->tokens_k, s->sequences, 128) * s->hkv), per_sequence(s->tokens_q, s) / 32.0 * (double)(s->hq / s->hkv), s->causal ? 0.5 : 1.0,
                             s->d <= 64 ? 1.0 : 1.3, (double)s->tokens_k * (double)s->hkv * (double)s->d * 8.0);
@@ -790,7 +816,7 @@ extern "C" int s24_attn_fwd(const s24_attn_shape *shape, const s24_heads *Q, con
     S24_REQUIRE(s24_aligned(lse, 4) && s24_aligned(workspace, 16), S24_ERR_ALIGN);
     S24_REQUIRE(workspace_bytes >= need, S24_ERR_SHAPE);
     const int parts = forward_parts(shape);
-    const int64_t groups = most_tiles(shape->tokens_q, shape->sequences, 128) * shape->hq * parts;
+    const int64_t groups = query_groups(shape, 128) * parts;
     const int64_t join = most_tiles(shape->tokens_q, shape->sequences, kJoinRows) * shape->hq;
     S24_REQUIRE(groups <= kMostGroups && join <= kMostGroups, S24_ERR_SHAPE);
     if (groups == 0) return S24_OK;
@@ -804,11 +830,10 @@ extern "C" int s24_attn_fwd(const s24_attn_shape *shape, const s24_heads *Q, con
 }
 
 namespace s24_attn {
-template <typename T, int D> static int backward(Problem a, bool joint, hipStream_t st)
+template <typename T, int D> static int backward(Problem a, bool joint, int64_t query_groups, hipStream_t st)
 {
     const dim3 block(256);
-    const int64_t hkv = a.hq / a.group, key_groups = most_tiles(a.tokens_k, a.sequences, 128) * hkv * a.by_key.parts,
-                  query_groups = most_tiles(a.tokens_q, a.sequences, joint ? 64 : 128) * a.hq * a.by_query.parts;
+    const int64_t hkv = a.hq / a.group, key_groups = most_tiles(a.tokens_k, a.sequences, 128) * hkv * a.by_key.parts;
     if (query_groups == 0 && key_groups == 0) return S24_OK;
     if (joint && query_groups > 0) {
         a.key_blocks = (unsigned)((key_groups + 7) / 8 * 8);   // dQ's workgroups meet the XCDs as they would in a launch of their own
@@ -857,6 +882,7 @@ extern "C" int s24_attn_bwd(const s24_attn_shape *shape, const s24_heads *Q, con
     a.by_query = {plan.query_parts, reinterpret_cast<float *>(sums)};
     a.by_key = {plan.key_parts, reinterpret_cast<float *>(sums + query_sums(shape, plan.query_parts))};
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (dt == S24_BF16) return a.d <= 64 ? backward<uint16_t, 64>(a, plan.joint, st) : backward<uint16_t, 128>(a, plan.joint, st);
-    return a.d <= 64 ? backward<s24_half, 64>(a, plan.joint, st) : backward<s24_half, 128>(a, plan.joint, st);
+    const int64_t groups = query_groups(shape, plan.joint ? 64 : 128) * plan.query_parts;
+    if (dt == S24_BF16) return a.d <= 64 ? backward<uint16_t, 64>(a, plan.joint, groups, st) : backward<uint16_t, 128>(a, plan.joint, groups, st);
+    return a.d <= 64 ? backward<s24_half, 64>(a, plan.joint, groups, st) : backward<s24_half, 128>(a, plan.joint, groups, st);
 }
