@@ -656,14 +656,14 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_bwd_kernel(const Pr
     if (blockIdx.x < a.key_blocks) dkv_tile<T, D>(a, blockIdx.x, (lds_byte *)values, (lds_byte *)stages);
     else dq_tile<T, D, 2, true>(a, blockIdx.x - a.key_blocks, (lds_byte *)values, (lds_byte *)stages);
 }
-// stats[h][t]: what a row's exponents are taken from, and delta = dO.O; by 16 lanes, one for each of a row's (at most) 16 pieces
-template <typename T>
+// stats[h][t]: what a row's exponents are taken from, and delta = dO.O; by LANES lanes, one for each of a row's pieces of 16 bytes
+template <typename T, int LANES>
 __global__ __launch_bounds__(256) void attn_stats_kernel(const Problem a)
 {
     using Num = s24_num<T>;
     using L = Lift<T>;
-    const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4;
-    const int lane = threadIdx.x & 15;
+    const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES;
+    const int lane = threadIdx.x & (LANES - 1);
     if (item >= (int64_t)a.tokens_q * a.hq) return;
     const int64_t t = item / a.hq;
     const int h = (int)(item - t * a.hq);
@@ -676,7 +676,7 @@ __global__ __launch_bounds__(256) void attn_stats_kernel(const Problem a)
         for (int i = 0; i < 4; ++i) sum = fmaf(Num::lo(xs[i]), Num::lo(ys[i]), fmaf(Num::hi(xs[i]), Num::hi(ys[i]), sum));
     }
 #pragma unroll
-    for (int s = 1; s < 16; s <<= 1) sum += __shfl_xor(sum, s);
+    for (int s = 1; s < LANES; s <<= 1) sum += __shfl_xor(sum, s);
     const int64_t at = h * (int64_t)a.tokens_q + t;
     if (lane == 0) a.stats[at] = make_float2(fmaf(a.lse[at], kLog2e, -L::kUp), sum * L::kDown);
 }
@@ -837,7 +837,7 @@ template <typename T, int D> static int backward(Problem a, bool joint, int64_t 
     if (query_groups == 0 && key_groups == 0) return S24_OK;
     if (joint && query_groups > 0) {
         a.key_blocks = (unsigned)((key_groups + 7) / 8 * 8);   // dQ's workgroups meet the XCDs as they would in a launch of their own
-        attn_stats_kernel<T><<<dim3((unsigned)(((int64_t)a.tokens_q * a.hq + 15) / 16)), block, 0, st>>>(a);
+        attn_stats_kernel<T, D / 8><<<dim3((unsigned)(((int64_t)a.tokens_q * a.hq + 2048 / D - 1) / (2048 / D))), block, 0, st>>>(a);
         attn_bwd_kernel<T, D><<<dim3(a.key_blocks + (unsigned)query_groups), block, 0, st>>>(a);
     } else {
         if (query_groups > 0) attn_dq_kernel<T, D><<<dim3((unsigned)query_groups), block, 0, st>>>(a);

@@ -340,6 +340,7 @@ struct DecodeArgs {
     int64_t width;
     int sequences, hq, group, sixteens, shares;   // sixteens: of query heads in a group; shares: of the positions of all sequences, for each of the heads
     float scale;
+    bool whole;    // a share is a sequence
     float *part;   // [2 shares][hq][d + 4]: sums, reference, weight, and two unused
 };
 __device__ __forceinline__ int length_of(const DecodeArgs &a, int b) { return min(max(a.lengths[b], 0), (int)(a.width << a.c.shift)); }
@@ -347,13 +348,17 @@ __device__ __forceinline__ int length_of(const DecodeArgs &a, int b) { return mi
 // (p + 1)*each - 1 of them.  A sequence that lies within one share is finished there.  Of others each share leaves the sums of its part: at 2p if the sequence
 // starts no later than the share, at 2p + 1 otherwise (a share has one such part at either end, at most).
 __device__ __forceinline__ int blocks_of(int length) { return (length + 63) >> 6; }
-__device__ __forceinline__ int total_blocks(const DecodeArgs &a, int before, int lane)   // of the sequences before that one
-{
-    int total = 0;   // below 2^31, as the host has seen to
-    for (int base = 0; base < before; base += 64)
-        total += __builtin_amdgcn_readlane(running_sum(base + lane < before ? blocks_of(length_of(a, base + lane)) : 0), 63);
-    return total;
-}
+// The blocks of 256 sequences, four to a lane: for more than 64, whose lengths else lie one to a lane.  (Looked through 64 at a time instead, 600 sequences cost
+// a launch 10 us.)
+struct Lists {
+    int n[4], sum;
+    __device__ __forceinline__ Lists(const DecodeArgs &a, int base, int lane)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) n[i] = base + 4 * lane + i < a.sequences ? blocks_of(length_of(a, base + 4 * lane + i)) : 0;
+        sum = n[0] + n[1] + n[2] + n[3];
+    }
+};
 
 // Sixteen bytes of the cache as operands of 8 channels (tokens) each
 __device__ __forceinline__ uint4 halves(uint32_t a, uint32_t b)
@@ -384,9 +389,7 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
     const int d = EXACT ? D : a.c.d;
     const int heads = a.c.hkv * a.sixteens, item = 4 * blockIdx.x + wave, share = item / heads, which = item - share * heads;
     const int h = which / a.sixteens, q0 = 16 * (which - h * a.sixteens), mine = min(16, a.group - q0);   // of the group's query heads
-    const int total = total_blocks(a, a.sequences, lane), each = (total + a.shares - 1) / a.shares, begin = share * each;
-    const int steps = min(total - begin, each);
-    if (share >= a.shares || steps <= 0) return;
+    if (share >= a.shares) return;
     struct Cursor { int b, first, pos, length; };   // a block: its sequence, which has `first` as its first block; the position at which it starts
     auto advance = [&](Cursor c) {
         c.pos += 64;
@@ -397,14 +400,50 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
         } while (c.length == 0);
         return c;
     };
-    Cursor now;
-    {
-        int place, count;
-        find_item(a.sequences, begin, lane, now.b, place, count, [&](int i) { return blocks_of(length_of(a, i)); });
-        now.first = begin - place, now.pos = 64 * place, now.length = __builtin_amdgcn_readfirstlane(length_of(a, now.b));
+    int each, begin, steps;
+    Cursor now{share, 0, 0, 0};
+    if (a.whole) {
+        now.length = __builtin_amdgcn_readfirstlane(length_of(a, share));
+        each = steps = blocks_of(now.length), begin = 0;
+        if (steps == 0)
+            for (int i = lane; i < mine * (d >> 3); i += 64) {
+                const int n = i / (d >> 3);
+                *reinterpret_cast<uint4 *>(a.o.p + share * a.o.token + (h * a.group + q0 + n) * a.o.head + 8 * (i - n * (d >> 3))) = make_uint4(0, 0, 0, 0);
+            }
+    } else if (a.sequences <= 64) {
+        const int length = lane < a.sequences ? length_of(a, lane) : 0, n = blocks_of(length), sum = running_sum(n), total = __builtin_amdgcn_readlane(sum, 63);
+        each = (total + a.shares - 1) / a.shares, begin = share * each, steps = min(total - begin, each);
+        now.b = steps > 0 ? __ffsll((unsigned long long)__ballot(begin < sum)) - 1 : 0;
+        now.first = __builtin_amdgcn_readlane(sum - n, now.b), now.length = __builtin_amdgcn_readlane(length, now.b);
+    } else {
+        Lists lists(a, 0, lane);
+        int total = lists.sum;
+        for (int base = 256; base < a.sequences; base += 256) total += Lists(a, base, lane).sum;
+        total = __builtin_amdgcn_readlane(running_sum(total), 63);   // below 2^31, as the host has seen to
+        each = (total + a.shares - 1) / a.shares, begin = share * each, steps = min(total - begin, each);
+        for (int base = 0, before = 0; base < a.sequences && steps > 0; base += 256) {
+            if (base > 0) lists = Lists(a, base, lane);
+            const int sum = running_sum(lists.sum);
+            const unsigned long long past = __ballot(begin < before + sum);
+            if (past == 0) {
+                before += __builtin_amdgcn_readlane(sum, 63);
+                continue;
+            }
+            const int owner = __ffsll(past) - 1, b = base + 4 * owner;
+            now.first = before + __builtin_amdgcn_readlane(sum - lists.sum, owner), now.b = b;
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+                const int n = __builtin_amdgcn_readlane(lists.n[i], owner);
+                if (now.b == b + i && begin >= now.first + n) now.first += n, ++now.b;
+            }
+            now.length = __builtin_amdgcn_readfirstlane(length_of(a, now.b));
+            break;
+        }
     }
+    if (steps <= 0) return;
+    now.pos = 64 * (begin - now.first);
 
-    // Positions 16*(col/4) .. of a block for K, 16*g .. for V: each sixteen lie in one page.  Offsets into the cache, for each in values of one byte or two.
+    // Positions 16*(col/4) .. of a block for K, 16*g .. for V: each sixteen lie in one page.
     const int token = d * (BITS / 8);   // bytes of a token of one head
     const uint32_t page_tokens = (uint32_t)a.c.hkv << a.c.shift;
     const unsigned char *const lane_k = a.c.k + ((int64_t)h << a.c.shift) * token + (col & 3) * token, *const lane_v = a.c.v + ((int64_t)h << a.c.shift) * token;
@@ -607,21 +646,37 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
     }
 }
 
-// The parts of a sequence that lies in more than one share, added: a workgroup a query head, a lane two channels, a wave every fourth part.
+// The parts of a sequence that lies in more than one share, added: WAVES waves a query head, a lane two channels, a wave every WAVES-th part.
 // A sequence of no positions, which no share has, gets its zeros.
-template <typename T>
+template <typename T, int WAVES>
 __global__ __launch_bounds__(256) void attn_join_kernel(const DecodeArgs a)
 {
     __shared__ float4 waves[4][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), b = blockIdx.x / a.hq, head = blockIdx.x - b * a.hq, d = a.c.d;
-    const int e = min(2 * lane, d - 2), length = length_of(a, b);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), d = a.c.d;
+    const int item = WAVES == 4 ? blockIdx.x : 4 * blockIdx.x + wave, b = item / a.hq, head = item - b * a.hq;
+    if (b >= a.sequences) return;
+    const int e = min(2 * lane, d - 2);
+    int total = 0, first = 0, blocks;   // of all sequences, of those before this one, of this one
+    if (a.sequences <= 64) {
+        const int n = lane < a.sequences ? blocks_of(length_of(a, lane)) : 0, sum = running_sum(n);
+        total = __builtin_amdgcn_readlane(sum, 63), blocks = __builtin_amdgcn_readlane(n, b), first = __builtin_amdgcn_readlane(sum, b) - blocks;
+    } else {
+        for (int base = 0; base < a.sequences; base += 256) {
+            const Lists lists(a, base, lane);
+            total += lists.sum;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) first += base + 4 * lane + i < b ? lists.n[i] : 0;
+        }
+        total = __builtin_amdgcn_readlane(running_sum(total), 63), first = __builtin_amdgcn_readlane(running_sum(first), 63);
+        blocks = blocks_of(length_of(a, b));
+    }
+    const int last = first + blocks - 1;
     uint32_t *out = reinterpret_cast<uint32_t *>(a.o.p + b * a.o.token + head * a.o.head + e);
-    if (length == 0) {
-        if (wave == 0 && 2 * lane < d) *out = 0;
+    if (last < first) {
+        if ((WAVES == 1 || wave == 0) && 2 * lane < d) *out = 0;
         return;
     }
-    const int each = (total_blocks(a, a.sequences, lane) + a.shares - 1) / a.shares, first = total_blocks(a, b, lane), last = first + blocks_of(length) - 1;
-    const int p0 = first / each, count = last / each - p0 + 1;
+    const int each = (total + a.shares - 1) / a.shares, p0 = first / each, count = last / each - p0 + 1;
     if (count == 1) return;
     const int64_t step = 2 * (int64_t)a.hq * (d + 4);
     const float *part = a.part + p0 * step + (int64_t)head * (d + 4);
@@ -632,22 +687,24 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const DecodeArgs a)
     for (int s = 1; s < 64; s <<= 1) ref = fmaxf(ref, __shfl_xor(ref, s));
     float x = 0.0f, y = 0.0f, w = 0.0f;
 #pragma unroll 4
-    for (int i = wave; i < count; i += 4) {
+    for (int i = WAVES == 4 ? wave : 0; i < count; i += WAVES) {
         const float *from = i == 0 ? part0 : part + i * step;
         const float2 of = *reinterpret_cast<const float2 *>(from + d), v = *reinterpret_cast<const float2 *>(from + e);
         const float f = __builtin_amdgcn_exp2f(of.x - ref);
         x = fmaf(f, v.x, x), y = fmaf(f, v.y, y), w = fmaf(f, of.y, w);
     }
-    waves[wave][lane] = make_float4(x, y, w, 0.0f);
-    __syncthreads();
-    if (wave != 0 || 2 * lane >= d) return;
+    if constexpr (WAVES == 4) {
+        waves[wave][lane] = make_float4(x, y, w, 0.0f);
+        __syncthreads();
+        if (wave != 0) return;
 #pragma unroll
-    for (int i = 1; i < 4; ++i) {
-        const float4 v = waves[i][lane];
-        x += v.x, y += v.y, w += v.z;
+        for (int i = 1; i < 4; ++i) {
+            const float4 v = waves[i][lane];
+            x += v.x, y += v.y, w += v.z;
+        }
     }
     const float inverse = w == 0.0f ? 0.0f : 1.0f / w;
-    *out = pack2<T>(x * inverse, y * inverse);
+    if (2 * lane < d) *out = pack2<T>(x * inverse, y * inverse);
 }
 
 // ------------------------------------------------------------------ host
@@ -755,7 +812,12 @@ template <typename T, int BITS> static void decode(const DecodeArgs &a, dim3 gri
     else if (a.c.d == 128) attn_decode_kernel<T, 128, BITS, true><<<grid, block, 0, st>>>(a);
     else if (a.c.d < 64) attn_decode_kernel<T, 64, BITS, false><<<grid, block, 0, st>>>(a);
     else attn_decode_kernel<T, 128, BITS, false><<<grid, block, 0, st>>>(a);
-    attn_join_kernel<T><<<dim3((unsigned)(a.sequences * a.hq)), block, 0, st>>>(a);
+    if (a.whole) return;
+    // A wave adds the parts of a row where there are few of them.  (Four and one: 64 sequences of 512 positions, 64 heads on 8 of 128 in 8 bits, 27.6 and 23.9 us;
+    // one of 4096 10.6 and 14.7.)
+    const int64_t rows = (int64_t)a.sequences * a.hq;
+    if (a.shares <= 8 * (int64_t)a.sequences) attn_join_kernel<T, 1><<<dim3((unsigned)((rows + 3) / 4)), block, 0, st>>>(a);
+    else attn_join_kernel<T, 4><<<dim3((unsigned)rows), block, 0, st>>>(a);
 }
 }  // namespace s24_kv
 
@@ -776,9 +838,14 @@ extern "C" int s24_attn_decode(const s24_kv_cache *cache, const s24_heads *Q, in
     a.sequences = (int)sequences, a.hq = (int)hq, a.group = (int)(hq / cache->hkv), a.sixteens = (a.group + 15) / 16;
     const int64_t heads = cache->hkv * a.sixteens;
     // (No more than there are blocks: for a few short sequences the host knows of fewer.)
-    const int64_t most = sequences * ((a.width * cache->page + 63) / 64), fit = shares_of(heads, cache->d), shares = most < fit ? (most > 0 ? most : 1) : fit;
+    const int64_t most = sequences * ((a.width * cache->page + 63) / 64), fit = shares_of(heads, cache->d);
+    // A wave has whole sequences, and nothing is left to add, where the table holds few positions: up to 128, or 512 if there are as many sequences as shares.
+    // (Shared out and whole: one sequence of 128 positions of 12 heads of 64 7.3 and 5.0 us, 8 of 256 8.8 and 10.8; 256 of 64 heads on 8 of 128 in 8 bits, 128
+    // positions 39 and 17, 512 positions 71 and 48; 64 of 1024 positions of 32 heads on 8 in 16 bits 55 and 75.)
+    a.whole = a.width * cache->page <= (sequences >= fit ? 512 : 128);
+    const int64_t shares = a.whole ? sequences : most < fit ? (most > 0 ? most : 1) : fit;
     const int64_t groups = (shares * heads + 3) / 4;
-    S24_REQUIRE(sequences * hq <= kMostGroups, S24_ERR_SHAPE);
+    S24_REQUIRE(sequences * hq <= kMostGroups / 2, S24_ERR_SHAPE);
     a.shares = (int)shares, a.scale = scale, a.part = static_cast<float *>(workspace);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const dim3 grid((unsigned)groups);

@@ -598,3 +598,26 @@ def test_tiles_of_many_sequences_are_all_taken(s24, count, causal):
     lk = [rng.choice([0, 1, 20, 129, 400, rng.randrange(1, 700)]) for _ in range(count - 1)] + [650]
     lq = [rng.choice([n, n, n, n // 2, n + rng.choice([0, 140])]) for n in lk]
     run(s24, lq, lk, 2, 1, 64, BF16, causal=causal, seed=count)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("count", [64, 65, 256, 257, 600])
+def test_decode_shares_of_many_sequences(s24, count, bits):
+    """One long sequence, so that the shares do not go by sequences, among short and empty ones, also at either end."""
+    rng = random.Random(count)
+    lens = [rng.choice([0, 0, 1, 5, 64, 65, 130]) for _ in range(count)]
+    for at in (0, count // 2, count - 1):
+        run = list(lens)
+        run[at] = 700
+        decode(s24, run, 2, 1, 64, BF16, bits, 32, seed=at)
+    decode(s24, [0] * (count - 1) + [600], 2, 1, 64, BF16, bits, 32, seed=1)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("longest", [16, 128, 129, 512, 513])
+def test_decode_sequences_short_enough_for_one_wave(s24, longest, bits):
+    """With few sequences up to 128 positions, with many up to 512; some are empty."""
+    rng = random.Random(longest)
+    for count, hq, hkv in ((5, 20, 1), (90, 34, 34)):
+        lens = [rng.choice([0, 1, longest // 2, longest]) for _ in range(count - 1)] + [longest]
+        decode(s24, lens, hq, hkv, 64, BF16, bits, 16, seed=longest)
