@@ -69,13 +69,6 @@ template <typename T> __device__ __forceinline__ float step_for(uint32_t two)
     const float most = s24_num<T>::lo(max(two & 0xFFFFu, two >> 16));
     return most < INFINITY ? fmaxf(__fdiv_rn(most, 127.0f), 0x1p-126f) : NAN;
 }
-__device__ __forceinline__ uint32_t swap_neighbours(uint32_t x)
-{
-#if defined(__HIP_DEVICE_COMPILE__)
-    x = __builtin_amdgcn_mov_dpp(x, 0xB1, 0xf, 0xf, true);
-#endif
-    return x;
-}
 // Rows of 16 lanes: the odd rows of a and the even rows of b change places / the last two of a and the first two of b
 __device__ __forceinline__ void swap_rows(uint32_t &a, uint32_t &b)
 {
@@ -129,8 +122,8 @@ template <typename T, bool PAIR> __device__ __forceinline__ float step_of(uint4 
 // Many tokens: a wave looks at sixteen of them and takes, of K or of V, those runs that begin there and lie within sixteen aligned places of a page, one after
 // the other.  Of a prompt, whatever place it starts at, that is sixteen tokens to a wave: V then leaves in pieces of 16 bytes.  (Of single tokens of many
 // sequences it is one at a time, which the kernel below does better.)
-// Bound by memory: 17408 tokens of 8 heads of 128 take 22 us in 8 bits and 30 in 16 (4.9 and 4.7 TB/s; a plain copy of as many bytes reaches 5.7).  K and, in 8
-// bits, V go past the caches in whole lines (24 and 33 us with plain stores); V in 16 bits is written in parts of lines, which the L2 has to join.
+// Bound by memory: 17408 tokens of 8 heads of 128 take 27 us in 8 bits and 33 in 16 (4.0 and 4.3 TB/s; a plain copy of as many bytes reaches 5.7).  Stores past
+// the caches, in whole lines, take 25 and 31; but the reading back that follows then takes longer by more: both together 44 us with these, 50 with those.
 template <typename T, int BITS, bool PAIR>
 __global__ __launch_bounds__(256) void kv_write_runs_kernel(const WriteArgs a)
 {
@@ -165,7 +158,7 @@ __global__ __launch_bounds__(256) void kv_write_runs_kernel(const WriteArgs a)
             if (!values) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (live[i]) s24_store_stream(a.c.k + ((base + 4 * at.r + i) * a.c.d + at.c) * 2, x[i]);
+                    if (live[i]) *reinterpret_cast<uint4 *>(a.c.k + ((base + 4 * at.r + i) * a.c.d + at.c) * 2) = x[i];
                 continue;
             }
             uint32_t lo[8], hi[8];   // of a channel: tokens 4r, 4r + 1 and 4r + 2, 4r + 3
@@ -204,30 +197,20 @@ __global__ __launch_bounds__(256) void kv_write_runs_kernel(const WriteArgs a)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (live[i])
-                        __builtin_nontemporal_store((uint64_t)four_bytes(bytes[i][4], bytes[i][5], bytes[i][6], bytes[i][7]) << 32 |
-                                                        four_bytes(bytes[i][0], bytes[i][1], bytes[i][2], bytes[i][3]),
-                                                    reinterpret_cast<uint64_t *>(a.c.k + (base + 4 * at.r + i) * a.c.d + at.c));
+                        *reinterpret_cast<uint2 *>(a.c.k + (base + 4 * at.r + i) * a.c.d + at.c) =
+                            make_uint2(four_bytes(bytes[i][0], bytes[i][1], bytes[i][2], bytes[i][3]), four_bytes(bytes[i][4], bytes[i][5], bytes[i][6], bytes[i][7]));
                 continue;
             }
             unsigned char *v = a.c.v + base * a.c.d + at.c * 16;
             if (n == 16) {
-                uint32_t w[2][4];
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {   // row r gets all sixteen tokens of channel 4*half + r
+                    uint32_t w[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) w[half][e] = four_bytes(bytes[0][4 * half + e], bytes[1][4 * half + e], bytes[2][4 * half + e], bytes[3][4 * half + e]);
-                    transpose_rows(w[half]);
+                    for (int e = 0; e < 4; ++e) w[e] = four_bytes(bytes[0][4 * half + e], bytes[1][4 * half + e], bytes[2][4 * half + e], bytes[3][4 * half + e]);
+                    transpose_rows(w);
+                    if (at.live) *reinterpret_cast<uint4 *>(v + 16 * (4 * half + at.r)) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
-                const bool odd = lane & 1;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {   // of two neighbours the even one gets the first halves, the odd one the second: a store is of whole lines
-                    const uint32_t got = swap_neighbours(odd ? w[0][e] : w[1][e]);
-                    w[0][e] = odd ? got : w[0][e], w[1][e] = odd ? w[1][e] : got;
-                }
-                v = a.c.v + base * a.c.d + 16 * (4 * odd + at.r);
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    if (at.live) s24_store_stream(v + (at.c - 8 * odd + 8 * i) * 16, make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]));
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
