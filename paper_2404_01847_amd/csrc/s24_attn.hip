@@ -34,7 +34,8 @@ struct Problem {
 };
 
 // For the scheduler: the LDS reads of a product come a step ahead of its matrix instructions, of which there are STEPS times MATRIX, READS for each.  (Left to itself
-// it reads two operands, waits for them, and multiplies: 
+// it reads two operands, waits for them, and multiplies: the forward pass of 8192 tokens, 64 heads on 8 of 128, takes 970 us so and 950 with this.  Heads of 64
+// have too few steps for it: 31.5 us with it, 30.7 without, 8 x 1024 tokens of 12 heads.)
 template <int READS, int MATRIX, int STEPS> __device__ __forceinline__ void reads_ahead()
 {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -323,8 +324,8 @@ template <typename T, int D> __device__ __forceinline__ void dkv_tile(const Prob
     const int64_t all_steps = (int64_t)each * a.group;
     const int begin = (int)(all_steps * part / a.by_key.parts), steps = (int)(all_steps * (part + 1) / a.by_key.parts) - begin;
 
-    // The keys' fragments stay in registers, the values' come from LDS: with both, two waves would not fit a SIMD (3.6 ms instead of MEASURE for 8192 tokens,
-    // 64 heads on 8 of 128).
+    // The keys' fragments stay in registers, the values' come from LDS: with both, two waves would not fit a SIMD (8192 tokens, 64 heads on 8 of 128: 3.6 ms
+    // with both in registers, 2.0 so, before dS went in two parts).
     uint4 fk[2][D / 32];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -656,29 +657,39 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_bwd_kernel(const Pr
     if (blockIdx.x < a.key_blocks) dkv_tile<T, D>(a, blockIdx.x, (lds_byte *)values, (lds_byte *)stages);
     else dq_tile<T, D, 2, true>(a, blockIdx.x - a.key_blocks, (lds_byte *)values, (lds_byte *)stages);
 }
-// stats[h][t]: what a row's exponents are taken from, and delta = dO.O; by LANES lanes, one for each of a row's pieces of 16 bytes
+// stats[h][t]: what a row's exponents are taken from, and delta = dO.O; by LANES lanes, one for each of a row's pieces of 16 bytes, for four rows at a time so that
+// enough loads are under way.  (Both passes of 8 x 1024 tokens of 12 heads of 64: 108.9 us with one row, 107.6 with four.)
+constexpr int kStatsRows = 4;
 template <typename T, int LANES>
 __global__ __launch_bounds__(256) void attn_stats_kernel(const Problem a)
 {
     using Num = s24_num<T>;
     using L = Lift<T>;
-    const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES;
+    constexpr int ROWS = 256 / LANES;   // of a workgroup at a time
     const int lane = threadIdx.x & (LANES - 1);
-    if (item >= (int64_t)a.tokens_q * a.hq) return;
-    const int64_t t = item / a.hq;
-    const int h = (int)(item - t * a.hq);
-    float sum = 0.0f;
-    if (8 * lane < a.d) {
-        const uint4 x = *reinterpret_cast<const uint4 *>(a.dO.p + t * a.dO.token + h * a.dO.head + 8 * lane);
-        const uint4 y = *reinterpret_cast<const uint4 *>(a.o.p + t * a.o.token + h * a.o.head + 8 * lane);
-        const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+    const int64_t rows = (int64_t)a.tokens_q * a.hq, first = (int64_t)blockIdx.x * (ROWS * kStatsRows) + threadIdx.x / LANES;
+    uint4 x[kStatsRows], y[kStatsRows];
+    float lse[kStatsRows];
+    int64_t at[kStatsRows];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum = fmaf(Num::lo(xs[i]), Num::lo(ys[i]), fmaf(Num::hi(xs[i]), Num::hi(ys[i]), sum));
+    for (int r = 0; r < kStatsRows; ++r) {
+        const int64_t item = min(first + r * ROWS, rows - 1), t = item / a.hq;
+        const int h = (int)(item - t * a.hq), i = min(8 * lane, a.d - 8);
+        x[r] = *reinterpret_cast<const uint4 *>(a.dO.p + t * a.dO.token + h * a.dO.head + i);
+        y[r] = *reinterpret_cast<const uint4 *>(a.o.p + t * a.o.token + h * a.o.head + i);
+        at[r] = h * (int64_t)a.tokens_q + t, lse[r] = a.lse[at[r]];
     }
 #pragma unroll
-    for (int s = 1; s < LANES; s <<= 1) sum += __shfl_xor(sum, s);
-    const int64_t at = h * (int64_t)a.tokens_q + t;
-    if (lane == 0) a.stats[at] = make_float2(fmaf(a.lse[at], kLog2e, -L::kUp), sum * L::kDown);
+    for (int r = 0; r < kStatsRows; ++r) {
+        float sum = 0.0f;
+        const uint32_t xs[4] = {x[r].x, x[r].y, x[r].z, x[r].w}, ys[4] = {y[r].x, y[r].y, y[r].z, y[r].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum = fmaf(Num::lo(xs[i]), Num::lo(ys[i]), fmaf(Num::hi(xs[i]), Num::hi(ys[i]), sum));
+        if (8 * lane >= a.d) sum = 0.0f;
+#pragma unroll
+        for (int s = 1; s < LANES; s <<= 1) sum += __shfl_xor(sum, s);
+        if (lane == 0 && first + r * ROWS < rows) a.stats[at[r]] = make_float2(fmaf(lse[r], kLog2e, -L::kUp), sum * L::kDown);
+    }
 }
 
 // dQ from the sums of the parts
@@ -837,7 +848,8 @@ template <typename T, int D> static int backward(Problem a, bool joint, int64_t 
     if (query_groups == 0 && key_groups == 0) return S24_OK;
     if (joint && query_groups > 0) {
         a.key_blocks = (unsigned)((key_groups + 7) / 8 * 8);   // dQ's workgroups meet the XCDs as they would in a launch of their own
-        attn_stats_kernel<T, D / 8><<<dim3((unsigned)(((int64_t)a.tokens_q * a.hq + 2048 / D - 1) / (2048 / D))), block, 0, st>>>(a);
+        const int64_t rows = (int64_t)a.tokens_q * a.hq, of_group = 2048 / D * kStatsRows;
+        attn_stats_kernel<T, D / 8><<<dim3((unsigned)((rows + of_group - 1) / of_group)), block, 0, st>>>(a);
         attn_bwd_kernel<T, D><<<dim3(a.key_blocks + (unsigned)query_groups), block, 0, st>>>(a);
     } else {
         if (query_groups > 0) attn_dq_kernel<T, D><<<dim3((unsigned)query_groups), block, 0, st>>>(a);
