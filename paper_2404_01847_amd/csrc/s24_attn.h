@@ -54,7 +54,7 @@ template <typename T> __device__ __forceinline__ uint4 operand(f32x4 a, f32x4 b)
 
 // What such an operand leaves of the accumulators: a second operand, which gives a product 16 bits of them.  The gradients of the queries and keys take dS so.  With
 // dS rounded once they are 1.65 times as far from 64 bits as a result is that is rounded at its end alone (bf16: 0.0028 to 0.0017, normwise), with both parts
-// 1.3 times (what stays is in delta: O was rounded); 8192 tokens, 64 heads on 8 of 128, both passes, take 5.15 ms for 4.47.
+// 1.3 times (what stays is in delta: O was rounded); both passes of 8192 tokens, 64 heads on 8 of 128, take 15 % longer for it.
 template <typename T> __device__ __forceinline__ uint4 rest(uint4 x, f32x4 a, f32x4 b)
 {
     using Num = s24_num<T>;

@@ -5,8 +5,11 @@
 // but a rare one, and the rounded P is the second product's operand as it lies in the registers.
 // Backward, from lse_i = log sum_j exp S_ij and delta_i = dO_i.O_i:  P_ij = exp(S_ij - lse_i),  dV = P^T dO,  dS_ij = P_ij (dO_i.v_j - delta_i),
 // dQ = c dS K,  dK = c dS^T Q.
-// Sums run over queries for dK and dV and over keys for dQ: two kernels, each of which forms S and dO V^T for itself (7 products instead
-// of 5).  One kernel would have to add to dQ from many workgroups, in an order that no two runs share.
+// Sums run over queries for dK and dV and over keys for dQ: two parts, each of which forms S and dO V^T for itself (7 products instead of 5, and two more
+// for the second halves of dS).  One kernel would have to add to dQ from many workgroups, in an order that no two runs share.
+// What bounds it: the matrix instructions and the vector instructions on the scores, which a compute unit runs at the same time only in part.  (Two waves of nothing
+// but 16x16x32 instructions take 8.1 ns for each on a SIMD; with four fma to each 12.2.)  8192 tokens, 64 heads on 8 of 128: 970 us for O (1.13 PFLOP/s, of the
+// 1.18 that a library's plain product of 8192 x 8192 x 8192 reaches), matrix cores 53 % busy; 1730 us for dQ, 59 %; 2350 us for dK and dV, 52 %.
 #include "s24_attn.h"
 
 #include <math.h>
@@ -107,7 +110,11 @@ __device__ __forceinline__ bool find_keys(const Problem &a, int rows, int t, int
 }
 
 // ------------------------------------------------------------------ forward
-// Four waves of 32 rows.  Keys and values in tiles of 64, two of them in LDS: the next one is copied during the work on this one.
+// Four waves of 32 rows.  Keys and values in tiles of 64, two of them in LDS: the next one is copied during the work on this one, with one barrier a tile.
+// (Instructions of 32 x 32 x 16 in place of 16 x 16 x 32 are half as many, but the products wait more: 4 x 4096 tokens of 32 heads of 128 578 us for 543, 8 x 1024
+// of 12 heads of 64, both passes, 112 for 108.  Keys and values in one array of LDS cost 5 %: the compiler then
+// cannot tell the copies of the one from the reads of the other.
+// Tiles of 32 keys with three waves to a SIMD, and tiles of 64 rows, were no faster on operands that come from memory.)
 template <int D> struct Forward {
     static constexpr int BK = 64, TILE = BK * 2 * D;
 };
@@ -299,7 +306,8 @@ template <> struct Lift<uint16_t> { static constexpr float kUp = 32.0f, kDown = 
 template <> struct Lift<s24_half> { static constexpr float kUp = 15.0f, kDown = 0x1p-15f, kOfP = 0x1p-15f, kOfDs = 1.0f; };
 
 // dK and dV of 128 keys of a key-value head, four waves of 32: over the query heads of the group and their queries, 32 at a time.
-// S has the queries as rows, so that P and dS are, as they lie, the operands that contract over the queries.
+// S has the queries as rows, so that P and dS are, as they lie, the operands that contract over the queries.  A step has 80 matrix instructions of a wave (heads of
+// 128), 28 reads of 16 bytes and 32 transposed ones; at two waves to a SIMD it takes 2.0 us, of which the matrix instructions are 1.1.
 template <int D> struct Backward {
     static constexpr int BK = 128, BQ = 32, TILE = BQ * 2 * D, STAGE = 2 * TILE + 8 * BQ, VALUES = BK * 2 * D;   // a stage: queries, gradients, row statistics
 };
@@ -646,8 +654,9 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dkv_kernel(const Pr
     __shared__ __align__(16) unsigned char values[C::VALUES], stages[2 * C::STAGE];
     dkv_tile<T, D>(a, blockIdx.x, (lds_byte *)values, (lds_byte *)stages);
 }
-// Small grids: all three in one launch, since neither fills the device to its end; the row statistics are formed before.  (16 heads of 128, 2048 tokens: 123 us
-// in turn, 97 together; 12 heads of 64, 1024 tokens 46 and 36; 32 heads of 128 on 8, 4096 tokens 485 and 480; 12 heads of 64, 8 x 1024 tokens 101 and 103.)
+// Small grids: all three in one launch, since neither fills the device to its end; the row statistics are formed before.  (The gradients, in turn and so: 16 heads
+// of 128, 2048 tokens 193 and 119 us; 12 heads of 64, 1024 tokens 70 and 38, 8 x 1024 tokens 106 and 94; 16 heads on 4 of 128, 9 ragged sequences 179 and 116.
+// At four workgroups a compute unit, 32 heads on 8 of 128 and 4096 tokens, 620 both ways.)
 template <typename T, int D>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_bwd_kernel(const Problem a)
 {
