@@ -345,13 +345,17 @@ typedef struct {
 } s24_heads;
 
 /* d: values of a head, a multiple of 16 up to 128 (beyond: S24_ERR_UNSUPPORTED); below 64 and between 64 and 128 it costs what 64 and 128 do.
- * scale: the factor c > 0 of the scores, 1 / sqrt(d) as a rule. */
+ * scale: the factor c > 0 of the scores, 1 / sqrt(d) as a rule.
+ * o_rest: device [tokens_q][hq][d], may be NULL.  What the rounding of O took away, in 256ths of the last place: s24_attn_fwd writes it, and s24_attn_bwd adds it to O in
+ * delta.  Without it the gradients of the queries and keys are about 1.3 times as far from the exact ones as results are that are rounded at their end alone, of short
+ * sequences up to 1.6 times; with it, 1.0 times. */
 typedef struct {
     const int32_t *cu_q, *cu_k;   /* device, may be one array */
     int64_t sequences, tokens_q, tokens_k;
     int64_t hq, hkv, d;
     float scale;
     int causal;
+    int8_t *o_rest;
 } s24_attn_shape;
 
 /* O_i = sum_j P_ij v_j, P_ij = exp(c q_i.k_j - lse_i), lse_i = log sum_j exp(c q_i.k_j) over the keys j that query i sees.

@@ -23,6 +23,8 @@ class Attention:
         self.causal, self.scale = causal, scale
         self.dtype, self.device = dtype, device
         self.O = torch.empty((tokens_q, hq, d), dtype=dtype, device=device)
+        self.rest = torch.empty((tokens_q, hq, d), dtype=torch.int8, device=device)   # what the rounding of O took away: the backward pass takes delta from both
+        self._rest = self.rest.data_ptr()
         self.lse = torch.empty((hq, tokens_q), dtype=torch.float32, device=device)
         self.dQ = self.dK = self.dV = None   # allocated by the first backward pass
         self.work = {}
@@ -37,7 +39,7 @@ class Attention:
 
     def forward(self, Q, K, V, cu_q, cu_k=None):
         """O [tokens_q, hq, d].  Q, K, V may be views of one projection's result; cu_q, cu_k: int32 offsets of the sequences."""
-        return s24.attn_fwd(Q, K, V, self.O, self.lse, self._workspace(s24.attn_fwd_workspace, cu_q), cu_q, cu_k, self.causal, self.scale)
+        return s24.attn_fwd(Q, K, V, self.O, self.lse, self._workspace(s24.attn_fwd_workspace, cu_q), cu_q, cu_k, self.causal, self.scale, self._rest)
 
     def backward(self, Q, K, V, dO, cu_q, cu_k=None):
         """dQ, dK, dV of the last forward pass, whose operands are given again."""
@@ -51,7 +53,7 @@ class Attention:
                 self.dQKV = None
                 self.dQ = torch.empty((self.tokens_q, self.hq, self.d), dtype=self.dtype, device=self.device)
                 self.dK, self.dV = (torch.empty((self.tokens_k, self.hkv, self.d), dtype=self.dtype, device=self.device) for _ in range(2))
-        return s24.attn_bwd(Q, K, V, self.O, dO, self.lse, self.dQ, self.dK, self.dV, work, cu_q, cu_k, self.causal, self.scale)
+        return s24.attn_bwd(Q, K, V, self.O, dO, self.lse, self.dQ, self.dK, self.dV, work, cu_q, cu_k, self.causal, self.scale, self._rest)
 
 
 class PagedKV:

@@ -475,7 +475,7 @@ class _Heads(C.Structure):
 
 class _AttnShape(C.Structure):
     _fields_ = [("cu_q", _vp), ("cu_k", _vp), ("sequences", _i64), ("tokens_q", _i64), ("tokens_k", _i64), ("hq", _i64), ("hkv", _i64), ("d", _i64),
-                ("scale", _f32), ("causal", _int)]
+                ("scale", _f32), ("causal", _int), ("o_rest", _vp)]
 
 
 class _KVCache(C.Structure):
@@ -513,7 +513,7 @@ def _whole(where, name, x, dtype, shape, device):
     return x.data_ptr()
 
 
-def _attn_operands(where, Q, K, cu_q, cu_k, causal, scale):
+def _attn_operands(where, Q, K, cu_q, cu_k, causal, scale, rest):
     """(shapes of the rows of queries and of keys, dtype, device, packed s24_attn_shape)"""
     sq, sk = Q.shape, K.shape
     if len(sq) != 3 or len(sk) != 3 or sk[2] != sq[2]:
@@ -523,15 +523,18 @@ def _attn_operands(where, Q, K, cu_q, cu_k, causal, scale):
     if len(n) != 1 or n[0] == 0:
         raise ValueError(f"{where}: cu_q needs an offset for each sequence and one more, got shape {tuple(n)}")
     pk = pq if cu_k is None or cu_k is cu_q else _whole(where, "cu_k", cu_k, torch.int32, n, device)
-    return sq, sk, Q.dtype, device, _pack_shape(pq, pk, n[0] - 1, sq[0], sk[0], sq[1], sk[1], sq[2], sq[2] ** -0.5 if scale is None else scale, bool(causal))
+    if type(rest) is not int:
+        rest = 0 if rest is None else _whole(where, "rest", rest, torch.int8, sq, device)
+    return sq, sk, Q.dtype, device, _pack_shape(pq, pk, n[0] - 1, sq[0], sk[0], sq[1], sk[1], sq[2], sq[2] ** -0.5 if scale is None else scale, bool(causal), rest)
 
 
-def attn_fwd(Q, K, V, O, lse, workspace, cu_q, cu_k=None, causal=True, scale=None):
+def attn_fwd(Q, K, V, O, lse, workspace, cu_q, cu_k=None, causal=True, scale=None, rest=None):
     """Attention over packed sequences.  Q, O [tokens_q, hq, d], K, V [tokens_k, hkv, d], with any strides along the first two axes; lse [hq, tokens_q]
     float32 or None; cu_q, cu_k: int32 offsets of the sequences (cu_k None: those of the queries); scale None: 1 / sqrt(d);
-    workspace: a uint8 tensor of attn_fwd_workspace(...) bytes, None where that is 0."""
+    workspace: a uint8 tensor of attn_fwd_workspace(...) bytes, None where that is 0; rest: None, or an int8 tensor like O without gaps (or the
+    address of one that has been checked), which receives what the rounding of O takes away."""
     where = "s24_attn_fwd"
-    sq, sk, dtype, device, shape = _attn_operands(where, Q, K, cu_q, cu_k, causal, scale)
+    sq, sk, dtype, device, shape = _attn_operands(where, Q, K, cu_q, cu_k, causal, scale, rest)
     args = (shape, _heads(where, "Q", Q, sq, dtype, device), _heads(where, "K", K, sk, dtype, device), _heads(where, "V", V, sk, dtype, device),
             _heads(where, "O", O, sq, dtype, device),
             None if lse is None else _whole(where, "lse", lse, torch.float32, (sq[1], sq[0]), device),
@@ -547,18 +550,18 @@ def attn_fwd(Q, K, V, O, lse, workspace, cu_q, cu_k=None, causal=True, scale=Non
 
 def attn_fwd_workspace(tokens_q, tokens_k, hq, hkv, d, sequences):
     """Bytes of workspace that attn_fwd needs for so many tokens, heads and sequences."""
-    return lib().s24_attn_fwd_workspace(_pack_shape(0, 0, sequences, tokens_q, tokens_k, hq, hkv, d, 1.0, True))
+    return lib().s24_attn_fwd_workspace(_pack_shape(0, 0, sequences, tokens_q, tokens_k, hq, hkv, d, 1.0, True, 0))
 
 
 def attn_bwd_workspace(tokens_q, tokens_k, hq, hkv, d, sequences):
     """Bytes of workspace that attn_bwd needs for so many tokens, heads and sequences."""
-    return lib().s24_attn_bwd_workspace(_pack_shape(0, 0, sequences, tokens_q, tokens_k, hq, hkv, d, 1.0, True))
+    return lib().s24_attn_bwd_workspace(_pack_shape(0, 0, sequences, tokens_q, tokens_k, hq, hkv, d, 1.0, True, 0))
 
 
-def attn_bwd(Q, K, V, O, dO, lse, dQ, dK, dV, workspace, cu_q, cu_k=None, causal=True, scale=None):
-    """Gradients dQ, dK, dV of attn_fwd, from its O and lse; workspace: a uint8 tensor of attn_bwd_workspace(...) bytes."""
+def attn_bwd(Q, K, V, O, dO, lse, dQ, dK, dV, workspace, cu_q, cu_k=None, causal=True, scale=None, rest=None):
+    """Gradients dQ, dK, dV of attn_fwd, from its O and lse, and its rest if it had one; workspace: a uint8 tensor of attn_bwd_workspace(...) bytes."""
     where = "s24_attn_bwd"
-    sq, sk, dtype, device, shape = _attn_operands(where, Q, K, cu_q, cu_k, causal, scale)
+    sq, sk, dtype, device, shape = _attn_operands(where, Q, K, cu_q, cu_k, causal, scale, rest)
     args = (shape, _heads(where, "Q", Q, sq, dtype, device), _heads(where, "K", K, sk, dtype, device), _heads(where, "V", V, sk, dtype, device),
             _heads(where, "O", O, sq, dtype, device), _heads(where, "dO", dO, sq, dtype, device),
             _whole(where, "lse", lse, torch.float32, (sq[1], sq[0]), device), _heads(where, "dQ", dQ, sq, dtype, device),

@@ -52,14 +52,72 @@ template <typename T> __device__ __forceinline__ uint4 operand(f32x4 a, f32x4 b)
     return make_uint4(pack2<T>(a[0], a[1]), pack2<T>(a[2], a[3]), pack2<T>(b[0], b[1]), pack2<T>(b[2], b[3]));
 }
 
-// What such an operand leaves of the accumulators: a second operand, which gives a product 16 bits of them.  The gradients of the queries and keys take dS so.  With
-// dS rounded once they are 1.65 times as far from 64 bits as a result is that is rounded at its end alone (bf16: 0.0028 to 0.0017, normwise), with both parts
-// 1.3 times (what stays is in delta: O was rounded); both passes of 8192 tokens, 64 heads on 8 of 128, take 15 % longer for it.
+// What such an operand leaves of the accumulators: a second operand, which gives a product 16 bits of them.  The gradients of the queries and keys take dS so: rounded
+// once it costs them as much as the rounding of their results does.  Both passes of 8192 tokens, 64 heads on 8 of 128, take 15 % longer for it.
 template <typename T> __device__ __forceinline__ uint4 rest(uint4 x, f32x4 a, f32x4 b)
 {
     using Num = s24_num<T>;
     return operand<T>(f32x4{a[0] - Num::lo(x.x), a[1] - Num::hi(x.x), a[2] - Num::lo(x.y), a[3] - Num::hi(x.y)},
                       f32x4{b[0] - Num::lo(x.z), b[1] - Num::hi(x.z), b[2] - Num::lo(x.w), b[3] - Num::hi(x.w)});
+}
+
+// Rows of 16 lanes: the odd rows of a and the even rows of b change places / the last two of a and the first two of b
+__device__ __forceinline__ void swap_rows(uint32_t &a, uint32_t &b)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    const auto v = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    a = v[0], b = v[1];
+#endif
+}
+__device__ __forceinline__ void swap_halves(uint32_t &a, uint32_t &b)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    const auto v = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+    a = v[0], b = v[1];
+#endif
+}
+// x[j] of row r <-> x[r] of row j (its own inverse)
+__device__ __forceinline__ void transpose_rows(uint32_t (&x)[4])
+{
+    swap_halves(x[0], x[2]), swap_halves(x[1], x[3]), swap_rows(x[0], x[1]), swap_rows(x[2], x[3]);
+}
+// Their lowest bytes
+__device__ __forceinline__ uint32_t four_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
+}
+// What a stored value left of x: the difference of their bits as fp32, in 256ths of the stored value's last place, -128 .. 127.  (Of binary16 below 2^-14, whose
+// last places are further apart, what does not fit is left out.)
+template <typename T> struct Left;
+template <> struct Left<uint16_t> { static constexpr int kShift = 8; };
+template <> struct Left<s24_half> { static constexpr int kShift = 5; };
+template <typename T> __device__ __forceinline__ uint32_t left_of(float x, float stored)
+{
+    constexpr int S = Left<T>::kShift;
+    return (uint32_t)((min(max((int)(__float_as_uint(x) - __float_as_uint(stored)), -(128 << S)), (127 << S) + (1 << (S - 1)) - 1) + (1 << (S - 1))) >> S);
+}
+template <typename T> __device__ __forceinline__ uint32_t four_left(f32x4 x, uint2 stored)
+{
+    using Num = s24_num<T>;
+    return four_bytes(left_of<T>(x[0], Num::lo(stored.x)), left_of<T>(x[1], Num::hi(stored.x)), left_of<T>(x[2], Num::lo(stored.y)), left_of<T>(x[3], Num::hi(stored.y)));
+}
+// The other way: a stored value with what it left, of which byte i of `four` tells
+template <typename T> __device__ __forceinline__ float with_left(float stored, uint32_t four, int i)
+{
+    return __uint_as_float(__float_as_uint(stored) + ((uint32_t)(int)(int8_t)(four >> (8 * i)) << Left<T>::kShift));
+}
+// Sum over eight values of x times y, of which x has the rests `left`
+template <typename T> __device__ __forceinline__ float dot(uint4 x, uint2 left, uint4 y)
+{
+    using Num = s24_num<T>;
+    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+    float sum = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t four = e < 2 ? left.x : left.y;
+        sum = fmaf(with_left<T>(Num::lo(xs[e]), four, 2 * (e & 1)), Num::lo(ys[e]), fmaf(with_left<T>(Num::hi(xs[e]), four, 2 * (e & 1) + 1), Num::hi(ys[e]), sum));
+    }
+    return sum;
 }
 
 // A tile of rows of D 16-bit values in LDS.  It is read in two ways, neither with bank conflicts: 16-byte pieces of 16 rows, of which the LDS takes rows 0-3 and

@@ -3,7 +3,8 @@
 // S_ij = c q_i.k_j over the visible pairs, P = softmax of its rows, O = P V.  Forward: one pass over the keys with the running maximum and sum
 // of each row; S^T is formed with the keys as rows, so that a lane holds one query's scores, the row statistics need no exchange between lanes
 // but a rare one, and the rounded P is the second product's operand as it lies in the registers.
-// Backward, from lse_i = log sum_j exp S_ij and delta_i = dO_i.O_i:  P_ij = exp(S_ij - lse_i),  dV = P^T dO,  dS_ij = P_ij (dO_i.v_j - delta_i),
+// Backward, from lse_i = log sum_j exp S_ij and delta_i = dO_i.O_i (of O with what its rounding took away, which
+// the forward pass leaves in a byte for each value):  P_ij = exp(S_ij - lse_i),  dV = P^T dO,  dS_ij = P_ij (dO_i.v_j - delta_i),
 // dQ = c dS K,  dK = c dS^T Q.
 // Sums run over queries for dK and dV and over keys for dQ: two parts, each of which forms S and dO V^T for itself (7 products instead of 5, and two more
 // for the second halves of dS).  One kernel would have to add to dQ from many workgroups, in an order that no two runs share.
@@ -21,6 +22,7 @@ struct Out { uint16_t *p; int64_t token, head; };
 struct Problem {
     Rows q, k, v, o, dO;
     Out out, dq, dk, dv;
+    int8_t *rest;          // [tokens_q][hq][d]: what the rounding of O took away; or NULL
     float *lse;            // [hq][tokens_q]
     float2 *stats;         // [hq][tokens_q], of the backward pass: what a row's exponents are taken from, and delta
     // Where a kernel's workgroups are few, what a tile sums over is cut into parts, whose sums another kernel adds
@@ -245,11 +247,24 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
         const int head = of.head;
         if (a.by_query.parts == 1) {
             uint16_t *out = a.out.p + token * a.out.token + head * a.out.head;
+            int8_t *rest = a.rest + (token * a.hq + head) * a.d;
 #pragma unroll
-            for (int n = 0; n < D / 16; ++n)
-                if (16 * n < a.d)
-                    *reinterpret_cast<uint2 *>(out + 16 * n + 4 * g) =
-                        make_uint2(pack2<T>(o[n][j][0] * inverse, o[n][j][1] * inverse), pack2<T>(o[n][j][2] * inverse, o[n][j][3] * inverse));
+            for (int n = 0; n < D / 16; n += 4) {   // of four such pieces of a row a lane gets one whole: lines are written with few stores
+                uint32_t x[4], y[4], left[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f32x4 v = o[n + i][j] * inverse;
+                    x[i] = pack2<T>(v[0], v[1]), y[i] = pack2<T>(v[2], v[3]);
+                    left[i] = a.rest != nullptr ? four_left<T>(v, make_uint2(x[i], y[i])) : 0;
+                }
+                transpose_rows(x), transpose_rows(y);
+                if (a.rest != nullptr) transpose_rows(left);
+                const int at = 16 * (n + g);
+                if (at >= a.d) continue;
+                *reinterpret_cast<uint4 *>(out + at) = make_uint4(x[0], y[0], x[1], y[1]);
+                *reinterpret_cast<uint4 *>(out + at + 8) = make_uint4(x[2], y[2], x[3], y[3]);
+                if (a.rest != nullptr) *reinterpret_cast<uint4 *>(rest + at) = make_uint4(left[0], left[1], left[2], left[3]);
+            }
             if (a.lse != nullptr && g == 0) a.lse[(int64_t)head * a.tokens_q + token] = sum == 0.0f ? -INFINITY : (m[j] + __builtin_amdgcn_logf(sum)) * kLn2;
         } else {
             const int64_t at = (unit.part * (int64_t)a.tokens_q + token) * a.hq + head;
@@ -293,7 +308,9 @@ __global__ __launch_bounds__(256) void attn_fwd_join_kernel(const Problem a)
             l = fmaf(w.y, f, l), x += *reinterpret_cast<const f32x4 *>(a.by_query.sums + (at + p * step) * a.d + i) * f;
         }
         x *= l == 0.0f ? 0.0f : 1.0f / l;
-        *reinterpret_cast<uint2 *>(a.out.p + t * a.out.token + j.head * a.out.head + i) = make_uint2(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]));
+        const uint2 stored = make_uint2(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]));
+        *reinterpret_cast<uint2 *>(a.out.p + t * a.out.token + j.head * a.out.head + i) = stored;
+        if (a.rest != nullptr) *reinterpret_cast<uint32_t *>(a.rest + at * a.d + i) = four_left<T>(x, stored);
         if (i == 0 && a.lse != nullptr) a.lse[(int64_t)j.head * a.tokens_q + t] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
     }
 }
@@ -528,11 +545,9 @@ template <typename T, int D, int KS, bool STATS> __device__ __forceinline__ void
             q[j][k] = i < a.d ? *reinterpret_cast<const uint4 *>(a.q.p + t * a.q.token + head * a.q.head + i) : make_uint4(0, 0, 0, 0);
             dO[j][k] = i < a.d ? *reinterpret_cast<const uint4 *>(a.dO.p + t * a.dO.token + head * a.dO.head + i) : make_uint4(0, 0, 0, 0);
             if (STATS) continue;
-            const uint4 o = i < a.d ? *reinterpret_cast<const uint4 *>(a.o.p + t * a.o.token + head * a.o.head + i) : make_uint4(0, 0, 0, 0);
-            using Num = s24_num<T>;
-            const uint32_t xs[4] = {o.x, o.y, o.z, o.w}, ys[4] = {dO[j][k].x, dO[j][k].y, dO[j][k].z, dO[j][k].w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sum = fmaf(Num::lo(xs[e]), Num::lo(ys[e]), fmaf(Num::hi(xs[e]), Num::hi(ys[e]), sum));
+            if (i < a.d)
+                sum += dot<T>(*reinterpret_cast<const uint4 *>(a.o.p + t * a.o.token + head * a.o.head + i),
+                              a.rest != nullptr ? *reinterpret_cast<const uint2 *>(a.rest + (t * a.hq + head) * a.d + i) : make_uint2(0, 0), dO[j][k]);
         }
         if (STATS) {
             const float2 of_row = a.stats[at];
@@ -672,12 +687,12 @@ constexpr int kStatsRows = 4;
 template <typename T, int LANES>
 __global__ __launch_bounds__(256) void attn_stats_kernel(const Problem a)
 {
-    using Num = s24_num<T>;
     using L = Lift<T>;
     constexpr int ROWS = 256 / LANES;   // of a workgroup at a time
     const int lane = threadIdx.x & (LANES - 1);
     const int64_t rows = (int64_t)a.tokens_q * a.hq, first = (int64_t)blockIdx.x * (ROWS * kStatsRows) + threadIdx.x / LANES;
-    uint4 x[kStatsRows], y[kStatsRows];
+    uint4 x[kStatsRows], y[kStatsRows];   // of dO, of O
+    uint2 left[kStatsRows];
     float lse[kStatsRows];
     int64_t at[kStatsRows];
 #pragma unroll
@@ -686,15 +701,12 @@ __global__ __launch_bounds__(256) void attn_stats_kernel(const Problem a)
         const int h = (int)(item - t * a.hq), i = min(8 * lane, a.d - 8);
         x[r] = *reinterpret_cast<const uint4 *>(a.dO.p + t * a.dO.token + h * a.dO.head + i);
         y[r] = *reinterpret_cast<const uint4 *>(a.o.p + t * a.o.token + h * a.o.head + i);
+        left[r] = a.rest != nullptr ? *reinterpret_cast<const uint2 *>(a.rest + item * a.d + i) : make_uint2(0, 0);
         at[r] = h * (int64_t)a.tokens_q + t, lse[r] = a.lse[at[r]];
     }
 #pragma unroll
     for (int r = 0; r < kStatsRows; ++r) {
-        float sum = 0.0f;
-        const uint32_t xs[4] = {x[r].x, x[r].y, x[r].z, x[r].w}, ys[4] = {y[r].x, y[r].y, y[r].z, y[r].w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum = fmaf(Num::lo(xs[i]), Num::lo(ys[i]), fmaf(Num::hi(xs[i]), Num::hi(ys[i]), sum));
-        if (8 * lane >= a.d) sum = 0.0f;
+        float sum = 8 * lane < a.d ? dot<T>(y[r], left[r], x[r]) : 0.0f;
 #pragma unroll
         for (int s = 1; s < LANES; s <<= 1) sum += __shfl_xor(sum, s);
         if (lane == 0 && first + r * ROWS < rows) a.stats[at[r]] = make_float2(fmaf(lse[r], kLog2e, -L::kUp), sum * L::kDown);
@@ -729,7 +741,7 @@ static int check_shape(const s24_attn_shape *s, s24_dtype dt)
     S24_REQUIRE((s->tokens_q > s->tokens_k ? s->tokens_q : s->tokens_k) * (s->hq / s->hkv) < INT32_MAX / 2, S24_ERR_SHAPE);
     S24_REQUIRE(s->d >= 16 && s->d % 16 == 0, S24_ERR_SHAPE);
     S24_REQUIRE(s->scale > 0.0f && s->scale <= 3.0e38f, S24_ERR_SHAPE);
-    S24_REQUIRE(s24_aligned(s->cu_q, 4) && s24_aligned(s->cu_k, 4), S24_ERR_ALIGN);
+    S24_REQUIRE(s24_aligned(s->cu_q, 4) && s24_aligned(s->cu_k, 4) && s24_aligned(s->o_rest, 16), S24_ERR_ALIGN);
     S24_REQUIRE(dt != S24_F32 && s->d <= 128, S24_ERR_UNSUPPORTED);
     return S24_OK;
 }
@@ -743,7 +755,7 @@ static Out out_of(const s24_heads *v) { return {static_cast<uint16_t *>(v->data)
 static Problem problem_of(const s24_attn_shape *s)
 {
     Problem a{};
-    a.cu_q = s->cu_q, a.cu_k = s->cu_k;
+    a.cu_q = s->cu_q, a.cu_k = s->cu_k, a.rest = s->o_rest;
     a.sequences = (int)s->sequences, a.tokens_q = (int)s->tokens_q, a.tokens_k = (int)s->tokens_k;
     a.hq = (int)s->hq, a.group = (int)(s->hq / s->hkv), a.d = (int)s->d, a.causal = s->causal != 0, a.scale = s->scale;
     // By length, unless the launch has many times the workgroups that the device holds, and the order matters less than keys that are still in the L2s; or the

@@ -69,26 +69,6 @@ template <typename T> __device__ __forceinline__ float step_for(uint32_t two)
     const float most = s24_num<T>::lo(max(two & 0xFFFFu, two >> 16));
     return most < INFINITY ? fmaxf(__fdiv_rn(most, 127.0f), 0x1p-126f) : NAN;
 }
-// Rows of 16 lanes: the odd rows of a and the even rows of b change places / the last two of a and the first two of b
-__device__ __forceinline__ void swap_rows(uint32_t &a, uint32_t &b)
-{
-#if defined(__HIP_DEVICE_COMPILE__)
-    const auto v = __builtin_amdgcn_permlane16_swap(a, b, false, false);
-    a = v[0], b = v[1];
-#endif
-}
-__device__ __forceinline__ void swap_halves(uint32_t &a, uint32_t &b)
-{
-#if defined(__HIP_DEVICE_COMPILE__)
-    const auto v = __builtin_amdgcn_permlane32_swap(a, b, false, false);
-    a = v[0], b = v[1];
-#endif
-}
-// x[j] of row r <-> x[r] of row j (its own inverse)
-__device__ __forceinline__ void transpose_rows(uint32_t (&x)[4])
-{
-    swap_halves(x[0], x[2]), swap_halves(x[1], x[3]), swap_rows(x[0], x[1]), swap_rows(x[2], x[3]);
-}
 // The whole numbers + 128 of eight values, each in the low byte: rounded by adding what pushes the fraction out, and where one lies so close to
 // the middle of two that the product's own rounding could decide, taken again exactly.
 template <typename T> __device__ __forceinline__ void eight_numbers(uint4 packed, float step, float inverse, uint32_t (&n)[8])
@@ -108,10 +88,6 @@ template <typename T> __device__ __forceinline__ void eight_numbers(uint4 packed
 #pragma unroll
         for (int i = 0; i < 8; ++i) n[i] = (uint32_t)(nearest(x[i], step, inverse) + 128);
     }
-}
-__device__ __forceinline__ uint32_t four_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
-{
-    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
 }
 template <typename T, bool PAIR> __device__ __forceinline__ float step_of(uint4 x)
 {

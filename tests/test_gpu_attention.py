@@ -621,3 +621,33 @@ def test_decode_sequences_short_enough_for_one_wave(s24, longest, bits):
     for count, hq, hkv in ((5, 20, 1), (90, 34, 34)):
         lens = [rng.choice([0, 1, longest // 2, longest]) for _ in range(count - 1)] + [longest]
         decode(s24, lens, hq, hkv, 64, BF16, bits, 16, seed=longest)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("d", [64, 80, 128])
+@pytest.mark.parametrize("lens,heads", [([2, 3, 5, 8, 13, 21, 34, 1], (6, 3)), ([700], (1, 1)), ([9000], (4, 1))])     # few tiles; several parts; a launch for each gradient
+def test_gradients_are_about_as_exact_as_their_own_rounding(s24, lens, heads, d, dtype):
+    """In the 2-norm, against results of 64 bits that are rounded once.  dS is in 16 bits or more, delta in 15, P (of dV) in the type's: its rounding, which no sum
+    makes larger than the result's own, allows dV the square root of two; a fifth more for what is left of the others."""
+    from paper_2404_01847_amd.attention import Attention
+    (hq, hkv), n = heads, sum(lens)
+    if n == 9000:
+        lens, hq, hkv, n = [300] * 30, 16, 16, 9000
+    cu = offsets(lens)
+    layer = Attention(hq, hkv, d, n, n, dtype)
+    Q, K, V, dO = normal((n, hq, d), dtype, 1), normal((n, hkv, d), dtype, 2), normal((n, hkv, d), dtype, 3), normal((n, hq, d), dtype, 4)
+    K = (K.float() * torch.exp(0.5 * torch.randn((1, hkv, d), generator=torch.Generator().manual_seed(5))).cuda()).to(dtype)
+    layer.forward(Q, K, V, gpu_i32(cu))
+    grads = layer.backward(Q, K, V, dO, gpu_i32(cu))
+    ref, _ = packed(Q, K, V, cu, cu, d ** -0.5, True, dO)
+    for name, got in zip(("dQ", "dK", "dV"), grads):
+        want = ref[name].reshape(got.shape)
+        off, own = (got.cpu().double() - want).norm(), (want.to(dtype).double() - want).norm()
+        assert off <= (1.7 if name == "dV" else 1.2) * own, (name, (off / own).item())
+
+
+def test_a_rest_of_the_wrong_kind_is_refused(s24):
+    x, cu = normal((8, 2, 64), BF16, 1), gpu_i32([0, 8])
+    for rest in (torch.empty((8, 2, 64), dtype=torch.uint8, device="cuda"), torch.empty((8, 2, 32), dtype=torch.int8, device="cuda"), torch.empty((8, 2, 64), dtype=torch.int8)):
+        with pytest.raises(ValueError, match="rest"):
+            s24.attn_fwd(x, x, x, torch.empty_like(x), None, None, cu, rest=rest)
