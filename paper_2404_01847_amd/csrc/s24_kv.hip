@@ -361,17 +361,20 @@ __device__ __forceinline__ uint4 halves(uint32_t a, uint32_t b)
 // weights are those of 16 consecutive positions, which is what it holds of V.
 // Softmax in 8 bits: the weights go to the product as exp(s - ref) * (step of V) in binary16, where ref has the largest step so far as a factor too, so that
 // they stay at 2^9 or less; the factor is in the sum of the weights as well and cancels.  (A step below 2^-100 counts as that, for ref to stay in range.)
-// EXACT: d is D, and the addresses within a page are constants.
+// Heads of every size have a kernel of their own, in which the addresses within a page are constants.  (With those of 64 and 128 for all, 32 sequences of 4096 positions,
+// 32 heads on 8
+// in 16 bits, take 98 us for heads of 96 and 92 for 80; so 74 and 72.)
 constexpr float kRise = 8.0f;   // as in the forward pass over packed sequences: how far a score may exceed the reference before it moves
-template <typename T, int D, int BITS, bool EXACT>
+template <typename T, int D, int BITS>
 __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
 {
     using M = typename std::conditional<BITS == 8, s24_half, T>::type;   // the products of an 8-bit cache are binary16: it holds -127 .. 127
     using Num = s24_num<T>;
-    constexpr int KL = BITS == 8 ? D / 64 : D / 32, VL = BITS == 8 ? 1 : 2;   // 16-byte loads of a key; of a channel's positions
+    constexpr int KL = BITS == 8 ? (D + 63) / 64 : (D + 31) / 32, VL = BITS == 8 ? 1 : 2;   // 16-byte loads of a key; of a channel's positions
+    constexpr int QL = BITS == 8 ? 2 * KL : KL;   // operands of a query
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
-    const int d = EXACT ? D : a.c.d;
+    constexpr int d = D;
     const int heads = a.c.hkv * a.sixteens, item = 4 * blockIdx.x + wave, share = item / heads, which = item - share * heads;
     const int h = which / a.sixteens, q0 = 16 * (which - h * a.sixteens), mine = min(16, a.group - q0);   // of the group's query heads
     if (share >= a.shares) return;
@@ -429,7 +432,7 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
     now.pos = 64 * (begin - now.first);
 
     // Positions 16*(col/4) .. of a block for K, 16*g .. for V: each sixteen lie in one page.
-    const int token = d * (BITS / 8);   // bytes of a token of one head
+    constexpr int token = d * (BITS / 8);   // bytes of a token of one head
     const uint32_t page_tokens = (uint32_t)a.c.hkv << a.c.shift;
     const unsigned char *const lane_k = a.c.k + ((int64_t)h << a.c.shift) * token + (col & 3) * token, *const lane_v = a.c.v + ((int64_t)h << a.c.shift) * token;
     struct Place { int64_t k, v; };   // in tokens of one head
@@ -451,7 +454,7 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
         for (int t = 0; t < 4; ++t) {
 #pragma unroll
             for (int k = 0; k < KL; ++k)
-                fk[t][k] = s24_load_stream(row + 4 * t * token + 16 * (EXACT ? 4 * k + g : min(4 * k + g, (token >> 4) - 1)));
+                fk[t][k] = s24_load_stream(row + 4 * t * token + 16 * (64 * k + 64 <= token ? 4 * k + g : min(4 * k + g, (token >> 4) - 1)));   // (past it the query has zeros)
             if (BITS == 8) sk[t] = *reinterpret_cast<const f32x4 *>(step + 4 * t);
         }
     };
@@ -465,31 +468,31 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
         for (int n = 0; n < D / 16; ++n)
 #pragma unroll
             for (int u = 0; u < VL; ++u)
-                fv[n][u] = s24_load_stream(page + (u * d + (EXACT ? 16 * n + col : min(16 * n + col, d - 1))) * 16);
+                fv[n][u] = s24_load_stream(page + (u * d + 16 * n + col) * 16);
     };
     // the queries, an operand of 16 columns
-    uint4 q[D / 32];
+    uint4 q[QL];
     float c = 0.0f;
     auto load_q = [&](int b) {
         const uint16_t *row = a.q.p + b * a.q.token + (h * a.group + q0 + min(col, mine - 1)) * a.q.head;
         float most = 0.0f;
         c = a.scale * kLog2e;
 #pragma unroll
-        for (int k = 0; k < D / 32; ++k) {
+        for (int k = 0; k < QL; ++k) {
             const int i = BITS == 8 ? 64 * (k >> 1) + 16 * g + 8 * (k & 1) : 32 * k + 8 * g;
             q[k] = i < d && col < mine ? *reinterpret_cast<const uint4 *>(row + i) : make_uint4(0, 0, 0, 0);
         }
         if (BITS == 8) {   // scaled by a power of two into what binary16 holds
             const uint32_t *x = reinterpret_cast<const uint32_t *>(q);
 #pragma unroll
-            for (int i = 0; i < D / 8; ++i) most = fmaxf(most, fmaxf(fabsf(Num::lo(x[i])), fabsf(Num::hi(x[i]))));
+            for (int i = 0; i < 4 * QL; ++i) most = fmaxf(most, fmaxf(fabsf(Num::lo(x[i])), fabsf(Num::hi(x[i]))));
             most = column_max(most);
             const int e = most > 0.0f ? ilogbf(most) : 0;
-            uint32_t y[D / 8];
+            uint32_t y[4 * QL];
 #pragma unroll
-            for (int i = 0; i < D / 8; ++i) y[i] = pack2<s24_half>(ldexpf(Num::lo(x[i]), -e), ldexpf(Num::hi(x[i]), -e));
+            for (int i = 0; i < 4 * QL; ++i) y[i] = pack2<s24_half>(ldexpf(Num::lo(x[i]), -e), ldexpf(Num::hi(x[i]), -e));
 #pragma unroll
-            for (int k = 0; k < D / 32; ++k) q[k] = make_uint4(y[4 * k], y[4 * k + 1], y[4 * k + 2], y[4 * k + 3]);
+            for (int k = 0; k < QL; ++k) q[k] = make_uint4(y[4 * k], y[4 * k + 1], y[4 * k + 2], y[4 * k + 3]);
             c = ldexpf(c, e);
         }
     };
@@ -610,16 +613,15 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
             if (col < mine) {
 #pragma unroll
                 for (int n = 0; n < D / 16; ++n)
-                    if (EXACT || 16 * n < d)
-                        *reinterpret_cast<uint2 *>(out + 16 * n + 4 * g) =
-                            make_uint2(pack2<T>(o[n][0] * inverse, o[n][1] * inverse), pack2<T>(o[n][2] * inverse, o[n][3] * inverse));
+                    *reinterpret_cast<uint2 *>(out + 16 * n + 4 * g) =
+                        make_uint2(pack2<T>(o[n][0] * inverse, o[n][1] * inverse), pack2<T>(o[n][2] * inverse, o[n][3] * inverse));
             }
         } else {
             float *to = a.part + ((int64_t)(2 * share + (now.first > begin)) * a.hq + head) * (d + 4);
             if (col < mine) {
 #pragma unroll
                 for (int n = 0; n < D / 16; ++n)
-                    if (EXACT || 16 * n < d) *reinterpret_cast<f32x4 *>(to + 16 * n + 4 * g) = o[n];
+                    *reinterpret_cast<f32x4 *>(to + 16 * n + 4 * g) = o[n];
                 if (g == 0) *reinterpret_cast<float2 *>(to + d) = make_float2(m, l);
             }
         }
@@ -793,10 +795,16 @@ namespace s24_kv {
 template <typename T, int BITS> static void decode(const DecodeArgs &a, dim3 grid, hipStream_t st)
 {
     const dim3 block(256);
-    if (a.c.d == 64) attn_decode_kernel<T, 64, BITS, true><<<grid, block, 0, st>>>(a);
-    else if (a.c.d == 128) attn_decode_kernel<T, 128, BITS, true><<<grid, block, 0, st>>>(a);
-    else if (a.c.d < 64) attn_decode_kernel<T, 64, BITS, false><<<grid, block, 0, st>>>(a);
-    else attn_decode_kernel<T, 128, BITS, false><<<grid, block, 0, st>>>(a);
+    switch (a.c.d) {
+    case 16: attn_decode_kernel<T, 16, BITS><<<grid, block, 0, st>>>(a); break;
+    case 32: attn_decode_kernel<T, 32, BITS><<<grid, block, 0, st>>>(a); break;
+    case 48: attn_decode_kernel<T, 48, BITS><<<grid, block, 0, st>>>(a); break;
+    case 64: attn_decode_kernel<T, 64, BITS><<<grid, block, 0, st>>>(a); break;
+    case 80: attn_decode_kernel<T, 80, BITS><<<grid, block, 0, st>>>(a); break;
+    case 96: attn_decode_kernel<T, 96, BITS><<<grid, block, 0, st>>>(a); break;
+    case 112: attn_decode_kernel<T, 112, BITS><<<grid, block, 0, st>>>(a); break;
+    default: attn_decode_kernel<T, 128, BITS><<<grid, block, 0, st>>>(a); break;
+    }
     if (a.whole) return;
     // A wave adds the parts of a row where there are few of them.  (Four and one: 64 sequences of 512 positions, 64 heads on 8 of 128 in 8 bits, 27.6 and 23.9 us;
     // one of 4096 10.6 and 14.7.)
