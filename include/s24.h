@@ -344,7 +344,7 @@ typedef struct {
     int64_t token, head;
 } s24_heads;
 
-/* d: values of a head, a multiple of 16 up to 128 (beyond: S24_ERR_UNSUPPORTED); below 64 and between 64 and 128 it costs what 64 and 128 do.
+/* d: values of a head, a multiple of 16 up to 128 (beyond: S24_ERR_UNSUPPORTED); products of packed sequences cost what the next of 64, 96 and 128 does.
  * scale: the factor c > 0 of the scores, 1 / sqrt(d) as a rule.
  * o_rest: device [tokens_q][hq][d], may be NULL.  What the rounding of O took away, in 256ths of the last place: s24_attn_fwd writes it, and s24_attn_bwd adds it to O in
  * delta.  Without it the gradients of the queries and keys are about 1.3 times as far from the exact ones as results are that are rounded at their end alone, of short

@@ -125,7 +125,9 @@ template <int D> struct Forward {
 // the same relative precision, and the sums stay far inside fp32.
 constexpr float kGrowth = 8.0f;
 
-template <typename T, int D>
+// D: values of a tile's row; E: values that the products go over.  (Heads of 96 in tiles of 128 by products of 128: 8192 tokens of 16 heads on 4, 152 us forward and 607
+// backward; of 96 127 and 505.  Heads of 80 take 133 and 505 so.)
+template <typename T, int D, int E>
 __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
 {
     using C = Forward<D>;
@@ -143,7 +145,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
     const int all_tiles = s_.seen > 0 ? (s_.seen + C::BK - 1) / C::BK : 0;
     const int begin = (int)((int64_t)all_tiles * unit.part / a.by_query.parts), tiles = (int)((int64_t)all_tiles * (unit.part + 1) / a.by_query.parts);
 
-    uint4 q[2][D / 32];
+    uint4 q[2][E / 32];
     int last[2];   // that a row sees
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -151,14 +153,14 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
         const uint16_t *row = a.q.p + of.token * a.q.token + of.head * a.q.head;
         last[j] = a.causal ? min(sk.count - 1, of.at + s_.ahead) : sk.count - 1;
 #pragma unroll
-        for (int k = 0; k < D / 32; ++k)
+        for (int k = 0; k < E / 32; ++k)
             q[j][k] = 32 * k + 8 * g < a.d ? *reinterpret_cast<const uint4 *>(row + 32 * k + 8 * g) : make_uint4(0, 0, 0, 0);
     }
     const float c = a.scale * kLog2e;
     float m[2] = {-1e30f, -1e30f}, l[2] = {0.0f, 0.0f};
-    f32x4 o[D / 16][2];
+    f32x4 o[E / 16][2];
 #pragma unroll
-    for (int n = 0; n < D / 16; ++n) o[n][0] = o[n][1] = f32x4{};
+    for (int n = 0; n < E / 16; ++n) o[n][0] = o[n][1] = f32x4{};
 
     const uint16_t *keys = a.k.p + sk.first * a.k.token + kv * a.k.head, *values = a.v.p + sk.first * a.v.token + kv * a.v.head;
     Copy<D, C::BK, 4> ck, cv;
@@ -180,14 +182,14 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
 #pragma unroll
         for (int i = 0; i < NI; ++i) s[i][0] = s[i][1] = f32x4{};
 #pragma unroll
-        for (int k = 0; k < D / 32; ++k)
+        for (int k = 0; k < E / 32; ++k)
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
                 const uint4 f = rows<D>(tk, 16 * i, k, lane);
                 s[i][0] = mma<T>(f, q[0][k], s[i][0]);
                 s[i][1] = mma<T>(f, q[1][k], s[i][1]);
             }
-        if (D == 128) reads_ahead<NI, 2 * NI, D / 32>();
+        if (D == 128) reads_ahead<NI, 2 * NI, E / 32>();
         if (k0 + C::BK > s_.wave_all) {
 #pragma unroll
             for (int j = 0; j < 2; ++j)
@@ -212,7 +214,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
                 const float now = fmaxf(m[j], column_max(top[j])), shrink = __builtin_amdgcn_exp2f(m[j] - now);
                 m[j] = now, l[j] *= shrink;
 #pragma unroll
-                for (int n = 0; n < D / 16; ++n) o[n][j] *= shrink;
+                for (int n = 0; n < E / 16; ++n) o[n][j] *= shrink;
             }
         }
         uint4 p[NI / 2][2];
@@ -231,7 +233,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
 #pragma unroll
         for (int u = 0; u < NI / 2; ++u)
 #pragma unroll
-            for (int n = 0; n < D / 16; ++n) {
+            for (int n = 0; n < E / 16; ++n) {
                 const uint4 f = columns<D>(tv, 32 * u, n, lane);
                 o[n][0] = mma<T>(f, p[u][0], o[n][0]);
                 o[n][1] = mma<T>(f, p[u][1], o[n][1]);
@@ -249,11 +251,11 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
             uint16_t *out = a.out.p + token * a.out.token + head * a.out.head;
             int8_t *rest = a.rest + (token * a.hq + head) * a.d;
 #pragma unroll
-            for (int n = 0; n < D / 16; n += 4) {   // of four such pieces of a row a lane gets one whole: lines are written with few stores
+            for (int n = 0; n < E / 16; n += 4) {   // of four such pieces of a row a lane gets one whole: lines are written with few stores
                 uint32_t x[4], y[4], left[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const f32x4 v = o[n + i][j] * inverse;
+                    const f32x4 v = n + i < E / 16 ? o[n + i < E / 16 ? n + i : 0][j] * inverse : f32x4{};
                     x[i] = pack2<T>(v[0], v[1]), y[i] = pack2<T>(v[2], v[3]);
                     left[i] = a.rest != nullptr ? four_left<T>(v, make_uint2(x[i], y[i])) : 0;
                 }
@@ -269,7 +271,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
         } else {
             const int64_t at = (unit.part * (int64_t)a.tokens_q + token) * a.hq + head;
 #pragma unroll
-            for (int n = 0; n < D / 16; ++n)
+            for (int n = 0; n < E / 16; ++n)
                 if (16 * n < a.d) *reinterpret_cast<f32x4 *>(a.by_query.sums + at * a.d + 16 * n + 4 * g) = o[n][j];
             if (g == 0) a.weights[at] = make_float2(m[j], sum);
         }
@@ -329,7 +331,7 @@ template <int D> struct Backward {
     static constexpr int BK = 128, BQ = 32, TILE = BQ * 2 * D, STAGE = 2 * TILE + 8 * BQ, VALUES = BK * 2 * D;   // a stage: queries, gradients, row statistics
 };
 // tv, stages: C::VALUES and two times C::STAGE bytes of LDS
-template <typename T, int D> __device__ __forceinline__ void dkv_tile(const Problem &a, unsigned block, lds_byte *tv, lds_byte *stages)
+template <typename T, int D, int E> __device__ __forceinline__ void dkv_tile(const Problem &a, unsigned block, lds_byte *tv, lds_byte *stages)
 {
     using C = Backward<D>;
     using L = Lift<T>;
@@ -351,12 +353,12 @@ template <typename T, int D> __device__ __forceinline__ void dkv_tile(const Prob
 
     // The keys' fragments stay in registers, the values' come from LDS: with both, two waves would not fit a SIMD (8192 tokens, 64 heads on 8 of 128: 3.6 ms
     // with both in registers, 2.0 so, before dS went in two parts).
-    uint4 fk[2][D / 32];
+    uint4 fk[2][E / 32];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const int64_t t = sk.first + min(wk0 + 16 * j + col, sk.count - 1);
 #pragma unroll
-        for (int k = 0; k < D / 32; ++k) {
+        for (int k = 0; k < E / 32; ++k) {
             const int i = 32 * k + 8 * g;
             fk[j][k] = i < a.d ? *reinterpret_cast<const uint4 *>(a.k.p + t * a.k.token + kv * a.k.head + i) : make_uint4(0, 0, 0, 0);
         }
@@ -372,9 +374,9 @@ template <typename T, int D> __device__ __forceinline__ void dkv_tile(const Prob
                 if (8 * (i % (D / 8)) >= a.d) lds_store(tv + piece<D>(i / (D / 8), i % (D / 8)), make_uint4(0, 0, 0, 0));
         }
     }
-    f32x4 dk[D / 16][2], dv[D / 16][2];
+    f32x4 dk[E / 16][2], dv[E / 16][2];
 #pragma unroll
-    for (int n = 0; n < D / 16; ++n) dk[n][0] = dk[n][1] = dv[n][0] = dv[n][1] = f32x4{};
+    for (int n = 0; n < E / 16; ++n) dk[n][0] = dk[n][1] = dv[n][0] = dv[n][1] = f32x4{};
     const float c = a.scale * kLog2e;
 
     Copy<D, C::BQ, 4> cq, cdo;
@@ -404,7 +406,7 @@ template <typename T, int D> __device__ __forceinline__ void dkv_tile(const Prob
 #pragma unroll
         for (int i = 0; i < 2; ++i) s[i][0] = s[i][1] = dp[i][0] = dp[i][1] = f32x4{};
 #pragma unroll
-        for (int k = 0; k < D / 32; ++k) {
+        for (int k = 0; k < E / 32; ++k) {
             uint4 fv[2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) fv[j] = rows<D>(tv, 32 * wave + 16 * j, k, lane);
@@ -453,7 +455,7 @@ template <typename T, int D> __device__ __forceinline__ void dkv_tile(const Prob
 #pragma unroll
         for (int j = 0; j < 2; ++j) p[j] = operand<T>(s[0][j], s[1][j]), ds[j] = operand<T>(dp[0][j], dp[1][j]), lo[j] = rest<T>(ds[j], dp[0][j], dp[1][j]);
 #pragma unroll
-        for (int n = 0; n < D / 16; ++n) {
+        for (int n = 0; n < E / 16; ++n) {
             const uint4 x = columns<D>(tdo, 0, n, lane), y = columns<D>(tq, 0, n, lane);
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
@@ -471,7 +473,7 @@ template <typename T, int D> __device__ __forceinline__ void dkv_tile(const Prob
         if (a.by_key.parts == 1) {
             uint16_t *to_k = a.dk.p + t * a.dk.token + kv * a.dk.head, *to_v = a.dv.p + t * a.dv.token + kv * a.dv.head;
 #pragma unroll
-            for (int n = 0; n < D / 16; ++n)
+            for (int n = 0; n < E / 16; ++n)
                 if (16 * n < a.d) {
                     const f32x4 x = dk[n][j] * (a.scale * L::kOfDs), y = dv[n][j] * L::kOfP;
                     *reinterpret_cast<uint2 *>(to_k + 16 * n + 4 * g) = make_uint2(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]));
@@ -480,7 +482,7 @@ template <typename T, int D> __device__ __forceinline__ void dkv_tile(const Prob
         } else {
             float *to = a.by_key.sums + ((part * (int64_t)a.tokens_k + t) * hkv + kv) * 2 * a.d;
 #pragma unroll
-            for (int n = 0; n < D / 16; ++n)
+            for (int n = 0; n < E / 16; ++n)
                 if (16 * n < a.d) {
                     *reinterpret_cast<f32x4 *>(to + 16 * n + 4 * g) = dk[n][j] * (a.scale * L::kOfDs);
                     *reinterpret_cast<f32x4 *>(to + a.d + 16 * n + 4 * g) = dv[n][j] * L::kOfP;
@@ -511,7 +513,7 @@ __global__ __launch_bounds__(256) void attn_dkv_join_kernel(const Problem a)
 // dQ, over the keys that a workgroup's queries see, 32 at a time and wave: four waves of 32 queries (KS = 1), or two pairs, of which each wave takes half of a
 // tile's keys (KS = 2): twice the workgroups, each of half the length, for twice the copies.  STATS: it reads the row statistics; else it forms them, and leaves them to dK and dV.
 // lk, lv: two tiles of LDS each, for keys and values
-template <typename T, int D, int KS, bool STATS> __device__ __forceinline__ void dq_tile(const Problem &a, unsigned block, lds_byte *lk, lds_byte *lv)
+template <typename T, int D, int E, int KS, bool STATS> __device__ __forceinline__ void dq_tile(const Problem &a, unsigned block, lds_byte *lk, lds_byte *lv)
 {
     using L = Lift<T>;
     constexpr int BQ = 128 / KS, BK = 32 * KS, TILE = BK * 2 * D;
@@ -526,7 +528,7 @@ template <typename T, int D, int KS, bool STATS> __device__ __forceinline__ void
     const Span sk = s_.k;
     const int all_tiles = s_.seen > 0 ? (s_.seen + BK - 1) / BK : 0;
     const int begin = (int)((int64_t)all_tiles * unit.part / a.by_query.parts), tiles = (int)((int64_t)all_tiles * (unit.part + 1) / a.by_query.parts);
-    uint4 q[2][D / 32], dO[2][D / 32];
+    uint4 q[2][E / 32], dO[2][E / 32];
     float lse[2], delta[2];
     int last[2];   // that a row sees
 #pragma unroll
@@ -540,7 +542,7 @@ template <typename T, int D, int KS, bool STATS> __device__ __forceinline__ void
         last[j] = !live ? -1 : a.causal ? min(sk.count - 1, of.at + s_.ahead) : sk.count - 1;
         float sum = 0.0f;
 #pragma unroll
-        for (int k = 0; k < D / 32; ++k) {
+        for (int k = 0; k < E / 32; ++k) {
             const int i = 32 * k + 8 * g;
             q[j][k] = i < a.d ? *reinterpret_cast<const uint4 *>(a.q.p + t * a.q.token + head * a.q.head + i) : make_uint4(0, 0, 0, 0);
             dO[j][k] = i < a.d ? *reinterpret_cast<const uint4 *>(a.dO.p + t * a.dO.token + head * a.dO.head + i) : make_uint4(0, 0, 0, 0);
@@ -558,9 +560,9 @@ template <typename T, int D, int KS, bool STATS> __device__ __forceinline__ void
         }
     }
     const float c = a.scale * kLog2e;
-    f32x4 dq[D / 16][2];
+    f32x4 dq[E / 16][2];
 #pragma unroll
-    for (int n = 0; n < D / 16; ++n) dq[n][0] = dq[n][1] = f32x4{};
+    for (int n = 0; n < E / 16; ++n) dq[n][0] = dq[n][1] = f32x4{};
 
     const uint16_t *keys = a.k.p + sk.first * a.k.token + kv * a.k.head, *values = a.v.p + sk.first * a.v.token + kv * a.v.head;
     Copy<D, BK, 4> ck, cv;
@@ -582,7 +584,7 @@ template <typename T, int D, int KS, bool STATS> __device__ __forceinline__ void
 #pragma unroll
         for (int i = 0; i < 2; ++i) s[i][0] = s[i][1] = dp[i][0] = dp[i][1] = f32x4{};
 #pragma unroll
-        for (int k = 0; k < D / 32; ++k)
+        for (int k = 0; k < E / 32; ++k)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const uint4 x = rows<D>(tk, first_key + 16 * i, k, lane), y = rows<D>(tv, first_key + 16 * i, k, lane);
@@ -609,7 +611,7 @@ template <typename T, int D, int KS, bool STATS> __device__ __forceinline__ void
             ds[j] = operand<T>(s[0][j], s[1][j]), lo[j] = rest<T>(ds[j], s[0][j], s[1][j]);
         }
 #pragma unroll
-        for (int n = 0; n < D / 16; ++n) {
+        for (int n = 0; n < E / 16; ++n) {
             const uint4 x = columns<D>(tk, first_key, n, lane);
             dq[n][0] = mma<T>(x, ds[0], dq[n][0]);
             dq[n][1] = mma<T>(x, ds[1], dq[n][1]);
@@ -618,20 +620,20 @@ template <typename T, int D, int KS, bool STATS> __device__ __forceinline__ void
         }
     }
     if constexpr (KS == 2) {   // the wave of a pair that has the later keys hands its sums over, in LDS that no wave reads any more
-        constexpr int SUMS = D / 16 * 2 * 1024;
+        constexpr int SUMS = E / 16 * 2 * 1024;
         static_assert(SUMS <= 2 * TILE, "the sums must fit");
         lds_byte *const to = qw == 0 ? lk : lv;
         wait_and_barrier<0>();
         if (wave >= 2) {
 #pragma unroll
-            for (int n = 0; n < D / 16; ++n)
+            for (int n = 0; n < E / 16; ++n)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) lds_store(to + (2 * n + j) * 1024 + 16 * lane, dq[n][j]);
         }
         wait_and_barrier<0>();
         if (wave >= 2) return;
 #pragma unroll
-        for (int n = 0; n < D / 16; ++n)
+        for (int n = 0; n < E / 16; ++n)
 #pragma unroll
             for (int j = 0; j < 2; ++j) dq[n][j] += __builtin_bit_cast(f32x4, lds_load(to + (2 * n + j) * 1024 + 16 * lane));
     }
@@ -643,7 +645,7 @@ template <typename T, int D, int KS, bool STATS> __device__ __forceinline__ void
         const int64_t token = of.token;
         const int head = of.head;
 #pragma unroll
-        for (int n = 0; n < D / 16; ++n)
+        for (int n = 0; n < E / 16; ++n)
             if (16 * n < a.d) {
                 const f32x4 x = dq[n][j] * (a.scale * L::kOfDs);
                 if (a.by_query.parts == 1)
@@ -655,31 +657,31 @@ template <typename T, int D, int KS, bool STATS> __device__ __forceinline__ void
 }
 
 // Large grids: dQ, which runs first and leaves the row statistics; dK and dV
-template <typename T, int D>
+template <typename T, int D, int E>
 __global__ __launch_bounds__(256, 2) void attn_dq_kernel(const Problem a)
 {
     constexpr int TILE = 32 * 2 * D;
     __shared__ __align__(16) unsigned char lds_k[2 * TILE], lds_v[2 * TILE];
-    dq_tile<T, D, 1, false>(a, blockIdx.x, (lds_byte *)lds_k, (lds_byte *)lds_v);
+    dq_tile<T, D, E, 1, false>(a, blockIdx.x, (lds_byte *)lds_k, (lds_byte *)lds_v);
 }
-template <typename T, int D>
+template <typename T, int D, int E>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dkv_kernel(const Problem a)
 {
     using C = Backward<D>;
     __shared__ __align__(16) unsigned char values[C::VALUES], stages[2 * C::STAGE];
-    dkv_tile<T, D>(a, blockIdx.x, (lds_byte *)values, (lds_byte *)stages);
+    dkv_tile<T, D, E>(a, blockIdx.x, (lds_byte *)values, (lds_byte *)stages);
 }
 // Small grids: all three in one launch, since neither fills the device to its end; the row statistics are formed before.  (The gradients, in turn and so: 16 heads
 // of 128, 2048 tokens 193 and 119 us; 12 heads of 64, 1024 tokens 70 and 38, 8 x 1024 tokens 106 and 94; 16 heads on 4 of 128, 9 ragged sequences 179 and 116.
 // At four workgroups a compute unit, 32 heads on 8 of 128 and 4096 tokens, 620 both ways.)
-template <typename T, int D>
+template <typename T, int D, int E>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_bwd_kernel(const Problem a)
 {
     using C = Backward<D>;
     static_assert(2 * 64 * 2 * D <= C::VALUES && 2 * 64 * 2 * D <= 2 * C::STAGE, "two tiles must fit");
     __shared__ __align__(16) unsigned char values[C::VALUES], stages[2 * C::STAGE];
-    if (blockIdx.x < a.key_blocks) dkv_tile<T, D>(a, blockIdx.x, (lds_byte *)values, (lds_byte *)stages);
-    else dq_tile<T, D, 2, true>(a, blockIdx.x - a.key_blocks, (lds_byte *)values, (lds_byte *)stages);
+    if (blockIdx.x < a.key_blocks) dkv_tile<T, D, E>(a, blockIdx.x, (lds_byte *)values, (lds_byte *)stages);
+    else dq_tile<T, D, E, 2, true>(a, blockIdx.x - a.key_blocks, (lds_byte *)values, (lds_byte *)stages);
 }
 // stats[h][t]: what a row's exponents are taken from, and delta = dO.O; by LANES lanes, one for each of a row's pieces of 16 bytes, for four rows at a time so that
 // enough loads are under way.  (Both passes of 8 x 1024 tokens of 12 heads of 64: 108.9 us with one row, 107.6 with four.)
@@ -821,8 +823,9 @@ static int64_t stats_bytes(const s24_attn_shape *s) { return (s->tokens_q * s->h
 template <typename T> static int forward(const Problem &a, dim3 grid, dim3 join, hipStream_t st)
 {
     const dim3 block(256);
-    if (a.d <= 64) attn_fwd_kernel<T, 64><<<grid, block, 0, st>>>(a);
-    else attn_fwd_kernel<T, 128><<<grid, block, 0, st>>>(a);
+    if (a.d <= 64) attn_fwd_kernel<T, 64, 64><<<grid, block, 0, st>>>(a);
+    else if (a.d <= 96) attn_fwd_kernel<T, 128, 96><<<grid, block, 0, st>>>(a);
+    else attn_fwd_kernel<T, 128, 128><<<grid, block, 0, st>>>(a);
     if (a.by_query.parts > 1) attn_fwd_join_kernel<T><<<join, block, 0, st>>>(a);
     return s24_launch_status();
 }
@@ -862,7 +865,7 @@ extern "C" int s24_attn_fwd(const s24_attn_shape *shape, const s24_heads *Q, con
 }
 
 namespace s24_attn {
-template <typename T, int D> static int backward(Problem a, bool joint, int64_t query_groups, hipStream_t st)
+template <typename T, int D, int E> static int backward(Problem a, bool joint, int64_t query_groups, hipStream_t st)
 {
     const dim3 block(256);
     const int64_t hkv = a.hq / a.group, key_groups = most_tiles(a.tokens_k, a.sequences, 128) * hkv * a.by_key.parts;
@@ -871,16 +874,20 @@ template <typename T, int D> static int backward(Problem a, bool joint, int64_t 
         a.key_blocks = (unsigned)((key_groups + 7) / 8 * 8);   // dQ's workgroups meet the XCDs as they would in a launch of their own
         const int64_t rows = (int64_t)a.tokens_q * a.hq, of_group = 2048 / D * kStatsRows;
         attn_stats_kernel<T, D / 8><<<dim3((unsigned)((rows + of_group - 1) / of_group)), block, 0, st>>>(a);
-        attn_bwd_kernel<T, D><<<dim3(a.key_blocks + (unsigned)query_groups), block, 0, st>>>(a);
+        attn_bwd_kernel<T, D, E><<<dim3(a.key_blocks + (unsigned)query_groups), block, 0, st>>>(a);
     } else {
-        if (query_groups > 0) attn_dq_kernel<T, D><<<dim3((unsigned)query_groups), block, 0, st>>>(a);
-        if (key_groups > 0) attn_dkv_kernel<T, D><<<dim3((unsigned)key_groups), block, 0, st>>>(a);
+        if (query_groups > 0) attn_dq_kernel<T, D, E><<<dim3((unsigned)query_groups), block, 0, st>>>(a);
+        if (key_groups > 0) attn_dkv_kernel<T, D, E><<<dim3((unsigned)key_groups), block, 0, st>>>(a);
     }
     if (query_groups > 0 && a.by_query.parts > 1)
         attn_dq_join_kernel<T><<<dim3((unsigned)(most_tiles(a.tokens_q, a.sequences, kJoinRows) * a.hq)), block, 0, st>>>(a);
     if (key_groups > 0 && a.by_key.parts > 1)
         attn_dkv_join_kernel<T><<<dim3((unsigned)(most_tiles(a.tokens_k, a.sequences, kJoinRows) * hkv)), block, 0, st>>>(a);
     return s24_launch_status();
+}
+template <typename T> static int backward(const Problem &a, bool joint, int64_t query_groups, hipStream_t st)
+{
+    return a.d <= 64 ? backward<T, 64, 64>(a, joint, query_groups, st) : a.d <= 96 ? backward<T, 128, 96>(a, joint, query_groups, st) : backward<T, 128, 128>(a, joint, query_groups, st);
 }
 static int64_t query_sums(const s24_attn_shape *s, int parts) { return parts > 1 ? parts * s->tokens_q * s->hq * s->d * 4 : 0; }
 static int64_t key_sums(const s24_attn_shape *s, int parts) { return parts > 1 ? parts * s->tokens_k * s->hkv * s->d * 8 : 0; }
@@ -916,6 +923,5 @@ extern "C" int s24_attn_bwd(const s24_attn_shape *shape, const s24_heads *Q, con
     a.by_key = {plan.key_parts, reinterpret_cast<float *>(sums + query_sums(shape, plan.query_parts))};
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const int64_t groups = query_groups(shape, plan.joint ? 64 : 128) * plan.query_parts;
-    if (dt == S24_BF16) return a.d <= 64 ? backward<uint16_t, 64>(a, plan.joint, groups, st) : backward<uint16_t, 128>(a, plan.joint, groups, st);
-    return a.d <= 64 ? backward<s24_half, 64>(a, plan.joint, groups, st) : backward<s24_half, 128>(a, plan.joint, groups, st);
+    return dt == S24_BF16 ? backward<uint16_t>(a, plan.joint, groups, st) : backward<s24_half>(a, plan.joint, groups, st);
 }

@@ -362,8 +362,7 @@ __device__ __forceinline__ uint4 halves(uint32_t a, uint32_t b)
 // Softmax in 8 bits: the weights go to the product as exp(s - ref) * (step of V) in binary16, where ref has the largest step so far as a factor too, so that
 // they stay at 2^9 or less; the factor is in the sum of the weights as well and cancels.  (A step below 2^-100 counts as that, for ref to stay in range.)
 // Heads of every size have a kernel of their own, in which the addresses within a page are constants.  (With those of 64 and 128 for all, 32 sequences of 4096 positions,
-// 32 heads on 8
-// in 16 bits, take 98 us for heads of 96 and 92 for 80; so 74 and 72.)
+// 32 heads on 8 in 16 bits, take 98 us for heads of 96 and 92 for 80; so 74 and 72.)
 constexpr float kRise = 8.0f;   // as in the forward pass over packed sequences: how far a score may exceed the reference before it moves
 template <typename T, int D, int BITS>
 __global__ __launch_bounds__(256, 2) void attn_decode_kernel(const DecodeArgs a)
