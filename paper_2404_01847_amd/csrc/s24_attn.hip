@@ -327,7 +327,7 @@ template <> struct Lift<s24_half> { static constexpr float kUp = 15.0f, kDown = 
 
 // dK and dV of 128 keys of a key-value head, four waves of 32: over the query heads of the group and their queries, 32 at a time.
 // S has the queries as rows, so that P and dS are, as they lie, the operands that contract over the queries.  A step has 80 matrix instructions of a wave (heads of
-// 128), 28 reads of 16 bytes and 32 transposed ones; at two waves to a SIMD it takes 2.0 us, of which the matrix instructions are 1.1.
+// 128), 28 reads of 16 bytes and 32 transposed ones; at two waves to a SIMD it takes 1.9 us, of which the matrix instructions are 1.1.
 template <int D> struct Backward {
     static constexpr int BK = 128, BQ = 32, TILE = BQ * 2 * D, STAGE = 2 * TILE + 8 * BQ, VALUES = BK * 2 * D;   // a stage: queries, gradients, row statistics
 };
@@ -674,8 +674,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dkv_kernel(const Pr
     dkv_tile<T, D, E>(a, blockIdx.x, (lds_byte *)values, (lds_byte *)stages);
 }
 // Small grids: all three in one launch, since neither fills the device to its end; the row statistics are formed before.  (The gradients, in turn and so: 16 heads
-// of 128, 2048 tokens 193 and 119 us; 12 heads of 64, 1024 tokens 70 and 38, 8 x 1024 tokens 106 and 94; 16 heads on 4 of 128, 9 ragged sequences 179 and 116.
-// At four workgroups a compute unit, 32 heads on 8 of 128 and 4096 tokens, 620 both ways.)
+// of 128, 2048 tokens 193 and 119 us; 12 heads of 64, 1024 tokens 70 and 38, 8 x 1024 tokens 106 and 94.  At four workgroups a compute unit, 32 heads on 8 of 128 and 4096 tokens, 620 both ways.)
 template <typename T, int D, int E>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_bwd_kernel(const Problem a)
 {
