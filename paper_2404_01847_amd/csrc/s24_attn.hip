@@ -674,7 +674,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dkv_kernel(const Pr
     dkv_tile<T, D, E>(a, blockIdx.x, (lds_byte *)values, (lds_byte *)stages);
 }
 // Small grids: all three in one launch, since neither fills the device to its end; the row statistics are formed before.  (The gradients, in turn and so: 16 heads
-// of 128, 2048 tokens 193 and 119 us; 12 heads of 64, 1024 tokens 70 and 38, 8 x 1024 tokens 106 and 94.  At four workgroups a compute unit, 32 heads on 8 of 128 and 4096 tokens, 620 both ways.)
+// of 128, 2048 tokens 193 and 119 us; 12 heads of 64, 1024 tokens 70 and 38, 8 x 1024 tokens 106 and 94.  At four workgroups a
+// compute unit, 32 heads on 8 of 128 and 4096 tokens, 620 both ways.)
 template <typename T, int D, int E>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_bwd_kernel(const Problem a)
 {
