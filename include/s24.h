@@ -332,7 +332,8 @@ int s24_l1_norm_gap(const void *W, s24_dtype dt, int64_t r, int64_t q, int64_t l
  * sequence are left as they are).  With lq queries and lk keys, query i sees the keys j < lk, and if `causal` of these j <= i + lk - lq: the
  * queries are the last ones of the keys (a prompt that is read in chunks; lq = lk in training).  A query that sees none gives a row of zeros.
  * S24_BF16 and S24_F16; S24_F32 returns S24_ERR_UNSUPPORTED.  Scores, row statistics and sums are fp32; the weights P are rounded to the storage
- * type as operands of the second products, dS of the backward pass goes into them as two parts (its rounded value and the rounded rest).
+ * type as operands of the second products, dS of the backward pass goes into them as two parts (its rounded value and the rounded rest), in binary16 both times a power
+ * of two that follows its size: dO may be of any size whose gradients the type holds.
  * The scores' size must stay below 2^23, up to which fp32 still holds their fractions' halves; NaN among what a query sees gives NaN.
  * Nothing is added in an order that depends on scheduling. */
 

@@ -57,8 +57,12 @@ template <typename T> __device__ __forceinline__ uint4 operand(f32x4 a, f32x4 b)
 template <typename T> __device__ __forceinline__ uint4 rest(uint4 x, f32x4 a, f32x4 b)
 {
     using Num = s24_num<T>;
-    return operand<T>(f32x4{a[0] - Num::lo(x.x), a[1] - Num::hi(x.x), a[2] - Num::lo(x.y), a[3] - Num::hi(x.y)},
-                      f32x4{b[0] - Num::lo(x.z), b[1] - Num::hi(x.z), b[2] - Num::lo(x.w), b[3] - Num::hi(x.w)});
+    // (Of binary16 as a product with -1 that the compiler does not know: an fma converts its operand itself, a subtraction does not.  2 % of the gradients' time.)
+    float minus = -1.0f;
+    if (!std::is_same<T, uint16_t>::value) asm("" : "+v"(minus));
+    auto less = [&](float value, float held) { return std::is_same<T, uint16_t>::value ? value - held : fmaf(held, minus, value); };
+    return operand<T>(f32x4{less(a[0], Num::lo(x.x)), less(a[1], Num::hi(x.x)), less(a[2], Num::lo(x.y)), less(a[3], Num::hi(x.y))},
+                      f32x4{less(b[0], Num::lo(x.z)), less(b[1], Num::hi(x.z)), less(b[2], Num::lo(x.w)), less(b[3], Num::hi(x.w))});
 }
 
 // Rows of 16 lanes: the odd rows of a and the even rows of b change places / the last two of a and the first two of b
