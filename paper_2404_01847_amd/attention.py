@@ -12,6 +12,12 @@ import torch
 from . import binding as s24
 
 
+def _capturing():
+    """Whether the current stream's calls go into a graph.  Such a call gets a workspace of its own, from the graph's memory: graphs that were captured on one
+    stream may be replayed on several at the same time."""
+    return torch.cuda.is_initialized() and torch.cuda.is_current_stream_capturing()
+
+
 class Attention:
     """Buffers and call sequence of one attention layer: hq query heads on hkv key-value heads of d values, up to tokens_q query rows
     (tokens_k key rows; None: as many) of packed sequences.  dtype: torch.bfloat16 or torch.float16."""
@@ -32,9 +38,12 @@ class Attention:
     def _workspace(self, need, cu_q):
         """What a pass takes depends on the number of sequences."""
         key = (need, cu_q.shape[0])
-        if key not in self.work:
+        if key not in self.work or _capturing():
             n = need(self.tokens_q, self.tokens_k, self.hq, self.hkv, self.d, cu_q.shape[0] - 1)
-            self.work[key] = torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
+            work = torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
+            if _capturing():
+                return work
+            self.work[key] = work
         return self.work[key]
 
     def forward(self, Q, K, V, cu_q, cu_k=None):
@@ -81,7 +90,9 @@ class PagedKV:
     def attend(self, Q, table, lengths, O, scale=None):
         """O [sequences, hq, d]: attention of one new token of each sequence over its first lengths[i] positions."""
         key = (Q.shape[:2], s24._stream())
-        work = self.work.get(key)
+        work = None if _capturing() else self.work.get(key)
         if work is None:   # one for each stream: calls on two streams may run at the same time
-            work = self.work[key] = torch.empty(s24.attn_decode_workspace(self.buffers, Q.shape[0], Q.shape[1]), dtype=torch.uint8, device=self.K.device)
+            work = torch.empty(s24.attn_decode_workspace(self.buffers, Q.shape[0], Q.shape[1]), dtype=torch.uint8, device=self.K.device)
+            if not _capturing():
+                self.work[key] = work
         return s24.attn_decode(self.buffers, Q, table, lengths, O, work, scale)
