@@ -7,15 +7,38 @@ prompt attends to the earlier ones.
 """
 from __future__ import annotations
 
+import threading
+
 import torch
 
 from . import binding as s24
 
 
-def _capturing():
-    """Whether the current stream's calls go into a graph.  Such a call gets a workspace of its own, from the graph's memory: graphs that were captured on one
-    stream may be replayed on several at the same time."""
-    return torch.cuda.is_initialized() and torch.cuda.is_current_stream_capturing()
+class _Buffers(threading.local):
+    """A thread's workspaces, one for each device and stream."""
+
+    def __init__(self):
+        self.held = {}
+
+
+_buffers = _Buffers()
+
+
+def _workspace(n, beside):
+    """n bytes for a call on the current stream, on the device of the tensor `beside`.  A workspace holds nothing between calls, and those of a stream follow each other: they
+    all have one, as large as the largest of them needs (two threads may launch on one stream in between each other: each has its own).  A call that goes
+    into a graph has one from the graph's memory: graphs that were captured on one stream may be replayed on several at the same time, and outlive a
+    buffer that is outgrown."""
+    if n == 0:
+        return None
+    stream, held = s24._stream(), _buffers.held
+    if stream != 0 and torch.cuda.is_current_stream_capturing():   # (the default stream cannot be captured)
+        return torch.empty(n, dtype=torch.uint8, device=beside.device)
+    key = (beside.get_device(), stream)
+    work = held.get(key)
+    if work is None or work.numel() < n:
+        work = held[key] = torch.empty(n, dtype=torch.uint8, device=beside.device)
+    return work
 
 
 class Attention:
@@ -33,18 +56,15 @@ class Attention:
         self._rest = self.rest.data_ptr()
         self.lse = torch.empty((hq, tokens_q), dtype=torch.float32, device=device)
         self.dQ = self.dK = self.dV = None   # allocated by the first backward pass
-        self.work = {}
+        self.need = {}   # bytes of workspace that a pass over so many sequences takes
 
     def _workspace(self, need, cu_q):
         """What a pass takes depends on the number of sequences."""
         key = (need, cu_q.shape[0])
-        if key not in self.work or _capturing():
-            n = need(self.tokens_q, self.tokens_k, self.hq, self.hkv, self.d, cu_q.shape[0] - 1)
-            work = torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
-            if _capturing():
-                return work
-            self.work[key] = work
-        return self.work[key]
+        n = self.need.get(key)
+        if n is None:
+            n = self.need[key] = need(self.tokens_q, self.tokens_k, self.hq, self.hkv, self.d, cu_q.shape[0] - 1)
+        return _workspace(n, self.O)
 
     def forward(self, Q, K, V, cu_q, cu_k=None):
         """O [tokens_q, hq, d].  Q, K, V may be views of one projection's result; cu_q, cu_k: int32 offsets of the sequences."""
@@ -77,7 +97,7 @@ class PagedKV:
         self.K, self.V = (torch.empty(shape, dtype=dtype if bits == 16 else torch.uint8, device=device) for _ in range(2))
         self.k_step, self.v_step = (torch.empty(shape[:3], dtype=torch.float32, device=device) if bits == 8 else None for _ in range(2))
         self.buffers = s24.KVBuffers(self.K, self.V, dtype, self.k_step, self.v_step)
-        self.work = {}
+        self.need = {}   # bytes of workspace that queries of a shape take
 
     def write(self, K, V, places):
         """Rows of K and V [tokens, hkv, d] to their places: page number * page + position in the page (int64; negative ones are skipped)."""
@@ -89,10 +109,7 @@ class PagedKV:
 
     def attend(self, Q, table, lengths, O, scale=None):
         """O [sequences, hq, d]: attention of one new token of each sequence over its first lengths[i] positions."""
-        key = (Q.shape[:2], s24._stream())
-        work = None if _capturing() else self.work.get(key)
-        if work is None:   # one for each stream: calls on two streams may run at the same time
-            work = torch.empty(s24.attn_decode_workspace(self.buffers, Q.shape[0], Q.shape[1]), dtype=torch.uint8, device=self.K.device)
-            if not _capturing():
-                self.work[key] = work
-        return s24.attn_decode(self.buffers, Q, table, lengths, O, work, scale)
+        n = self.need.get(Q.shape)
+        if n is None:
+            n = self.need[Q.shape] = s24.attn_decode_workspace(self.buffers, Q.shape[0], Q.shape[1])
+        return s24.attn_decode(self.buffers, Q, table, lengths, O, _workspace(n, self.K), scale)

@@ -64,3 +64,43 @@ def test_captured_calls_share_no_workspace(calls):
             one()
         plain, first, second, again = calls.addresses()
         assert plain == again and len({plain, first, second}) == 3
+
+
+def test_workspaces_do_not_pile_up(calls):
+    """Batches of every size, of several layers and caches, over and over: what is held is the largest that a call needs."""
+    caches, layers = [cache() for _ in range(3)], [attention.Attention(4, 2, 64, 64, device="cpu") for _ in range(3)]
+    attention._buffers.held.clear()
+    for _ in range(2):
+        for n in range(1, 30):
+            for c in caches:
+                attend(c, n)
+            for layer in layers:
+                layer.forward(rows(64, 4), rows(64, 2), rows(64, 2), offsets(n))
+                layer.backward(rows(64, 4), rows(64, 2), rows(64, 2), rows(64, 4), offsets(n))
+    kept = list(attention._buffers.held.values())
+    assert len(kept) == 1 and kept[0].numel() == 4000
+    calls.work.clear()
+    attend(caches[0], 5)
+    layers[1].forward(rows(64, 4), rows(64, 2), rows(64, 2), offsets(3))
+    assert calls.addresses() == [kept[0].data_ptr()] * 2
+
+
+def test_a_larger_call_after_a_smaller_one(calls):
+    attention._buffers.held.clear()
+    c = cache()
+    for hq in (2, 8, 4):
+        attend(c, 2, hq)
+    assert [w.numel() for w in calls.work] == [2000, 8000, 8000]
+
+
+def test_streams_and_threads_have_their_own(calls):
+    import threading
+    attention._buffers.held.clear()
+    c = cache()
+    for calls.stream in (1, 2, 1):
+        attend(c, 2)
+    thread = threading.Thread(target=attend, args=(c, 2))
+    thread.start()
+    thread.join()
+    one, two, again, other = calls.addresses()
+    assert one == again and len({one, two, other}) == 3
