@@ -20,12 +20,12 @@ def offsets(lengths):
 
 
 class DecoderLayer:
-    """Weights, buffers and call sequence of one layer for up to `tokens` tokens a call."""
+    """Weights, buffers and call sequence of one layer: `tokens` tokens in a training step, up to as many in a call that serves."""
 
     def __init__(self, width, d_ff, hq, hkv, d, tokens, dtype=torch.bfloat16, seed=0):
         gen = torch.Generator(device="cuda").manual_seed(seed)
         weight = lambda r, q: (torch.randn((r, q), generator=gen, device="cuda") * q ** -0.5).to(dtype)
-        self.hq, self.hkv, self.d, self.dtype = hq, hkv, d, dtype
+        self.hq, self.hkv, self.d, self.tokens, self.dtype = hq, hkv, d, tokens, dtype
         self.Wqkv, self.Wo = weight((hq + 2 * hkv) * d, width), weight(width, hq * d)
         self.ffn = SparseFFN({"Wg": weight(d_ff, width), "Wu": weight(d_ff, width), "Wd": weight(width, d_ff)}, tokens, "swiglu", 2e-4, concat_gate_up=True)
         self.attention = Attention(hq, hkv, d, tokens, dtype=dtype)
@@ -46,6 +46,8 @@ class DecoderLayer:
     # ---- training
     def step(self, X, dY, cu):
         """Forward and backward over packed sequences: Y and dX; the weights' gradients are in `grads` and in `ffn.w[...].grad`."""
+        if X.shape[0] != self.tokens:   # the FFN's weight gradients go over all rows of its buffers
+            raise ValueError(f"a training step of this layer takes {self.tokens} tokens, got {X.shape[0]}")
         self.ffn.prune()
         Q, K, V = self._heads(X)
         O = self.attention.forward(Q, K, V, cu)
@@ -69,7 +71,7 @@ class DecoderLayer:
         cache.write(K, V, table[sequence, rows // cache.page].long() * cache.page + rows % cache.page)
         Ka, Va = (torch.empty((sum(every), self.hkv, self.d), dtype=self.dtype, device="cuda") for _ in range(2))
         cache.read(table, offsets(every), Ka, Va)
-        O = Attention(self.hq, self.hkv, self.d, X.shape[0], sum(every), self.dtype).forward(Q, Ka, Va, offsets(new), offsets(every))
+        O = self.attention.forward(Q, Ka, Va, offsets(new), offsets(every))
         return self._finish(X, O)[1]
 
     def sample(self, X, lengths, cache, table):

@@ -43,7 +43,8 @@ def _workspace(n, beside):
 
 class Attention:
     """Buffers and call sequence of one attention layer: hq query heads on hkv key-value heads of d values, up to tokens_q query rows
-    (tokens_k key rows; None: as many) of packed sequences.  dtype: torch.bfloat16 or torch.float16."""
+    (in the backward pass up to tokens_k key rows; None: as many) of packed sequences.  dtype: torch.bfloat16 or torch.float16.  lse [hq, rows] is that of the last
+    forward pass."""
 
     def __init__(self, hq: int, hkv: int, d: int, tokens_q: int, tokens_k: int | None = None, dtype=torch.bfloat16, device="cuda", causal: bool = True,
                  scale: float | None = None):
@@ -54,25 +55,30 @@ class Attention:
         self.O = torch.empty((tokens_q, hq, d), dtype=dtype, device=device)
         self.rest = torch.empty((tokens_q, hq, d), dtype=torch.int8, device=device)   # what the rounding of O took away: the backward pass takes delta from both
         self._rest = self.rest.data_ptr()
-        self.lse = torch.empty((hq, tokens_q), dtype=torch.float32, device=device)
+        self.lse = self._lse = torch.empty((hq, tokens_q), dtype=torch.float32, device=device)
         self.dQ = self.dK = self.dV = None   # allocated by the first backward pass
-        self.need = {}   # bytes of workspace that a pass over so many sequences takes
+        self.need = {}   # bytes of workspace that a pass over so many rows and sequences takes
 
-    def _workspace(self, need, cu_q):
-        """What a pass takes depends on the number of sequences."""
-        key = (need, cu_q.shape[0])
+    def _workspace(self, need, tokens_q, tokens_k, cu_q):
+        key = (need, tokens_q, tokens_k, cu_q.shape[0])
         n = self.need.get(key)
         if n is None:
-            n = self.need[key] = need(self.tokens_q, self.tokens_k, self.hq, self.hkv, self.d, cu_q.shape[0] - 1)
+            if len(self.need) >= 1024:   # (batches of ever new sizes)
+                self.need.clear()
+            n = self.need[key] = need(tokens_q, tokens_k, self.hq, self.hkv, self.d, cu_q.shape[0] - 1)
         return _workspace(n, self.O)
 
     def forward(self, Q, K, V, cu_q, cu_k=None):
-        """O [tokens_q, hq, d].  Q, K, V may be views of one projection's result; cu_q, cu_k: int32 offsets of the sequences."""
-        return s24.attn_fwd(Q, K, V, self.O, self.lse, self._workspace(s24.attn_fwd_workspace, cu_q), cu_q, cu_k, self.causal, self.scale, self._rest)
+        """O [rows of Q, hq, d].  Q, K, V may be views of one projection's result; cu_q, cu_k: int32 offsets of the sequences."""
+        n, O, self.lse = Q.shape[0], self.O, self._lse
+        if n < self.tokens_q:
+            O, self.lse = O[:n], self._lse.view(-1)[:self.hq * n].view(self.hq, n)
+        return s24.attn_fwd(Q, K, V, O, self.lse, self._workspace(s24.attn_fwd_workspace, n, K.shape[0], cu_q), cu_q, cu_k, self.causal, self.scale, self._rest)
 
     def backward(self, Q, K, V, dO, cu_q, cu_k=None):
         """dQ, dK, dV of the last forward pass, whose operands are given again."""
-        work = self._workspace(s24.attn_bwd_workspace, cu_q)
+        nq, nk = Q.shape[0], K.shape[0]
+        work = self._workspace(s24.attn_bwd_workspace, nq, nk, cu_q)
         if self.dQ is None:
             # the layout of the projection's gradient: dQ, dK and dV are its parts
             if self.tokens_q == self.tokens_k:
@@ -82,7 +88,12 @@ class Attention:
                 self.dQKV = None
                 self.dQ = torch.empty((self.tokens_q, self.hq, self.d), dtype=self.dtype, device=self.device)
                 self.dK, self.dV = (torch.empty((self.tokens_k, self.hkv, self.d), dtype=self.dtype, device=self.device) for _ in range(2))
-        return s24.attn_bwd(Q, K, V, self.O, dO, self.lse, self.dQ, self.dK, self.dV, work, cu_q, cu_k, self.causal, self.scale, self._rest)
+        O, dQ, dK, dV = self.O, self.dQ, self.dK, self.dV
+        if nq < self.tokens_q:
+            O, dQ = O[:nq], dQ[:nq]
+        if nk < self.tokens_k:
+            dK, dV = dK[:nk], dV[:nk]
+        return s24.attn_bwd(Q, K, V, O, dO, self.lse, dQ, dK, dV, work, cu_q, cu_k, self.causal, self.scale, self._rest)
 
 
 class PagedKV:
