@@ -591,6 +591,8 @@ class KVBuffers:
         self.buffers, self.dtype, self.device, self.bits = (K, V, k_step, v_step), dtype, device, bits
         self.pages, self.hkv, self.page, self.d = K.shape
         self.packed = _pack_cache(_ptr(K), _ptr(V), _ptr(k_step) or 0, _ptr(v_step) or 0, self.pages, self.page, self.hkv, self.d, bits)
+        nothing = _pack_heads(0, 0, 0)   # no tokens: the library looks at the cache alone, and launches nothing
+        _check(lib().s24_kv_write(self.packed, nothing, nothing, None, 0, _DTYPES[dtype], None), f"{where}: pages of {self.page} tokens, {self.hkv} heads of {self.d}")
 
 
 def kv_write(cache, K, V, places):
