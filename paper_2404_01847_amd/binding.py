@@ -506,6 +506,14 @@ def _heads(where, name, x, shape, dtype, device):
     return _pack_heads(x.data_ptr(), token if shape[0] > 1 else 0, head if shape[1] > 1 else 0)
 
 
+def _axes(where, name, x, axes):
+    """The shape of a tensor whose sizes the call goes by."""
+    shape = x.shape
+    if len(shape) != len(axes):
+        raise ValueError(f"{where}: {name} must have shape [{', '.join(axes)}], got {tuple(shape)}")
+    return shape
+
+
 def _whole(where, name, x, dtype, shape, device):
     """A contiguous tensor of whole numbers (offsets, lengths, places, tables), statistics or bytes."""
     if x.dtype is not dtype or x.shape != shape or x.get_device() != device or not x.is_contiguous():
@@ -518,6 +526,10 @@ def _attn_operands(where, Q, K, cu_q, cu_k, causal, scale, rest):
     sq, sk = Q.shape, K.shape
     if len(sq) != 3 or len(sk) != 3 or sk[2] != sq[2]:
         raise ValueError(f"{where}: Q and K must have shape [tokens, heads, d] with one d, got {tuple(sq)} and {tuple(sk)}")
+    if scale is None:
+        if sq[2] == 0:
+            raise ValueError(f"{where}: heads need at least one value, got Q of shape {tuple(sq)}")
+        scale = sq[2] ** -0.5
     device, n = Q.get_device(), cu_q.shape
     pq = _whole(where, "cu_q", cu_q, torch.int32, n, device)
     if len(n) != 1 or n[0] == 0:
@@ -525,7 +537,7 @@ def _attn_operands(where, Q, K, cu_q, cu_k, causal, scale, rest):
     pk = pq if cu_k is None or cu_k is cu_q else _whole(where, "cu_k", cu_k, torch.int32, n, device)
     if type(rest) is not int:
         rest = 0 if rest is None else _whole(where, "rest", rest, torch.int8, sq, device)
-    return sq, sk, Q.dtype, device, _pack_shape(pq, pk, n[0] - 1, sq[0], sk[0], sq[1], sk[1], sq[2], sq[2] ** -0.5 if scale is None else scale, bool(causal), rest)
+    return sq, sk, Q.dtype, device, _pack_shape(pq, pk, n[0] - 1, sq[0], sk[0], sq[1], sk[1], sq[2], scale, bool(causal), rest)
 
 
 def attn_fwd(Q, K, V, O, lse, workspace, cu_q, cu_k=None, causal=True, scale=None, rest=None):
@@ -598,7 +610,7 @@ class KVBuffers:
 def kv_write(cache, K, V, places):
     """Rows of K and V [tokens, hkv, d] to the places (int64: page number * page + position in the page; negative: skipped) of the cache (KVBuffers)."""
     where, device = "s24_kv_write", cache.device
-    tokens = K.shape[0]
+    tokens = _axes(where, "K", K, ("tokens", "heads", "d"))[0]
     shape = (tokens, cache.hkv, cache.d)
     args = (cache.packed, _heads(where, "K", K, shape, cache.dtype, device), _heads(where, "V", V, shape, cache.dtype, device),
             _whole(where, "places", places, torch.int64, (tokens,), device), tokens, _dt(K))
@@ -611,9 +623,10 @@ def kv_write(cache, K, V, places):
 
 def kv_read(cache, table, cu, K, V):
     """Position j of sequence i, in page table[i, j // page] (int32), to row cu[i] + j of K and V [tokens, hkv, d]."""
-    where, device, n = "s24_kv_read", cache.device, table.shape
-    shape = (K.shape[0], cache.hkv, cache.d)
-    args = (cache.packed, _whole(where, "table", table, torch.int32, (n[0], n[-1]), device), n[-1],
+    where, device = "s24_kv_read", cache.device
+    n = _axes(where, "table", table, ("sequences", "pages"))
+    shape = (_axes(where, "K", K, ("tokens", "heads", "d"))[0], cache.hkv, cache.d)
+    args = (cache.packed, _whole(where, "table", table, torch.int32, n, device), n[1],
             _whole(where, "cu", cu, torch.int32, (n[0] + 1,), device), n[0], shape[0], _heads(where, "K", K, shape, cache.dtype, device),
             _heads(where, "V", V, shape, cache.dtype, device), _dt(K))
     if device < 0:
@@ -632,11 +645,12 @@ def attn_decode_workspace(cache, sequences, hq):
 def attn_decode(cache, Q, table, lengths, O, workspace, scale=None):
     """O[i] = softmax(scale Q[i].K) V over the first lengths[i] (int32) positions of sequence i.  Q, O [sequences, hq, d]; workspace: a uint8 tensor of
     attn_decode_workspace(...) bytes."""
-    where, device, n = "s24_attn_decode", cache.device, table.shape
-    sequences, hq, d = Q.shape
+    where, device = "s24_attn_decode", cache.device
+    n = _axes(where, "table", table, ("sequences", "pages"))
+    sequences, hq, d = _axes(where, "Q", Q, ("sequences", "heads", "d"))
     shape = (sequences, hq, cache.d)
-    args = (cache.packed, _heads(where, "Q", Q, shape, cache.dtype, device), hq, _whole(where, "table", table, torch.int32, (sequences, n[-1]), device),
-            n[-1], _whole(where, "lengths", lengths, torch.int32, (sequences,), device), sequences, d ** -0.5 if scale is None else scale,
+    args = (cache.packed, _heads(where, "Q", Q, shape, cache.dtype, device), hq, _whole(where, "table", table, torch.int32, (sequences, n[1]), device),
+            n[1], _whole(where, "lengths", lengths, torch.int32, (sequences,), device), sequences, d ** -0.5 if scale is None else scale,
             _heads(where, "O", O, shape, cache.dtype, device), _whole(where, "workspace", workspace, torch.uint8, workspace.shape, device),
             workspace.numel(), _dt(Q))
     if device < 0:

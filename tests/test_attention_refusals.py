@@ -22,3 +22,26 @@ def test_caches_that_the_calls_take():
             for dtype in (torch.bfloat16, torch.float16):
                 assert PagedKV(1, page, hkv, d, dtype, bits, device="cpu").buffers.page == page
     assert PagedKV(0, 16, 2, 64, device="cpu").pages == 0
+
+
+def test_tensors_without_the_axes_of_an_operand_are_refused():
+    """As ValueError or by the library, not as an error of what the check itself does."""
+    x, cu, table, at = torch.zeros(8, 2, 64, dtype=torch.bfloat16), torch.tensor([0, 8], dtype=torch.int32), torch.zeros((1, 2), dtype=torch.int32), torch.zeros(8, dtype=torch.int64)
+    c = PagedKV(4, 16, 2, 64, device="cpu").buffers
+    for scalar in (x[0, 0, 0], x[0, 0]):
+        with pytest.raises(ValueError, match="K must have shape"):
+            s24.kv_write(c, scalar, x, at)
+        with pytest.raises(ValueError, match="K must have shape"):
+            s24.kv_read(c, table, cu, scalar, x)
+        with pytest.raises(ValueError, match="Q must have shape"):
+            s24.attn_decode(c, scalar, table, cu[:1], x, torch.zeros(16, dtype=torch.uint8))
+    for bad in (table[0, 0], table[0]):
+        with pytest.raises(ValueError, match="table must have shape"):
+            s24.kv_read(c, bad, cu, x, x)
+        with pytest.raises(ValueError, match="table must have shape"):
+            s24.attn_decode(c, x[:1], bad, cu[:1], x[:1], torch.zeros(16, dtype=torch.uint8))
+    with pytest.raises(ValueError, match="buffers"):
+        s24.KVBuffers(x[0, 0, 0], x[0, 0, 0], torch.bfloat16)
+    none = x[:, :, :0]
+    with pytest.raises(ValueError, match="at least one value"):
+        s24.attn_fwd(none, none, none, none, None, None, cu)
