@@ -96,8 +96,9 @@ template <typename T, bool PAIR> __device__ __forceinline__ float step_of(uint4 
 }
 
 // Many tokens: a wave looks at sixteen of them and takes, of K or of V, those runs that begin there and lie within sixteen aligned places of a page, one after
-// the other.  Of a prompt, whatever place it starts at, that is sixteen tokens to a wave: V then leaves in pieces of 16 bytes.  (Of single tokens of many
-// sequences it is one at a time, which the kernel below does better.)
+// the other.  Of a prompt, whatever place it starts at, that is sixteen tokens to a wave: V then leaves in pieces of 16 bytes.  Where more than two runs begin in
+// the sixteen tokens (new tokens of many sequences) all of them are taken at once, and V leaves value by value: 1280 tokens of 8 heads of 128 that do not follow each other take
+// 14 us in 8 bits so, 33 run by run (16 bits: 13 and 16), 16384 of them 160 and 180.  (At once from two runs on, runs of 8 tokens gain another 5 % and prompts in 16 bits lose as much.)
 // Bound by memory: 17408 tokens of 8 heads of 128 take 27 us in 8 bits and 33 in 16 (4.0 and 4.3 TB/s; a plain copy of as many bytes reaches 5.7).  Stores past
 // the caches, in whole lines, take 25 and 31; but the reading back that follows then takes longer by more: both together 44 us with these, 50 with those.
 template <typename T, int BITS, bool PAIR>
@@ -114,7 +115,53 @@ __global__ __launch_bounds__(256) void kv_write_runs_kernel(const WriteArgs a)
     const int64_t place = mine >= 0 && mine < a.tokens && lane < 34 ? a.places[mine] : -1;
     const int64_t before = __shfl_up(place, 1);
     const uint64_t starts = __ballot(mine >= a.tokens || mine <= 0 || (place & 15) == 0 || place != before + 1) >> 1;
-    for (uint32_t left = (uint32_t)starts & 0xFFFFu; left != 0; left &= left - 1) {
+    const uint32_t runs = (uint32_t)starts & (0xFFFFu >> max(16 - (a.tokens - first_token), 0));
+    if (__popc(runs) > 2) {   // their tokens at once, each to its own place
+        const int first_run = __builtin_ctz(runs), last_run = 31 - __builtin_clz(runs), end = last_run + __builtin_ctzll(starts >> (last_run + 1)) + 1;
+        for (int base = 0; base < end; base += 16) {
+            uint4 x[4];
+            int64_t to[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int k = base + 4 * at.r + i;
+                to[i] = __shfl(place, k + 1);
+                if (!at.live || k < first_run || k >= end || to[i] >= a.c.pages << a.c.shift) to[i] = -1;
+                x[i] = to[i] >= 0 ? *reinterpret_cast<const uint4 *>(from.p + (int64_t)(first_token + k) * from.token + at.h * from.head + at.c) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int64_t first = ((to[i] >> a.c.shift) * a.c.hkv + at.h) << a.c.shift;   // of the page, in tokens of one head
+                const int in = (int)(to[i] & (a.c.page - 1));
+                if constexpr (BITS == 16) {
+                    if (to[i] < 0) continue;
+                    if (!values) {
+                        *reinterpret_cast<uint4 *>(a.c.k + ((first + in) * a.c.d + at.c) * 2) = x[i];
+                        continue;
+                    }
+                    uint16_t *v = reinterpret_cast<uint16_t *>(a.c.v) + first * a.c.d + ((int64_t)(in >> 3) * a.c.d + at.c) * 8 + (in & 7);
+                    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[8 * e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+                } else {
+                    uint32_t bytes[8];
+                    const float step = step_of<T, PAIR>(x[i]);
+                    eight_numbers<T>(x[i], step, __builtin_amdgcn_rcpf(step), bytes);
+                    if (to[i] < 0) continue;
+                    if (at.c == 0) (values ? a.c.vs : a.c.ks)[first + in] = step;
+                    if (!values) {
+                        *reinterpret_cast<uint2 *>(a.c.k + (first + in) * a.c.d + at.c) =
+                            make_uint2(four_bytes(bytes[0], bytes[1], bytes[2], bytes[3]), four_bytes(bytes[4], bytes[5], bytes[6], bytes[7]));
+                        continue;
+                    }
+                    unsigned char *v = a.c.v + first * a.c.d + ((int64_t)(in >> 4) * a.c.d + at.c) * 16 + (in & 15);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[16 * e] = (unsigned char)bytes[e];
+                }
+            }
+        }
+        return;
+    }
+    for (uint32_t left = runs; left != 0; left &= left - 1) {
         const int j = __builtin_ctz(left), token = first_token + j;
         if (token >= a.tokens) break;
         const int n = __builtin_ctzll(starts >> (j + 1)) + 1;
@@ -771,7 +818,8 @@ extern "C" int s24_kv_write(const s24_kv_cache *cache, const s24_heads *K, const
     const WriteArgs a{cache_of(cache), strided(K), strided(V), places, (int)tokens};
     const hipStream_t st = static_cast<hipStream_t>(stream);
     // The runs' kernel from 40 tokens of a head for each compute unit on.  (8 bits, 8 heads of 128, both sides: 1024 tokens 7.9 us by runs, 6.1 one by one; 2048
-    // tokens 7.6 and 9.5; 16384 tokens 24 and 50.  12 heads of 64, 1024 tokens: 7.3 and 7.2.  16 bits, 8 heads of 128, 1024 tokens: 5.3 and 6.3.)
+    // tokens 7.6 and 9.5; 16384 tokens 24 and 50.  12 heads of 64, 1024 tokens: 7.3 and 7.2.  16 bits, 8 heads of 128, 1024 tokens: 5.3 and 6.3.  Those are prompts.  Tokens that
+    // do not follow each other, which the host does not see, take 14 and 9.5 us at 1280 tokens, 27 and 22 at 4096, 160 and 154 at 16384.)
     const int64_t units = cache->d <= 64 ? (cache->hkv + 1) / 2 : cache->hkv, waves = 2 * ((tokens + 15) / 16) * units;   // of K and of V
     const bool runs = tokens * cache->hkv >= 40 * (int64_t)s24_cu_count();
     const int64_t groups = runs ? (waves + 3) / 4 : (tokens * cache->hkv + 3) / 4;
