@@ -823,7 +823,7 @@ extern "C" int s24_kv_write(const s24_kv_cache *cache, const s24_heads *K, const
     const int64_t units = cache->d <= 64 ? (cache->hkv + 1) / 2 : cache->hkv, waves = 2 * ((tokens + 15) / 16) * units;   // of K and of V
     const bool runs = tokens * cache->hkv >= 40 * (int64_t)s24_cu_count();
     const int64_t groups = runs ? (waves + 3) / 4 : (tokens * cache->hkv + 3) / 4;
-    S24_REQUIRE(groups <= kMostGroups, S24_ERR_SHAPE);
+    S24_REQUIRE((runs ? waves + 3 : groups) <= kMostGroups, S24_ERR_SHAPE);   // (the runs' kernel numbers its waves in an int)
     const dim3 grid((unsigned)groups);
     if (cache->bits == 16) write<uint16_t, 16>(a, runs, grid, st);   // a copy, whatever the type
     else if (dt == S24_BF16) write<uint16_t, 8>(a, runs, grid, st);

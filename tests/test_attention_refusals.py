@@ -45,3 +45,11 @@ def test_tensors_without_the_axes_of_an_operand_are_refused():
     none = x[:, :, :0]
     with pytest.raises(ValueError, match="at least one value"):
         s24.attn_fwd(none, none, none, none, None, None, cu)
+
+
+def test_more_waves_than_a_launch_numbers_are_refused():
+    """Windows of sixteen tokens of 65535 heads: their waves are numbered in 31 bits, whatever a launch would take."""
+    from test_attention_host import BF16, OK, P, cache, rows
+    write = lambda tokens: s24.lib().s24_kv_write(cache(hkv=65535, d=128), rows(65535, token=1 << 22, head=0), rows(65535, token=1 << 22, head=0), P, tokens, BF16, None)
+    assert write(16 * (1 << 14) + 1) == SHAPE and write(1 << 19) == SHAPE
+    assert write(0) == OK
