@@ -20,7 +20,6 @@ typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef short v4i16 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
-typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
 
 // 16 x 16 x 32: lane l holds row (A) or column (B) l%16, its elements 8*(l/16) .. + 7 of the contraction; accumulator i is row
 // 4*(l/16) + i of column l%16.
