@@ -334,7 +334,9 @@ int s24_l1_norm_gap(const void *W, s24_dtype dt, int64_t r, int64_t q, int64_t l
  * S24_BF16 and S24_F16; S24_F32 returns S24_ERR_UNSUPPORTED.  Scores, row statistics and sums are fp32; the weights P are rounded to the storage
  * type as operands of the second products, dS of the backward pass goes into them as two parts (its rounded value and the rounded rest), in binary16 both times a power
  * of two that follows its size: dO may be of any size whose gradients the type holds.
- * The scores' size must stay below 2^23, up to which fp32 still holds their fractions' halves; NaN among what a query sees gives NaN.
+ * The scores' size must stay below 2^23, up to which fp32 still holds their fractions' halves; NaN among what a query sees gives NaN.  (A key that the causal mask hides has
+ * the weight 0, and 0 times NaN or infinity is NaN: such a value of V, in the backward pass also of Q, K and dO, may reach rows of its own sequence in its tile that do
+ * not see it, as it would in a product of the whole matrices.  It reaches no other sequence.)
  * Nothing is added in an order that depends on scheduling. */
 
 /* Rows of heads: element (t, h, i) of token t, head h at data + t*token + h*head + i (strides in elements), so that the parts of one

@@ -33,11 +33,11 @@ def _workspace(n, beside):
         return None
     stream, held = s24._stream(), _buffers.held
     if stream != 0 and torch.cuda.is_current_stream_capturing():   # (the default stream cannot be captured)
-        return torch.empty(n, dtype=torch.uint8, device=beside.device)
+        return s24.Workspace(n, beside.device)
     key = (beside.get_device(), stream)
     work = held.get(key)
-    if work is None or work.numel() < n:
-        work = held[key] = torch.empty(n, dtype=torch.uint8, device=beside.device)
+    if work is None or work.bytes < n:
+        work = held[key] = s24.Workspace(n, beside.device)
     return work
 
 

@@ -521,6 +521,30 @@ def _whole(where, name, x, dtype, shape, device):
     return x.data_ptr()
 
 
+class Workspace:
+    """Bytes on the GPU for calls to use as their workspace, looked at once for all of them."""
+    __slots__ = ("buffer", "address", "bytes")
+
+    def __init__(self, n, device):
+        self.buffer = torch.empty(n, dtype=torch.uint8, device=device)
+        self.address, self.bytes = self.buffer.data_ptr(), n
+
+    def data_ptr(self):
+        return self.address
+
+    def numel(self):
+        return self.bytes
+
+
+def _work(where, workspace, device):
+    """Address and bytes of a workspace: a Workspace, a uint8 tensor or None."""
+    if type(workspace) is Workspace:
+        return workspace.address, workspace.bytes
+    if workspace is None:
+        return None, 0
+    return _whole(where, "workspace", workspace, torch.uint8, workspace.shape, device), workspace.numel()
+
+
 def _attn_operands(where, Q, K, cu_q, cu_k, causal, scale, rest):
     """(shapes of the rows of queries and of keys, dtype, device, packed s24_attn_shape)"""
     sq, sk = Q.shape, K.shape
@@ -543,15 +567,14 @@ def _attn_operands(where, Q, K, cu_q, cu_k, causal, scale, rest):
 def attn_fwd(Q, K, V, O, lse, workspace, cu_q, cu_k=None, causal=True, scale=None, rest=None):
     """Attention over packed sequences.  Q, O [tokens_q, hq, d], K, V [tokens_k, hkv, d], with any strides along the first two axes; lse [hq, tokens_q]
     float32 or None; cu_q, cu_k: int32 offsets of the sequences (cu_k None: those of the queries); scale None: 1 / sqrt(d);
-    workspace: a uint8 tensor of attn_fwd_workspace(...) bytes, None where that is 0; rest: None, or an int8 tensor like O without gaps (or the
+    workspace: a Workspace or a uint8 tensor of attn_fwd_workspace(...) bytes, None where that is 0; rest: None, or an int8 tensor like O without gaps (or the
     address of one that has been checked), which receives what the rounding of O takes away."""
     where = "s24_attn_fwd"
     sq, sk, dtype, device, shape = _attn_operands(where, Q, K, cu_q, cu_k, causal, scale, rest)
     args = (shape, _heads(where, "Q", Q, sq, dtype, device), _heads(where, "K", K, sk, dtype, device), _heads(where, "V", V, sk, dtype, device),
             _heads(where, "O", O, sq, dtype, device),
             None if lse is None else _whole(where, "lse", lse, torch.float32, (sq[1], sq[0]), device),
-            *((None, 0) if workspace is None else (_whole(where, "workspace", workspace, torch.uint8, workspace.shape, device), workspace.numel())),
-            _dt(Q))
+            *_work(where, workspace, device), _dt(Q))
     if device < 0:
         raise ValueError(f"{where}: the tensors must lie on a GPU")
     status = lib().s24_attn_fwd(*args, _stream())
@@ -571,14 +594,14 @@ def attn_bwd_workspace(tokens_q, tokens_k, hq, hkv, d, sequences):
 
 
 def attn_bwd(Q, K, V, O, dO, lse, dQ, dK, dV, workspace, cu_q, cu_k=None, causal=True, scale=None, rest=None):
-    """Gradients dQ, dK, dV of attn_fwd, from its O and lse, and its rest if it had one; workspace: a uint8 tensor of attn_bwd_workspace(...) bytes."""
+    """Gradients dQ, dK, dV of attn_fwd, from its O and lse, and its rest if it had one; workspace: a Workspace or a uint8 tensor of attn_bwd_workspace(...) bytes."""
     where = "s24_attn_bwd"
     sq, sk, dtype, device, shape = _attn_operands(where, Q, K, cu_q, cu_k, causal, scale, rest)
     args = (shape, _heads(where, "Q", Q, sq, dtype, device), _heads(where, "K", K, sk, dtype, device), _heads(where, "V", V, sk, dtype, device),
             _heads(where, "O", O, sq, dtype, device), _heads(where, "dO", dO, sq, dtype, device),
             _whole(where, "lse", lse, torch.float32, (sq[1], sq[0]), device), _heads(where, "dQ", dQ, sq, dtype, device),
             _heads(where, "dK", dK, sk, dtype, device), _heads(where, "dV", dV, sk, dtype, device),
-            _whole(where, "workspace", workspace, torch.uint8, workspace.shape, device), workspace.numel(), _dt(Q))
+            *_work(where, workspace, device), _dt(Q))
     if device < 0:
         raise ValueError(f"{where}: the tensors must lie on a GPU")
     status = lib().s24_attn_bwd(*args, _stream())
@@ -643,7 +666,7 @@ def attn_decode_workspace(cache, sequences, hq):
 
 
 def attn_decode(cache, Q, table, lengths, O, workspace, scale=None):
-    """O[i] = softmax(scale Q[i].K) V over the first lengths[i] (int32) positions of sequence i.  Q, O [sequences, hq, d]; workspace: a uint8 tensor of
+    """O[i] = softmax(scale Q[i].K) V over the first lengths[i] (int32) positions of sequence i.  Q, O [sequences, hq, d]; workspace: a Workspace or a uint8 tensor of
     attn_decode_workspace(...) bytes."""
     where, device = "s24_attn_decode", cache.device
     n = _axes(where, "table", table, ("sequences", "pages"))
@@ -651,8 +674,7 @@ def attn_decode(cache, Q, table, lengths, O, workspace, scale=None):
     shape = (sequences, hq, cache.d)
     args = (cache.packed, _heads(where, "Q", Q, shape, cache.dtype, device), hq, _whole(where, "table", table, torch.int32, (sequences, n[1]), device),
             n[1], _whole(where, "lengths", lengths, torch.int32, (sequences,), device), sequences, d ** -0.5 if scale is None else scale,
-            _heads(where, "O", O, shape, cache.dtype, device), _whole(where, "workspace", workspace, torch.uint8, workspace.shape, device),
-            workspace.numel(), _dt(Q))
+            _heads(where, "O", O, shape, cache.dtype, device), *_work(where, workspace, device), _dt(Q))
     if device < 0:
         raise ValueError(f"{where}: the tensors must lie on a GPU")
     status = lib().s24_attn_decode(*args, _stream())
