@@ -9,8 +9,8 @@
 // Sums run over queries for dK and dV and over keys for dQ: two parts, each of which forms S and dO V^T for itself (7 products instead of 5, and two more
 // for the second halves of dS).  One kernel would have to add to dQ from many workgroups, in an order that no two runs share.
 // What bounds it: the matrix instructions and the vector instructions on the scores, which a compute unit runs at the same time only in part.  (Two waves of nothing
-// but 16x16x32 instructions take 8.1 ns for each on a SIMD; with four fma to each 12.2.)  8192 tokens, 64 heads on 8 of 128: 970 us for O (1.13 PFLOP/s, of the
-// 1.18 that a library's plain product of 8192 x 8192 x 8192 reaches), matrix cores 53 % busy; 1730 us for dQ, 59 %; 2350 us for dK and dV, 52 %.
+// but 16x16x32 instructions take 8.1 ns for each on a SIMD; with four fma to each 12.2.)  8192 tokens, 64 heads on 8 of 128: 1.00 ms for O (1.10 PFLOP/s; a library's plain
+// products of 8192 x 8192 x 8192 reach 1.37 to 1.58), matrix cores 53 % busy; 1.81 ms for dQ, 57 %; 2.39 ms for dK and dV, 55 %.
 #include "s24_attn.h"
 
 #include <math.h>
@@ -126,8 +126,8 @@ template <int D> struct Forward {
 // the same relative precision, and the sums stay far inside fp32.
 constexpr float kGrowth = 8.0f;
 
-// D: values of a tile's row; E: values that the products go over.  (Heads of 96 in tiles of 128 by products of 128: 8192 tokens of 16 heads on 4, 152 us forward and 607
-// backward; of 96 127 and 505.  Heads of 80 take 133 and 505 so.)
+// D: values of a tile's row; E: values that the products go over.  (Heads of 96 in tiles of 128 by products of 128: two sequences of 4096 tokens, 16 heads on 4, 139 us forward
+// and 565 backward; of 96 120 and 477.  Heads of 80 137 and 554, and 118 and 471.  One sequence of 8192, heads of 96: 257 and 1065, and 217 and 896.)
 template <typename T, int D, int E>
 __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
 {
