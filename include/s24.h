@@ -410,6 +410,56 @@ int64_t s24_attn_decode_workspace(const s24_kv_cache *cache, int64_t sequences, 
 int s24_attn_decode(const s24_kv_cache *cache, const s24_heads *Q, int64_t hq, const int32_t *table, int64_t width, const int32_t *lengths,
                     int64_t sequences, float scale, const s24_heads *O, void *workspace, int64_t workspace_bytes, s24_dtype dt, void *stream);
 
+/* Attention of new tokens over the cache, which has them already: the tokens cu[i] .. cu[i+1] - 1 (device, as cu_q above) of Q and O are the last ones of sequence i's first
+ * lengths[i] (device) positions, their own included.  Query t of lq sees the positions j <= t + lengths[i] - lq, or all of them where not `causal`; zeros for a query that sees none.
+ * Any number of new tokens of each sequence, one too (s24_attn_decode is the faster call where all have one).  Lengths beyond width*page are cut; width*page up to 2^30, and
+ * times hq / hkv below 2^36 (S24_ERR_SHAPE).  Precision, and what NaN does, are those of s24_attn_fwd and in an 8-bit cache those of s24_attn_decode.
+ *   workspace  device, s24_attn_chunk_workspace(cache, width, tokens, sequences, hq) bytes (0 for many tokens: then NULL will do), 16-byte aligned; holds nothing between calls */
+int64_t s24_attn_chunk_workspace(const s24_kv_cache *cache, int64_t width, int64_t tokens, int64_t sequences, int64_t hq);
+int s24_attn_chunk(const s24_kv_cache *cache, const s24_heads *Q, int64_t hq, const int32_t *cu, const int32_t *table, int64_t width, const int32_t *lengths,
+                   int64_t sequences, int64_t tokens, float scale, int causal, const s24_heads *O, void *workspace, int64_t workspace_bytes, s24_dtype dt, void *stream);
+
+/* ---- Norms of queries and keys for each head, and the rotation of their positions ----
+ *
+ * A head x of d values becomes z:  y_i = x_i w_i / sqrt(mean(x^2) + eps), or y = x where it is not normalised;  the pair (y_a, y_b) number p is turned by the angle
+ * position * frequencies[p] (in radians):  z_a = y_a cos - y_b sin,  z_b = y_b cos + y_a sin;  what lies past the first `rotated` values is not turned.  Pair p is (p, p + rotated / 2),
+ * or (2p, 2p + 1) where `interleaved`.  A token has `axes` positions, of which pair p turns by number axis[p] (of an image or a video: time, height and width).
+ * All arithmetic is fp32 and rounded once; a turn is reduced exactly, so that angles of far positions are as good as those of near ones.  x^2 has to stay within
+ * fp32; eps = 0 gives NaN for a head of zeros.  S24_BF16 and S24_F16; S24_F32 returns S24_ERR_UNSUPPORTED.
+ *   frequencies  device fp64 [rotated / 2]
+ *   axis         device int32 [rotated / 2] of 0 .. axes - 1 (others are cut to the last), or NULL: all turn by the first
+ *   wq, wk       device [d] values of the calls' dtype, 16-byte aligned: weights of the queries' and of the keys' norm; NULL: not normalised
+ *   rotated      a multiple of 16 up to d; 0: nothing is turned (frequencies and positions may be NULL)
+ *   positions    (of each call) device int32 [axes][tokens]
+ * d is a multiple of 16 up to 128 (beyond: S24_ERR_UNSUPPORTED).  hq or hkv may be 0: then those operands are not looked at. */
+typedef struct {
+    const double *frequencies;
+    const int32_t *axis;
+    const void *wq, *wk;
+    int64_t axes, rotated;
+    float eps;
+    int interleaved;
+} s24_rotary;
+
+/* Qo, Ko = z of Q [tokens][hq][d] and K [tokens][hkv][d].  Qo may be Q itself and Ko be K (the same address and strides); other overlaps are not allowed. */
+int s24_rotary_fwd(const s24_rotary *rotary, const int32_t *positions, const s24_heads *Q, const s24_heads *K, const s24_heads *Qo, const s24_heads *Ko, int64_t tokens,
+                   int64_t hq, int64_t hkv, int64_t d, s24_dtype dt, void *stream);
+
+/* Gradients of s24_rotary_fwd from those of its results: with g = dz turned back, r = 1 / sqrt(mean(x^2) + eps) and y = x r,
+ * dx_i = r (g_i w_i - y_i mean_j(g_j w_j y_j)), or g;  dw_i = beta dw_i + sum of g_i y_i over tokens and heads, in fp32 and in a fixed order; beta is 0 or 1.
+ * dQ may be dQo itself and dK be dKo.  Q and K (those of the forward pass, before it) are read where they are normalised, and may be NULL otherwise, as dwq and dwk may.
+ *   workspace  device, s24_rotary_bwd_workspace(...) bytes (0 without norms), 16-byte aligned; holds nothing between calls */
+int64_t s24_rotary_bwd_workspace(const s24_rotary *rotary, int64_t tokens, int64_t hq, int64_t hkv, int64_t d);
+int s24_rotary_bwd(const s24_rotary *rotary, const int32_t *positions, const s24_heads *dQo, const s24_heads *dKo, const s24_heads *Q, const s24_heads *K,
+                   const s24_heads *dQ, const s24_heads *dK, float *dwq, float *dwk, float beta, int64_t tokens, int64_t hq, int64_t hkv, int64_t d, void *workspace,
+                   int64_t workspace_bytes, s24_dtype dt, void *stream);
+
+/* Appends tokens to the cache, normalised and turned on the way: Qo = z of Q as s24_rotary_fwd gives it (for all tokens, skipped ones too; Qo may be Q), z of K and V itself to the
+ * places as s24_kv_write has it.  In 16 bits K is what s24_rotary_fwd gives; in 8 bits z is quantised from fp32 without a rounding in between: step and whole numbers are those of
+ * z up to its fp32 error.  hq may be 0. */
+int s24_kv_append(const s24_kv_cache *cache, const s24_rotary *rotary, const int32_t *positions, const s24_heads *Q, int64_t hq, const s24_heads *K, const s24_heads *V,
+                  const s24_heads *Qo, const int64_t *places, int64_t tokens, s24_dtype dt, void *stream);
+
 /* Instrumentation, not part of the method: registers a DEVICE buffer of two uint64 (8-byte aligned), or
  * NULL to switch the probe off (the default).  While a buffer is registered, workgroup 0 of every
  * large-tile 16-bit GEMM launched by s24_spmm_fwd / s24_spmm_bwd_dx / s24_dense_dw / s24_dense_gemm

@@ -2,8 +2,8 @@
 
 Only call ordering and buffer ownership live here; every arithmetic step is a libs24 kernel.  In training, Attention owns what one layer keeps
 between its passes.  In sampling, PagedKV holds the keys and values of the sequences that are being sampled, in 16 or 8 bits: the tokens of a
-prompt are written to it as they come, each new token attends over it, and whole sequences are read back where the next chunk of a
-prompt attends to the earlier ones.
+prompt are written to it as they come, each new token attends over it, and so do the tokens of a prompt's next chunk (or whole sequences are read back).
+Rotary stands between the projection and either: norms of queries and keys for each head, and the rotation of their positions.
 """
 from __future__ import annotations
 
@@ -96,6 +96,46 @@ class Attention:
         return s24.attn_bwd(Q, K, V, O, dO, self.lse, dQ, dK, dV, work, cu_q, cu_k, self.causal, self.scale, self._rest)
 
 
+class Rotary:
+    """Norms of queries and keys for each head and the rotation of their positions, for up to `tokens` tokens: hq query heads and hkv key-value heads of d values.
+    frequencies [rotated / 2] float64, on the GPU: radians for each step of the position (rotary_frequencies gives the usual ones; None: nothing is turned).  wq, wk [d]: weights of
+    the norms, in `dtype` (None: not normalised).  A token has one position, or one on each of several `axes` (time, height, width): axis [rotated / 2] int32 says which a pair turns
+    by.  Pairs are (p, p + rotated / 2), or (2p, 2p + 1) where `interleaved`.  dwq, dwk [d] float32: gradients of the weights, of the last backward pass."""
+
+    def __init__(self, hq: int, hkv: int, d: int, tokens: int, frequencies=None, wq=None, wk=None, eps: float = 1e-6, axis=None, axes: int = 1, interleaved: bool = False,
+                 dtype=torch.bfloat16, device="cuda"):
+        self.hq, self.hkv, self.d, self.tokens, self.dtype = hq, hkv, d, tokens, dtype
+        self.plan = s24.RotaryPlan(d, dtype, frequencies, wq, wk, eps, axis, axes, interleaved)
+        self.Q, self.K = (torch.empty((tokens, h, d), dtype=dtype, device=device) for h in (hq, hkv))
+        self.dwq, self.dwk = (None if w is None else torch.zeros(d, dtype=torch.float32, device=device) for w in (wq, wk))
+        self.need = {}   # bytes of workspace that a backward pass over so many tokens takes
+
+    def _own(self, Q, K):
+        n = Q.shape[0]
+        return (self.Q, self.K) if n == self.tokens else (self.Q[:n], self.K[:n])
+
+    def forward(self, Q, K, positions, out=None):
+        """Q and K [tokens, heads, d], normalised and turned: in the layer's own buffers, or in out = (Q, K), which may be the operands where no backward pass needs them (without
+        norms it needs none).  positions: int32 [axes, tokens], or [tokens] of one axis."""
+        return s24.rotary_fwd(self.plan, Q, K, positions, *(self._own(Q, K) if out is None else out))
+
+    def backward(self, dQ, dK, Q, K, positions, out=None, beta=0.0):
+        """Gradients of forward's operands, whose values Q and K are given again (None, None without norms): in place of dQ and dK, or in out = (dQ, dK).  Those of the weights go to
+        dwq and dwk, added to what they hold where beta is 1."""
+        tokens = s24._axes("Rotary.backward", "dQ", dQ, ("tokens", "heads", "d"))[0]
+        n = self.need.get(tokens)
+        if n is None:
+            if len(self.need) >= 1024:   # (batches of ever new sizes)
+                self.need.clear()
+            n = self.need[tokens] = s24.rotary_bwd_workspace(self.plan, tokens, self.hq, self.hkv)
+        return s24.rotary_bwd(self.plan, dQ, dK, Q, K, positions, *((dQ, dK) if out is None else out), self.dwq, self.dwk, beta, _workspace(n, dQ))
+
+
+def rotary_frequencies(rotated: int, base: float = 10000.0, device="cuda"):
+    """base^(-2p / rotated) for the pairs p of `rotated` values, in 64 bits."""
+    return base ** (torch.arange(rotated // 2, dtype=torch.float64, device=device) * (-2.0 / rotated))
+
+
 class PagedKV:
     """Keys and values of many sequences in pages of `page` tokens, in 16 bits (the values as they are) or 8 (whole numbers and a step for each token
     and head).  Which page belongs to whom is the caller's: a table [sequences, pages of the longest] of page numbers."""
@@ -114,6 +154,13 @@ class PagedKV:
         """Rows of K and V [tokens, hkv, d] to their places: page number * page + position in the page (int64; negative ones are skipped)."""
         s24.kv_write(self.buffers, K, V, places)
 
+    def append(self, rotary, Q, K, V, positions, places, out=None):
+        """What stands before the attention of new tokens, in one pass: Q [tokens, hq, d] normalised and turned as `rotary` (Rotary) has it, into its own buffer or into `out` (which
+        may be Q); K likewise and V as it is to their places."""
+        if out is None:
+            out = rotary._own(Q, K)[0]
+        return s24.kv_append(self.buffers, rotary.plan, Q, K, V, positions, places, out)
+
     def read(self, table, cu, K, V):
         """The sequences, one after the other from the offsets cu on, into K and V [tokens, hkv, d]: as Attention.forward takes them."""
         return s24.kv_read(self.buffers, table, cu, K, V)
@@ -124,3 +171,15 @@ class PagedKV:
         if n is None:
             n = self.need[Q.shape] = s24.attn_decode_workspace(self.buffers, Q.shape[0], Q.shape[1])
         return s24.attn_decode(self.buffers, Q, table, lengths, O, _workspace(n, self.K), scale)
+
+    def attend_chunk(self, Q, cu, table, lengths, O, scale=None, causal=True):
+        """O [tokens, hq, d]: attention of new tokens that the cache has already.  Those of sequence i are the rows cu[i] .. cu[i+1] - 1 of Q, the last ones of its first lengths[i]
+        positions, and see the positions up to their own (all of them where not `causal`)."""
+        where = "PagedKV.attend_chunk"
+        key = s24._axes(where, "Q", Q, ("tokens", "heads", "d")), s24._axes(where, "table", table, ("sequences", "pages"))
+        n = self.need.get(key)
+        if n is None:
+            if len(self.need) >= 1024:   # (batches of ever new sizes)
+                self.need.clear()
+            n = self.need[key] = s24.attn_chunk_workspace(self.buffers, table.shape[1], Q.shape[0], table.shape[0], Q.shape[1])
+        return s24.attn_chunk(self.buffers, Q, cu, table, lengths, O, _workspace(n, self.K), scale, causal)

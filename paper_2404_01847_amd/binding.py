@@ -68,6 +68,12 @@ _SIGNATURES = {
     "s24_kv_read": (_int, [_vp, _vp, _i64, _vp, _i64, _i64, _vp, _vp, _int, _vp]),
     "s24_attn_decode_workspace": (_i64, [_vp, _i64, _i64]),
     "s24_attn_decode": (_int, [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _f32, _vp, _vp, _i64, _int, _vp]),
+    "s24_attn_chunk_workspace": (_i64, [_vp, _i64, _i64, _i64, _i64]),
+    "s24_attn_chunk": (_int, [_vp, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _i64, _f32, _int, _vp, _vp, _i64, _int, _vp]),
+    "s24_rotary_fwd": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _i64, _int, _vp]),
+    "s24_rotary_bwd_workspace": (_i64, [_vp, _i64, _i64, _i64, _i64]),
+    "s24_rotary_bwd": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _f32, _i64, _i64, _i64, _i64, _vp, _i64, _int, _vp]),
+    "s24_kv_append": (_int, [_vp, _vp, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _int, _vp]),
 }
 EXPORTS = tuple(_SIGNATURES)
 
@@ -482,7 +488,11 @@ class _KVCache(C.Structure):
     _fields_ = [("K", _vp), ("V", _vp), ("k_step", _vp), ("v_step", _vp), ("pages", _i64), ("page", _i64), ("hkv", _i64), ("d", _i64), ("bits", _int)]
 
 
-_pack_heads, _pack_shape, _pack_cache = _packer(_Heads), _packer(_AttnShape), _packer(_KVCache)
+class _Rotary(C.Structure):
+    _fields_ = [("frequencies", _vp), ("axis", _vp), ("wq", _vp), ("wk", _vp), ("axes", _i64), ("rotated", _i64), ("eps", _f32), ("interleaved", _int)]
+
+
+_pack_heads, _pack_shape, _pack_cache, _pack_rotary = _packer(_Heads), _packer(_AttnShape), _packer(_KVCache), _packer(_Rotary)
 
 
 def _refused(where, name, x, dtype, shape, device):
@@ -681,6 +691,119 @@ def attn_decode(cache, Q, table, lengths, O, workspace, scale=None):
     if status != 0:
         raise S24Error(status, where)
     return O
+
+
+def attn_chunk_workspace(cache, width, tokens, sequences, hq):
+    """Bytes of workspace that attn_chunk needs for a table of `width` pages a sequence, so many new tokens, sequences and query heads."""
+    return lib().s24_attn_chunk_workspace(cache.packed, width, tokens, sequences, hq)
+
+
+def attn_chunk(cache, Q, cu, table, lengths, O, workspace, scale=None, causal=True):
+    """Attention of the tokens cu[i] .. cu[i+1] - 1 (int32) of Q and O [tokens, hq, d], which are the last ones of the first lengths[i] (int32) positions of sequence i in the
+    cache; workspace: a Workspace or a uint8 tensor of attn_chunk_workspace(...) bytes, None where that is 0."""
+    where, device = "s24_attn_chunk", cache.device
+    n = _axes(where, "table", table, ("sequences", "pages"))
+    tokens, hq, d = _axes(where, "Q", Q, ("tokens", "heads", "d"))
+    shape = (tokens, hq, cache.d)
+    args = (cache.packed, _heads(where, "Q", Q, shape, cache.dtype, device), hq, _whole(where, "cu", cu, torch.int32, (n[0] + 1,), device),
+            _whole(where, "table", table, torch.int32, n, device), n[1], _whole(where, "lengths", lengths, torch.int32, (n[0],), device), n[0], tokens,
+            cache.d ** -0.5 if scale is None else scale, bool(causal), _heads(where, "O", O, shape, cache.dtype, device), *_work(where, workspace, device), _dt(Q))
+    if device < 0:
+        raise ValueError(f"{where}: the tensors must lie on a GPU")
+    status = lib().s24_attn_chunk(*args, _stream())
+    if status != 0:
+        raise S24Error(status, where)
+    return O
+
+
+class RotaryPlan:
+    """How heads are normalised and turned, checked and packed once for all calls.  frequencies [rotated / 2] float64: radians for each step of the position (None: nothing is
+    turned); wq, wk [d]: weights of the norms, of the calls' dtype (None: not normalised); axis [rotated / 2] int32: which of the `axes` positions of a token a pair turns by."""
+
+    def __init__(self, d, dtype, frequencies=None, wq=None, wk=None, eps=1e-6, axis=None, axes=1, interleaved=False):
+        where = "RotaryPlan"
+        if dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError(f"{where}: heads of bfloat16 or float16, not {dtype}")
+        given = [x for x in (frequencies, wq, wk, axis) if x is not None]
+        device = given[0].get_device() if given else None   # (None: any)
+        pairs = 0 if frequencies is None else _axes(where, "frequencies", frequencies, ("pairs",))[0]
+        address = lambda name, x, kind, n: 0 if x is None else _whole(where, name, x, kind, (n,), device)
+        self.packed = _pack_rotary(address("frequencies", frequencies, torch.float64, pairs), address("axis", axis, torch.int32, pairs), address("wq", wq, dtype, d),
+                                   address("wk", wk, dtype, d), axes, 2 * pairs, eps, bool(interleaved))
+        self.held, self.d, self.dtype, self.device, self.axes, self.pairs = given, d, dtype, device, axes, pairs
+        self.norms = wq is not None, wk is not None
+        _check(lib().s24_rotary_fwd(self.packed, None, None, None, None, None, 0, 0, 0, d, _DTYPES[dtype], None),   # no heads: the library looks at the plan alone
+               f"{where}: heads of {d}, {2 * pairs} values turned, {axes} axes, eps {eps}")
+
+    def positions(self, where, positions, tokens, device):
+        if self.device is not None and self.device != device:
+            raise ValueError(f"{where}: the plan lies on device {self.device}, not where the tensors do")
+        if positions is None and self.pairs == 0:
+            return 0
+        if positions is None:
+            raise ValueError(f"{where}: heads that are turned need positions")
+        return _whole(where, "positions", positions, torch.int32, (tokens,) if self.axes == 1 and positions.dim() == 1 else (self.axes, tokens), device)
+
+
+def _of_gpu(where, device):
+    if device < 0:
+        raise ValueError(f"{where}: the tensors must lie on a GPU")
+
+
+def rotary_fwd(plan, Q, K, positions, Qo, Ko):
+    """Qo, Ko [tokens, heads, d]: Q and K normalised and turned as the plan (RotaryPlan) has it.  positions: int32 [axes, tokens], or [tokens] of one axis.  Qo may be Q and Ko be K."""
+    where, device = "s24_rotary_fwd", Q.get_device()
+    (tokens, hq, _), (_, hkv, _) = _axes(where, "Q", Q, ("tokens", "heads", "d")), _axes(where, "K", K, ("tokens", "heads", "d"))
+    sq, sk, dtype = (tokens, hq, plan.d), (tokens, hkv, plan.d), plan.dtype
+    args = (plan.packed, plan.positions(where, positions, tokens, device), _heads(where, "Q", Q, sq, dtype, device), _heads(where, "K", K, sk, dtype, device),
+            _heads(where, "Qo", Qo, sq, dtype, device), _heads(where, "Ko", Ko, sk, dtype, device), tokens, hq, hkv, plan.d, _dt(Q))
+    _of_gpu(where, device)
+    status = lib().s24_rotary_fwd(*args, _stream())
+    if status != 0:
+        raise S24Error(status, where)
+    return Qo, Ko
+
+
+def rotary_bwd_workspace(plan, tokens, hq, hkv):
+    """Bytes of workspace that rotary_bwd needs for so many tokens and heads."""
+    return lib().s24_rotary_bwd_workspace(plan.packed, tokens, hq, hkv, plan.d)
+
+
+def rotary_bwd(plan, dQo, dKo, Q, K, positions, dQ, dK, dwq=None, dwk=None, beta=0.0, workspace=None):
+    """Gradients dQ, dK (which may be dQo and dKo) and dw = beta dw + its gradient (float32 [d]) of rotary_fwd.  Q, K: those of the forward pass where they are normalised (else
+    they may be None); workspace: a Workspace or a uint8 tensor of rotary_bwd_workspace(...) bytes, None where that is 0."""
+    where, device = "s24_rotary_bwd", dQo.get_device()
+    (tokens, hq, _), (_, hkv, _) = _axes(where, "dQo", dQo, ("tokens", "heads", "d")), _axes(where, "dKo", dKo, ("tokens", "heads", "d"))
+    sq, sk, dtype = (tokens, hq, plan.d), (tokens, hkv, plan.d), plan.dtype
+    heads = lambda name, x, shape, needed=True: _heads(where, name, x, shape, dtype, device) if needed else None
+    weights = lambda name, x, needed: _whole(where, name, x, torch.float32, (plan.d,), device) if needed else None
+    for (name, x), needed in zip((("Q", Q), ("K", K), ("dwq", dwq), ("dwk", dwk)), plan.norms * 2):
+        if needed and x is None:
+            raise ValueError(f"{where}: {name} is needed where there is a norm")
+    nq, nk = plan.norms
+    args = (plan.packed, plan.positions(where, positions, tokens, device), heads("dQo", dQo, sq), heads("dKo", dKo, sk), heads("Q", Q, sq, nq), heads("K", K, sk, nk),
+            heads("dQ", dQ, sq), heads("dK", dK, sk), weights("dwq", dwq, nq), weights("dwk", dwk, nk), beta, tokens, hq, hkv, plan.d, *_work(where, workspace, device), _dt(dQo))
+    _of_gpu(where, device)
+    status = lib().s24_rotary_bwd(*args, _stream())
+    if status != 0:
+        raise S24Error(status, where)
+    return dQ, dK
+
+
+def kv_append(cache, plan, Q, K, V, positions, places, Qo):
+    """Qo = Q [tokens, hq, d] normalised and turned (it may be Q); K [tokens, hkv, d] likewise and V as it is to the places (int64, as kv_write has them) of the cache."""
+    where, device = "s24_kv_append", cache.device
+    tokens, hq, _ = _axes(where, "Q", Q, ("tokens", "heads", "d"))
+    if plan.d != cache.d or plan.dtype is not cache.dtype:
+        raise ValueError(f"{where}: a plan for heads of {plan.d} in {plan.dtype}, a cache of heads of {cache.d} in {cache.dtype}")
+    sq, sk, dtype = (tokens, hq, cache.d), (tokens, cache.hkv, cache.d), cache.dtype
+    args = (cache.packed, plan.packed, plan.positions(where, positions, tokens, device), _heads(where, "Q", Q, sq, dtype, device), hq, _heads(where, "K", K, sk, dtype, device),
+            _heads(where, "V", V, sk, dtype, device), _heads(where, "Qo", Qo, sq, dtype, device), _whole(where, "places", places, torch.int64, (tokens,), device), tokens, _dt(Q))
+    _of_gpu(where, device)
+    status = lib().s24_kv_append(*args, _stream())
+    if status != 0:
+        raise S24Error(status, where)
+    return Qo
 
 
 def set_clock_probe(buf):

@@ -256,9 +256,80 @@ template <typename Of> __device__ __forceinline__ bool find_by_length(bool mixed
 // share keys and values in its L2.
 __device__ __forceinline__ int head_of(int s, int heads) { return heads % 8 == 0 ? (s & 7) * (heads >> 3) + (s >> 3) : s; }
 
+// For the scheduler: the LDS reads of a product come a step ahead of its matrix instructions, of which there are STEPS times MATRIX, READS for each.  (Left to itself
+// it reads two operands, waits for them, and multiplies: the forward pass of 8192 tokens, 64 heads on 8 of 128, takes 970 us so and 950 with this.  Heads of 64
+// have too few steps for it: 31.5 us with it, 30.7 without, 8 x 1024 tokens of 12 heads.  In the sums of dK and dV it takes the gradients of 9 ragged sequences of 16
+// heads on 4 of 128 from 116 us to 111, in the other products of the backward pass nothing or less.)
+template <int READS, int MATRIX, int STEPS> __device__ __forceinline__ void reads_ahead()
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_sched_group_barrier(0x100, 2 * READS, 0);
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, MATRIX, 0);
+        if (i + 2 < STEPS) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+    }
+#endif
+}
+
+// Which tile, head and part a workgroup has
+struct Unit { int tile, head, part; };
+__device__ __forceinline__ Unit unit_of(unsigned block, int heads, int parts)
+{
+    const int units = heads * parts, tile = block / units, unit = head_of(block - tile * units, units), head = unit / parts;
+    return {tile, head, unit - head * parts};
+}
+// The rows of a workgroup that goes over the keys of a key-value head: the queries of the head's whole group, token by token.  So a tile's rows see almost the same
+// keys, and a sequence of few tokens fills a tile with those of several heads.  (512, 446 and 43 tokens after 4700 to 7400, 64 heads on 8 of 128: 309 us with one
+// head to a tile, 245 so; 8192 tokens of one sequence take the same.)
+struct Queries {
+    Span q, k;
+    int rows, row0, token0, extra, ahead;   // of the sequence; first one of the workgroup, its token, its place among the token's; token i sees the keys up to i + ahead
+    int seen, wave_seen, wave_all;          // keys that some row of the workgroup may see, that one of the wave may see, that all of them see
+    float inverse;
+    __device__ __forceinline__ void init(Span queries, Span keys, int group, bool causal, int tile, int rows_of_tile, int first_of_wave)
+    {
+        q = queries, k = keys;
+        rows = q.count * group, row0 = tile * rows_of_tile, token0 = row0 / group, extra = row0 - token0 * group, ahead = k.count - q.count;
+        inverse = 1.0f / (float)group;
+        const int w0 = row0 + first_of_wave;
+        auto up_to = [&](int row) { return causal ? min(k.count, token0 + place_of(row - row0) + 1 + ahead) : k.count; };
+        seen = up_to(min(row0 + rows_of_tile, rows) - 1);
+        wave_seen = w0 < rows ? up_to(min(w0 + 32, rows) - 1) : 0;
+        wave_all = w0 + 32 > rows ? 0 : up_to(w0);
+        seen = __builtin_amdgcn_readfirstlane(seen), wave_seen = __builtin_amdgcn_readfirstlane(wave_seen), wave_all = __builtin_amdgcn_readfirstlane(wave_all);
+    }
+    // Tokens from the workgroup's first one to that of its row i.  (Half a step of the quotient is far more than the product's rounding: i + extra < 2^17.)
+    __device__ __forceinline__ int place_of(int i) const { return (int)(((float)(i + extra) + 0.5f) * inverse); }
+    // Token (of the packed ones), place in the sequence and head of the workgroup's row i; of its last one for those past the sequence
+    struct Row { int64_t token; int at, head; };
+    __device__ __forceinline__ Row row(int group, int kv, int i) const
+    {
+        const int mine = min(i, rows - 1 - row0), place = place_of(mine);
+        return {q.first + token0 + place, token0 + place, kv * group + mine + extra - place * group};
+    }
+};
+
 // Sum / maximum over the four lanes of a column
 __device__ __forceinline__ float column_sum(float x) { x += __shfl_xor(x, 16); return x + __shfl_xor(x, 32); }
 __device__ __forceinline__ float column_max(float x) { x = fmaxf(x, __shfl_xor(x, 16)); return fmaxf(x, __shfl_xor(x, 32)); }
+
+// Scores whose maximum grew by less than this (as a power of two) keep the reference they have: P then reaches 2^8, which the 16-bit types hold with
+// the same relative precision, and the sums stay far inside fp32.
+constexpr float kGrowth = 8.0f;
+
+// Rows of a join: a workgroup takes a few of a sequence, for one head
+constexpr int kJoinRows = 16;
+struct Joined { int64_t first; int rows, head; };
+__device__ __forceinline__ bool join_rows(const int *cu, int sequences, int tokens, int heads, Joined &j)
+{
+    const int tile = blockIdx.x / heads;
+    int sequence, index, count;
+    if (!find_tile(cu, sequences, tokens, kJoinRows, tile, threadIdx.x & 63, sequence, index, count)) return false;
+    const Span s = span(cu, sequence, tokens);
+    j = {s.first + (int64_t)index * kJoinRows, min(kJoinRows, s.count - index * kJoinRows), (int)(blockIdx.x - tile * heads)};
+    return true;
+}
 
 // ---- host
 inline int check_rows(const s24_heads *v, int64_t tokens, int64_t heads, int64_t d, bool written)
@@ -275,6 +346,25 @@ inline int check_rows(const s24_heads *v, int64_t tokens, int64_t heads, int64_t
 // Workgroups for tiles of `rows` of packed sequences: no more tiles than this, however the tokens are shared out.  A launch takes fewer than 2^31.
 inline int64_t most_tiles(int64_t tokens, int64_t sequences, int rows) { return tokens / rows + (tokens < sequences ? tokens : sequences); }
 constexpr int64_t kMostGroups = 0x7FFFFFFF;
+
+// How the work of a launch is cut up.  A workgroup's steps follow each other, and when causal the last queries (the first keys) take twice the average: few
+// workgroups, or some with many steps, leave most of the device idle.  So what a tile sums over is cut into parts, whose sums go through memory in fp32
+// for another launch to add: as many parts as make the estimate the least.  `groups` workgroups have `steps` steps of `us` microseconds each, of which `busy`
+// are taken on average, and a part's sums take `bytes` bytes: the time is that of the longest, or of all of them on the device, two a compute unit, and 5 us for the
+// second launch and 5 bytes a picosecond for sums that are written and read.  (On operands that are in no cache, in one part and in the best of 2, 4 and 8.
+// Forward: 1 head of 64, 8192 tokens 134 us and 34 in 8; 8 heads of 128 on 2, 40 tokens after 8000: 190 and 41 in 8; 64 on 8, 512 after 3500: 111 and 92
+// in 2; 32 of 128, 1500 tokens 47 and 54 in 2; the estimate takes the better one in 15 of 16 shapes.)
+inline int parts_for(double groups, double steps, double busy, double us, double bytes)
+{
+    int best = 1;
+    double least = 0.0;
+    for (int p = 1; p <= 16; p *= 2) {
+        const double rounds = groups * p * busy / (2.0 * s24_cu_count());
+        const double t = us * steps / p * (rounds > 1.0 ? rounds : 1.0) + (p > 1 ? 5.0 + p * bytes * 2.0 / 5e6 : 0.0);
+        if (p == 1 || t < least) best = p, least = t;
+    }
+    return best;
+}
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 }  // namespace s24_attn

@@ -38,59 +38,6 @@ struct Problem {
     float scale;
 };
 
-// For the scheduler: the LDS reads of a product come a step ahead of its matrix instructions, of which there are STEPS times MATRIX, READS for each.  (Left to itself
-// it reads two operands, waits for them, and multiplies: the forward pass of 8192 tokens, 64 heads on 8 of 128, takes 970 us so and 950 with this.  Heads of 64
-// have too few steps for it: 31.5 us with it, 30.7 without, 8 x 1024 tokens of 12 heads.  In the sums of dK and dV it takes the gradients of 9 ragged sequences of 16
-// heads on 4 of 128 from 116 us to 111, in the other products of the backward pass nothing or less.)
-template <int READS, int MATRIX, int STEPS> __device__ __forceinline__ void reads_ahead()
-{
-#if defined(__HIP_DEVICE_COMPILE__)
-    __builtin_amdgcn_sched_group_barrier(0x100, 2 * READS, 0);
-#pragma unroll
-    for (int i = 0; i < STEPS; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x8, MATRIX, 0);
-        if (i + 2 < STEPS) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
-    }
-#endif
-}
-
-// Which tile, head and part a workgroup has
-struct Unit { int tile, head, part; };
-__device__ __forceinline__ Unit unit_of(unsigned block, int heads, int parts)
-{
-    const int units = heads * parts, tile = block / units, unit = head_of(block - tile * units, units), head = unit / parts;
-    return {tile, head, unit - head * parts};
-}
-// The rows of a workgroup that goes over the keys of a key-value head: the queries of the head's whole group, token by token.  So a tile's rows see almost the same
-// keys, and a sequence of few tokens fills a tile with those of several heads.  (512, 446 and 43 tokens after 4700 to 7400, 64 heads on 8 of 128: 309 us with one
-// head to a tile, 245 so; 8192 tokens of one sequence take the same.)
-struct Queries {
-    Span q, k;
-    int rows, row0, token0, extra, ahead;   // of the sequence; first one of the workgroup, its token, its place among the token's; token i sees the keys up to i + ahead
-    int seen, wave_seen, wave_all;          // keys that some row of the workgroup may see, that one of the wave may see, that all of them see
-    float inverse;
-    __device__ __forceinline__ void init(const Problem &a, int sequence, int tile, int rows_of_tile, int first_of_wave)
-    {
-        q = span(a.cu_q, sequence, a.tokens_q), k = span(a.cu_k, sequence, a.tokens_k);
-        rows = q.count * a.group, row0 = tile * rows_of_tile, token0 = row0 / a.group, extra = row0 - token0 * a.group, ahead = k.count - q.count;
-        inverse = 1.0f / (float)a.group;
-        const int w0 = row0 + first_of_wave;
-        auto up_to = [&](int row) { return a.causal ? min(k.count, token0 + place_of(row - row0) + 1 + ahead) : k.count; };
-        seen = up_to(min(row0 + rows_of_tile, rows) - 1);
-        wave_seen = w0 < rows ? up_to(min(w0 + 32, rows) - 1) : 0;
-        wave_all = w0 + 32 > rows ? 0 : up_to(w0);
-        seen = __builtin_amdgcn_readfirstlane(seen), wave_seen = __builtin_amdgcn_readfirstlane(wave_seen), wave_all = __builtin_amdgcn_readfirstlane(wave_all);
-    }
-    // Tokens from the workgroup's first one to that of its row i.  (Half a step of the quotient is far more than the product's rounding: i + extra < 2^17.)
-    __device__ __forceinline__ int place_of(int i) const { return (int)(((float)(i + extra) + 0.5f) * inverse); }
-    // Token (of the packed ones), place in the sequence and head of the workgroup's row i; of its last one for those past the sequence
-    struct Row { int64_t token; int at, head; };
-    __device__ __forceinline__ Row row(const Problem &a, int kv, int i) const
-    {
-        const int mine = min(i, rows - 1 - row0), place = place_of(mine);
-        return {q.first + token0 + place, token0 + place, kv * a.group + mine + extra - place * a.group};
-    }
-};
 // The workgroup's tile: a sequence, and which of its tiles.  When causal the last ones see the most keys.
 __device__ __forceinline__ bool find_queries(const Problem &a, int rows, int t, int lane, int &sequence, int &tile)
 {
@@ -122,10 +69,6 @@ template <int D> struct Forward {
     static constexpr int BK = 64, TILE = BK * 2 * D;
 };
 
-// Scores whose maximum grew by less than this (as a power of two) keep the reference they have: P then reaches 2^8, which the 16-bit types hold with
-// the same relative precision, and the sums stay far inside fp32.
-constexpr float kGrowth = 8.0f;
-
 // D: values of a tile's row; E: values that the products go over.  (Heads of 96 in tiles of 128 by products of 128: two sequences of 4096 tokens, 16 heads on 4, 139 us forward
 // and 565 backward; of 96 120 and 477.  Heads of 80 137 and 554, and 118 and 471.  One sequence of 8192, heads of 96: 257 and 1065, and 217 and 896.)
 template <typename T, int D, int E>
@@ -141,7 +84,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
     int sequence, index;
     if (!find_queries(a, BQ, unit.tile, lane, sequence, index)) return;
     Queries s_;
-    s_.init(a, sequence, index, BQ, 32 * wave);
+    s_.init(span(a.cu_q, sequence, a.tokens_q), span(a.cu_k, sequence, a.tokens_k), a.group, a.causal, index, BQ, 32 * wave);
     const Span sk = s_.k;
     const int all_tiles = s_.seen > 0 ? (s_.seen + C::BK - 1) / C::BK : 0;
     const int begin = (int)((int64_t)all_tiles * unit.part / a.by_query.parts), tiles = (int)((int64_t)all_tiles * (unit.part + 1) / a.by_query.parts);
@@ -150,7 +93,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
     int last[2];   // that a row sees
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const Queries::Row of = s_.row(a, kv, 32 * wave + 16 * j + col);
+        const Queries::Row of = s_.row(a.group, kv, 32 * wave + 16 * j + col);
         const uint16_t *row = a.q.p + of.token * a.q.token + of.head * a.q.head;
         last[j] = a.causal ? min(sk.count - 1, of.at + s_.ahead) : sk.count - 1;
 #pragma unroll
@@ -245,7 +188,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
         const int row = 32 * wave + 16 * j + col;
         const float sum = column_sum(l[j]), inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
         if (s_.row0 + row >= s_.rows) continue;
-        const Queries::Row of = s_.row(a, kv, row);
+        const Queries::Row of = s_.row(a.group, kv, row);
         const int64_t token = of.token;
         const int head = of.head;
         if (a.by_query.parts == 1) {
@@ -279,18 +222,6 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(const Problem a)
     }
 }
 
-// Rows of a join: a workgroup takes a few of a sequence, for one head
-constexpr int kJoinRows = 16;
-struct Joined { int64_t first; int rows, head; };
-__device__ __forceinline__ bool join_rows(const int *cu, int sequences, int tokens, int heads, Joined &j)
-{
-    const int tile = blockIdx.x / heads;
-    int sequence, index, count;
-    if (!find_tile(cu, sequences, tokens, kJoinRows, tile, threadIdx.x & 63, sequence, index, count)) return false;
-    const Span s = span(cu, sequence, tokens);
-    j = {s.first + (int64_t)index * kJoinRows, min(kJoinRows, s.count - index * kJoinRows), (int)(blockIdx.x - tile * heads)};
-    return true;
-}
 // O and lse from the sums of the parts
 template <typename T>
 __global__ __launch_bounds__(256) void attn_fwd_join_kernel(const Problem a)
@@ -566,7 +497,7 @@ template <typename T, int D, int E, int KS, bool STATS> __device__ __forceinline
     int sequence, index;
     if (!find_queries(a, BQ, unit.tile, lane, sequence, index)) return;
     Queries s_;
-    s_.init(a, sequence, index, BQ, 32 * qw);
+    s_.init(span(a.cu_q, sequence, a.tokens_q), span(a.cu_k, sequence, a.tokens_k), a.group, a.causal, index, BQ, 32 * qw);
     const Span sk = s_.k;
     const int all_tiles = s_.seen > 0 ? (s_.seen + BK - 1) / BK : 0;
     const int begin = (int)((int64_t)all_tiles * unit.part / a.by_query.parts), tiles = (int)((int64_t)all_tiles * (unit.part + 1) / a.by_query.parts);
@@ -578,7 +509,7 @@ template <typename T, int D, int E, int KS, bool STATS> __device__ __forceinline
     for (int j = 0; j < 2; ++j) {
         const int of_tile = 32 * qw + 16 * j + col;
         const bool live = s_.row0 + of_tile < s_.rows;
-        const Queries::Row of = s_.row(a, kv, of_tile);
+        const Queries::Row of = s_.row(a.group, kv, of_tile);
         const int64_t t = of.token;
         const int head = of.head;
         const int64_t at = (int64_t)head * a.tokens_q + t;
@@ -706,7 +637,7 @@ template <typename T, int D, int E, int KS, bool STATS> __device__ __forceinline
     for (int j = 0; j < 2; ++j) {
         const int row = 32 * qw + 16 * j + col;
         if (s_.row0 + row >= s_.rows) continue;
-        const Queries::Row of = s_.row(a, kv, row);
+        const Queries::Row of = s_.row(a.group, kv, row);
         const int64_t token = of.token;
         const int head = of.head;
 #pragma unroll
@@ -838,24 +769,6 @@ static Problem problem_of(const s24_attn_shape *s)
 using namespace s24_attn;
 
 namespace s24_attn {
-// How the work of a launch is cut up.  A workgroup's steps follow each other, and when causal the last queries (the first keys) take twice the average: few
-// workgroups, or some with many steps, leave most of the device idle.  So what a tile sums over is cut into parts, whose sums go through memory in fp32
-// for another launch to add: as many parts as make the estimate the least.  `groups` workgroups have `steps` steps of `us` microseconds each, of which `busy`
-// are taken on average, and a part's sums take `bytes` bytes: the time is that of the longest, or of all of them on the device, two a compute unit, and 5 us for the
-// second launch and 5 bytes a picosecond for sums that are written and read.  (On operands that are in no cache, in one part and in the best of 2, 4 and 8.
-// Forward: 1 head of 64, 8192 tokens 134 us and 34 in 8; 8 heads of 128 on 2, 40 tokens after 8000: 190 and 41 in 8; 64 on 8, 512 after 3500: 111 and 92
-// in 2; 32 of 128, 1500 tokens 47 and 54 in 2; the estimate takes the better one in 15 of 16 shapes.)
-static int parts_for(double groups, double steps, double busy, double us, double bytes)
-{
-    int best = 1;
-    double least = 0.0;
-    for (int p = 1; p <= 16; p *= 2) {
-        const double rounds = groups * p * busy / (2.0 * s24_cu_count());
-        const double t = us * steps / p * (rounds > 1.0 ? rounds : 1.0) + (p > 1 ? 5.0 + p * bytes * 2.0 / 5e6 : 0.0);
-        if (p == 1 || t < least) best = p, least = t;
-    }
-    return best;
-}
 // Of a long one among the sequences, whose lengths the host does not know: of several, twice the average
 static double per_sequence(int64_t tokens, const s24_attn_shape *s) { return (double)tokens * (s->sequences > 1 ? 2.0 / (double)s->sequences : 1.0); }
 static double busy_keys(const s24_attn_shape *s)   // part of the keys that a query sees

@@ -1,25 +1,12 @@
 // The paged key-value cache: tokens written to it (in 8 bits: quantised), sequences read back, and attention of one new token over it.
 //
-// Layout of a page, for one of its key-value heads:  K [page][d], a token's key in one piece;  V [page / E][d][E] with E = 8 tokens for 16-bit
-// values and 16 for 8-bit ones: 16 bytes are E consecutive tokens of one channel.  Both products of the attention of a token are matrix
-// instructions whose contracted axis lies along a lane's 16 bytes: the channels of K, the tokens of V.  So both go from memory to registers in
-// 16-byte loads with nothing in between.
-// 8 bits: x ~ s n with n = -127 .. 127 held as n + 128, s = max(max|x| / 127, 2^-126) in fp32 for each token and head.
-#include "s24_attn.h"
+// The cache's layout: s24_kv.h.
+#include "s24_kv.h"
+#include "s24_rotary.h"
 
 #include <math.h>
 
 namespace s24_kv {
-using namespace s24_attn;
-
-struct Cache {
-    unsigned char *k, *v;
-    float *ks, *vs;   // [pages][hkv][page]
-    int64_t pages;
-    int page, shift, hkv, d;   // page = 1 << shift
-};
-struct Strided { uint16_t *p; int64_t token, head; };
-
 // n nearest to x / s, ties to even, exactly: the estimate is at most one off, and x - n s is exact in fp32 for 16-bit x (a multiple of the last
 // place of s, and no larger than s).
 __device__ __forceinline__ int nearest(float x, float s, float inverse)
@@ -101,13 +88,9 @@ template <typename T, bool PAIR> __device__ __forceinline__ float step_of(uint4 
 // 14 us in 8 bits so, 33 run by run (16 bits: 13 and 16), 16384 of them 160 and 180.  (At once from two runs on, runs of 8 tokens gain another 5 % and prompts in 16 bits lose as much.)
 // Bound by memory: 17408 tokens of 8 heads of 128 take 27 us in 8 bits and 33 in 16 (4.0 and 4.3 TB/s; a plain copy of as many bytes reaches 5.7).  Stores past
 // the caches, in whole lines, take 25 and 31; but the reading back that follows then takes longer by more: both together 44 us with these, 50 with those.
-template <typename T, int BITS, bool PAIR>
-__global__ __launch_bounds__(256) void kv_write_runs_kernel(const WriteArgs a)
+template <typename T, int BITS, bool PAIR> __device__ __forceinline__ void write_runs(const WriteArgs &a, int window, int unit, bool values, int lane)
 {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int units = PAIR ? (a.c.hkv + 1) / 2 : a.c.hkv, item = 4 * blockIdx.x + wave, window = (item >> 1) / units;
-    const bool values = item & 1;
-    const Lane<PAIR> at(a.c, (item >> 1) - window * units, lane);
+    const Lane<PAIR> at(a.c, unit, lane);
     const int first_token = 16 * window;
     if (first_token >= a.tokens) return;
     const Strided from = values ? a.v : a.k;
@@ -246,13 +229,18 @@ __global__ __launch_bounds__(256) void kv_write_runs_kernel(const WriteArgs a)
     }
 }
 
-// Few tokens, in any order: a wave takes one token of one head, a lane two channels.  V is written value by value.  Bound by the launch.
-template <typename T, int BITS>
-__global__ __launch_bounds__(256) void kv_write_kernel(const WriteArgs a)
+template <typename T, int BITS, bool PAIR>
+__global__ __launch_bounds__(256) void kv_write_runs_kernel(const WriteArgs a)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int units = PAIR ? (a.c.hkv + 1) / 2 : a.c.hkv, item = 4 * blockIdx.x + wave, window = (item >> 1) / units;
+    write_runs<T, BITS, PAIR>(a, window, (item >> 1) - window * units, item & 1, lane);
+}
+
+// Few tokens, in any order: a wave takes one token of one head, a lane two channels.  V is written value by value.  Bound by the launch.  (KEYS: K too.)
+template <typename T, int BITS, bool KEYS> __device__ __forceinline__ void write_token(const WriteArgs &a, int64_t item, int lane)
 {
     using Num = s24_num<T>;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t item = (int64_t)blockIdx.x * 4 + wave;
     if (item >= (int64_t)a.tokens * a.c.hkv) return;
     const int token = (int)(item / a.c.hkv), h = (int)(item - (int64_t)token * a.c.hkv);
     const int64_t place = a.places[token];
@@ -262,12 +250,12 @@ __global__ __launch_bounds__(256) void kv_write_kernel(const WriteArgs a)
     const bool live = i < a.c.d;
     uint32_t xk = 0, xv = 0;
     if (live) {
-        xk = *reinterpret_cast<const uint32_t *>(a.k.p + token * a.k.token + h * a.k.head + i);
+        if (KEYS) xk = *reinterpret_cast<const uint32_t *>(a.k.p + token * a.k.token + h * a.k.head + i);
         xv = *reinterpret_cast<const uint32_t *>(a.v.p + token * a.v.token + h * a.v.head + i);
     }
     if (BITS == 16) {
         if (!live) return;
-        *reinterpret_cast<uint32_t *>(a.c.k + ((first + at) * a.c.d + i) * 2) = xk;
+        if (KEYS) *reinterpret_cast<uint32_t *>(a.c.k + ((first + at) * a.c.d + i) * 2) = xk;
         uint16_t *v = reinterpret_cast<uint16_t *>(a.c.v) + first * a.c.d + ((int64_t)(at >> 3) * a.c.d + i) * 8 + (at & 7);
         v[0] = (uint16_t)xv, v[8] = (uint16_t)(xv >> 16);
     } else {
@@ -276,13 +264,89 @@ __global__ __launch_bounds__(256) void kv_write_kernel(const WriteArgs a)
         for (int s = 1; s < 64; s <<= 1) mk = larger(mk, __shfl_xor(mk, s)), mv = larger(mv, __shfl_xor(mv, s));
         const float sk = step_for<T>(mk), sv = step_for<T>(mv);
         const float ik = __builtin_amdgcn_rcpf(sk), iv = __builtin_amdgcn_rcpf(sv);
-        if (lane == 0) a.c.ks[first + at] = sk, a.c.vs[first + at] = sv;
+        if (KEYS && lane == 0) a.c.ks[first + at] = sk;
+        if (lane == 0) a.c.vs[first + at] = sv;
         if (!live) return;
-        *reinterpret_cast<uint16_t *>(a.c.k + (first + at) * a.c.d + i) =
+        if (KEYS) *reinterpret_cast<uint16_t *>(a.c.k + (first + at) * a.c.d + i) =
             (uint16_t)((nearest(Num::lo(xk), sk, ik) + 128) | (nearest(Num::hi(xk), sk, ik) + 128) << 8);
         unsigned char *v = a.c.v + first * a.c.d + ((int64_t)(at >> 4) * a.c.d + i) * 16 + (at & 15);
         v[0] = (unsigned char)(nearest(Num::lo(xv), sv, iv) + 128), v[16] = (unsigned char)(nearest(Num::hi(xv), sv, iv) + 128);
     }
+}
+template <typename T, int BITS>
+__global__ __launch_bounds__(256) void kv_write_kernel(const WriteArgs a)
+{
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    write_token<T, BITS, true>(a, (int64_t)blockIdx.x * 4 + wave, threadIdx.x & 63);
+}
+
+// ------------------------------------------------------------------ appending: queries and keys normalised and turned on the way
+struct AppendArgs {
+    WriteArgs w;               // its keys are what is to be turned
+    s24_rotary_rows::Turn t;
+    Strided q, qo;
+    int value_blocks, shares;  // workgroups that write V, after which come those of the rows; waves that share a token's rows
+    bool runs;
+};
+// The whole numbers + 128 of the 16 values of a lane, four to a word, and their step.  (From the turned values in fp32: rounded to 16 bits in between, the largest of them
+// would be off by a quarter of a step more.)
+template <int LANES> __device__ __forceinline__ float sixteen_numbers(const float (&x)[16], bool in, uint32_t (&w)[4])
+{
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) most = max(most, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+    const float largest = __uint_as_float(s24_rotary_rows::row_max<LANES>(in ? most : 0u));
+    const float step = largest < INFINITY ? fmaxf(__fdiv_rn(largest, 127.0f), 0x1p-126f) : NAN, inverse = 1.0f / step;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t n[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) n[e] = (uint32_t)((int)rintf(x[4 * i + e] * inverse) + 128);
+        w[i] = four_bytes(n[0], n[1], n[2], n[3]);
+    }
+    return step;
+}
+// One launch: waves that write V as above, and waves that have the rows of the queries and keys of a token.
+template <typename T, int BITS, int LANES, bool NEIGHBOURS>
+__global__ __launch_bounds__(256) void kv_append_kernel(const AppendArgs a)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Cache &c = a.w.c;
+    if ((int)blockIdx.x < a.value_blocks) {
+        const int item = 4 * blockIdx.x + wave;
+        constexpr bool PAIR = LANES == 4;
+        const int units = PAIR ? (c.hkv + 1) / 2 : c.hkv, window = item / units;
+        if (a.runs) write_runs<T, BITS, PAIR>(a.w, window, item - window * units, true, lane);
+        else write_token<T, BITS, false>(a.w, item, lane);
+        return;
+    }
+    const int64_t item = (int64_t)(blockIdx.x - a.value_blocks) * 4 + wave;
+    const int token = (int)(item / a.shares), share = (int)(item - (int64_t)token * a.shares);
+    if (token >= a.w.tokens) return;
+    s24_rotary_rows::Part<T, LANES, NEIGHBOURS> part(a.t, lane);
+    uint16_t *const qo = a.qo.p + token * a.qo.token;
+    const int64_t place = a.w.places[token], in_page = place & (c.page - 1);
+    const bool held = place >= 0 && place < c.pages << c.shift;
+    const int64_t page = (place >> c.shift) * c.hkv;   // of its heads the first
+    s24_rotary_rows::turned_rows(a.t, part, a.q.p + token * a.q.token, a.q.head, a.w.k.p + token * a.w.k.token, a.w.k.head, token, share, a.shares, false,
+                                 [&](bool keys, int head, const float (&x)[16]) {
+        if (!keys) {
+            if (part.in && head < a.t.hq) part.store(qo + head * a.qo.head, x);
+            return;
+        }
+        const bool live = part.in && head < c.hkv && held;
+        const int64_t row = ((page + head) << c.shift) + in_page;   // in tokens of one head
+        if constexpr (BITS == 16) {
+            if (live) part.store(reinterpret_cast<uint16_t *>(c.k) + row * c.d, x);
+        } else {
+            uint32_t w[4];
+            const float step = sixteen_numbers<LANES>(x, part.in, w);
+            if (!live) return;
+            if (part.j == 0) c.ks[row] = step;
+            *reinterpret_cast<uint2 *>(c.k + row * c.d + part.a) = make_uint2(w[0], w[1]);
+            *reinterpret_cast<uint2 *>(c.k + row * c.d + part.b) = make_uint2(w[2], w[3]);
+        }
+    });
 }
 
 // ------------------------------------------------------------------ reading back
@@ -386,17 +450,6 @@ struct Lists {
         sum = n[0] + n[1] + n[2] + n[3];
     }
 };
-
-// Sixteen bytes of the cache as operands of 8 channels (tokens) each
-__device__ __forceinline__ uint4 halves(uint32_t a, uint32_t b)
-{
-    // a byte under the exponent of 1024 is 1024 + byte
-    auto two = [](uint32_t x, uint32_t select) {
-        const f16x2 v = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(x, 0x64646464u, select));
-        return __builtin_bit_cast(uint32_t, v - (f16x2){(_Float16)1152.0f, (_Float16)1152.0f});
-    };
-    return make_uint4(two(a, 0x00050004u), two(a, 0x00070006u), two(b, 0x00050004u), two(b, 0x00070006u));
-}
 
 // A wave takes a share of the positions for one key-value head and 16 of its query heads, in blocks of 64; the four of a workgroup know nothing of each other.
 // Bound by memory where the cache is large: 8 sequences of 60000 to 65536 positions, 64 heads on 8 of 128 in 8 bits, take 177 us (5.9 TB/s of 6.6 that a large copy
@@ -761,26 +814,14 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const DecodeArgs a)
 }
 
 // ------------------------------------------------------------------ host
-static int check_cache(const s24_kv_cache *c, s24_dtype dt)
-{
-    S24_REQUIRE(c != nullptr, S24_ERR_NULL);
-    S24_REQUIRE(s24_valid_dtype(dt), S24_ERR_DTYPE);
-    S24_REQUIRE(c->bits == 16 || c->bits == 8, S24_ERR_DTYPE);
-    S24_REQUIRE(c->pages >= 0 && c->pages < INT32_MAX && c->hkv > 0 && c->hkv < 65536, S24_ERR_SHAPE);
-    S24_REQUIRE(c->page >= 16 && c->page <= 1 << 16 && (c->page & (c->page - 1)) == 0, S24_ERR_SHAPE);
-    S24_REQUIRE(c->d >= 16 && c->d % 16 == 0, S24_ERR_SHAPE);
-    S24_REQUIRE(dt != S24_F32 && c->d <= 128, S24_ERR_UNSUPPORTED);
-    if (c->pages > 0) S24_REQUIRE(c->K != nullptr && c->V != nullptr && (c->bits == 16 || (c->k_step != nullptr && c->v_step != nullptr)), S24_ERR_NULL);
-    S24_REQUIRE(s24_aligned(c->K, 16) && s24_aligned(c->V, 16) && s24_aligned(c->k_step, 16) && s24_aligned(c->v_step, 16), S24_ERR_ALIGN);
-    return S24_OK;
-}
-static Cache cache_of(const s24_kv_cache *c)
-{
-    return {static_cast<unsigned char *>(c->K), static_cast<unsigned char *>(c->V), c->k_step, c->v_step, c->pages, (int)c->page,
-            __builtin_ctzll((unsigned long long)c->page), (int)c->hkv, (int)c->d};
-}
 static Strided strided(const s24_heads *v) { return {static_cast<uint16_t *>(v->data), v->token, v->head}; }
 
+// Waves for sixteen tokens of K or of V
+static int64_t write_units(const s24_kv_cache *cache) { return cache->d <= 64 ? (cache->hkv + 1) / 2 : cache->hkv; }
+// The runs' kernel from 40 tokens of a head for each compute unit on.  (8 bits, 8 heads of 128, both sides: 1024 tokens 7.9 us by runs, 6.1 one by one; 2048
+// tokens 7.6 and 9.5; 16384 tokens 24 and 50.  12 heads of 64, 1024 tokens: 7.3 and 7.2.  16 bits, 8 heads of 128, 1024 tokens: 5.3 and 6.3.  Those are prompts.  Tokens that
+// do not follow each other, which the host does not see, take 14 and 9.5 us at 1280 tokens, 27 and 22 at 4096, 160 and 154 at 16384.)
+static bool by_runs(const s24_kv_cache *cache, int64_t tokens) { return tokens * cache->hkv >= 40 * (int64_t)s24_cu_count(); }
 template <typename T, int BITS> static void write(const WriteArgs &a, bool runs, dim3 grid, hipStream_t st)
 {
     const dim3 block(256);
@@ -817,17 +858,57 @@ extern "C" int s24_kv_write(const s24_kv_cache *cache, const s24_heads *K, const
     if (tokens == 0 || cache->pages == 0) return S24_OK;
     const WriteArgs a{cache_of(cache), strided(K), strided(V), places, (int)tokens};
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    // The runs' kernel from 40 tokens of a head for each compute unit on.  (8 bits, 8 heads of 128, both sides: 1024 tokens 7.9 us by runs, 6.1 one by one; 2048
-    // tokens 7.6 and 9.5; 16384 tokens 24 and 50.  12 heads of 64, 1024 tokens: 7.3 and 7.2.  16 bits, 8 heads of 128, 1024 tokens: 5.3 and 6.3.  Those are prompts.  Tokens that
-    // do not follow each other, which the host does not see, take 14 and 9.5 us at 1280 tokens, 27 and 22 at 4096, 160 and 154 at 16384.)
-    const int64_t units = cache->d <= 64 ? (cache->hkv + 1) / 2 : cache->hkv, waves = 2 * ((tokens + 15) / 16) * units;   // of K and of V
-    const bool runs = tokens * cache->hkv >= 40 * (int64_t)s24_cu_count();
+    const int64_t waves = 2 * ((tokens + 15) / 16) * write_units(cache);   // of K and of V
+    const bool runs = by_runs(cache, tokens);
     const int64_t groups = runs ? (waves + 3) / 4 : (tokens * cache->hkv + 3) / 4;
     S24_REQUIRE((runs ? waves + 3 : groups) <= kMostGroups, S24_ERR_SHAPE);   // (the runs' kernel numbers its waves in an int)
     const dim3 grid((unsigned)groups);
     if (cache->bits == 16) write<uint16_t, 16>(a, runs, grid, st);   // a copy, whatever the type
     else if (dt == S24_BF16) write<uint16_t, 8>(a, runs, grid, st);
     else write<s24_half, 8>(a, runs, grid, st);
+    return s24_launch_status();
+}
+
+namespace s24_kv {
+template <typename T, int BITS> static void append(const AppendArgs &a, bool neighbours, dim3 grid, hipStream_t st)
+{
+    const dim3 block(256);
+    if (a.t.d <= 64) {
+        if (neighbours) kv_append_kernel<T, BITS, 4, true><<<grid, block, 0, st>>>(a);
+        else kv_append_kernel<T, BITS, 4, false><<<grid, block, 0, st>>>(a);
+    } else {
+        if (neighbours) kv_append_kernel<T, BITS, 8, true><<<grid, block, 0, st>>>(a);
+        else kv_append_kernel<T, BITS, 8, false><<<grid, block, 0, st>>>(a);
+    }
+}
+}  // namespace s24_kv
+
+extern "C" int s24_kv_append(const s24_kv_cache *cache, const s24_rotary *rotary, const int32_t *positions, const s24_heads *Q, int64_t hq, const s24_heads *K, const s24_heads *V,
+                             const s24_heads *Qo, const int64_t *places, int64_t tokens, s24_dtype dt, void *stream)
+{
+    S24_TRY(check_cache(cache, dt));
+    S24_TRY(s24_rotary_rows::check_rotary(rotary, positions, tokens, hq, cache->hkv, cache->d, dt));
+    if (hq > 0) S24_TRY(check_rows(Q, tokens, hq, cache->d, false));
+    if (hq > 0) S24_TRY(check_rows(Qo, tokens, hq, cache->d, true));
+    S24_TRY(check_rows(K, tokens, cache->hkv, cache->d, false));
+    S24_TRY(check_rows(V, tokens, cache->hkv, cache->d, false));
+    S24_REQUIRE(places != nullptr || tokens == 0, S24_ERR_NULL);
+    S24_REQUIRE(s24_aligned(places, 8), S24_ERR_ALIGN);
+    if (tokens == 0) return S24_OK;
+    const Strided none{};
+    AppendArgs a{{cache_of(cache), strided(K), strided(V), places, (int)tokens}, s24_rotary_rows::turn_args(rotary, positions, tokens, hq, cache->hkv, cache->d),
+                 hq > 0 ? strided(Q) : none, hq > 0 ? strided(Qo) : none};
+    a.runs = by_runs(cache, tokens);
+    const int64_t waves = a.runs ? ((tokens + 15) / 16) * write_units(cache) : tokens * cache->hkv;
+    a.shares = s24_rotary_rows::shares_of_token(tokens, hq, cache->hkv, cache->d);
+    const int64_t values = cache->pages > 0 ? (waves + 3) / 4 : 0, groups = values + (tokens * a.shares + 3) / 4;
+    S24_REQUIRE(waves + 3 <= kMostGroups && groups <= kMostGroups, S24_ERR_SHAPE);   // (the waves that write V are numbered in an int)
+    a.value_blocks = (int)values;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const dim3 grid((unsigned)groups);
+    const bool neighbours = rotary->interleaved != 0;
+    if (dt == S24_BF16) cache->bits == 16 ? append<uint16_t, 16>(a, neighbours, grid, st) : append<uint16_t, 8>(a, neighbours, grid, st);
+    else cache->bits == 16 ? append<s24_half, 16>(a, neighbours, grid, st) : append<s24_half, 8>(a, neighbours, grid, st);
     return s24_launch_status();
 }
 

@@ -1,0 +1,191 @@
+// Heads as rows that are normalised and turned by their token's position, for the kernels that do so on the way (training, the cache).
+//
+// y_i = x_i w_i r with r = (mean x^2 + eps)^-1/2, or y = x;  a pair (a, b) of y turned by its angle: (a cos - b sin, b cos + a sin).
+// A lane has eight pairs of a row: 16 bytes of their first values and 16 of their second (or both in one piece of 32, where neighbours are pairs), so that a row of d
+// values is d / 16 lanes, each pair lies within a lane, and all is moved in pieces of 16 bytes.
+#pragma once
+#include "s24_attn.h"
+
+namespace s24_rotary_rows {
+using namespace s24_attn;
+
+struct Turn {
+    const int32_t *positions;    // [axes][tokens]
+    const double *frequencies;   // [rotated / 2]: radians for each step of the position
+    const int32_t *axis;         // [rotated / 2], or NULL: all pairs turn by the first
+    const uint16_t *wq, *wk;     // [d], or NULL: not normalised
+    float eps, share;            // 1 / d
+    int axes, rotated, d, tokens, hq, hkv;
+};
+
+// Cosine and sine of a fraction of a turn in 32 bits.  An eighth of a turn to either side of a multiple of a quarter: there the Taylor series to the 9th and 8th power are
+// within 2e-9 and 3e-8.
+__device__ __forceinline__ void turn_of(uint32_t phase, float &cosine, float &sine)
+{
+    const uint32_t quarter = (phase + 0x20000000u) >> 30;
+    const float x = (float)(int32_t)(phase - (quarter << 30)) * 1.46291807926715968e-9f;   // 2 pi / 2^32
+    const float u = x * x;
+    const float s = fmaf(x * u, fmaf(u, fmaf(u, fmaf(u, 2.75573192e-6f, -1.98412698e-4f), 8.33333333e-3f), -0.166666667f), x);
+    const float c = fmaf(u, fmaf(u, fmaf(u, fmaf(u, 2.48015873e-5f, -1.38888889e-3f), 4.16666667e-2f), -0.5f), 1.0f);
+    const float p = quarter & 1 ? s : c, q = quarter & 1 ? c : s;
+    cosine = __uint_as_float(__float_as_uint(p) ^ ((quarter + 1) & 2) << 30);
+    sine = __uint_as_float(__float_as_uint(q) ^ (quarter & 2) << 30);
+}
+
+// Sum over the lanes of a row
+template <int LANES> __device__ __forceinline__ float row_sum(float x)
+{
+    static_assert(LANES == 4 || LANES == 8, "a row's lanes");
+#if defined(__HIP_DEVICE_COMPILE__)
+    auto moved = [](float v, auto control) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(control)::value, 0xf, 0xf, true)); };
+    x += moved(x, std::integral_constant<int, 0xB1>());                     // lanes 1 0 3 2 of four
+    x += moved(x, std::integral_constant<int, 0x4E>());                     // 2 3 0 1
+    if (LANES == 8) x += moved(x, std::integral_constant<int, 0x141>());    // eight, the other way round
+#endif
+    return x;
+}
+// Largest of their magnitudes, compared as bits: what is no number is the largest of all
+template <int LANES> __device__ __forceinline__ uint32_t row_max(uint32_t x)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xf, 0xf, true));
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xf, 0xf, true));
+    if (LANES == 8) x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xf, 0xf, true));
+#endif
+    return x;
+}
+
+struct Pieces { uint4 a, b; };
+// The 16 values of a lane, and how they are paired
+template <typename T, int LANES, bool NEIGHBOURS> struct Part {
+    static constexpr int ROWS = 64 / LANES;   // that a wave has at a time
+    int j, r, a, b;    // lane of a row, row; where its two pieces start
+    bool in, turned;   // whether it has values, and whether they are turned
+    float cosine[8], sine[8];
+    __device__ __forceinline__ Part(const Turn &t, int lane)
+    {
+        j = lane & (LANES - 1), r = lane / LANES;
+        in = 16 * j < t.d, turned = 16 * j < t.rotated;
+        const bool apart = turned && !NEIGHBOURS;
+        a = apart ? 8 * j : 16 * j, b = apart ? (t.rotated >> 1) + 8 * j : 16 * j + 8;
+    }
+    // Angles of a token.  They are reduced without an error that grows with the position: a frequency as a fraction of a turn in 63 bits, times the position, of which whole
+    // turns fall out of the word.
+    __device__ __forceinline__ void angles(const Turn &t, int token, bool back)
+    {
+        if (!turned) return;
+        const int64_t first = t.axes == 1 ? t.positions[token] : 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int pair = 8 * j + e;
+            const double turns = t.frequencies[pair] * 0.15915494309189535;
+            const int64_t step = (int64_t)((turns - rint(turns)) * 0x1p63);
+            const int64_t at = t.axes == 1 ? first : t.positions[(int64_t)(t.axis != nullptr ? min((uint32_t)t.axis[pair], (uint32_t)t.axes - 1) : 0u) * t.tokens + token];
+            turn_of((uint32_t)((uint64_t)at * (uint64_t)step >> 31), cosine[e], sine[e]);
+            if (back) sine[e] = -sine[e];
+        }
+    }
+    __device__ __forceinline__ Pieces load(const uint16_t *row) const
+    {
+        return {*reinterpret_cast<const uint4 *>(row + a), *reinterpret_cast<const uint4 *>(row + b)};
+    }
+    static __device__ __forceinline__ void widen(const Pieces &p, float (&x)[16])
+    {
+        using Num = s24_num<T>;
+        const uint32_t w[8] = {p.a.x, p.a.y, p.a.z, p.a.w, p.b.x, p.b.y, p.b.z, p.b.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[2 * i] = Num::lo(w[i]), x[2 * i + 1] = Num::hi(w[i]);
+    }
+    __device__ __forceinline__ void store(uint16_t *row, const float (&x)[16]) const
+    {
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = pack2<T>(x[2 * i], x[2 * i + 1]);
+        *reinterpret_cast<uint4 *>(row + a) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint4 *>(row + b) = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+    // 1 / sqrt(mean x^2 + eps) of the row
+    __device__ __forceinline__ float factor(const Turn &t, const float (&x)[16]) const
+    {
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum = fmaf(x[i], x[i], sum);
+        sum = row_sum<LANES>(in ? sum : 0.0f);
+        const float mean = fmaf(sum, t.share, t.eps), y = __builtin_amdgcn_rsqf(mean);
+        return y * fmaf(-0.5f * mean * y, y, 1.5f);   // (the estimate and a Newton step: a few tenths of a step more exact)
+    }
+    __device__ __forceinline__ void turn(float (&x)[16]) const
+    {
+        if (!turned) return;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int p = NEIGHBOURS ? 2 * e : e, q = NEIGHBOURS ? 2 * e + 1 : 8 + e;
+            const float u = x[p], v = x[q];
+            x[p] = fmaf(u, cosine[e], -v * sine[e]), x[q] = fmaf(v, cosine[e], u * sine[e]);
+        }
+    }
+};
+
+// Rows of a token's heads, ROWS at a time, queries before keys: a wave takes every `shares`-th such group from `share` on, the next one's loads ahead of this one's
+// arithmetic.  use(keys, head, x): the row of a lane, turned; `head` is past the last one for lanes that have none.
+template <typename P, typename Use>
+__device__ __forceinline__ void turned_rows(const Turn &t, P &part, const uint16_t *q, int64_t q_head, const uint16_t *k, int64_t k_head, int token, int share, int shares, bool back, Use use)
+{
+    const int of_q = (t.hq + P::ROWS - 1) / P::ROWS, all = of_q + (t.hkv + P::ROWS - 1) / P::ROWS;
+    if (share >= all) return;
+    auto load = [&](int group) {
+        const bool keys = group >= of_q;
+        const int head = (keys ? group - of_q : group) * P::ROWS + part.r;
+        return part.in && head < (keys ? t.hkv : t.hq) ? part.load(keys ? k + head * k_head : q + head * q_head) : Pieces{};
+    };
+    auto weights = [&](bool keys) {
+        const uint16_t *w = keys ? t.wk : t.wq;
+        return w != nullptr && part.in ? part.load(w) : Pieces{};
+    };
+    Pieces next = load(share), w = weights(share >= of_q);
+    part.angles(t, token, back);
+    for (int group = share; group < all; group += shares) {
+        const Pieces now = next;
+        const bool keys = group >= of_q;
+        if (keys && group - shares < of_q && group != share) w = weights(true);
+        if (group + shares < all) next = load(group + shares);
+        float x[16];
+        P::widen(now, x);
+        if ((keys ? t.wk : t.wq) != nullptr) {
+            float by[16];
+            P::widen(w, by);
+            const float f = part.factor(t, x);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] *= f * by[i];
+        }
+        part.turn(x);
+        use(keys, (keys ? group - of_q : group) * P::ROWS + part.r, x);
+    }
+}
+
+// ---- host
+inline int check_rotary(const s24_rotary *r, const int32_t *positions, int64_t tokens, int64_t hq, int64_t hkv, int64_t d, s24_dtype dt)
+{
+    S24_REQUIRE(r != nullptr, S24_ERR_NULL);
+    S24_REQUIRE(s24_valid_dtype(dt), S24_ERR_DTYPE);
+    S24_REQUIRE(tokens >= 0 && tokens < INT32_MAX / 2 && hq >= 0 && hkv >= 0 && hq < 65536 && hkv < 65536, S24_ERR_SHAPE);
+    S24_REQUIRE(d >= 16 && d % 16 == 0 && r->rotated >= 0 && r->rotated % 16 == 0 && r->rotated <= d, S24_ERR_SHAPE);
+    S24_REQUIRE(r->axes >= 1 && r->axes <= 65535 && r->eps >= 0.0f && r->eps <= 3.0e38f, S24_ERR_SHAPE);
+    S24_REQUIRE(dt != S24_F32 && d <= 128, S24_ERR_UNSUPPORTED);
+    if (r->rotated > 0) S24_REQUIRE(r->frequencies != nullptr && (positions != nullptr || tokens == 0), S24_ERR_NULL);
+    S24_REQUIRE(s24_aligned(r->frequencies, 8) && s24_aligned(r->axis, 4) && s24_aligned(positions, 4) && s24_aligned(r->wq, 16) && s24_aligned(r->wk, 16), S24_ERR_ALIGN);
+    return S24_OK;
+}
+inline Turn turn_args(const s24_rotary *r, const int32_t *positions, int64_t tokens, int64_t hq, int64_t hkv, int64_t d)
+{
+    return {positions, r->frequencies, r->axis, static_cast<const uint16_t *>(r->wq), static_cast<const uint16_t *>(r->wk), r->eps, 1.0f / (float)d,
+            (int)r->axes, (int)r->rotated, (int)d, (int)tokens, (int)hq, (int)hkv};
+}
+// Waves that share a token's groups of rows: one, unless there are too few tokens for sixteen waves a compute unit
+inline int shares_of_token(int64_t tokens, int64_t hq, int64_t hkv, int64_t d)
+{
+    const int rows = d <= 64 ? 16 : 8;
+    const int64_t groups = (hq + rows - 1) / rows + (hkv + rows - 1) / rows, most = tokens > 0 ? 16 * (int64_t)s24_cu_count() / tokens : 1;
+    return (int)(most < 1 ? 1 : most > groups ? groups : most);
+}
+}  // namespace s24_rotary_rows
