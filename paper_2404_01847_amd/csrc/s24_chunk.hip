@@ -70,7 +70,7 @@ template <int D> struct Sixteen<D, 16> {
             buffer_to_lds<16>(bv, (lds_ptr)(tv + (wave * PER + i) * 1024), v[i]);
         }
     }
-    __device__ __forceinline__ void finish(lds_byte *, lds_byte *, float *) {}
+    __device__ __forceinline__ void finish(lds_byte *, lds_byte *, float *, int) {}
 };
 template <int D> struct Sixteen<D, 8> {
     static constexpr int PER = D / 64;
@@ -97,7 +97,8 @@ template <int D> struct Sixteen<D, 8> {
         }
         step = (lane & 16 ? c.vs : c.ks)[first + (lane & 15)];
     }
-    __device__ __forceinline__ void finish(lds_byte *tk, lds_byte *tv, float *steps)
+    // `left`: how many of the positions the sequence has.  (What lies past its end may hold anything: there V has the step 0.)
+    __device__ __forceinline__ void finish(lds_byte *tk, lds_byte *tv, float *steps, int left)
     {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
@@ -108,7 +109,7 @@ template <int D> struct Sixteen<D, 8> {
             lds_store(tv + (2 * wave * D + at) * 16, halves(v[i].x, v[i].y));
             lds_store(tv + ((2 * wave + 1) * D + at) * 16, halves(v[i].z, v[i].w));
         }
-        if (lane < 32) steps[(lane >> 4) * kChunkKeys + 16 * wave + (lane & 15)] = step;
+        if (lane < 32) steps[(lane >> 4) * kChunkKeys + 16 * wave + (lane & 15)] = lane < 16 || (lane & 15) < left ? step : 0.0f;
     }
 };
 
@@ -179,7 +180,7 @@ __global__ __launch_bounds__(256, 2) void chunk_kernel(const ChunkArgs a)
     if (begin < tiles) {
         sixteen.start(a.c, place(begin, page_of(begin)), (lds_byte *)lds_k[begin & 1], (lds_byte *)lds_v[begin & 1], steps[begin & 1]);
         if (begin + 1 < tiles) id = page_of(begin + 1);
-        sixteen.finish((lds_byte *)lds_k[begin & 1], (lds_byte *)lds_v[begin & 1], steps[begin & 1]);
+        sixteen.finish((lds_byte *)lds_k[begin & 1], (lds_byte *)lds_v[begin & 1], steps[begin & 1], length - begin * BK - 16 * wave);
     }
     for (int t = begin; t < tiles; ++t) {
         wait_and_barrier<0>();
@@ -189,6 +190,19 @@ __global__ __launch_bounds__(256, 2) void chunk_kernel(const ChunkArgs a)
             if (t + 2 < tiles) id = page_of(t + 2);
         }
         const int k0 = t * BK;
+        if (BITS == 16 && k0 + BK > length) {   // what lies past the sequence's end may hold anything: V has zeros there
+            for (int i = threadIdx.x; i < 8 * D; i += 256) {
+                const int left = length - k0 - 8 * (i / D);
+                if (left >= 8) continue;
+                lds_byte *const at = (lds_byte *)lds_v[t & 1] + 16 * i;
+                uint4 x = lds_load(at);
+                uint32_t *const two = reinterpret_cast<uint32_t *>(&x);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) two[e] = left - 2 * e >= 2 ? two[e] : left - 2 * e == 1 ? two[e] & 0xFFFFu : 0u;
+                lds_store(at, x);
+            }
+            wait_and_barrier<0>();
+        }
         if (k0 < s_.wave_seen) {
             const lds_byte *tk = (const lds_byte *)lds_k[t & 1], *tv = (const lds_byte *)lds_v[t & 1];
             f32x4 s[4][2];
@@ -203,9 +217,9 @@ __global__ __launch_bounds__(256, 2) void chunk_kernel(const ChunkArgs a)
                     s[i][0] = mma<M>(f, q[0][k], s[i][0]);
                     s[i][1] = mma<M>(f, q[1][k], s[i][1]);
                 }
+            if (D == 128) reads_ahead<4, 8, E / 32>();
             f32x4 sv[4];
             float step = 0.0f;
-            const bool tail = k0 + BK > length;
             if constexpr (BITS == 8) {
                 const float *now = steps[t & 1];
 #pragma unroll
@@ -213,10 +227,6 @@ __global__ __launch_bounds__(256, 2) void chunk_kernel(const ChunkArgs a)
                     const f32x4 sk = *reinterpret_cast<const f32x4 *>(now + 16 * g + 4 * i);
                     sv[i] = *reinterpret_cast<const f32x4 *>(now + BK + 16 * g + 4 * i);
                     s[i][0] *= sk, s[i][1] *= sk;
-                    if (tail) {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) sv[i][r] = k0 + 16 * g + 4 * i + r < length ? sv[i][r] : 0.0f;
-                    }
                     step = fmaxf(step, fmaxf(fmaxf(sv[i][0], sv[i][1]), fmaxf(sv[i][2], sv[i][3])));
                 }
             }
@@ -272,20 +282,12 @@ __global__ __launch_bounds__(256, 2) void chunk_kernel(const ChunkArgs a)
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int n = 0; n < E / 16; ++n) {
-                    uint4 f = lds_load(tv + ((2 * g + u) * D + 16 * n + col) * 16);
-                    if (BITS == 16 && tail) {   // what lies past the sequence's end may hold anything
-                        uint32_t *x = reinterpret_cast<uint32_t *>(&f);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int left = length - (k0 + 16 * g + 8 * u + 2 * i);
-                            x[i] = left >= 2 ? x[i] : left == 1 ? x[i] & 0xFFFFu : 0u;
-                        }
-                    }
+                    const uint4 f = lds_load(tv + ((2 * g + u) * D + 16 * n + col) * 16);
                     o[n][0] = mma<M>(f, p[u][0], o[n][0]);
                     o[n][1] = mma<M>(f, p[u][1], o[n][1]);
                 }
         }
-        if (t + 1 < tiles) sixteen.finish((lds_byte *)lds_k[other], (lds_byte *)lds_v[other], steps[other]);
+        if (t + 1 < tiles) sixteen.finish((lds_byte *)lds_k[other], (lds_byte *)lds_v[other], steps[other], length - (t + 1) * BK - 16 * wave);
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {

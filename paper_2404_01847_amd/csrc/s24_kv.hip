@@ -310,6 +310,7 @@ template <int LANES> __device__ __forceinline__ float sixteen_numbers(const floa
 template <typename T, int BITS, int LANES, bool NEIGHBOURS>
 __global__ __launch_bounds__(256) void kv_append_kernel(const AppendArgs a)
 {
+    __shared__ __align__(16) s24_rotary_rows::Angles angles[4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Cache &c = a.w.c;
     if ((int)blockIdx.x < a.value_blocks) {
@@ -323,12 +324,12 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const AppendArgs a)
     const int64_t item = (int64_t)(blockIdx.x - a.value_blocks) * 4 + wave;
     const int token = (int)(item / a.shares), share = (int)(item - (int64_t)token * a.shares);
     if (token >= a.w.tokens) return;
-    s24_rotary_rows::Part<T, LANES, NEIGHBOURS> part(a.t, lane);
+    s24_rotary_rows::Part<T, LANES, NEIGHBOURS> part(a.t, lane, (s24_rotary_rows::lds_angles *)&angles[wave]);
     uint16_t *const qo = a.qo.p + token * a.qo.token;
     const int64_t place = a.w.places[token], in_page = place & (c.page - 1);
     const bool held = place >= 0 && place < c.pages << c.shift;
     const int64_t page = (place >> c.shift) * c.hkv;   // of its heads the first
-    s24_rotary_rows::turned_rows(a.t, part, a.q.p + token * a.q.token, a.q.head, a.w.k.p + token * a.w.k.token, a.w.k.head, token, share, a.shares, false,
+    s24_rotary_rows::turned_rows(a.t, part, a.q.p + token * a.q.token, a.q.head, a.w.k.p + token * a.w.k.token, a.w.k.head, token, share, a.shares, false, lane,
                                  [&](bool keys, int head, const float (&x)[16]) {
         if (!keys) {
             if (part.in && head < a.t.hq) part.store(qo + head * a.qo.head, x);

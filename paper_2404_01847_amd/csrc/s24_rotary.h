@@ -56,35 +56,52 @@ template <int LANES> __device__ __forceinline__ uint32_t row_max(uint32_t x)
 }
 
 struct Pieces { uint4 a, b; };
+// Cosines and sines of a token's pairs, of a wave
+struct Angles { float cosine[64], sine[64]; };
+typedef __attribute__((address_space(3))) Angles lds_angles;
 // The 16 values of a lane, and how they are paired
 template <typename T, int LANES, bool NEIGHBOURS> struct Part {
     static constexpr int ROWS = 64 / LANES;   // that a wave has at a time
     int j, r, a, b;    // lane of a row, row; where its two pieces start
     bool in, turned;   // whether it has values, and whether they are turned
     float cosine[8], sine[8];
-    __device__ __forceinline__ Part(const Turn &t, int lane)
+    // The pair that the lane finds the angle of: its frequency as a fraction of a turn, high + low / 2^32 in 2^-32, and where its axis has the positions
+    uint32_t high, low;
+    const int32_t *at;
+    lds_angles *shared;
+    __device__ __forceinline__ Part(const Turn &t, int lane, lds_angles *angles)
     {
-        j = lane & (LANES - 1), r = lane / LANES;
+        j = lane & (LANES - 1), r = lane / LANES, shared = angles;
         in = 16 * j < t.d, turned = 16 * j < t.rotated;
         const bool apart = turned && !NEIGHBOURS;
         a = apart ? 8 * j : 16 * j, b = apart ? (t.rotated >> 1) + 8 * j : 16 * j + 8;
+        high = low = 0, at = t.positions;
+        if (2 * lane >= t.rotated) return;
+        if (t.axis != nullptr) at += (int64_t)min((uint32_t)t.axis[lane], (uint32_t)t.axes - 1) * t.tokens;
+        const double turns = t.frequencies[lane] * 0.15915494309189535, steps = (turns - rint(turns)) * 0x1p32, whole = fmin(floor(steps), 2147483647.0);
+        high = (uint32_t)(int32_t)whole, low = (uint32_t)fmin((steps - whole) * 0x1p32, 4294967295.0);
     }
-    // Angles of a token.  They are reduced without an error that grows with the position: a frequency as a fraction of a turn in 63 bits, times the position, of which whole
-    // turns fall out of the word.
-    __device__ __forceinline__ void angles(const Turn &t, int token, bool back)
+    // The angles of a token: each lane has one, and its row's eight come from the others'.  They are reduced without an error that grows with the position: of the
+    // frequency's fraction of a turn in 64 bits times the position whole turns fall out of the word.
+    __device__ __forceinline__ void angles(const Turn &t, int32_t position, bool back, int lane)
     {
-        if (!turned) return;
-        const int64_t first = t.axes == 1 ? t.positions[token] : 0;
+        if (t.rotated == 0) return;
+        const uint32_t n = (uint32_t)position;
+        float c, s;
+        turn_of(n * high + __umulhi(n, low) - (position < 0 ? low : 0), c, s);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        shared->cosine[lane] = c, shared->sine[lane] = back ? -s : s;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const lds_byte *from = (const lds_byte *)shared + 32 * j;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int pair = 8 * j + e;
-            const double turns = t.frequencies[pair] * 0.15915494309189535;
-            const int64_t step = (int64_t)((turns - rint(turns)) * 0x1p63);
-            const int64_t at = t.axes == 1 ? first : t.positions[(int64_t)(t.axis != nullptr ? min((uint32_t)t.axis[pair], (uint32_t)t.axes - 1) : 0u) * t.tokens + token];
-            turn_of((uint32_t)((uint64_t)at * (uint64_t)step >> 31), cosine[e], sine[e]);
-            if (back) sine[e] = -sine[e];
+        for (int e = 0; e < 8; e += 4) {
+            const f32x4 x = __builtin_bit_cast(f32x4, lds_load(from + 4 * e)), y = __builtin_bit_cast(f32x4, lds_load(from + 256 + 4 * e));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) cosine[e + i] = x[i], sine[e + i] = y[i];
         }
     }
+    // Position of a token on the lane's axis
+    __device__ __forceinline__ int32_t position(const Turn &t, int token) const { return t.rotated > 0 ? at[token] : 0; }
     __device__ __forceinline__ Pieces load(const uint16_t *row) const
     {
         return {*reinterpret_cast<const uint4 *>(row + a), *reinterpret_cast<const uint4 *>(row + b)};
@@ -96,13 +113,18 @@ template <typename T, int LANES, bool NEIGHBOURS> struct Part {
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[2 * i] = Num::lo(w[i]), x[2 * i + 1] = Num::hi(w[i]);
     }
-    __device__ __forceinline__ void store(uint16_t *row, const float (&x)[16]) const
+    template <bool PAST = false> __device__ __forceinline__ void store(uint16_t *row, const float (&x)[16]) const
     {
         uint32_t w[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] = pack2<T>(x[2 * i], x[2 * i + 1]);
-        *reinterpret_cast<uint4 *>(row + a) = make_uint4(w[0], w[1], w[2], w[3]);
-        *reinterpret_cast<uint4 *>(row + b) = make_uint4(w[4], w[5], w[6], w[7]);
+        const uint4 first = make_uint4(w[0], w[1], w[2], w[3]), second = make_uint4(w[4], w[5], w[6], w[7]);
+        if (PAST) {
+            s24_store_stream(row + a, first), s24_store_stream(row + b, second);
+        } else {
+            *reinterpret_cast<uint4 *>(row + a) = first;
+            *reinterpret_cast<uint4 *>(row + b) = second;
+        }
     }
     // 1 / sqrt(mean x^2 + eps) of the row
     __device__ __forceinline__ float factor(const Turn &t, const float (&x)[16]) const
@@ -129,7 +151,7 @@ template <typename T, int LANES, bool NEIGHBOURS> struct Part {
 // Rows of a token's heads, ROWS at a time, queries before keys: a wave takes every `shares`-th such group from `share` on, the next one's loads ahead of this one's
 // arithmetic.  use(keys, head, x): the row of a lane, turned; `head` is past the last one for lanes that have none.
 template <typename P, typename Use>
-__device__ __forceinline__ void turned_rows(const Turn &t, P &part, const uint16_t *q, int64_t q_head, const uint16_t *k, int64_t k_head, int token, int share, int shares, bool back, Use use)
+__device__ __forceinline__ void turned_rows(const Turn &t, P &part, const uint16_t *q, int64_t q_head, const uint16_t *k, int64_t k_head, int token, int share, int shares, bool back, int lane, Use use)
 {
     const int of_q = (t.hq + P::ROWS - 1) / P::ROWS, all = of_q + (t.hkv + P::ROWS - 1) / P::ROWS;
     if (share >= all) return;
@@ -143,7 +165,7 @@ __device__ __forceinline__ void turned_rows(const Turn &t, P &part, const uint16
         return w != nullptr && part.in ? part.load(w) : Pieces{};
     };
     Pieces next = load(share), w = weights(share >= of_q);
-    part.angles(t, token, back);
+    part.angles(t, part.position(t, token), back, lane);
     for (int group = share; group < all; group += shares) {
         const Pieces now = next;
         const bool keys = group >= of_q;
@@ -181,11 +203,14 @@ inline Turn turn_args(const s24_rotary *r, const int32_t *positions, int64_t tok
     return {positions, r->frequencies, r->axis, static_cast<const uint16_t *>(r->wq), static_cast<const uint16_t *>(r->wk), r->eps, 1.0f / (float)d,
             (int)r->axes, (int)r->rotated, (int)d, (int)tokens, (int)hq, (int)hkv};
 }
-// Waves that share a token's groups of rows: one, unless there are too few tokens for sixteen waves a compute unit
+// Waves that share a token's groups of rows: three groups to a wave at most, fewer where there are too few tokens for sixteen waves a compute unit.  (All of a token's in one
+// wave leave the last waves of a launch long ones: 13868 tokens of 64 + 8 heads of 128 appended in 8 bits 114 us so, 106 with four to a wave, 106 with three, 105 with two, 119 with one;
+// 8192 tokens of them normalised and turned 51, 49, 49, 50 and 59; 5338 tokens of 20 + 20 heads of 64 appended 27, 27, 24, 24 and 26.)
 inline int shares_of_token(int64_t tokens, int64_t hq, int64_t hkv, int64_t d)
 {
     const int rows = d <= 64 ? 16 : 8;
-    const int64_t groups = (hq + rows - 1) / rows + (hkv + rows - 1) / rows, most = tokens > 0 ? 16 * (int64_t)s24_cu_count() / tokens : 1;
+    const int64_t groups = (hq + rows - 1) / rows + (hkv + rows - 1) / rows, fill = tokens > 0 ? 16 * (int64_t)s24_cu_count() / tokens : 1, third = (groups + 2) / 3;
+    const int64_t most = fill > third ? fill : third;
     return (int)(most < 1 ? 1 : most > groups ? groups : most);
 }
 }  // namespace s24_rotary_rows

@@ -16,15 +16,18 @@ struct ForwardArgs {
 template <typename T, int LANES, bool NEIGHBOURS>
 __global__ __launch_bounds__(256) void rotary_kernel(const ForwardArgs a)
 {
+    __shared__ __align__(16) Angles angles[4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t item = (int64_t)blockIdx.x * 4 + wave;
     const int token = (int)(item / a.shares), share = (int)(item - (int64_t)token * a.shares);
     if (token >= a.t.tokens) return;
-    Part<T, LANES, NEIGHBOURS> part(a.t, lane);
+    Part<T, LANES, NEIGHBOURS> part(a.t, lane, (lds_angles *)&angles[wave]);
     uint16_t *const qo = a.qo.p + token * a.qo.token, *const ko = a.ko.p + token * a.ko.token;
-    turned_rows(a.t, part, a.q.p + token * a.q.token, a.q.head, a.k.p + token * a.k.token, a.k.head, token, share, a.shares, a.back, [&](bool keys, int head, const float (&x)[16]) {
+    turned_rows(a.t, part, a.q.p + token * a.q.token, a.q.head, a.k.p + token * a.k.token, a.k.head, token, share, a.shares, a.back, lane, [&](bool keys, int head, const float (&x)[16]) {
         if (!part.in || head >= (keys ? a.t.hkv : a.t.hq)) return;
-        part.store(keys ? ko + head * a.ko.head : qo + head * a.qo.head, x);
+        uint16_t *const to = keys ? ko + head * a.ko.head : qo + head * a.qo.head;
+        if (a.back) part.template store<true>(to, x);
+        else part.store(to, x);
     });
 }
 
@@ -39,23 +42,28 @@ struct BackwardArgs {
     int q_blocks, k_blocks;
 };
 template <typename T, int LANES, bool NEIGHBOURS>
-__global__ __launch_bounds__(256) void rotary_bwd_kernel(const BackwardArgs a)
+__global__ __launch_bounds__(256, 4) void rotary_bwd_kernel(const BackwardArgs a)
 {
     using P = Part<T, LANES, NEIGHBOURS>;
     __shared__ float sums[4][16 * LANES];
+    __shared__ __align__(16) Angles angles[4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const bool keys = (int)blockIdx.x >= a.q_blocks;
     const int heads = keys ? a.t.hkv : a.t.hq, groups = (heads + P::ROWS - 1) / P::ROWS;
     const Strided &dz = keys ? a.dzk : a.dzq, &x = keys ? a.xk : a.xq, &dx = keys ? a.dxk : a.dxq;
     const uint16_t *const w = keys ? a.t.wk : a.t.wq;
-    const int64_t items = (int64_t)a.t.tokens * groups, waves = 4 * (int64_t)(keys ? a.k_blocks : a.q_blocks), mine = 4 * (int64_t)((int)blockIdx.x - (keys ? a.q_blocks : 0)) + wave;
-    const int64_t begin = items * mine / waves, end = items * (mine + 1) / waves;
-    P part(a.t, lane);
+    // Runs of `run` groups of rows, dealt to the waves one by one: a token's, or where there are fewer tokens than waves single ones.  (A stretch of its own for each wave
+    // reads the tokens from many places at once: RUNS_FIGURE.)
+    const int waves = 4 * (keys ? a.k_blocks : a.q_blocks), run = a.t.tokens >= waves ? groups : 1;
+    const int64_t items = (int64_t)a.t.tokens * groups, step = (int64_t)waves * run;
+    int64_t at = (int64_t)run * (4 * ((int)blockIdx.x - (keys ? a.q_blocks : 0)) + wave);   // the first item of the run
+    int token = 0, group = 0, left = 0, of = -1;
+    auto start = [&] { token = (int)(at / groups), group = (int)(at - (int64_t)token * groups), left = run; };
+    P part(a.t, lane, (lds_angles *)&angles[wave]);
     float by[16], dw[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) by[i] = dw[i] = 0.0f;
     if (w != nullptr && part.in) P::widen(part.load(w), by);
-    int token = (int)(begin / groups), group = (int)(begin - (int64_t)token * groups), of = -1;
     auto loads = [&](Pieces &p, Pieces &q) {
         const int head = group * P::ROWS + part.r;
         const bool live = part.in && head < heads;
@@ -63,13 +71,20 @@ __global__ __launch_bounds__(256) void rotary_bwd_kernel(const BackwardArgs a)
         q = live && w != nullptr ? part.load(x.p + token * x.token + head * x.head) : Pieces{};
     };
     Pieces next_g{}, next_x{};
-    if (begin < end) loads(next_g, next_x);
-    for (int64_t item = begin; item < end; ++item) {
+    int32_t next_position = 0;
+    bool more = at < items;
+    if (more) start(), loads(next_g, next_x), next_position = part.position(a.t, token);
+    while (more) {
         const Pieces now_g = next_g, now_x = next_x;
+        const int32_t position = next_position;
         const int this_token = token, head = group * P::ROWS + part.r;
-        if (++group == groups) group = 0, ++token;
-        if (item + 1 < end) loads(next_g, next_x);
-        if (of != this_token) part.angles(a.t, this_token, true), of = this_token;
+        ++group;
+        if (--left == 0) {
+            at += step, more = at < items;
+            if (more) start(), next_position = part.position(a.t, token);
+        }
+        if (more) loads(next_g, next_x);
+        if (of != this_token) part.angles(a.t, position, true, lane), of = this_token;
         float g[16];
         P::widen(now_g, g);
         part.turn(g);
@@ -89,7 +104,7 @@ __global__ __launch_bounds__(256) void rotary_bwd_kernel(const BackwardArgs a)
 #pragma unroll
             for (int i = 0; i < 16; ++i) g[i] = r * fmaf(-y[i], mean, g[i]);
         }
-        if (part.in && head < heads) part.store(dx.p + this_token * dx.token + head * dx.head, g);
+        if (part.in && head < heads) part.template store<true>(dx.p + this_token * dx.token + head * dx.head, g);
     }
     if (w == nullptr) return;
 #pragma unroll
@@ -102,23 +117,34 @@ __global__ __launch_bounds__(256) void rotary_bwd_kernel(const BackwardArgs a)
     // in the order of the head's values
     for (int v = threadIdx.x; v < 16 * LANES; v += 256) {
         const int i = v & 15;
-        const P of_lane(a.t, v >> 4);
-        const int at = i < 8 ? of_lane.a + i : of_lane.b + i - 8;
-        if (of_lane.in) a.sums[(int64_t)blockIdx.x * a.t.d + at] = (sums[0][v] + sums[1][v]) + (sums[2][v] + sums[3][v]);
+        const int j = v >> 4;
+        const bool apart = 16 * j < a.t.rotated && !NEIGHBOURS;
+        const int at = apart ? 8 * j + (i & 7) + (i < 8 ? 0 : a.t.rotated >> 1) : v;
+        if (16 * j < a.t.d) a.sums[(int64_t)blockIdx.x * a.t.d + at] = (sums[0][v] + sums[1][v]) + (sums[2][v] + sums[3][v]);
     }
 }
-// dw = beta dw + the workgroups' sums: a workgroup has four values of the queries' weights or of the keys', 64 lanes for each
-__global__ __launch_bounds__(256) void rotary_dw_kernel(const BackwardArgs a)
+// dw = beta dw + the workgroups' sums: a workgroup has sixteen values of the queries' weights or of the keys', and 64 lanes for each
+__global__ __launch_bounds__(1024) void rotary_dw_kernel(const BackwardArgs a)
 {
-    const int lane = threadIdx.x & 63, quarters = a.t.d >> 2, keys = (int)blockIdx.x >= quarters, at = 4 * ((int)blockIdx.x - (keys ? quarters : 0)) + (threadIdx.x >> 6);
+    __shared__ float sums[64][17];
+    const int sixteens = a.t.d >> 4, keys = (int)blockIdx.x >= sixteens, at = 16 * ((int)blockIdx.x - (keys ? sixteens : 0)) + (threadIdx.x & 15), row = threadIdx.x >> 4;
     float *const dw = keys ? a.dwk : a.dwq;
     if (dw == nullptr) return;
-    const int first = keys ? a.q_blocks : 0, count = keys ? a.k_blocks : a.q_blocks;
+    const int count = keys ? a.k_blocks : a.q_blocks;
+    const float *const from = a.sums + (int64_t)(keys ? a.q_blocks : 0) * a.t.d + at;
     float sum = 0.0f;
-    for (int i = lane; i < count; i += 64) sum += a.sums[(int64_t)(first + i) * a.t.d + at];
+#pragma unroll 8
+    for (int i = row; i < count; i += 64) sum += from[(int64_t)i * a.t.d];
+    sums[row][threadIdx.x & 15] = sum;
+    __syncthreads();
+    if (threadIdx.x >= 256) return;
+    const int v = threadIdx.x >> 4, part = threadIdx.x & 15;   // sixteen lanes to a value
+    sum = (sums[part][v] + sums[part + 16][v]) + (sums[part + 32][v] + sums[part + 48][v]);
 #pragma unroll
-    for (int s = 1; s < 64; s <<= 1) sum += __shfl_xor(sum, s);
-    if (lane == 0) dw[at] = a.beta == 0.0f ? sum : fmaf(a.beta, dw[at], sum);
+    for (int s = 1; s < 16; s <<= 1) sum += __shfl_xor(sum, s);
+    if (part != 0) return;
+    float *const to = dw + 16 * ((int)blockIdx.x - (keys ? sixteens : 0)) + v;
+    *to = a.beta == 0.0f ? sum : fmaf(a.beta, *to, sum);
 }
 
 // ------------------------------------------------------------------ host
@@ -228,6 +254,6 @@ extern "C" int s24_rotary_bwd(const s24_rotary *rotary, const int32_t *positions
         if (dt == S24_BF16) gradients<uint16_t>(a, neighbours, grid, st);
         else gradients<s24_half>(a, neighbours, grid, st);
     }
-    rotary_dw_kernel<<<dim3((unsigned)(d / 2)), dim3(256), 0, st>>>(a);
+    rotary_dw_kernel<<<dim3((unsigned)(d / 8)), dim3(1024), 0, st>>>(a);
     return s24_launch_status();
 }
