@@ -17,25 +17,104 @@ struct ChunkArgs {
     Strided q, o;
     const int *cu, *table, *lengths;
     int64_t width;
-    int sequences, tokens, hq, group, causal, parts;
-    bool mix;          // order of the tiles: by length alone, or sequence by sequence
+    int sequences, tokens, hq, group, causal;
+    int pieces;        // that the tiles of a key-value head are cut into at most, as many as the device holds workgroups; 0: none is cut
+    int sum_rows;      // that a workgroup adds the parts of
     float scale;
-    float2 *weights;   // [parts][tokens][hq]: reference and sum
-    float *sums;       // [parts][tokens][hq][d]
+    float2 *weights;   // [hkv][pieces][kChunkRows]: reference and sum
+    float *sums;       // [hkv][pieces][kChunkRows][d]
 };
 constexpr int kChunkRows = 128, kChunkKeys = 64;
 __device__ __forceinline__ Span keys_of(const ChunkArgs &a, int i) { return {0, min(max(a.lengths[i], 0), (int)(a.width << a.c.shift))}; }
-// The workgroup's tile: a sequence, and which of its tiles, the last ones first
-__device__ __forceinline__ bool find_chunk(const ChunkArgs &a, int t, int lane, int &sequence, int &tile)
+__device__ __forceinline__ int row_tiles(const ChunkArgs &a, int i) { return (int)(((int64_t)span(a.cu, i, a.tokens).count * a.group + kChunkRows - 1) / kChunkRows); }
+__device__ __forceinline__ int key_tiles(const ChunkArgs &a, int i) { return (keys_of(a, i).count + kChunkKeys - 1) / kChunkKeys; }
+// Where tiles of rows are few, the positions that they go over are cut into parts, those of a sequence of one size, which leave their sums for another kernel to add; a tile in one part
+// is finished where it is.  A part has about `each` steps (tiles of positions): as few as make no more pieces than the device holds workgroups, two to a compute unit, since
+// a second round would take as long as the first.  (12 sequences of 2 to 512 tokens after up to 4000, 32 heads on 8 of 128, 43 tiles of 35 to 62 steps: PARTS_FIGURE.  Steps dealt out
+// evenly, whatever tiles they belong to, took EVEN_FIGURE: a piece of a tile costs 5 to 10 us besides its steps.)
+constexpr int kFewRows = 32;      // of a sequence
+constexpr int kLeastSteps = 8;    // of a part
+__device__ __forceinline__ bool is_few(const ChunkArgs &a, int i) { return (int64_t)span(a.cu, i, a.tokens).count * a.group <= kFewRows; }
+__device__ __forceinline__ int lanes_sum(int x)
 {
-    int at;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) x += __shfl_xor(x, s);
+    return __builtin_amdgcn_readfirstlane(x);
+}
+struct Parts { int count, steps; };   // of a tile of a sequence, and the steps of each
+__device__ __forceinline__ Parts parts_in(int keys, int each)
+{
+    const int count = max(1, (int)((2 * (unsigned)keys + each) / (2 * (unsigned)each)));
+    return {count, (keys + count - 1) / count};
+}
+__device__ __forceinline__ Parts parts_of(const ChunkArgs &a, int each, int i) { return parts_in(key_tiles(a, i), each); }
+__device__ __forceinline__ int steps_of_parts(const ChunkArgs &a, int lane)
+{
+    int64_t steps = 0;
+    int longest = 0, tiles = 0;
+    for (int i = lane; i < a.sequences; i += 64) {
+        const int n = row_tiles(a, i), keys = key_tiles(a, i);
+        steps += (int64_t)n * keys, tiles += n, longest = n > 0 ? max(longest, keys) : longest;
+    }
+    const int mine = tiles;   // of the lane's sequence, where each has one
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) steps += __shfl_xor(steps, s), tiles += __shfl_xor(tiles, s), longest = max(longest, __shfl_xor(longest, s));
+    longest = max(__builtin_amdgcn_readfirstlane(longest), 1), tiles = __builtin_amdgcn_readfirstlane(tiles);
+    // (More steps than the host has seen to have offsets that do not ascend: then nothing is cut.)
+    const int all = __builtin_amdgcn_readfirstlane(steps <= INT32_MAX / 2 ? (int)steps : INT32_MAX);
+    if (tiles > a.pieces || all == INT32_MAX) return longest;
+    if (a.sequences > 64) return max(2 * (all / a.pieces) + 1, min(kLeastSteps, longest));   // (count <= 4/3 of the quotient in what is cut: no more than a.pieces)
+    const int keys = lane < a.sequences ? key_tiles(a, lane) : 0;
+    int lo = max(all / a.pieces, min(kLeastSteps, longest)), hi = max(longest, lo);   // `hi` makes few enough pieces
+    while (lo < hi) {
+        const int middle = (lo + hi) >> 1;
+        if (lanes_sum(mine * parts_in(keys, middle).count) <= a.pieces) hi = middle;
+        else lo = middle + 1;
+    }
+    return hi;
+}
+// Sums that the sequences before this one leave
+__device__ __forceinline__ int slots_before(const ChunkArgs &a, int each, int sequence, int lane)
+{
+    int before = 0;
+    for (int i = lane; i < sequence; i += 64) {
+        const int count = parts_of(a, each, i).count;
+        before += count > 1 ? row_tiles(a, i) * count : 0;
+    }
+    return lanes_sum(before);
+}
+// A workgroup's work: steps begin .. end - 1 of a tile of rows (its steps are all of the sequence's); where its sums go, or -1: to O
+struct Piece { int sequence, tile, begin, end, slot; };
+// Piece t of those of a key-value head: the longest come first, and those of few rows last; of a sequence all tiles' first parts, then all tiles' next ones, so that workgroups which
+// run at the same time read the same positions.
+__device__ __forceinline__ bool find_part(const ChunkArgs &a, int t, int lane, Piece &piece)
+{
+    const int each = steps_of_parts(a, lane), most = (int)((a.width << a.c.shift) / kChunkKeys) + 2;
+    int wide = 0, sequence, at;
+    for (int i = lane; i < a.sequences; i += 64) wide += is_few(a, i) ? 0 : row_tiles(a, i) * parts_of(a, each, i).count;
+    wide = lanes_sum(wide);
+    const bool few = t >= wide;
     auto of = [&](int i) {
-        const int n = (int)(((int64_t)span(a.cu, i, a.tokens).count * a.group + kChunkRows - 1) / kChunkRows), keys = (int)(((int64_t)keys_of(a, i).count * a.group + kChunkRows - 1) / kChunkRows);
+        const Parts p = parts_of(a, each, i);
+        return is_few(a, i) == few ? Lengths{row_tiles(a, i) * p.count, INT32_MAX, max(p.steps, 1)} : Lengths{0, 0, 0};
+    };
+    if (!find_by_length(true, a.sequences, few ? t - wide : t, most, lane, sequence, at, of)) return false;
+    const Parts p = parts_of(a, each, sequence);
+    const int n = row_tiles(a, sequence), part = at / n, slot = p.count == 1 ? -1 : slots_before(a, each, sequence, lane) + at;
+    piece = {sequence, n - 1 - (at - part * n), part * p.steps, min(key_tiles(a, sequence), (part + 1) * p.steps), slot};
+    return at >= 0 && part < p.count && slot < a.pieces;   // (as they are, where the offsets ascend)
+}
+// The workgroup's tile where each has one: a sequence, and which of its tiles, the last ones first.  The longest come first.
+__device__ __forceinline__ bool find_chunk(const ChunkArgs &a, int t, int lane, Piece &piece)
+{
+    int sequence, at;
+    auto of = [&](int i) {
+        const int n = row_tiles(a, i), keys = (int)(((int64_t)keys_of(a, i).count * a.group + kChunkRows - 1) / kChunkRows);
         return a.causal ? Lengths{n, max(keys, n), INT32_MAX} : Lengths{n, INT32_MAX, max(keys, 1)};
     };
     const int64_t most = max((int64_t)a.tokens, a.width << a.c.shift) * a.group / kChunkRows + 1;
-    if (!find_by_length(a.mix, a.sequences, t, (int)most, lane, sequence, at, of)) return false;
-    tile = of(sequence).tiles - 1 - at;
+    if (!find_by_length(true, a.sequences, t, (int)most, lane, sequence, at, of)) return false;
+    piece = {sequence, row_tiles(a, sequence) - 1 - at, 0, key_tiles(a, sequence), -1};
     return true;
 }
 
@@ -113,25 +192,295 @@ template <int D> struct Sixteen<D, 8> {
     }
 };
 
-// D: values of a tile's row; E: values that the products go over
-template <typename T, int D, int E, int BITS>
-__global__ __launch_bounds__(256, 2) void chunk_kernel(const ChunkArgs a)
+// Where a row's sums lie
+__device__ __forceinline__ int64_t slot_row(const ChunkArgs &a, int kv, int slot, int row) { return ((int64_t)kv * a.pieces + slot) * kChunkRows + row; }
+// The result of a row (a lane has 4 of each 16 values; `sum` of its weights): to O, or as sums
+template <typename T, int E> __device__ __forceinline__ void write_row(const ChunkArgs &a, const Queries::Row &of, f32x4 (&o)[E / 16], float m, float sum, int kv, int slot, int row, bool live, int g)
+{
+    const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
+    if (slot < 0) {
+        uint16_t *out = a.o.p + of.token * a.o.token + of.head * a.o.head;
+#pragma unroll
+        for (int n = 0; n < E / 16; n += 4) {   // of four such pieces of a row a lane gets one whole: lines are written with few stores
+            uint32_t x[4], y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x4 v = n + i < E / 16 ? o[n + i < E / 16 ? n + i : 0] * inverse : f32x4{};
+                x[i] = pack2<T>(v[0], v[1]), y[i] = pack2<T>(v[2], v[3]);
+            }
+            transpose_rows(x), transpose_rows(y);
+            const int at = 16 * (n + g);
+            if (at >= a.c.d || !live) continue;
+            *reinterpret_cast<uint4 *>(out + at) = make_uint4(x[0], y[0], x[1], y[1]);
+            *reinterpret_cast<uint4 *>(out + at + 8) = make_uint4(x[2], y[2], x[3], y[3]);
+        }
+    } else if (live) {
+        const int64_t at = slot_row(a, kv, slot, row);
+#pragma unroll
+        for (int n = 0; n < E / 16; ++n)
+            if (16 * n < a.c.d) *reinterpret_cast<f32x4 *>(a.sums + at * a.c.d + 16 * n + 4 * g) = o[n];
+        if (g == 0) a.weights[at] = make_float2(m, sum);
+    }
+}
+
+// What the reference and the sums of a row (a column of the products) are taken to when its scores grow.  In an 8-bit cache the reference has a factor for the steps of V, which
+// are at most `wide`.
+template <int BITS> struct Reference {
+    float rise = BITS == 8 ? -100.0f : 0.0f, wide = 0x1p-100f;
+    // Whether scores up to `top` (or steps up to `step`) ask for another one
+    __device__ __forceinline__ bool low(float m, float top, float step) const { return top > m - rise + kGrowth || (BITS == 8 && step > wide); }
+    // Its new part from the steps
+    __device__ __forceinline__ float lift(float step)
+    {
+        if (BITS != 8) return 0.0f;
+        step = column_max(step);
+        if (step > wide) wide = 2.0f * step;
+        return __builtin_amdgcn_logf(wide);
+    }
+};
+
+// Queries as operands, and the factor of their scores.  8 bits: scaled by a power of two into what binary16 holds
+template <typename T, int N> __device__ __forceinline__ float scaled_queries(uint4 (&q)[N], float c)
+{
+    using Num = s24_num<T>;
+    float most = 0.0f;
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+        for (const uint32_t x : {q[k].x, q[k].y, q[k].z, q[k].w}) most = fmaxf(most, fmaxf(fabsf(Num::lo(x)), fabsf(Num::hi(x))));
+    most = column_max(most);
+    const int e = most > 0.0f ? ilogbf(most) : 0;
+    auto scaled = [&](uint32_t x) { return pack2<s24_half>(ldexpf(Num::lo(x), -e), ldexpf(Num::hi(x), -e)); };
+#pragma unroll
+    for (int k = 0; k < N; ++k) q[k] = make_uint4(scaled(q[k].x), scaled(q[k].y), scaled(q[k].z), scaled(q[k].w));
+    return ldexpf(c, e);
+}
+
+// A sequence of up to 32 rows (a few tokens, such as drafted ones): each of the four waves has all of the rows and a quarter of the piece's positions, and goes over them 32 at a
+// time from memory to registers, as in the attention of one token; their sums are added in LDS.  Bound by memory.
+// Row 4g + r of tile t of a product is position 8g + 4t + r, so that a lane's weights are those of 8 consecutive ones.
+// (HEAD: values of a head, with which the addresses within a page are constants.)
+template <typename T, int HEAD, int BITS, int TILE>
+__device__ __forceinline__ void few_rows(const ChunkArgs &a, const Queries &s_, const int *table, int kv, int begin, int tiles, int slot, int lane, int wave, lds_byte *lds_k, lds_byte *lds_v)
 {
     using M = typename std::conditional<BITS == 8, s24_half, T>::type;
-    using Num = s24_num<T>;
-    constexpr int BK = kChunkKeys, TILE = BK * 2 * D;
-    __shared__ __align__(16) unsigned char lds_k[2][TILE], lds_v[2][TILE];
-    __shared__ __align__(16) float steps[2][BITS == 8 ? 2 * BK : 4];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int BK = 32, d = HEAD, token = d * (BITS / 8);   // bytes of a token of one head
+    constexpr int KL = BITS == 8 ? (d + 63) / 64 : (d + 31) / 32, QL = BITS == 8 ? 2 * KL : KL;
     const int col = lane & 15, g = lane >> 4;
-    const Unit unit = unit_of(blockIdx.x, a.c.hkv, a.parts);
-    const int kv = unit.head;
-    int sequence, index;
-    if (!find_chunk(a, unit.tile, lane, sequence, index)) return;
+    const int length = s_.k.count, all_units = max(min(2 * tiles, (s_.seen + BK - 1) / BK) - 2 * begin, 0);
+    const int first = 2 * begin + all_units * wave / 4, end = 2 * begin + all_units * (wave + 1) / 4;
+
+    uint4 q[2][QL];
+    int last[2];
+    float c[2];
+    Queries::Row of[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        of[j] = s_.row(a.group, kv, 16 * j + col);
+        last[j] = a.causal ? min(length - 1, of[j].at + s_.ahead) : length - 1;
+        const uint16_t *row = a.q.p + of[j].token * a.q.token + of[j].head * a.q.head;
+        c[j] = a.scale * kLog2e;
+#pragma unroll
+        for (int k = 0; k < QL; ++k) {
+            const int i = BITS == 8 ? 64 * (k >> 1) + 16 * g + 8 * (k & 1) : 32 * k + 8 * g;
+            q[j][k] = i < d ? *reinterpret_cast<const uint4 *>(row + i) : make_uint4(0, 0, 0, 0);
+        }
+        if (BITS == 8) c[j] = scaled_queries<T>(q[j], c[j]);
+    }
+    const int all = __builtin_amdgcn_readfirstlane(last[0]) + 1;   // positions that all of the rows see: what the first one does
+
+    // A unit's positions 8*(col/4) .. for K, 8*g .. for V: each sixteen lie in one page.
+    auto position = [&](int t, int eight) { return min(t * BK + 16 * (eight >> 1), (length - 1) & ~15); };
+    struct Pages { uint32_t k, v; };
+    auto pages = [&](int t) { return Pages{(uint32_t)table[position(t, col >> 2) >> a.c.shift], (uint32_t)table[position(t, g) >> a.c.shift]}; };
+    // of the sixteen, in tokens of one head
+    auto place = [&](int t, int eight, uint32_t id) {
+        return (((int64_t)min(id, (uint32_t)a.c.pages - 1) * a.c.hkv + kv) << a.c.shift) + (position(t, eight) & (a.c.page - 1));
+    };
+    typedef typename std::conditional<BITS == 8, uint2, uint4>::type Values;   // 8 positions of a channel
+    typedef typename std::conditional<BITS == 8, unsigned int __attribute__((ext_vector_type(2))), s24_u32x4>::type Loaded;
+    uint4 fk[2][KL];
+    Values fv[d / 16];
+    f32x4 sk[2], sv[2];
+    auto load_k = [&](int t, Pages p) {
+        const unsigned char *from = a.c.k + (place(t, col >> 2, p.k) + 8 * (col >> 2 & 1) + (col & 3)) * token;
+        const float *step = a.c.ks + place(t, g, p.v) + 8 * (g & 1);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+            for (int k = 0; k < KL; ++k)   // (past the head's end the query has zeros)
+                fk[i][k] = s24_load_stream(from + 4 * i * token + 16 * (64 * k + 64 <= token ? 4 * k + g : min(4 * k + g, (token >> 4) - 1)));
+            if (BITS == 8) sk[i] = *reinterpret_cast<const f32x4 *>(step + 4 * i);
+        }
+    };
+    auto load_v = [&](int t, Pages p) {
+        const int64_t at = place(t, g, p.v);
+        const unsigned char *from = a.c.v + at * token + (BITS == 8 ? 8 * (g & 1) : (g & 1) * d * 16);
+        const float *step = a.c.vs + at + 8 * (g & 1);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (BITS == 8) sv[i] = *reinterpret_cast<const f32x4 *>(step + 4 * i);
+#pragma unroll
+        for (int n = 0; n < d / 16; ++n) fv[n] = __builtin_bit_cast(Values, __builtin_nontemporal_load(reinterpret_cast<const Loaded *>(from + (16 * n + col) * 16)));
+    };
+    float m[2] = {-1e30f, -1e30f}, l[2] = {0.0f, 0.0f};
+    Reference<BITS> reference;
+    f32x4 o[2][d / 16];
+#pragma unroll
+    for (int n = 0; n < d / 16; ++n) o[0][n] = o[1][n] = f32x4{};
+    Pages next{};
+    if (first < end) {
+        const Pages now = pages(first);
+        load_k(first, now), load_v(first, now);
+        if (first + 1 < end) next = pages(first + 1);
+    }
+    // The loads run ahead: a unit's keys are asked for as soon as the scores before them are formed, its values as soon as the ones before are summed, its pages a unit before that.
+    for (int t = first; t < end; ++t) {
+        const Pages coming = next;
+        if (t + 2 < end) next = pages(t + 2);
+        const int k0 = t * BK;
+        f32x4 s[2][2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            s[i][0] = s[i][1] = f32x4{};
+#pragma unroll
+            for (int k = 0; k < KL; ++k)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    if constexpr (BITS == 8) {
+                        s[i][j] = mma<M>(halves(fk[i][k].x, fk[i][k].y), q[j][2 * k], s[i][j]);
+                        s[i][j] = mma<M>(halves(fk[i][k].z, fk[i][k].w), q[j][2 * k + 1], s[i][j]);
+                    } else
+                        s[i][j] = mma<M>(fk[i][k], q[j][k], s[i][j]);
+                }
+            if (BITS == 8) s[i][0] *= sk[i], s[i][1] *= sk[i];
+        }
+        if (t + 1 < end) load_k(t + 1, coming);
+        if (k0 + BK > all) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[i][j][r] = k0 + 8 * g + 4 * i + r <= last[j] ? s[i][j][r] : -INFINITY;
+        }
+        if (k0 + BK > length) {   // what lies past the sequence's end may hold anything
+            if constexpr (BITS == 8) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) sv[i][r] = k0 + 8 * g + 4 * i + r < length ? sv[i][r] : 0.0f;
+            } else {
+#pragma unroll
+                for (int n = 0; n < d / 16; ++n) {
+                    uint32_t *x = reinterpret_cast<uint32_t *>(&fv[n]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int left = length - (k0 + 8 * g + 2 * i);
+                        x[i] = left >= 2 ? x[i] : left == 1 ? x[i] & 0xFFFFu : 0u;
+                    }
+                }
+            }
+        }
+        float top[2], step = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            top[j] = s[0][j][0];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) top[j] = fmaxf(top[j], s[i][j][r]);
+            top[j] *= c[j];
+        }
+        if (BITS == 8) step = fmaxf(fmaxf(fmaxf(sv[0][0], sv[0][1]), fmaxf(sv[0][2], sv[0][3])), fmaxf(fmaxf(sv[1][0], sv[1][1]), fmaxf(sv[1][2], sv[1][3])));
+        if (__any(reference.low(m[0], top[0], step) || reference.low(m[1], top[1], step))) {
+            const float before = reference.rise, lift = reference.lift(step);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float now = fmaxf(m[j] - before, column_max(top[j])) + lift, shrink = __builtin_amdgcn_exp2f(m[j] - now);
+                m[j] = now, l[j] *= shrink;
+#pragma unroll
+                for (int n = 0; n < d / 16; ++n) o[j][n] *= shrink;
+            }
+            reference.rise = lift;
+        }
+        uint4 p[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    s[i][j][r] = __builtin_amdgcn_exp2f(fmaf(s[i][j][r], c[j], -m[j]));
+                    l[j] += s[i][j][r];
+                }
+                if (BITS == 8) s[i][j] *= sv[i];
+            }
+            p[j] = operand<M>(s[0][j], s[1][j]);
+        }
+#pragma unroll
+        for (int n = 0; n < d / 16; ++n) {
+            uint4 f;
+            if constexpr (BITS == 8) f = halves(fv[n].x, fv[n].y);
+            else f = fv[n];
+            o[0][n] = mma<M>(f, p[0], o[0][n]);
+            o[1][n] = mma<M>(f, p[1], o[1][n]);
+        }
+        if (t + 1 < end) load_v(t + 1, coming);
+    }
+    // The waves' sums, in order
+    typedef __attribute__((address_space(3))) f32x2 lds_f32x2;
+    static_assert(d / 16 * 2048 <= TILE && 3 * 1024 <= TILE, "the sums must fit");
+    auto sums = [&](int w) { return w == 3 ? lds_v : lds_k + (w - 1) * TILE; };
+    lds_byte *const weights = lds_v + TILE;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) l[j] = column_sum(l[j]);
+    if (wave > 0) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int n = 0; n < d / 16; ++n) lds_store(sums(wave) + (j * (d / 16) + n) * 1024 + 16 * lane, o[j][n]);
+            *(lds_f32x2 *)(weights + ((2 * wave - 2 + j) * 64 + lane) * 8) = f32x2{m[j], l[j]};
+        }
+    }
+    wait_and_barrier<0>();
+    if (wave > 0) return;
+    for (int w = 1; w < 4; ++w)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const f32x2 theirs = *(const lds_f32x2 *)(weights + ((2 * w - 2 + j) * 64 + lane) * 8);
+            const float now = fmaxf(m[j], theirs[0]), f = __builtin_amdgcn_exp2f(m[j] - now), h = __builtin_amdgcn_exp2f(theirs[0] - now);
+            m[j] = now, l[j] = fmaf(l[j], f, theirs[1] * h);
+#pragma unroll
+            for (int n = 0; n < d / 16; ++n) o[j][n] = o[j][n] * f + __builtin_bit_cast(f32x4, lds_load(sums(w) + (j * (d / 16) + n) * 1024 + 16 * lane)) * h;
+        }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) write_row<T, d>(a, of[j], o[j], m[j], l[j], kv, slot, 16 * j + col, 16 * j + col < s_.rows, g);
+}
+
+template <int D, int BITS> struct ChunkLds {
+    static constexpr int TILE = kChunkKeys * 2 * D;
+    unsigned char (&k)[2][TILE], (&v)[2][TILE];
+    float (&steps)[2][BITS == 8 ? 2 * kChunkKeys : 4];
+};
+// D: values of a tile's row; E: values that the products go over
+// HEAD: values of a head, where sequences of few rows are taken apart; 0: they are not
+template <typename T, int D, int E, int BITS, int HEAD> __device__ __forceinline__ void chunk_piece(const ChunkArgs &a, const Piece &piece, int kv, int lane, int wave, const ChunkLds<D, BITS> &lds)
+{
+    using M = typename std::conditional<BITS == 8, s24_half, T>::type;
+    constexpr int BK = kChunkKeys;
+    const int col = lane & 15, g = lane >> 4;
+    auto &lds_k = lds.k, &lds_v = lds.v;
+    auto &steps = lds.steps;
     Queries s_;
-    s_.init(span(a.cu, sequence, a.tokens), keys_of(a, sequence), a.group, a.causal, index, kChunkRows, 32 * wave);
-    const int length = s_.k.count, all_tiles = s_.seen > 0 ? (s_.seen + BK - 1) / BK : 0;
-    const int begin = (int)((int64_t)all_tiles * unit.part / a.parts), tiles = (int)((int64_t)all_tiles * (unit.part + 1) / a.parts);
+    s_.init(span(a.cu, piece.sequence, a.tokens), keys_of(a, piece.sequence), a.group, a.causal, piece.tile, kChunkRows, 32 * wave);
+    const int length = s_.k.count, all_tiles = s_.seen > 0 ? (s_.seen + BK - 1) / BK : 0, begin = piece.begin, tiles = min(all_tiles, piece.end);
+    const int *table = a.table + piece.sequence * a.width;
+    if constexpr (HEAD > 0) {
+        if (s_.rows <= kFewRows) {
+            few_rows<T, HEAD, BITS, ChunkLds<D, BITS>::TILE>(a, s_, table, kv, begin, tiles, piece.slot, lane, wave, (lds_byte *)lds_k, (lds_byte *)lds_v);
+            return;
+        }
+    }
 
     uint4 q[2][E / 32];
     int last[2];     // that a row sees
@@ -145,28 +494,16 @@ __global__ __launch_bounds__(256, 2) void chunk_kernel(const ChunkArgs a)
 #pragma unroll
         for (int k = 0; k < E / 32; ++k)
             q[j][k] = 32 * k + 8 * g < a.c.d ? *reinterpret_cast<const uint4 *>(row + 32 * k + 8 * g) : make_uint4(0, 0, 0, 0);
-        if constexpr (BITS == 8) {   // scaled by a power of two into what binary16 holds
-            float most = 0.0f;
-#pragma unroll
-            for (int k = 0; k < E / 32; ++k)
-                for (const uint32_t x : {q[j][k].x, q[j][k].y, q[j][k].z, q[j][k].w}) most = fmaxf(most, fmaxf(fabsf(Num::lo(x)), fabsf(Num::hi(x))));
-            most = column_max(most);
-            const int e = most > 0.0f ? ilogbf(most) : 0;
-            auto scaled = [&](uint32_t x) { return pack2<s24_half>(ldexpf(Num::lo(x), -e), ldexpf(Num::hi(x), -e)); };
-#pragma unroll
-            for (int k = 0; k < E / 32; ++k) q[j][k] = make_uint4(scaled(q[j][k].x), scaled(q[j][k].y), scaled(q[j][k].z), scaled(q[j][k].w));
-            c[j] = ldexpf(c[j], e);
-        }
+        if (BITS == 8) c[j] = scaled_queries<T>(q[j], c[j]);
     }
     float m[2] = {-1e30f, -1e30f}, l[2] = {0.0f, 0.0f};
-    float rise = BITS == 8 ? -100.0f : 0.0f, wide = 0x1p-100f;   // the reference's part from the steps of V, which are at most `wide`
-    f32x4 o[E / 16][2];
+    Reference<BITS> reference;
+    f32x4 o[2][E / 16];
 #pragma unroll
-    for (int n = 0; n < E / 16; ++n) o[n][0] = o[n][1] = f32x4{};
+    for (int n = 0; n < E / 16; ++n) o[0][n] = o[1][n] = f32x4{};
 
     Sixteen<D, BITS> sixteen;
     sixteen.init(a.c, wave, lane);
-    const int *table = a.table + sequence * a.width;
     // Where the wave's positions of tile t are, in tokens of one head.  (Those past the sequence's end are its last ones again.)
     auto page_of = [&](int t) {
         const int pos = min(t * BK + 16 * wave, (length - 1) & ~15);
@@ -248,20 +585,16 @@ __global__ __launch_bounds__(256, 2) void chunk_kernel(const ChunkArgs a)
                     for (int r = 0; r < 4; ++r) top[j] = fmaxf(top[j], s[i][j][r]);
                 top[j] *= c[j];
             }
-            if (__any(top[0] > m[0] - rise + kGrowth || top[1] > m[1] - rise + kGrowth || (BITS == 8 && step > wide))) {
-                if (BITS == 8) {
-                    step = column_max(step);
-                    if (step > wide) wide = 2.0f * step;
-                }
-                const float lift = BITS == 8 ? __builtin_amdgcn_logf(wide) : 0.0f;
+            if (__any(reference.low(m[0], top[0], step) || reference.low(m[1], top[1], step))) {
+                const float before = reference.rise, lift = reference.lift(step);
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const float now = fmaxf(m[j] - rise, column_max(top[j])) + lift, shrink = __builtin_amdgcn_exp2f(m[j] - now);
+                    const float now = fmaxf(m[j] - before, column_max(top[j])) + lift, shrink = __builtin_amdgcn_exp2f(m[j] - now);
                     m[j] = now, l[j] *= shrink;
 #pragma unroll
-                    for (int n = 0; n < E / 16; ++n) o[n][j] *= shrink;
+                    for (int n = 0; n < E / 16; ++n) o[j][n] *= shrink;
                 }
-                rise = lift;
+                reference.rise = lift;
             }
             uint4 p[2][2];
 #pragma unroll
@@ -283,8 +616,8 @@ __global__ __launch_bounds__(256, 2) void chunk_kernel(const ChunkArgs a)
 #pragma unroll
                 for (int n = 0; n < E / 16; ++n) {
                     const uint4 f = lds_load(tv + ((2 * g + u) * D + 16 * n + col) * 16);
-                    o[n][0] = mma<M>(f, p[u][0], o[n][0]);
-                    o[n][1] = mma<M>(f, p[u][1], o[n][1]);
+                    o[0][n] = mma<M>(f, p[u][0], o[0][n]);
+                    o[1][n] = mma<M>(f, p[u][1], o[1][n]);
                 }
         }
         if (t + 1 < tiles) sixteen.finish((lds_byte *)lds_k[other], (lds_byte *)lds_v[other], steps[other], length - (t + 1) * BK - 16 * wave);
@@ -292,79 +625,120 @@ __global__ __launch_bounds__(256, 2) void chunk_kernel(const ChunkArgs a)
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const int row = 32 * wave + 16 * j + col;
-        const float sum = column_sum(l[j]), inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
-        if (s_.row0 + row >= s_.rows) continue;
-        const Queries::Row of = s_.row(a.group, kv, row);
-        if (a.parts == 1) {
-            uint16_t *out = a.o.p + of.token * a.o.token + of.head * a.o.head;
-#pragma unroll
-            for (int n = 0; n < E / 16; n += 4) {   // of four such pieces of a row a lane gets one whole: lines are written with few stores
-                uint32_t x[4], y[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const f32x4 v = n + i < E / 16 ? o[n + i < E / 16 ? n + i : 0][j] * inverse : f32x4{};
-                    x[i] = pack2<T>(v[0], v[1]), y[i] = pack2<T>(v[2], v[3]);
-                }
-                transpose_rows(x), transpose_rows(y);
-                const int at = 16 * (n + g);
-                if (at >= a.c.d) continue;
-                *reinterpret_cast<uint4 *>(out + at) = make_uint4(x[0], y[0], x[1], y[1]);
-                *reinterpret_cast<uint4 *>(out + at + 8) = make_uint4(x[2], y[2], x[3], y[3]);
-            }
-        } else {
-            const int64_t at = (unit.part * (int64_t)a.tokens + of.token) * a.hq + of.head;
-#pragma unroll
-            for (int n = 0; n < E / 16; ++n)
-                if (16 * n < a.c.d) *reinterpret_cast<f32x4 *>(a.sums + at * a.c.d + 16 * n + 4 * g) = o[n][j];
-            if (g == 0) a.weights[at] = make_float2(m[j], sum);
-        }
+        write_row<T, E>(a, s_.row(a.group, kv, row), o[j], m[j], column_sum(l[j]), kv, piece.slot, row, s_.row0 + row < s_.rows, g);
     }
 }
 
-// O from the sums of the parts
+template <typename T, int D, int E, int BITS, int HEAD>
+__global__ __launch_bounds__(256, 2) void chunk_kernel(const ChunkArgs a)
+{
+    using Lds = ChunkLds<D, BITS>;
+    __shared__ __align__(16) unsigned char lds_k[2][Lds::TILE], lds_v[2][Lds::TILE];
+    __shared__ __align__(16) float steps[2][BITS == 8 ? 2 * kChunkKeys : 4];
+    const Lds lds{lds_k, lds_v, steps};
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    const Unit unit = unit_of(blockIdx.x, a.c.hkv, 1);
+    Piece piece;
+    if (HEAD == 0 ? !find_chunk(a, unit.tile, lane, piece) : !find_part(a, unit.tile, lane, piece)) return;
+    chunk_piece<T, D, E, BITS, HEAD>(a, piece, unit.head, lane, wave, lds);
+}
+
+// O of rows whose tiles lie in several parts, from the sums that these left (those of a part past the causal diagonal have no weight).  A workgroup has a.sum_rows rows of a tile, eight
+// at a time by 32 lanes each, which add four values; where it has fewer the lanes that are left take every second, fourth or eighth part.
 template <typename T>
 __global__ __launch_bounds__(256) void chunk_join_kernel(const ChunkArgs a)
 {
-    Joined j;
-    if (!join_rows(a.cu, a.sequences, a.tokens, a.hq, j)) return;
-    const int d = a.c.d, quads = d >> 2;
-    const int64_t step = (int64_t)a.tokens * a.hq;
-    for (int item = threadIdx.x; item < j.rows * quads; item += 256) {
-        const int row = item / quads, i = 4 * (item - row * quads);
-        const int64_t t = j.first + row, at = t * a.hq + j.head;
+    constexpr int AT_ONCE = 4;
+    __shared__ float shared[256][7];
+    const int block = blockIdx.x / a.c.hkv, kv = blockIdx.x - block * a.c.hkv, lane = threadIdx.x & 63;
+    int sequence, index, unused;
+    if (!find_item(a.sequences, block, lane, sequence, index, unused, [&](int i) { return (int)(((int64_t)span(a.cu, i, a.tokens).count * a.group + a.sum_rows - 1) / a.sum_rows); })) return;
+    const int each = steps_of_parts(a, lane), parts = parts_of(a, each, sequence).count, n = row_tiles(a, sequence);
+    if (parts == 1) return;
+    const int before = slots_before(a, each, sequence, lane);
+    if (before + n * parts > a.pieces) return;
+    const Span s = span(a.cu, sequence, a.tokens);
+    const int row0 = index * a.sum_rows, rows = min(a.sum_rows, s.count * a.group - row0), tile = row0 / kChunkRows, d = a.c.d;
+    const int64_t first = slot_row(a, kv, before + n - 1 - tile, row0 - tile * kChunkRows), step = (int64_t)n * kChunkRows;   // from part to part
+    const int at_a_time = min(a.sum_rows, 8), groups = 8 / at_a_time, group = threadIdx.x / (32 * at_a_time), quad = threadIdx.x & 31, i = min(4 * quad, d - 4);
+    for (int base = 0; base < rows; base += at_a_time) {
+        const int row = base + (threadIdx.x >> 5) % at_a_time, of = min(row, rows - 1);
         float m = -1e30f, l = 0.0f;
-        for (int p = 0; p < a.parts; ++p) m = fmaxf(m, a.weights[at + p * step].x);
         f32x4 x = {};
-        for (int p = 0; p < a.parts; ++p) {
-            const float2 w = a.weights[at + p * step];
-            const float f = __builtin_amdgcn_exp2f(w.x - m);
-            l = fmaf(w.y, f, l), x += *reinterpret_cast<const f32x4 *>(a.sums + (at + p * step) * d + i) * f;
+        for (int p = group; p < parts; p += AT_ONCE * groups) {
+            float2 w[AT_ONCE];
+            f32x4 v[AT_ONCE];
+            float now = m;
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const int64_t at = first + of + min(p + u * groups, parts - 1) * step;
+                w[u] = a.weights[at], v[u] = *reinterpret_cast<const f32x4 *>(a.sums + at * d + i);
+            }
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                if (p + u * groups >= parts) w[u].y = 0.0f;
+                now = w[u].y != 0.0f ? fmaxf(now, w[u].x) : now;
+            }
+            const float f = __builtin_amdgcn_exp2f(m - now);
+            m = now, l *= f, x *= f;
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const float h = w[u].y != 0.0f ? __builtin_amdgcn_exp2f(w[u].x - now) : 0.0f;
+                l = fmaf(w[u].y, h, l), x += w[u].y != 0.0f ? v[u] * h : f32x4{};
+            }
         }
+        if (groups > 1) {   // (then there is one turn)
+            float *const mine = shared[threadIdx.x];
+            mine[0] = m, mine[1] = l, mine[2] = x[0], mine[3] = x[1], mine[4] = x[2], mine[5] = x[3];
+            __syncthreads();
+            if (group > 0) return;
+            for (int k = 1; k < groups; ++k) {
+                const float *const theirs = shared[threadIdx.x + 32 * at_a_time * k];
+                const float now = fmaxf(m, theirs[0]), f = __builtin_amdgcn_exp2f(m - now), h = __builtin_amdgcn_exp2f(theirs[0] - now);
+                m = now, l = fmaf(l, f, theirs[1] * h), x = x * f + f32x4{theirs[2], theirs[3], theirs[4], theirs[5]} * h;
+            }
+        }
+        if (row >= rows || 4 * quad >= d) continue;
         x *= l == 0.0f ? 0.0f : 1.0f / l;
-        *reinterpret_cast<uint2 *>(a.o.p + t * a.o.token + j.head * a.o.head + i) = make_uint2(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]));
+        const int token = (row0 + row) / a.group, head = kv * a.group + row0 + row - token * a.group;
+        *reinterpret_cast<uint2 *>(a.o.p + (s.first + token) * a.o.token + head * a.o.head + 4 * quad) = make_uint2(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]));
     }
 }
 
 // ------------------------------------------------------------------ host
-static int64_t chunk_groups(int64_t tokens, int64_t sequences, int64_t hq, int64_t hkv)
+// Tiles of rows of a key-value head at most, and pieces that they are cut into; 0: none is, where there are so many that the device is full to the end anyway
+static int64_t chunk_tiles(const s24_kv_cache *c, int64_t tokens, int64_t sequences, int64_t hq)
 {
-    return (tokens * (hq / hkv) / kChunkRows + (tokens < sequences ? tokens : sequences)) * hkv;
+    return tokens * (hq / c->hkv) / kChunkRows + (tokens < sequences ? tokens : sequences);
 }
-// Parts of the positions, by the estimate of the forward pass; the host knows of the lengths only what the table holds
-static int chunk_parts(const s24_kv_cache *c, int64_t width, int64_t tokens, int64_t sequences, int64_t hq)
+static int64_t chunk_pieces(const s24_kv_cache *c, int64_t width, int64_t tokens, int64_t sequences, int64_t hq)
 {
-    return parts_for((double)chunk_groups(tokens, sequences, hq, c->hkv), (double)(width * c->page) / kChunkKeys, 1.0, c->d <= 64 ? 1.05 : 1.5,
-                     (double)tokens * (double)hq * (double)c->d * 4.0);
+    const int64_t held = 2 * (int64_t)s24_cu_count(), steps = (width * c->page + kChunkKeys - 1) / kChunkKeys, tiles = chunk_tiles(c, tokens, sequences, hq);
+    if (tokens * (hq / c->hkv) / kChunkRows * c->hkv >= 2 * held || steps <= kLeastSteps || tiles * steps > INT32_MAX / 2) return 0;   // (steps are counted in an int)
+    const int64_t of_head = held / c->hkv, worth = tiles * (1 + steps / kLeastSteps);   // no more than have so many steps each
+    return of_head < worth ? of_head : worth;
 }
-static int64_t weight_bytes(int64_t tokens, int64_t hq) { return (tokens * hq * (int64_t)sizeof(float2) + 15) / 16 * 16; }
-
 template <typename T, int BITS> static void chunk(const ChunkArgs &a, dim3 grid, dim3 join, hipStream_t st)
 {
     const dim3 block(256);
-    if (a.c.d <= 64) chunk_kernel<T, 64, 64, BITS><<<grid, block, 0, st>>>(a);
-    else if (a.c.d <= 96) chunk_kernel<T, 128, 96, BITS><<<grid, block, 0, st>>>(a);
-    else chunk_kernel<T, 128, 128, BITS><<<grid, block, 0, st>>>(a);
-    if (a.parts > 1) chunk_join_kernel<T><<<join, block, 0, st>>>(a);
+    if (a.pieces == 0) {
+        if (a.c.d <= 64) chunk_kernel<T, 64, 64, BITS, 0><<<grid, block, 0, st>>>(a);
+        else if (a.c.d <= 96) chunk_kernel<T, 128, 96, BITS, 0><<<grid, block, 0, st>>>(a);
+        else chunk_kernel<T, 128, 128, BITS, 0><<<grid, block, 0, st>>>(a);
+        return;
+    }
+    switch (a.c.d) {
+    case 16: chunk_kernel<T, 64, 64, BITS, 16><<<grid, block, 0, st>>>(a); break;
+    case 32: chunk_kernel<T, 64, 64, BITS, 32><<<grid, block, 0, st>>>(a); break;
+    case 48: chunk_kernel<T, 64, 64, BITS, 48><<<grid, block, 0, st>>>(a); break;
+    case 64: chunk_kernel<T, 64, 64, BITS, 64><<<grid, block, 0, st>>>(a); break;
+    case 80: chunk_kernel<T, 128, 96, BITS, 80><<<grid, block, 0, st>>>(a); break;
+    case 96: chunk_kernel<T, 128, 96, BITS, 96><<<grid, block, 0, st>>>(a); break;
+    case 112: chunk_kernel<T, 128, 128, BITS, 112><<<grid, block, 0, st>>>(a); break;
+    default: chunk_kernel<T, 128, 128, BITS, 128><<<grid, block, 0, st>>>(a); break;
+    }
+    chunk_join_kernel<T><<<join, block, 0, st>>>(a);
 }
 }  // namespace s24_kv
 
@@ -373,8 +747,7 @@ using namespace s24_kv;
 extern "C" int64_t s24_attn_chunk_workspace(const s24_kv_cache *cache, int64_t width, int64_t tokens, int64_t sequences, int64_t hq)
 {
     if (cache == nullptr || cache->hkv <= 0 || cache->d <= 0 || cache->page <= 0 || width < 0 || tokens < 0 || sequences < 0 || hq <= 0 || hq % cache->hkv != 0) return 0;
-    const int64_t parts = chunk_parts(cache, width, tokens, sequences, hq);
-    return parts > 1 ? parts * (weight_bytes(tokens, hq) + tokens * hq * cache->d * 4) : 0;
+    return chunk_pieces(cache, width, tokens, sequences, hq) * cache->hkv * kChunkRows * ((int64_t)sizeof(float2) + cache->d * 4);
 }
 
 extern "C" int s24_attn_chunk(const s24_kv_cache *cache, const s24_heads *Q, int64_t hq, const int32_t *cu, const int32_t *table, int64_t width, const int32_t *lengths,
@@ -393,14 +766,17 @@ extern "C" int s24_attn_chunk(const s24_kv_cache *cache, const s24_heads *Q, int
     S24_REQUIRE(workspace != nullptr || need == 0, S24_ERR_NULL);
     S24_REQUIRE(s24_aligned(cu, 4) && s24_aligned(table, 4) && s24_aligned(lengths, 4) && s24_aligned(workspace, 16), S24_ERR_ALIGN);
     S24_REQUIRE(workspace_bytes >= need, S24_ERR_SHAPE);
-    const int parts = chunk_parts(cache, width, tokens, sequences, hq);
-    const int64_t groups = chunk_groups(tokens, sequences, hq, cache->hkv) * parts, join = most_tiles(tokens, sequences, kJoinRows) * hq;
+    const int64_t pieces = chunk_pieces(cache, width, tokens, sequences, hq), tiles = chunk_tiles(cache, tokens, sequences, hq), group = hq / cache->hkv;
+    const int64_t groups = (pieces > tiles ? pieces : tiles) * cache->hkv;
+    // About a thousand workgroups add the parts, each one to 64 rows.
+    int sum_rows = 1;
+    while (sum_rows < 64 && tokens * hq > 1024 * sum_rows) sum_rows *= 2;
+    const int64_t join = most_tiles(tokens * group, tokens < sequences ? tokens : sequences, sum_rows) * cache->hkv;
     S24_REQUIRE(groups <= kMostGroups && join <= kMostGroups, S24_ERR_SHAPE);
     ChunkArgs a{cache_of(cache), {static_cast<uint16_t *>(Q->data), Q->token, Q->head}, {static_cast<uint16_t *>(O->data), O->token, O->head}, cu, table, lengths,
-                cache->pages > 0 ? width : 0, (int)sequences, (int)tokens, (int)hq, (int)(hq / cache->hkv), causal != 0, parts};
-    a.mix = sequences > 1, a.scale = scale;
+                cache->pages > 0 ? width : 0, (int)sequences, (int)tokens, (int)hq, (int)group, causal != 0, (int)pieces, sum_rows, scale};
     a.weights = static_cast<float2 *>(workspace);
-    a.sums = reinterpret_cast<float *>(static_cast<char *>(workspace) + parts * weight_bytes(tokens, hq));
+    a.sums = reinterpret_cast<float *>(static_cast<char *>(workspace) + pieces * cache->hkv * kChunkRows * sizeof(float2));
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const dim3 grid((unsigned)groups), join_grid((unsigned)join);
     if (dt == S24_BF16) cache->bits == 16 ? chunk<uint16_t, 16>(a, grid, join_grid, st) : chunk<uint16_t, 8>(a, grid, join_grid, st);
