@@ -35,11 +35,19 @@ __device__ __forceinline__ int key_tiles(const ChunkArgs &a, int i) { return (ke
 constexpr int kFewRows = 32;      // of a sequence
 constexpr int kLeastSteps = 8;    // of a part
 __device__ __forceinline__ bool is_few(const ChunkArgs &a, int i) { return (int64_t)span(a.cu, i, a.tokens).count * a.group <= kFewRows; }
-__device__ __forceinline__ int lanes_sum(int x)
+__device__ __forceinline__ int lanes_sum(int x) { return __builtin_amdgcn_readlane(running_sum(x), 63); }
+// Largest of what the lanes have, none of it negative
+__device__ __forceinline__ int lanes_max(int x)
 {
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) x += __shfl_xor(x, s);
-    return __builtin_amdgcn_readfirstlane(x);
+#if defined(__HIP_DEVICE_COMPILE__)
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));   // the last lane of a row to the next
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));   // of the first half to the second
+#endif
+    return __builtin_amdgcn_readlane(x, 63);
 }
 struct Parts { int count, steps; };   // of a tile of a sequence, and the steps of each
 __device__ __forceinline__ Parts parts_in(int keys, int each)
@@ -47,61 +55,82 @@ __device__ __forceinline__ Parts parts_in(int keys, int each)
     const int count = max(1, (int)((2 * (unsigned)keys + each) / (2 * (unsigned)each)));
     return {count, (keys + count - 1) / count};
 }
-__device__ __forceinline__ Parts parts_of(const ChunkArgs &a, int each, int i) { return parts_in(key_tiles(a, i), each); }
-__device__ __forceinline__ int steps_of_parts(const ChunkArgs &a, int lane)
-{
-    int64_t steps = 0;
-    int longest = 0, tiles = 0;
-    for (int i = lane; i < a.sequences; i += 64) {
-        const int n = row_tiles(a, i), keys = key_tiles(a, i);
-        steps += (int64_t)n * keys, tiles += n, longest = n > 0 ? max(longest, keys) : longest;
+// The sequences as the cutting sees them.  Up to 64 of them are looked at once, a lane each.
+struct List { int tiles, keys, few; };   // of rows, of positions
+struct Lists {
+    const ChunkArgs &a;
+    int lane;
+    List mine;
+    __device__ __forceinline__ Lists(const ChunkArgs &args, int of_lane) : a(args), lane(of_lane) { mine = lane < a.sequences ? look(lane) : List{0, 0, 0}; }
+    __device__ __forceinline__ List look(int i) const { return {row_tiles(a, i), key_tiles(a, i), is_few(a, i)}; }
+    // That of sequence i, by the lane that has it in turn
+    __device__ __forceinline__ List in_turn(int i) const { return a.sequences <= 64 ? mine : look(i); }
+    // That of a sequence which is the same for all lanes
+    __device__ __forceinline__ List of(int i) const
+    {
+        if (a.sequences > 64) return look(i);
+        return {__builtin_amdgcn_readlane(mine.tiles, i), __builtin_amdgcn_readlane(mine.keys, i), __builtin_amdgcn_readlane(mine.few, i)};
     }
-    const int mine = tiles;   // of the lane's sequence, where each has one
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) steps += __shfl_xor(steps, s), tiles += __shfl_xor(tiles, s), longest = max(longest, __shfl_xor(longest, s));
-    longest = max(__builtin_amdgcn_readfirstlane(longest), 1), tiles = __builtin_amdgcn_readfirstlane(tiles);
-    // (More steps than the host has seen to have offsets that do not ascend: then nothing is cut.)
-    const int all = __builtin_amdgcn_readfirstlane(steps <= INT32_MAX / 2 ? (int)steps : INT32_MAX);
-    if (tiles > a.pieces || all == INT32_MAX) return longest;
-    if (a.sequences > 64) return max(2 * (all / a.pieces) + 1, min(kLeastSteps, longest));   // (count <= 4/3 of the quotient in what is cut: no more than a.pieces)
-    const int keys = lane < a.sequences ? key_tiles(a, lane) : 0;
-    int lo = max(all / a.pieces, min(kLeastSteps, longest)), hi = max(longest, lo);   // `hi` makes few enough pieces
-    while (lo < hi) {
-        const int middle = (lo + hi) >> 1;
-        if (lanes_sum(mine * parts_in(keys, middle).count) <= a.pieces) hi = middle;
-        else lo = middle + 1;
+    // Steps of a part
+    __device__ __forceinline__ int each() const
+    {
+        int64_t steps = 0;
+        int longest = 0, tiles = 0;
+        for (int i = lane; i < a.sequences; i += 64) {
+            const List x = in_turn(i);
+            steps += (int64_t)x.tiles * x.keys, tiles += x.tiles, longest = x.tiles > 0 ? max(longest, x.keys) : longest;
+        }
+        longest = max(lanes_max(longest), 1), tiles = lanes_sum(tiles);
+        const int high = lanes_sum((int)min(steps >> 12, (int64_t)1 << 24)), low = lanes_sum((int)(steps & 4095));
+        // (More steps than the host has seen to have offsets that do not ascend: then nothing is cut.)
+        if (high > 1 << 18 || tiles > a.pieces) return longest;
+        const int all = (high << 12) + low, least = min(kLeastSteps, longest);
+        if (a.sequences > 64) return max(2 * (all / a.pieces) + 1, least);   // (count <= 4/3 of the quotient in what is cut: no more than a.pieces)
+        int lo = max(all / a.pieces, least), hi = max(longest, lo);   // `hi` makes few enough pieces
+        while (lo < hi) {
+            const int middle = (lo + hi) >> 1;
+            if (lanes_sum(mine.tiles * parts_in(mine.keys, middle).count) <= a.pieces) hi = middle;
+            else lo = middle + 1;
+        }
+        return hi;
     }
-    return hi;
-}
-// Sums that the sequences before this one leave
-__device__ __forceinline__ int slots_before(const ChunkArgs &a, int each, int sequence, int lane)
-{
-    int before = 0;
-    for (int i = lane; i < sequence; i += 64) {
-        const int count = parts_of(a, each, i).count;
-        before += count > 1 ? row_tiles(a, i) * count : 0;
+    // Sums that the sequences before this one leave
+    __device__ __forceinline__ int slots_before(int each, int sequence) const
+    {
+        int before = 0;
+        for (int i = lane; i < sequence; i += 64) {
+            const List x = in_turn(i);
+            const int count = parts_in(x.keys, each).count;
+            before += count > 1 ? x.tiles * count : 0;
+        }
+        return lanes_sum(before);
     }
-    return lanes_sum(before);
-}
+};
 // A workgroup's work: steps begin .. end - 1 of a tile of rows (its steps are all of the sequence's); where its sums go, or -1: to O
 struct Piece { int sequence, tile, begin, end, slot; };
 // Piece t of those of a key-value head: the longest come first, and those of few rows last; of a sequence all tiles' first parts, then all tiles' next ones, so that workgroups which
 // run at the same time read the same positions.
 __device__ __forceinline__ bool find_part(const ChunkArgs &a, int t, int lane, Piece &piece)
 {
-    const int each = steps_of_parts(a, lane), most = (int)((a.width << a.c.shift) / kChunkKeys) + 2;
+    const Lists lists(a, lane);
+    const int each = lists.each(), most = (int)((a.width << a.c.shift) / kChunkKeys) + 2;
     int wide = 0, sequence, at;
-    for (int i = lane; i < a.sequences; i += 64) wide += is_few(a, i) ? 0 : row_tiles(a, i) * parts_of(a, each, i).count;
+    for (int i = lane; i < a.sequences; i += 64) {
+        const List x = lists.in_turn(i);
+        wide += x.few ? 0 : x.tiles * parts_in(x.keys, each).count;
+    }
     wide = lanes_sum(wide);
     const bool few = t >= wide;
     auto of = [&](int i) {
-        const Parts p = parts_of(a, each, i);
-        return is_few(a, i) == few ? Lengths{row_tiles(a, i) * p.count, INT32_MAX, max(p.steps, 1)} : Lengths{0, 0, 0};
+        const List x = lists.in_turn(i);
+        const Parts p = parts_in(x.keys, each);
+        return x.few == few ? Lengths{x.tiles * p.count, INT32_MAX, max(p.steps, 1)} : Lengths{0, 0, 0};
     };
     if (!find_by_length(true, a.sequences, few ? t - wide : t, most, lane, sequence, at, of)) return false;
-    const Parts p = parts_of(a, each, sequence);
-    const int n = row_tiles(a, sequence), part = at / n, slot = p.count == 1 ? -1 : slots_before(a, each, sequence, lane) + at;
-    piece = {sequence, n - 1 - (at - part * n), part * p.steps, min(key_tiles(a, sequence), (part + 1) * p.steps), slot};
+    const List x = lists.of(sequence);
+    const Parts p = parts_in(x.keys, each);
+    const int part = at / max(x.tiles, 1), slot = p.count == 1 ? -1 : lists.slots_before(each, sequence) + at;
+    piece = {sequence, x.tiles - 1 - (at - part * x.tiles), part * p.steps, min(x.keys, (part + 1) * p.steps), slot};
     return at >= 0 && part < p.count && slot < a.pieces;   // (as they are, where the offsets ascend)
 }
 // The workgroup's tile where each has one: a sequence, and which of its tiles, the last ones first.  The longest come first.
@@ -269,25 +298,6 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Queries &s_, 
     const int length = s_.k.count, all_units = max(min(2 * tiles, (s_.seen + BK - 1) / BK) - 2 * begin, 0);
     const int first = 2 * begin + all_units * wave / 4, end = 2 * begin + all_units * (wave + 1) / 4;
 
-    uint4 q[2][QL];
-    int last[2];
-    float c[2];
-    Queries::Row of[2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        of[j] = s_.row(a.group, kv, 16 * j + col);
-        last[j] = a.causal ? min(length - 1, of[j].at + s_.ahead) : length - 1;
-        const uint16_t *row = a.q.p + of[j].token * a.q.token + of[j].head * a.q.head;
-        c[j] = a.scale * kLog2e;
-#pragma unroll
-        for (int k = 0; k < QL; ++k) {
-            const int i = BITS == 8 ? 64 * (k >> 1) + 16 * g + 8 * (k & 1) : 32 * k + 8 * g;
-            q[j][k] = i < d ? *reinterpret_cast<const uint4 *>(row + i) : make_uint4(0, 0, 0, 0);
-        }
-        if (BITS == 8) c[j] = scaled_queries<T>(q[j], c[j]);
-    }
-    const int all = __builtin_amdgcn_readfirstlane(last[0]) + 1;   // positions that all of the rows see: what the first one does
-
     // A unit's positions 8*(col/4) .. for K, 8*g .. for V: each sixteen lie in one page.
     auto position = [&](int t, int eight) { return min(t * BK + 16 * (eight >> 1), (length - 1) & ~15); };
     struct Pages { uint32_t k, v; };
@@ -322,17 +332,33 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Queries &s_, 
 #pragma unroll
         for (int n = 0; n < d / 16; ++n) fv[n] = __builtin_bit_cast(Values, __builtin_nontemporal_load(reinterpret_cast<const Loaded *>(from + (16 * n + col) * 16)));
     };
+    Pages now{}, next{};
+    if (first < end) now = pages(first);
+    if (first + 1 < end) next = pages(first + 1);
+    uint4 q[2][QL];
+    int last[2];
+    float c[2];
+    Queries::Row of[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        of[j] = s_.row(a.group, kv, 16 * j + col);
+        last[j] = a.causal ? min(length - 1, of[j].at + s_.ahead) : length - 1;
+        const uint16_t *row = a.q.p + of[j].token * a.q.token + of[j].head * a.q.head;
+        c[j] = a.scale * kLog2e;
+#pragma unroll
+        for (int k = 0; k < QL; ++k) {
+            const int i = BITS == 8 ? 64 * (k >> 1) + 16 * g + 8 * (k & 1) : 32 * k + 8 * g;
+            q[j][k] = i < d ? *reinterpret_cast<const uint4 *>(row + i) : make_uint4(0, 0, 0, 0);
+        }
+    }
+    const int all = __builtin_amdgcn_readfirstlane(last[0]) + 1;   // positions that all of the rows see: what the first one does
+    if (first < end) load_k(first, now), load_v(first, now);
+    if (BITS == 8) c[0] = scaled_queries<T>(q[0], c[0]), c[1] = scaled_queries<T>(q[1], c[1]);
     float m[2] = {-1e30f, -1e30f}, l[2] = {0.0f, 0.0f};
     Reference<BITS> reference;
     f32x4 o[2][d / 16];
 #pragma unroll
     for (int n = 0; n < d / 16; ++n) o[0][n] = o[1][n] = f32x4{};
-    Pages next{};
-    if (first < end) {
-        const Pages now = pages(first);
-        load_k(first, now), load_v(first, now);
-        if (first + 1 < end) next = pages(first + 1);
-    }
     // The loads run ahead: a unit's keys are asked for as soon as the scores before them are formed, its values as soon as the ones before are summed, its pages a unit before that.
     for (int t = first; t < end; ++t) {
         const Pages coming = next;
@@ -482,6 +508,16 @@ template <typename T, int D, int E, int BITS, int HEAD> __device__ __forceinline
         }
     }
 
+    // Where the wave's positions of tile t are, in tokens of one head.  (Those past the sequence's end are its last ones again.)
+    auto page_of = [&](int t) {
+        const int pos = min(t * BK + 16 * wave, (length - 1) & ~15);
+        return min((uint32_t)table[pos >> a.c.shift], (uint32_t)a.c.pages - 1);
+    };
+    auto place = [&](int t, uint32_t id) {
+        const int pos = min(t * BK + 16 * wave, (length - 1) & ~15);
+        return (((int64_t)id * a.c.hkv + kv) << a.c.shift) + (pos & (a.c.page - 1));
+    };
+    uint32_t id = begin < tiles ? page_of(begin) : 0;   // of the next tile
     uint4 q[2][E / 32];
     int last[2];     // that a row sees
     float c[2];      // factor of the scores
@@ -504,18 +540,8 @@ template <typename T, int D, int E, int BITS, int HEAD> __device__ __forceinline
 
     Sixteen<D, BITS> sixteen;
     sixteen.init(a.c, wave, lane);
-    // Where the wave's positions of tile t are, in tokens of one head.  (Those past the sequence's end are its last ones again.)
-    auto page_of = [&](int t) {
-        const int pos = min(t * BK + 16 * wave, (length - 1) & ~15);
-        return min((uint32_t)table[pos >> a.c.shift], (uint32_t)a.c.pages - 1);
-    };
-    auto place = [&](int t, uint32_t id) {
-        const int pos = min(t * BK + 16 * wave, (length - 1) & ~15);
-        return (((int64_t)id * a.c.hkv + kv) << a.c.shift) + (pos & (a.c.page - 1));
-    };
-    uint32_t id = 0;   // of the next tile
     if (begin < tiles) {
-        sixteen.start(a.c, place(begin, page_of(begin)), (lds_byte *)lds_k[begin & 1], (lds_byte *)lds_v[begin & 1], steps[begin & 1]);
+        sixteen.start(a.c, place(begin, id), (lds_byte *)lds_k[begin & 1], (lds_byte *)lds_v[begin & 1], steps[begin & 1]);
         if (begin + 1 < tiles) id = page_of(begin + 1);
         sixteen.finish((lds_byte *)lds_k[begin & 1], (lds_byte *)lds_v[begin & 1], steps[begin & 1], length - begin * BK - 16 * wave);
     }
@@ -654,9 +680,10 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(const ChunkArgs a)
     const int block = blockIdx.x / a.c.hkv, kv = blockIdx.x - block * a.c.hkv, lane = threadIdx.x & 63;
     int sequence, index, unused;
     if (!find_item(a.sequences, block, lane, sequence, index, unused, [&](int i) { return (int)(((int64_t)span(a.cu, i, a.tokens).count * a.group + a.sum_rows - 1) / a.sum_rows); })) return;
-    const int each = steps_of_parts(a, lane), parts = parts_of(a, each, sequence).count, n = row_tiles(a, sequence);
+    const Lists lists(a, lane);
+    const int each = lists.each(), n = lists.of(sequence).tiles, parts = parts_in(lists.of(sequence).keys, each).count;
     if (parts == 1) return;
-    const int before = slots_before(a, each, sequence, lane);
+    const int before = lists.slots_before(each, sequence);
     if (before + n * parts > a.pieces) return;
     const Span s = span(a.cu, sequence, a.tokens);
     const int row0 = index * a.sum_rows, rows = min(a.sum_rows, s.count * a.group - row0), tile = row0 / kChunkRows, d = a.c.d;
