@@ -2,7 +2,8 @@
 
     python examples/decoder_layer.py            # a training step, prompts read in chunks into an 8-bit cache, and tokens sampled after them
 
-Y1 = X + Attention(X Wqkv^T) Wo^T,  Y = Y1 + FFN(Y1) over packed sequences; no norms and no positions, which are the caller's.
+Y1 = X + Attention(X Wqkv^T) Wo^T,  Y = Y1 + FFN(Y1) over packed sequences.  With `base` the heads of the queries and keys are normalised and turned by their positions before the
+attention; without it they are taken as they are.  Norms of X and Y1 are the caller's.
 """
 import os
 import sys
@@ -11,7 +12,7 @@ import torch
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 import paper_2404_01847_amd as s24                                   # noqa: E402
-from paper_2404_01847_amd.attention import Attention, PagedKV        # noqa: E402
+from paper_2404_01847_amd.attention import Attention, PagedKV, Rotary, rotary_frequencies   # noqa: E402
 from paper_2404_01847_amd.ffn import SparseFFN                       # noqa: E402
 
 
@@ -20,15 +21,20 @@ def offsets(lengths):
 
 
 class DecoderLayer:
-    """Weights, buffers and call sequence of one layer: `tokens` tokens in a training step, up to as many in a call that serves."""
+    """Weights, buffers and call sequence of one layer: `tokens` tokens in a training step, up to as many in a call that serves.  base: of the frequencies of the positions, or None:
+    there are none."""
 
-    def __init__(self, width, d_ff, hq, hkv, d, tokens, dtype=torch.bfloat16, seed=0):
+    def __init__(self, width, d_ff, hq, hkv, d, tokens, dtype=torch.bfloat16, seed=0, base=None):
         gen = torch.Generator(device="cuda").manual_seed(seed)
         weight = lambda r, q: (torch.randn((r, q), generator=gen, device="cuda") * q ** -0.5).to(dtype)
         self.hq, self.hkv, self.d, self.tokens, self.dtype = hq, hkv, d, tokens, dtype
         self.Wqkv, self.Wo = weight((hq + 2 * hkv) * d, width), weight(width, hq * d)
         self.ffn = SparseFFN({"Wg": weight(d_ff, width), "Wu": weight(d_ff, width), "Wd": weight(width, d_ff)}, tokens, "swiglu", 2e-4, concat_gate_up=True)
         self.attention = Attention(hq, hkv, d, tokens, dtype=dtype)
+        self.rotary = None
+        if base is not None:
+            self.wq, self.wk = (1 + 0.1 * torch.randn(d, generator=gen, device="cuda")).to(dtype), (1 + 0.1 * torch.randn(d, generator=gen, device="cuda")).to(dtype)
+            self.rotary = Rotary(hq, hkv, d, tokens, rotary_frequencies(d, base), self.wq, self.wk, dtype=dtype)
         self.grads = {n: torch.empty(w.shape, dtype=torch.float32, device="cuda") for n, w in (("Wqkv", self.Wqkv), ("Wo", self.Wo))}
 
     def _project(self, X, W):
@@ -49,14 +55,21 @@ class DecoderLayer:
         if X.shape[0] != self.tokens:   # the FFN's weight gradients go over all rows of its buffers
             raise ValueError(f"a training step of this layer takes {self.tokens} tokens, got {X.shape[0]}")
         self.ffn.prune()
-        Q, K, V = self._heads(X)
+        Q, K, V = heads = self._heads(X)
+        if self.rotary:
+            at = torch.arange(self.tokens, dtype=torch.int32, device="cuda")
+            at -= cu[torch.searchsorted(cu, at, right=True) - 1]
+            Q, K = self.rotary.forward(Q, K, at)
         O = self.attention.forward(Q, K, V, cu)
         Y1, Y = self._finish(X, O)
         dY1 = dY + self.ffn.backward(Y1, dY)
         flat = O.reshape(X.shape[0], -1)
         s24.dense_dw(dY1, flat, self.grads["Wo"])
         dO = self._project(dY1, self.Wo.t().contiguous()).view(O.shape)
-        self.attention.backward(Q, K, V, dO, cu)
+        dQ, dK, _ = self.attention.backward(Q, K, V, dO, cu)
+        if self.rotary:
+            self.rotary.backward(dQ, dK, *heads[:2], at)   # in place: dQ and dK are parts of the projection's gradient
+            self.grads |= {"wq": self.rotary.dwq, "wk": self.rotary.dwk}
         dQKV = self.attention.dQKV.view(X.shape[0], -1)
         s24.dense_dw(dQKV, X, self.grads["Wqkv"])
         return Y, dY1 + self._project(dQKV, self.Wqkv.t().contiguous())
@@ -68,7 +81,12 @@ class DecoderLayer:
         Q, K, V = self._heads(X)
         rows = torch.cat([torch.arange(a, b, device="cuda") for a, b in zip(past, every)])
         sequence = torch.repeat_interleave(torch.arange(len(new), device="cuda"), torch.tensor(new, device="cuda"))
-        cache.write(K, V, table[sequence, rows // cache.page].long() * cache.page + rows % cache.page)
+        places = table[sequence, rows // cache.page].long() * cache.page + rows % cache.page
+        if self.rotary:
+            Q = cache.append(self.rotary, Q, K, V, rows.to(torch.int32), places)
+            lengths = torch.tensor(every, dtype=torch.int32, device="cuda")
+            return self._finish(X, cache.attend_chunk(Q, offsets(new), table, lengths, torch.empty((X.shape[0], self.hq, self.d), dtype=self.dtype, device="cuda")))[1]
+        cache.write(K, V, places)
         Ka, Va = (torch.empty((sum(every), self.hkv, self.d), dtype=self.dtype, device="cuda") for _ in range(2))
         cache.read(table, offsets(every), Ka, Va)
         O = self.attention.forward(Q, Ka, Va, offsets(new), offsets(every))
@@ -78,16 +96,26 @@ class DecoderLayer:
         """One new token of each sequence (X [sequences, width]); `lengths` (int32, on the device) are those with it."""
         Q, K, V = self._heads(X)
         at = lengths.long() - 1
-        cache.write(K, V, table.gather(1, (at // cache.page)[:, None])[:, 0].long() * cache.page + at % cache.page)
+        places = table.gather(1, (at // cache.page)[:, None])[:, 0].long() * cache.page + at % cache.page
+        if self.rotary:
+            Q = cache.append(self.rotary, Q, K, V, at.to(torch.int32), places)
+        else:
+            cache.write(K, V, places)
         O = cache.attend(Q, table, lengths, torch.empty((X.shape[0], self.hq, self.d), dtype=self.dtype, device="cuda"))
         return self._finish(X, O)[1]
 
 
 def main():
+    for base in (None, 10000.0):
+        print("heads as they are:" if base is None else "heads normalised, and turned by their positions:")
+        run(base)
+
+
+def run(base):
     width, d_ff, hq, hkv, d = 1024, 2816, 16, 4, 64
     lengths = [700, 33, 1315]
     tokens = sum(lengths)
-    layer = DecoderLayer(width, d_ff, hq, hkv, d, tokens)
+    layer = DecoderLayer(width, d_ff, hq, hkv, d, tokens, base=base)
     X = torch.randn((tokens, width), device="cuda").to(torch.bfloat16)
     Y, dX = layer.step(X, 1e-2 * torch.randn_like(X), offsets(lengths))
     print(f"trained on {tokens} tokens of {len(lengths)} sequences: |Y| {Y.float().norm():.1f}, |dX| {dX.float().norm():.3f}, "

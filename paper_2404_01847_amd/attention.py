@@ -107,17 +107,20 @@ class Rotary:
         self.hq, self.hkv, self.d, self.tokens, self.dtype = hq, hkv, d, tokens, dtype
         self.plan = s24.RotaryPlan(d, dtype, frequencies, wq, wk, eps, axis, axes, interleaved)
         self.Q, self.K = (torch.empty((tokens, h, d), dtype=dtype, device=device) for h in (hq, hkv))
+        self._own = s24.OwnHeads(self.Q), s24.OwnHeads(self.K)
         self.dwq, self.dwk = (None if w is None else torch.zeros(d, dtype=torch.float32, device=device) for w in (wq, wk))
         self.need = {}   # bytes of workspace that a backward pass over so many tokens takes
-
-    def _own(self, Q, K):
-        n = Q.shape[0]
-        return (self.Q, self.K) if n == self.tokens else (self.Q[:n], self.K[:n])
 
     def forward(self, Q, K, positions, out=None):
         """Q and K [tokens, heads, d], normalised and turned: in the layer's own buffers, or in out = (Q, K), which may be the operands where no backward pass needs them (without
         norms it needs none).  positions: int32 [axes, tokens], or [tokens] of one axis."""
-        return s24.rotary_fwd(self.plan, Q, K, positions, *(self._own(Q, K) if out is None else out))
+        if out is not None:
+            return s24.rotary_fwd(self.plan, Q, K, positions, *out)
+        n = Q.shape[0] if Q.dim() > 0 else 0
+        if n == self.tokens:
+            s24.rotary_fwd(self.plan, Q, K, positions, *self._own)
+            return self.Q, self.K
+        return s24.rotary_fwd(self.plan, Q, K, positions, self.Q[:n], self.K[:n])
 
     def backward(self, dQ, dK, Q, K, positions, out=None, beta=0.0):
         """Gradients of forward's operands, whose values Q and K are given again (None, None without norms): in place of dQ and dK, or in out = (dQ, dK).  Those of the weights go to
@@ -157,9 +160,13 @@ class PagedKV:
     def append(self, rotary, Q, K, V, positions, places, out=None):
         """What stands before the attention of new tokens, in one pass: Q [tokens, hq, d] normalised and turned as `rotary` (Rotary) has it, into its own buffer or into `out` (which
         may be Q); K likewise and V as it is to their places."""
-        if out is None:
-            out = rotary._own(Q, K)[0]
-        return s24.kv_append(self.buffers, rotary.plan, Q, K, V, positions, places, out)
+        if out is not None:
+            return s24.kv_append(self.buffers, rotary.plan, Q, K, V, positions, places, out)
+        n = Q.shape[0] if Q.dim() > 0 else 0
+        if n == rotary.tokens:
+            s24.kv_append(self.buffers, rotary.plan, Q, K, V, positions, places, rotary._own[0])
+            return rotary.Q
+        return s24.kv_append(self.buffers, rotary.plan, Q, K, V, positions, places, rotary.Q[:n])
 
     def read(self, table, cu, K, V):
         """The sequences, one after the other from the offsets cu on, into K and V [tokens, hkv, d]: as Attention.forward takes them."""
@@ -175,11 +182,12 @@ class PagedKV:
     def attend_chunk(self, Q, cu, table, lengths, O, scale=None, causal=True):
         """O [tokens, hq, d]: attention of new tokens that the cache has already.  Those of sequence i are the rows cu[i] .. cu[i+1] - 1 of Q, the last ones of its first lengths[i]
         positions, and see the positions up to their own (all of them where not `causal`)."""
-        where = "PagedKV.attend_chunk"
-        key = s24._axes(where, "Q", Q, ("tokens", "heads", "d")), s24._axes(where, "table", table, ("sequences", "pages"))
+        key = Q.shape, table.shape
         n = self.need.get(key)
         if n is None:
+            where = "PagedKV.attend_chunk"
+            (tokens, hq, _), (sequences, width) = s24._axes(where, "Q", Q, ("tokens", "heads", "d")), s24._axes(where, "table", table, ("sequences", "pages"))
             if len(self.need) >= 1024:   # (batches of ever new sizes)
                 self.need.clear()
-            n = self.need[key] = s24.attn_chunk_workspace(self.buffers, table.shape[1], Q.shape[0], table.shape[0], Q.shape[1])
+            n = self.need[key] = s24.attn_chunk_workspace(self.buffers, width, tokens, sequences, hq)
         return s24.attn_chunk(self.buffers, Q, cu, table, lengths, O, _workspace(n, self.K), scale, causal)

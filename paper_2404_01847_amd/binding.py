@@ -701,15 +701,15 @@ def attn_chunk_workspace(cache, width, tokens, sequences, hq):
 def attn_chunk(cache, Q, cu, table, lengths, O, workspace, scale=None, causal=True):
     """Attention of the tokens cu[i] .. cu[i+1] - 1 (int32) of Q and O [tokens, hq, d], which are the last ones of the first lengths[i] (int32) positions of sequence i in the
     cache; workspace: a Workspace or a uint8 tensor of attn_chunk_workspace(...) bytes, None where that is 0."""
-    where, device = "s24_attn_chunk", cache.device
-    n = _axes(where, "table", table, ("sequences", "pages"))
-    tokens, hq, d = _axes(where, "Q", Q, ("tokens", "heads", "d"))
-    shape = (tokens, hq, cache.d)
-    args = (cache.packed, _heads(where, "Q", Q, shape, cache.dtype, device), hq, _whole(where, "cu", cu, torch.int32, (n[0] + 1,), device),
-            _whole(where, "table", table, torch.int32, n, device), n[1], _whole(where, "lengths", lengths, torch.int32, (n[0],), device), n[0], tokens,
-            cache.d ** -0.5 if scale is None else scale, bool(causal), _heads(where, "O", O, shape, cache.dtype, device), *_work(where, workspace, device), _dt(Q))
-    if device < 0:
-        raise ValueError(f"{where}: the tensors must lie on a GPU")
+    where, device, dtype, d = "s24_attn_chunk", cache.device, cache.dtype, cache.d
+    n, shape = table.shape, Q.shape
+    if len(n) != 2 or len(shape) != 3 or shape[2] != d:
+        raise ValueError(f"{where}: table must have shape [sequences, pages] and Q must have shape [tokens, heads, {d}], got {tuple(n)} and {tuple(shape)}")
+    sequences, width = n
+    args = (cache.packed, _heads(where, "Q", Q, shape, dtype, device), shape[1], _whole(where, "cu", cu, torch.int32, (sequences + 1,), device),
+            _whole(where, "table", table, torch.int32, n, device), width, _whole(where, "lengths", lengths, torch.int32, (sequences,), device), sequences, shape[0],
+            d ** -0.5 if scale is None else scale, bool(causal), _heads(where, "O", O, shape, dtype, device), *_work(where, workspace, device), _DTYPES[dtype])
+    _of_gpu(where, device)
     status = lib().s24_attn_chunk(*args, _stream())
     if status != 0:
         raise S24Error(status, where)
@@ -731,18 +731,19 @@ class RotaryPlan:
         self.packed = _pack_rotary(address("frequencies", frequencies, torch.float64, pairs), address("axis", axis, torch.int32, pairs), address("wq", wq, dtype, d),
                                    address("wk", wk, dtype, d), axes, 2 * pairs, eps, bool(interleaved))
         self.held, self.d, self.dtype, self.device, self.axes, self.pairs = given, d, dtype, device, axes, pairs
-        self.norms = wq is not None, wk is not None
+        self.norms, self.type = (wq is not None, wk is not None), _DTYPES[dtype]
         _check(lib().s24_rotary_fwd(self.packed, None, None, None, None, None, 0, 0, 0, d, _DTYPES[dtype], None),   # no heads: the library looks at the plan alone
                f"{where}: heads of {d}, {2 * pairs} values turned, {axes} axes, eps {eps}")
 
     def positions(self, where, positions, tokens, device):
-        if self.device is not None and self.device != device:
+        if device != self.device and self.device is not None:
             raise ValueError(f"{where}: the plan lies on device {self.device}, not where the tensors do")
-        if positions is None and self.pairs == 0:
-            return 0
         if positions is None:
-            raise ValueError(f"{where}: heads that are turned need positions")
-        return _whole(where, "positions", positions, torch.int32, (tokens,) if self.axes == 1 and positions.dim() == 1 else (self.axes, tokens), device)
+            if self.pairs > 0:
+                raise ValueError(f"{where}: heads that are turned need positions")
+            return 0
+        n = positions.shape
+        return _whole(where, "positions", positions, torch.int32, (tokens,) if self.axes == 1 and len(n) == 1 else (self.axes, tokens), device)
 
 
 def _of_gpu(where, device):
@@ -750,13 +751,34 @@ def _of_gpu(where, device):
         raise ValueError(f"{where}: the tensors must lie on a GPU")
 
 
+class OwnHeads:
+    """A buffer [tokens, heads, d] without gaps, looked at once for all calls that write all of it (few tokens wait for the host)."""
+    __slots__ = ("tensor", "packed", "key")
+
+    def __init__(self, x):
+        self.tensor, self.key = x, (x.shape, x.dtype, x.get_device())
+        self.packed = _pack_heads(x.data_ptr(), x.stride(0), x.stride(1))
+
+
+def _written(where, name, x, shape, dtype, device):
+    """Heads that a call writes: a tensor or an OwnHeads."""
+    if type(x) is not OwnHeads:
+        return _heads(where, name, x, shape, dtype, device)
+    if x.key != (shape, dtype, device):
+        _refused(where, name, x.tensor, dtype, shape, device)
+    return x.packed
+
+
 def rotary_fwd(plan, Q, K, positions, Qo, Ko):
-    """Qo, Ko [tokens, heads, d]: Q and K normalised and turned as the plan (RotaryPlan) has it.  positions: int32 [axes, tokens], or [tokens] of one axis.  Qo may be Q and Ko be K."""
-    where, device = "s24_rotary_fwd", Q.get_device()
-    (tokens, hq, _), (_, hkv, _) = _axes(where, "Q", Q, ("tokens", "heads", "d")), _axes(where, "K", K, ("tokens", "heads", "d"))
-    sq, sk, dtype = (tokens, hq, plan.d), (tokens, hkv, plan.d), plan.dtype
+    """Qo, Ko [tokens, heads, d]: Q and K normalised and turned as the plan (RotaryPlan) has it.  positions: int32 [axes, tokens], or [tokens] of one axis.  Qo may be Q and Ko be K
+    (and either an OwnHeads)."""
+    where, device, d, dtype = "s24_rotary_fwd", Q.get_device(), plan.d, plan.dtype
+    sq, sk = Q.shape, K.shape
+    if len(sq) != 3 or len(sk) != 3 or sq[2] != d or sk[2] != d or sk[0] != sq[0]:
+        raise ValueError(f"{where}: Q and K must have shape [tokens, heads, {d}] with as many tokens, got {tuple(sq)} and {tuple(sk)}")
+    tokens = sq[0]
     args = (plan.packed, plan.positions(where, positions, tokens, device), _heads(where, "Q", Q, sq, dtype, device), _heads(where, "K", K, sk, dtype, device),
-            _heads(where, "Qo", Qo, sq, dtype, device), _heads(where, "Ko", Ko, sk, dtype, device), tokens, hq, hkv, plan.d, _dt(Q))
+            _written(where, "Qo", Qo, sq, dtype, device), _written(where, "Ko", Ko, sk, dtype, device), tokens, sq[1], sk[1], d, plan.type)
     _of_gpu(where, device)
     status = lib().s24_rotary_fwd(*args, _stream())
     if status != 0:
@@ -772,17 +794,22 @@ def rotary_bwd_workspace(plan, tokens, hq, hkv):
 def rotary_bwd(plan, dQo, dKo, Q, K, positions, dQ, dK, dwq=None, dwk=None, beta=0.0, workspace=None):
     """Gradients dQ, dK (which may be dQo and dKo) and dw = beta dw + its gradient (float32 [d]) of rotary_fwd.  Q, K: those of the forward pass where they are normalised (else
     they may be None); workspace: a Workspace or a uint8 tensor of rotary_bwd_workspace(...) bytes, None where that is 0."""
-    where, device = "s24_rotary_bwd", dQo.get_device()
-    (tokens, hq, _), (_, hkv, _) = _axes(where, "dQo", dQo, ("tokens", "heads", "d")), _axes(where, "dKo", dKo, ("tokens", "heads", "d"))
-    sq, sk, dtype = (tokens, hq, plan.d), (tokens, hkv, plan.d), plan.dtype
-    heads = lambda name, x, shape, needed=True: _heads(where, name, x, shape, dtype, device) if needed else None
-    weights = lambda name, x, needed: _whole(where, name, x, torch.float32, (plan.d,), device) if needed else None
-    for (name, x), needed in zip((("Q", Q), ("K", K), ("dwq", dwq), ("dwk", dwk)), plan.norms * 2):
-        if needed and x is None:
-            raise ValueError(f"{where}: {name} is needed where there is a norm")
-    nq, nk = plan.norms
-    args = (plan.packed, plan.positions(where, positions, tokens, device), heads("dQo", dQo, sq), heads("dKo", dKo, sk), heads("Q", Q, sq, nq), heads("K", K, sk, nk),
-            heads("dQ", dQ, sq), heads("dK", dK, sk), weights("dwq", dwq, nq), weights("dwk", dwk, nk), beta, tokens, hq, hkv, plan.d, *_work(where, workspace, device), _dt(dQo))
+    where, device, d, dtype = "s24_rotary_bwd", dQo.get_device(), plan.d, plan.dtype
+    sq, sk = dQo.shape, dKo.shape
+    if len(sq) != 3 or len(sk) != 3 or sq[2] != d or sk[2] != d or sk[0] != sq[0]:
+        raise ValueError(f"{where}: dQo and dKo must have shape [tokens, heads, {d}] with as many tokens, got {tuple(sq)} and {tuple(sk)}")
+    tokens, (nq, nk) = sq[0], plan.norms
+    q = k = gq = gk = None
+    if nq or nk:
+        for name, x, needed in (("Q", Q, nq), ("K", K, nk), ("dwq", dwq, nq), ("dwk", dwk, nk)):
+            if needed and x is None:
+                raise ValueError(f"{where}: {name} is needed where there is a norm")
+        if nq:
+            q, gq = _heads(where, "Q", Q, sq, dtype, device), _whole(where, "dwq", dwq, torch.float32, (d,), device)
+        if nk:
+            k, gk = _heads(where, "K", K, sk, dtype, device), _whole(where, "dwk", dwk, torch.float32, (d,), device)
+    args = (plan.packed, plan.positions(where, positions, tokens, device), _heads(where, "dQo", dQo, sq, dtype, device), _heads(where, "dKo", dKo, sk, dtype, device), q, k,
+            _heads(where, "dQ", dQ, sq, dtype, device), _heads(where, "dK", dK, sk, dtype, device), gq, gk, beta, tokens, sq[1], sk[1], d, *_work(where, workspace, device), plan.type)
     _of_gpu(where, device)
     status = lib().s24_rotary_bwd(*args, _stream())
     if status != 0:
@@ -792,13 +819,16 @@ def rotary_bwd(plan, dQo, dKo, Q, K, positions, dQ, dK, dwq=None, dwk=None, beta
 
 def kv_append(cache, plan, Q, K, V, positions, places, Qo):
     """Qo = Q [tokens, hq, d] normalised and turned (it may be Q); K [tokens, hkv, d] likewise and V as it is to the places (int64, as kv_write has them) of the cache."""
-    where, device = "s24_kv_append", cache.device
-    tokens, hq, _ = _axes(where, "Q", Q, ("tokens", "heads", "d"))
-    if plan.d != cache.d or plan.dtype is not cache.dtype:
-        raise ValueError(f"{where}: a plan for heads of {plan.d} in {plan.dtype}, a cache of heads of {cache.d} in {cache.dtype}")
-    sq, sk, dtype = (tokens, hq, cache.d), (tokens, cache.hkv, cache.d), cache.dtype
-    args = (cache.packed, plan.packed, plan.positions(where, positions, tokens, device), _heads(where, "Q", Q, sq, dtype, device), hq, _heads(where, "K", K, sk, dtype, device),
-            _heads(where, "V", V, sk, dtype, device), _heads(where, "Qo", Qo, sq, dtype, device), _whole(where, "places", places, torch.int64, (tokens,), device), tokens, _dt(Q))
+    where, device, dtype = "s24_kv_append", cache.device, cache.dtype
+    if plan.d != cache.d or plan.dtype is not dtype:
+        raise ValueError(f"{where}: a plan for heads of {plan.d} in {plan.dtype}, a cache of heads of {cache.d} in {dtype}")
+    sq = Q.shape
+    if len(sq) != 3 or sq[2] != plan.d:
+        raise ValueError(f"{where}: Q must have shape [tokens, heads, {plan.d}], got {tuple(sq)}")
+    tokens = sq[0]
+    sk = (tokens, cache.hkv, cache.d)
+    args = (cache.packed, plan.packed, plan.positions(where, positions, tokens, device), _heads(where, "Q", Q, sq, dtype, device), sq[1], _heads(where, "K", K, sk, dtype, device),
+            _heads(where, "V", V, sk, dtype, device), _written(where, "Qo", Qo, sq, dtype, device), _whole(where, "places", places, torch.int64, (tokens,), device), tokens, plan.type)
     _of_gpu(where, device)
     status = lib().s24_kv_append(*args, _stream())
     if status != 0:

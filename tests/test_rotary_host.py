@@ -140,8 +140,8 @@ def test_the_binding_refuses_what_the_calls_cannot_see(lib):
     refused("positions must be", layer.forward, Q, K, at.long())
     refused("need positions", layer.forward, Q, K, None)
     refused("K must be", layer.forward, Q, K.half(), at)
-    refused("K must have shape", layer.forward, Q, K[:4], at)
-    refused("Q must have shape", layer.forward, Q[0], K, at)
+    refused("Q and K must have shape", layer.forward, Q, K[:4], at)
+    refused("Q and K must have shape", layer.forward, Q[0], K, at)
     refused("Qo must have shape", layer.forward, Q[:, :2], K, at)
     refused("Q needs unit stride", layer.forward, torch.zeros(8, 4, 128, dtype=bf)[..., ::2], K, at)
     refused("must lie on a GPU", layer.forward, Q, K, at)
@@ -168,6 +168,7 @@ def test_the_binding_refuses_what_the_calls_cannot_see(lib):
     refused("lengths must have shape", attend, lens=cu)
     refused("O must have shape", attend, O=K)
     refused("Q must have shape", attend, q=Q[..., :32])
+    refused("table must have shape", attend, table=table[0])
     refused("must lie on a GPU", attend)
     refused("table must have shape", c.attend_chunk, Q, cu, table[0], cu[:2], Q)
     refused("Q must have shape", c.attend_chunk, Q[0], cu, table, cu[:2], Q)
