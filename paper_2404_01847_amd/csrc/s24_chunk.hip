@@ -148,8 +148,11 @@ __device__ __forceinline__ bool find_chunk(const ChunkArgs &a, int t, int lane, 
 }
 
 // Keys of a tile in LDS: piece c of a row at slot c ^ flip.  The 16 rows of an operand are four of each sixteen positions, of which the LDS takes those of lanes 0-3 and 12-15
-// of one piece together with those of lanes 4-11 of the next in a cycle.
-template <int D> __device__ __forceinline__ int flip(int row) { return D == 128 ? ((row & 3) | (row >> 4 & 1) << 2) << 1 : ((row >> 1 & 1) | (row >> 4 & 1) << 1) << 1; }
+// of one piece together with those of lanes 4-11 of the next in a cycle.  In 8 bits rows are written every second piece at a time: there rows 4 and 5 have theirs where 0 and 1 have none.
+template <int D, int BITS> __device__ __forceinline__ int flip(int row)
+{
+    return (D == 128 ? ((row & 3) | (row >> 4 & 1) << 2) << 1 : ((row >> 1 & 1) | (row >> 4 & 1) << 1) << 1) | (BITS == 8 ? row >> 2 & 1 : 0);
+}
 
 // A wave's sixteen positions of a tile on their way into LDS.  K [64][D], V [8][D][8]
 template <int D, int BITS> struct Sixteen;
@@ -162,7 +165,7 @@ template <int D> struct Sixteen<D, 16> {
         wave = wave_;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int row = i * (512 / D) + lane / (D / 8), piece = (lane % (D / 8)) ^ flip<D>(16 * wave + row);
+            const int row = i * (512 / D) + lane / (D / 8), piece = (lane % (D / 8)) ^ flip<D, 16>(16 * wave + row);
             k[i] = (uint32_t)(row * 2 * c.d + 16 * min(piece, (c.d >> 3) - 1));
             const int at = 64 * i + lane, eight = at / D, channel = at % D;
             v[i] = (uint32_t)((eight * c.d + min(channel, c.d - 1)) * 16);
@@ -186,13 +189,15 @@ template <int D> struct Sixteen<D, 8> {
     float step;
     uint32_t from_k[PER], from_v[PER];
     int wave, lane;
+    // The row whose piece of 16 bytes is the at-th of the sixteen rows': 0 4 1 5 2 6 3 7 8 12 ...
+    static __device__ __forceinline__ int key_row(int at) { const int i = at / (D / 16); return (i & 8) | (i & 1) << 2 | (i >> 1 & 3); }
     __device__ __forceinline__ void init(const Cache &c, int wave_, int lane_)
     {
         wave = wave_, lane = lane_;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int at = 64 * i + lane;
-            from_k[i] = (uint32_t)((at / (D / 16)) * c.d + 16 * min(at % (D / 16), (c.d >> 4) - 1));
+            from_k[i] = (uint32_t)(key_row(at) * c.d + 16 * min(at % (D / 16), (c.d >> 4) - 1));
             from_v[i] = (uint32_t)(min(at, c.d - 1) * 16);
         }
     }
@@ -210,10 +215,10 @@ template <int D> struct Sixteen<D, 8> {
     {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int at = 64 * i + lane, row = 16 * wave + at / (D / 16), piece = 2 * (at % (D / 16));
+            const int at = 64 * i + lane, row = 16 * wave + key_row(at), piece = 2 * (at % (D / 16));
             lds_byte *const to = tk + row * 2 * D;
-            lds_store(to + ((piece ^ flip<D>(row)) << 4), halves(k[i].x, k[i].y));
-            lds_store(to + (((piece + 1) ^ flip<D>(row)) << 4), halves(k[i].z, k[i].w));
+            lds_store(to + ((piece ^ flip<D, 8>(row)) << 4), halves(k[i].x, k[i].y));
+            lds_store(to + (((piece + 1) ^ flip<D, 8>(row)) << 4), halves(k[i].z, k[i].w));
             lds_store(tv + (2 * wave * D + at) * 16, halves(v[i].x, v[i].y));
             lds_store(tv + ((2 * wave + 1) * D + at) * 16, halves(v[i].z, v[i].w));
         }
@@ -576,7 +581,7 @@ template <typename T, int D, int E, int BITS, int HEAD> __device__ __forceinline
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int row = 16 * (col >> 2) + 4 * i + (col & 3);
-                    const uint4 f = lds_load(tk + row * 2 * D + (((4 * k + g) ^ flip<D>(row)) << 4));
+                    const uint4 f = lds_load(tk + row * 2 * D + (((4 * k + g) ^ flip<D, BITS>(row)) << 4));
                     s[i][0] = mma<M>(f, q[0][k], s[i][0]);
                     s[i][1] = mma<M>(f, q[1][k], s[i][1]);
                 }
