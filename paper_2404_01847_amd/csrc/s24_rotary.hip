@@ -52,13 +52,10 @@ __global__ __launch_bounds__(256, 4) void rotary_bwd_kernel(const BackwardArgs a
     const int heads = keys ? a.t.hkv : a.t.hq, groups = (heads + P::ROWS - 1) / P::ROWS;
     const Strided &dz = keys ? a.dzk : a.dzq, &x = keys ? a.xk : a.xq, &dx = keys ? a.dxk : a.dxq;
     const uint16_t *const w = keys ? a.t.wk : a.t.wq;
-    // Runs of `run` groups of rows, dealt to the waves one by one: a token's, or where there are fewer tokens than waves single ones.  (A stretch of its own for each wave
-    // reads the tokens from many places at once: RUNS_FIGURE.)
-    const int waves = 4 * (keys ? a.k_blocks : a.q_blocks), run = a.t.tokens >= waves ? groups : 1;
-    const int64_t items = (int64_t)a.t.tokens * groups, step = (int64_t)waves * run;
-    int64_t at = (int64_t)run * (4 * ((int)blockIdx.x - (keys ? a.q_blocks : 0)) + wave);   // the first item of the run
-    int token = 0, group = 0, left = 0, of = -1;
-    auto start = [&] { token = (int)(at / groups), group = (int)(at - (int64_t)token * groups), left = run; };
+    // Groups of rows are dealt to the waves one by one.  (A stretch of its own for each wave reads from as many places at once as there are waves: 8192 tokens of 64 + 8 heads of 128, both
+    // passes, 169 us with whole tokens to a wave, 164 so.)
+    const int waves = 4 * (keys ? a.k_blocks : a.q_blocks), mine = 4 * ((int)blockIdx.x - (keys ? a.q_blocks : 0)) + wave, tokens_on = waves / groups, groups_on = waves - tokens_on * groups;
+    int token = mine / groups, group = mine - token * groups, of = -1;
     P part(a.t, lane, (lds_angles *)&angles[wave]);
     float by[16], dw[16];
 #pragma unroll
@@ -72,18 +69,14 @@ __global__ __launch_bounds__(256, 4) void rotary_bwd_kernel(const BackwardArgs a
     };
     Pieces next_g{}, next_x{};
     int32_t next_position = 0;
-    bool more = at < items;
-    if (more) start(), loads(next_g, next_x), next_position = part.position(a.t, token);
-    while (more) {
+    if (token < a.t.tokens) loads(next_g, next_x), next_position = part.position(a.t, token);
+    while (token < a.t.tokens) {
         const Pieces now_g = next_g, now_x = next_x;
         const int32_t position = next_position;
         const int this_token = token, head = group * P::ROWS + part.r;
-        ++group;
-        if (--left == 0) {
-            at += step, more = at < items;
-            if (more) start(), next_position = part.position(a.t, token);
-        }
-        if (more) loads(next_g, next_x);
+        group += groups_on, token += tokens_on;
+        if (group >= groups) group -= groups, ++token;
+        if (token < a.t.tokens) loads(next_g, next_x), next_position = part.position(a.t, token);
         if (of != this_token) part.angles(a.t, position, true, lane), of = this_token;
         float g[16];
         P::widen(now_g, g);
