@@ -176,12 +176,13 @@ static int launch_forward(const Turn &t, const Strided (&x)[4], bool neighbours,
     else rotate<s24_half>(a, neighbours, grid, st);
     return s24_launch_status();
 }
-// Workgroups that share the rows of the queries (the keys): up to four a compute unit for both, with four groups of rows to a wave at least
+// Workgroups that share the rows of the queries (the keys): up to sixteen a compute unit for both, with four groups of rows to a wave at least.  (No more than fit a compute unit
+// at once leave the last ones to end alone: 8192 tokens of 64 + 8 heads of 128, both passes, with four a compute unit 162 us, with eight 151, sixteen 150, 32 151.)
 struct Blocks { int q, k; };
 static Blocks blocks_of(int64_t tokens, int64_t hq, int64_t hkv, int64_t d)
 {
     const int rows = d <= 64 ? 16 : 8;
-    const int64_t q = tokens * ((hq + rows - 1) / rows), k = tokens * ((hkv + rows - 1) / rows), most = 4 * (int64_t)s24_cu_count();
+    const int64_t q = tokens * ((hq + rows - 1) / rows), k = tokens * ((hkv + rows - 1) / rows), most = 16 * (int64_t)s24_cu_count();
     auto blocks = [&](int64_t items) {
         const int64_t fit = (items + 15) / 16, share = q + k > 0 ? (most * items + q + k - 1) / (q + k) : 0;
         return (int)(fit < share ? fit : share);
