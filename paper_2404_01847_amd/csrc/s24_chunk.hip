@@ -85,7 +85,8 @@ struct Lists {
         // (More steps than the host has seen to have offsets that do not ascend: then nothing is cut.)
         if (high > 1 << 18 || tiles > a.pieces) return longest;
         const int all = (high << 12) + low, least = min(kLeastSteps, longest);
-        if (a.sequences > 64) return max(2 * (all / a.pieces) + 1, least);   // (count <= 4/3 of the quotient in what is cut: no more than a.pieces)
+        // (A tile of x `each` steps has no more than x parts besides its first: all of them at most as many as pieces are left.)
+        if (a.sequences > 64) return tiles == a.pieces ? longest : max(all / (a.pieces - tiles) + 1, least);
         int lo = max(all / a.pieces, least), hi = max(longest, lo);   // `hi` makes few enough pieces
         while (lo < hi) {
             const int middle = (lo + hi) >> 1;

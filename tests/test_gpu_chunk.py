@@ -109,6 +109,17 @@ def test_many_sequences(count, bits):
 
 
 @pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("short,long,positions,heads", [(90, 10, 20000, 4), (60, 6, 5000, 7), (200, 50, 1200, 2), (249, 1, 30000, 2), (100, 27, 3000, 4), (300, 2, 10000, 1)])
+def test_many_short_sequences_beside_long_ones(short, long, positions, heads, bits):
+    """More sequences than lanes, most of them of one step, a few cut into parts."""
+    gen = torch.Generator().manual_seed(short)
+    lens = torch.randint(1, 64, (short,), generator=gen).tolist()
+    for i in range(long):
+        lens.insert(i * (len(lens) // long), positions - 7 * i)
+    chunk([1 + (i % 9 == 0 and n > 1) for i, n in enumerate(lens)], lens, heads, heads, 16, BF16, bits, 64, seed=short)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("vstd,qstd", [(1e-5, 1.0), (1e4, 1.0), (1.0, 30.0), (1.0, 1e-6)])
 def test_scales_of_the_data(vstd, qstd, bits):
     chunk([20, 100], [500, 100], 4, 2, 128, BF16, bits, 32, vstd=vstd, qstd=qstd)
