@@ -424,8 +424,8 @@ int s24_attn_chunk(const s24_kv_cache *cache, const s24_heads *Q, int64_t hq, co
  * A head x of d values becomes z:  y_i = x_i w_i / sqrt(mean(x^2) + eps), or y = x where it is not normalised;  the pair (y_a, y_b) number p is turned by the angle
  * position * frequencies[p] (in radians):  z_a = y_a cos - y_b sin,  z_b = y_b cos + y_a sin;  what lies past the first `rotated` values is not turned.  Pair p is (p, p + rotated / 2),
  * or (2p, 2p + 1) where `interleaved`.  A token has `axes` positions, of which pair p turns by number axis[p] (of an image or a video: time, height and width).
- * All arithmetic is fp32 and rounded once; a turn is reduced exactly, so that angles of far positions are as good as those of near ones.  x^2 has to stay within
- * fp32; eps = 0 gives NaN for a head of zeros.  S24_BF16 and S24_F16; S24_F32 returns S24_ERR_UNSUPPORTED.
+ * All arithmetic is fp32 and rounded once; a turn is reduced exactly, so that angles of far positions are as good as those of near ones.  mean(x^2) + eps has to be a
+ * normal number of fp32; eps = 0 gives NaN for a head of zeros.  S24_BF16 and S24_F16; S24_F32 returns S24_ERR_UNSUPPORTED.
  *   frequencies  device fp64 [rotated / 2]
  *   axis         device int32 [rotated / 2] of 0 .. axes - 1 (others are cut to the last), or NULL: all turn by the first
  *   wq, wk       device [d] values of the calls' dtype, 16-byte aligned: weights of the queries' and of the keys' norm; NULL: not normalised
@@ -447,7 +447,7 @@ int s24_rotary_fwd(const s24_rotary *rotary, const int32_t *positions, const s24
 
 /* Gradients of s24_rotary_fwd from those of its results: with g = dz turned back, r = 1 / sqrt(mean(x^2) + eps) and y = x r,
  * dx_i = r (g_i w_i - y_i mean_j(g_j w_j y_j)), or g;  dw_i = beta dw_i + sum of g_i y_i over tokens and heads, in fp32 and in a fixed order; beta is 0 or 1.
- * dQ may be dQo itself and dK be dKo.  Q and K (those of the forward pass, before it) are read where they are normalised, and may be NULL otherwise, as dwq and dwk may.
+ * dQ may be dQo itself and dK be dKo.  Q and K (those of the forward pass, before it) are read where they are normalised, and may be NULL otherwise, as dwq and dwk may (those of no heads are beta dw).
  *   workspace  device, s24_rotary_bwd_workspace(...) bytes (0 without norms), 16-byte aligned; holds nothing between calls */
 int64_t s24_rotary_bwd_workspace(const s24_rotary *rotary, int64_t tokens, int64_t hq, int64_t hkv, int64_t d);
 int s24_rotary_bwd(const s24_rotary *rotary, const int32_t *positions, const s24_heads *dQo, const s24_heads *dKo, const s24_heads *Q, const s24_heads *K,

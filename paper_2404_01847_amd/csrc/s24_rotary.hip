@@ -231,17 +231,15 @@ extern "C" int s24_rotary_bwd(const s24_rotary *rotary, const int32_t *positions
     const int64_t need = s24_rotary_bwd_workspace(rotary, tokens, hq, hkv, d);
     S24_REQUIRE(workspace != nullptr || need == 0, S24_ERR_NULL);
     S24_REQUIRE(workspace_bytes >= need, S24_ERR_SHAPE);
-    if (hq + hkv == 0) return S24_OK;
-    Turn t = turn_args(rotary, positions, tokens, hq, hkv, d);
+    const Turn t = turn_args(rotary, positions, tokens, hq, hkv, d);
     const bool neighbours = rotary->interleaved != 0;
-    if (!norm_q && !norm_k) {
-        if (tokens == 0) return S24_OK;
-        t.wq = t.wk = nullptr;   // (of heads that there are none of)
+    if (rotary->wq == nullptr && rotary->wk == nullptr) {
+        if (tokens == 0 || hq + hkv == 0) return S24_OK;
         return launch_forward(t, {strided(dQo), strided(dKo), strided(dQ), strided(dK)}, neighbours, true, dt, stream);
     }
     const Blocks n = blocks_of(tokens, hq, hkv, d);
-    const BackwardArgs a{t, strided(dQo), strided(dKo), strided(Q), strided(K), strided(dQ), strided(dK), static_cast<float *>(workspace), norm_q ? dwq : nullptr,
-                         norm_k ? dwk : nullptr, beta, n.q, n.k};
+    const BackwardArgs a{t, strided(dQo), strided(dKo), strided(Q), strided(K), strided(dQ), strided(dK), static_cast<float *>(workspace), t.wq != nullptr ? dwq : nullptr,
+                         t.wk != nullptr ? dwk : nullptr, beta, n.q, n.k};
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (n.q + n.k > 0) {
         const dim3 grid((unsigned)(n.q + n.k));

@@ -84,6 +84,10 @@ def test_tokens(tokens, d, dtype):
     Case(tokens, 4, 2, d, dtype).check()
 
 
+def test_more_rows_than_the_workgroups_take_in_one_go():
+    Case(16000, 64, 8, 16, BF16).check()
+
+
 @pytest.mark.parametrize("norms", [(True, True), (False, False), (True, False), (False, True)])
 @pytest.mark.parametrize("hq,hkv", [(1, 1), (3, 1), (8, 8), (12, 4), (64, 8), (17, 16), (5, 0), (0, 3)])
 def test_heads(hq, hkv, norms):
@@ -181,6 +185,19 @@ def test_no_tokens(s24):
     assert bool((c.layer.dwq == 3.0).all()) and bool((c.layer.dwk == 4.0).all())
     c.layer.backward(c.dQ, c.dK, c.Q, c.K, c.positions)
     assert not c.layer.dwq.any() and not c.layer.dwk.any()
+
+
+@pytest.mark.parametrize("hq,hkv", [(0, 3), (5, 0), (0, 0)])
+def test_weights_of_no_heads_have_the_gradient_zero(s24, hq, hkv):
+    for norms in ((True, True), (True, False), (False, True)):
+        c = Case(50, hq, hkv, 64, BF16, norms=norms)
+        for beta, want in ((1.0, 3.0), (0.0, 0.0)):
+            for x in (c.layer.dwq, c.layer.dwk):
+                if x is not None:
+                    x.fill_(3.0)
+            c.layer.backward(c.dQ.clone(), c.dK.clone(), c.Q, c.K, c.positions, beta=beta)
+            for x, heads in ((c.layer.dwq, hq), (c.layer.dwk, hkv)):
+                assert x is None or heads > 0 or bool((x == want).all())
 
 
 def test_fewer_tokens_than_the_layer_has(s24):
