@@ -18,7 +18,7 @@ struct ChunkArgs {
     const int *cu, *table, *lengths;
     int64_t width;
     int sequences, tokens, hq, group, causal;
-    int pieces;        // that the tiles of a key-value head are cut into at most, as many as the device holds workgroups; 0: none is cut
+    int pieces, round; // that the tiles of a key-value head are cut into at most, 0: none is cut; as many of them as the device holds workgroups
     int sum_rows;      // that a workgroup adds the parts of
     float scale;
     float2 *weights;   // [hkv][pieces][kChunkRows]: reference and sum
@@ -29,11 +29,14 @@ __device__ __forceinline__ Span keys_of(const ChunkArgs &a, int i) { return {0, 
 __device__ __forceinline__ int row_tiles(const ChunkArgs &a, int i) { return (int)(((int64_t)span(a.cu, i, a.tokens).count * a.group + kChunkRows - 1) / kChunkRows); }
 __device__ __forceinline__ int key_tiles(const ChunkArgs &a, int i) { return (keys_of(a, i).count + kChunkKeys - 1) / kChunkKeys; }
 // Where tiles of rows are few, the positions that they go over are cut into parts, those of a sequence of one size, which leave their sums for another kernel to add; a tile in one part
-// is finished where it is.  A part has about `each` steps (tiles of positions): as few as make no more pieces than the device holds workgroups, two to a compute unit, since
-// a second round would take as long as the first.  (12 sequences of 2 to 512 tokens after up to 4000, 32 heads on 8 of 128, 43 tiles of 35 to 62 steps: PARTS_FIGURE.  Steps dealt out
-// evenly, whatever tiles they belong to, took EVEN_FIGURE: a piece of a tile costs 5 to 10 us besides its steps.)
+// is finished where it is.  A part has about `each` steps (tiles of positions): as few as make no more pieces than the device holds workgroups, two to a compute unit.  (12
+// sequences of 2 to 512 tokens after up to 4000, 32 heads on 8 of 128, 43 tiles of 35 to 62 steps: uncut 142 us, so 117.  Steps dealt out evenly, whatever tiles they belong to,
+// 157: a piece costs 5 to 10 us besides its steps.)  Where the tiles do not go evenly into them, so that the last piece would end more than a quarter later than an even share of all
+// steps, and eight steps, they are cut into twice as many pieces, of which a compute unit takes the next when it is done with one (the same batch after up to 12000: 310 us in one
+// round, 242 in two; with 32 heads on 2, after 8000, 184 and 153; where the pieces come out even, 512 tokens after 16000, 140 and 158).
 constexpr int kFewRows = 32;      // of a sequence
 constexpr int kLeastSteps = 8;    // of a part
+constexpr int kRound = 8;         // steps that a second round costs
 __device__ __forceinline__ bool is_few(const ChunkArgs &a, int i) { return (int64_t)span(a.cu, i, a.tokens).count * a.group <= kFewRows; }
 __device__ __forceinline__ int lanes_sum(int x) { return __builtin_amdgcn_readlane(running_sum(x), 63); }
 // Largest of what the lanes have, none of it negative
@@ -71,6 +74,20 @@ struct Lists {
         if (a.sequences > 64) return look(i);
         return {__builtin_amdgcn_readlane(mine.tiles, i), __builtin_amdgcn_readlane(mine.keys, i), __builtin_amdgcn_readlane(mine.few, i)};
     }
+    // Least steps of a part that make no more than so many pieces
+    __device__ __forceinline__ int least_steps(int pieces, int tiles, int all, int longest) const
+    {
+        const int least = min(kLeastSteps, longest);
+        // (A tile of x times as many steps has no more than x parts besides its first: all of them at most as many as pieces are left.)
+        if (a.sequences > 64) return tiles == pieces ? longest : max(all / (pieces - tiles) + 1, least);
+        int lo = max(all / pieces, least), hi = max(longest, lo);   // `hi` makes few enough pieces
+        while (lo < hi) {
+            const int middle = (lo + hi) >> 1;
+            if (lanes_sum(mine.tiles * parts_in(mine.keys, middle).count) <= pieces) hi = middle;
+            else lo = middle + 1;
+        }
+        return hi;
+    }
     // Steps of a part
     __device__ __forceinline__ int each() const
     {
@@ -84,16 +101,12 @@ struct Lists {
         const int high = lanes_sum((int)min(steps >> 12, (int64_t)1 << 24)), low = lanes_sum((int)(steps & 4095));
         // (More steps than the host has seen to have offsets that do not ascend: then nothing is cut.)
         if (high > 1 << 18 || tiles > a.pieces) return longest;
-        const int all = (high << 12) + low, least = min(kLeastSteps, longest);
-        // (A tile of x `each` steps has no more than x parts besides its first: all of them at most as many as pieces are left.)
-        if (a.sequences > 64) return tiles == a.pieces ? longest : max(all / (a.pieces - tiles) + 1, least);
-        int lo = max(all / a.pieces, least), hi = max(longest, lo);   // `hi` makes few enough pieces
-        while (lo < hi) {
-            const int middle = (lo + hi) >> 1;
-            if (lanes_sum(mine.tiles * parts_in(mine.keys, middle).count) <= a.pieces) hi = middle;
-            else lo = middle + 1;
-        }
-        return hi;
+        const int all = (high << 12) + low, once = tiles <= a.round ? least_steps(a.round, tiles, all, longest) : longest;
+        if (a.pieces == a.round) return once;
+        // When one round would end
+        const int even = all / a.round, half = a.sequences > 64 ? min(longest, once + once / 2) : lanes_max(mine.tiles > 0 ? parts_in(mine.keys, once).steps : 0);
+        const int last = tiles <= a.round ? half : even + longest / 2;
+        return last > even + even / 4 + kRound ? least_steps(a.pieces, tiles, all, longest) : once;
     }
     // Sums that the sequences before this one leave
     __device__ __forceinline__ int slots_before(int each, int sequence) const
@@ -749,7 +762,7 @@ static int64_t chunk_pieces(const s24_kv_cache *c, int64_t width, int64_t tokens
 {
     const int64_t held = 2 * (int64_t)s24_cu_count(), steps = (width * c->page + kChunkKeys - 1) / kChunkKeys, tiles = chunk_tiles(c, tokens, sequences, hq);
     if (tokens * (hq / c->hkv) / kChunkRows * c->hkv >= 2 * held || steps <= kLeastSteps || tiles * steps > INT32_MAX / 2) return 0;   // (steps are counted in an int)
-    const int64_t of_head = held / c->hkv, worth = tiles * (1 + steps / kLeastSteps);   // no more than have so many steps each
+    const int64_t of_head = 2 * (held / c->hkv), worth = tiles * (1 + steps / kLeastSteps);   // no more than have so many steps each
     return of_head < worth ? of_head : worth;
 }
 template <typename T, int BITS> static void chunk(const ChunkArgs &a, dim3 grid, dim3 join, hipStream_t st)
@@ -799,7 +812,7 @@ extern "C" int s24_attn_chunk(const s24_kv_cache *cache, const s24_heads *Q, int
     S24_REQUIRE(workspace != nullptr || need == 0, S24_ERR_NULL);
     S24_REQUIRE(s24_aligned(cu, 4) && s24_aligned(table, 4) && s24_aligned(lengths, 4) && s24_aligned(workspace, 16), S24_ERR_ALIGN);
     S24_REQUIRE(workspace_bytes >= need, S24_ERR_SHAPE);
-    const int64_t pieces = chunk_pieces(cache, width, tokens, sequences, hq), tiles = chunk_tiles(cache, tokens, sequences, hq), group = hq / cache->hkv;
+    const int64_t pieces = chunk_pieces(cache, width, tokens, sequences, hq), round = 2 * (int64_t)s24_cu_count() / cache->hkv, tiles = chunk_tiles(cache, tokens, sequences, hq), group = hq / cache->hkv;
     const int64_t groups = (pieces > tiles ? pieces : tiles) * cache->hkv;
     // About a thousand workgroups add the parts, each one to 64 rows.
     int sum_rows = 1;
@@ -807,7 +820,7 @@ extern "C" int s24_attn_chunk(const s24_kv_cache *cache, const s24_heads *Q, int
     const int64_t join = most_tiles(tokens * group, tokens < sequences ? tokens : sequences, sum_rows) * cache->hkv;
     S24_REQUIRE(groups <= kMostGroups && join <= kMostGroups, S24_ERR_SHAPE);
     ChunkArgs a{cache_of(cache), {static_cast<uint16_t *>(Q->data), Q->token, Q->head}, {static_cast<uint16_t *>(O->data), O->token, O->head}, cu, table, lengths,
-                cache->pages > 0 ? width : 0, (int)sequences, (int)tokens, (int)hq, (int)group, causal != 0, (int)pieces, sum_rows, scale};
+                cache->pages > 0 ? width : 0, (int)sequences, (int)tokens, (int)hq, (int)group, causal != 0, (int)pieces, (int)(pieces < round ? pieces : round), sum_rows, scale};
     a.weights = static_cast<float2 *>(workspace);
     a.sums = reinterpret_cast<float *>(static_cast<char *>(workspace) + pieces * cache->hkv * kChunkRows * sizeof(float2));
     const hipStream_t st = static_cast<hipStream_t>(stream);

@@ -120,6 +120,14 @@ def test_many_short_sequences_beside_long_ones(short, long, positions, heads, bi
 
 
 @pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("new,lens,heads", [([33, 40, 1], [5000, 4800, 300], 128), ([33] * 5 + [2], [3000, 2900, 2800, 900, 70, 2000], 128), ([20, 3, 33], [4000, 4000, 4100], 256),
+                                            ([33, 1] * 40 + [7] * 10, [6400] * 80 + [60] * 10, 4), ([1] * 150, [1500] * 75 + [3000] * 75, 4)])
+def test_tiles_that_do_not_go_evenly_into_the_workgroups(new, lens, heads, bits):
+    """They are cut into twice as many parts as the device holds at once."""
+    chunk(new, lens, heads, heads, 16, F16, bits, 64, seed=len(new))
+
+
+@pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("vstd,qstd", [(1e-5, 1.0), (1e4, 1.0), (1.0, 30.0), (1.0, 1e-6)])
 def test_scales_of_the_data(vstd, qstd, bits):
     chunk([20, 100], [500, 100], 4, 2, 128, BF16, bits, 32, vstd=vstd, qstd=qstd)
