@@ -516,6 +516,16 @@ def _heads(where, name, x, shape, dtype, device):
     return _pack_heads(x.data_ptr(), token if shape[0] > 1 else 0, head if shape[1] > 1 else 0)
 
 
+def _measured(where, name, x, shape, dtype, device):
+    """_heads of a tensor whose own shape this is, and which the other operands are held against."""
+    if x.dtype is not dtype or x.get_device() != device:
+        _refused(where, name, x, dtype, shape, device)
+    token, head, unit = x.stride()
+    if unit != 1:
+        _refused(where, name, x, dtype, shape, device)
+    return _pack_heads(x.data_ptr(), token if shape[0] > 1 else 0, head if shape[1] > 1 else 0)
+
+
 def _axes(where, name, x, axes):
     """The shape of a tensor whose sizes the call goes by."""
     shape = x.shape
@@ -706,10 +716,11 @@ def attn_chunk(cache, Q, cu, table, lengths, O, workspace, scale=None, causal=Tr
     if len(n) != 2 or len(shape) != 3 or shape[2] != d:
         raise ValueError(f"{where}: table must have shape [sequences, pages] and Q must have shape [tokens, heads, {d}], got {tuple(n)} and {tuple(shape)}")
     sequences, width = n
-    args = (cache.packed, _heads(where, "Q", Q, shape, dtype, device), shape[1], _whole(where, "cu", cu, torch.int32, (sequences + 1,), device),
+    args = (cache.packed, _measured(where, "Q", Q, shape, dtype, device), shape[1], _whole(where, "cu", cu, torch.int32, (sequences + 1,), device),
             _whole(where, "table", table, torch.int32, n, device), width, _whole(where, "lengths", lengths, torch.int32, (sequences,), device), sequences, shape[0],
             d ** -0.5 if scale is None else scale, bool(causal), _heads(where, "O", O, shape, dtype, device), *_work(where, workspace, device), _DTYPES[dtype])
-    _of_gpu(where, device)
+    if device < 0:
+        _no_gpu(where)
     status = lib().s24_attn_chunk(*args, _stream())
     if status != 0:
         raise S24Error(status, where)
@@ -742,13 +753,14 @@ class RotaryPlan:
             if self.pairs > 0:
                 raise ValueError(f"{where}: heads that are turned need positions")
             return 0
-        n = positions.shape
-        return _whole(where, "positions", positions, torch.int32, (tokens,) if self.axes == 1 and len(n) == 1 else (self.axes, tokens), device)
+        n, axes = positions.shape, self.axes
+        if n != (axes, tokens) and (axes != 1 or n != (tokens,)) or positions.dtype is not torch.int32 or positions.get_device() != device or not positions.is_contiguous():
+            _refused(where, "positions", positions, torch.int32, (tokens,) if axes == 1 and len(n) == 1 else (axes, tokens), device)
+        return positions.data_ptr()
 
 
-def _of_gpu(where, device):
-    if device < 0:
-        raise ValueError(f"{where}: the tensors must lie on a GPU")
+def _no_gpu(where):
+    raise ValueError(f"{where}: the tensors must lie on a GPU")
 
 
 class OwnHeads:
@@ -777,9 +789,10 @@ def rotary_fwd(plan, Q, K, positions, Qo, Ko):
     if len(sq) != 3 or len(sk) != 3 or sq[2] != d or sk[2] != d or sk[0] != sq[0]:
         raise ValueError(f"{where}: Q and K must have shape [tokens, heads, {d}] with as many tokens, got {tuple(sq)} and {tuple(sk)}")
     tokens = sq[0]
-    args = (plan.packed, plan.positions(where, positions, tokens, device), _heads(where, "Q", Q, sq, dtype, device), _heads(where, "K", K, sk, dtype, device),
+    args = (plan.packed, plan.positions(where, positions, tokens, device), _measured(where, "Q", Q, sq, dtype, device), _measured(where, "K", K, sk, dtype, device),
             _written(where, "Qo", Qo, sq, dtype, device), _written(where, "Ko", Ko, sk, dtype, device), tokens, sq[1], sk[1], d, plan.type)
-    _of_gpu(where, device)
+    if device < 0:
+        _no_gpu(where)
     status = lib().s24_rotary_fwd(*args, _stream())
     if status != 0:
         raise S24Error(status, where)
@@ -808,9 +821,10 @@ def rotary_bwd(plan, dQo, dKo, Q, K, positions, dQ, dK, dwq=None, dwk=None, beta
             q, gq = _heads(where, "Q", Q, sq, dtype, device), _whole(where, "dwq", dwq, torch.float32, (d,), device)
         if nk:
             k, gk = _heads(where, "K", K, sk, dtype, device), _whole(where, "dwk", dwk, torch.float32, (d,), device)
-    args = (plan.packed, plan.positions(where, positions, tokens, device), _heads(where, "dQo", dQo, sq, dtype, device), _heads(where, "dKo", dKo, sk, dtype, device), q, k,
+    args = (plan.packed, plan.positions(where, positions, tokens, device), _measured(where, "dQo", dQo, sq, dtype, device), _measured(where, "dKo", dKo, sk, dtype, device), q, k,
             _heads(where, "dQ", dQ, sq, dtype, device), _heads(where, "dK", dK, sk, dtype, device), gq, gk, beta, tokens, sq[1], sk[1], d, *_work(where, workspace, device), plan.type)
-    _of_gpu(where, device)
+    if device < 0:
+        _no_gpu(where)
     status = lib().s24_rotary_bwd(*args, _stream())
     if status != 0:
         raise S24Error(status, where)
@@ -827,9 +841,10 @@ def kv_append(cache, plan, Q, K, V, positions, places, Qo):
         raise ValueError(f"{where}: Q must have shape [tokens, heads, {plan.d}], got {tuple(sq)}")
     tokens = sq[0]
     sk = (tokens, cache.hkv, cache.d)
-    args = (cache.packed, plan.packed, plan.positions(where, positions, tokens, device), _heads(where, "Q", Q, sq, dtype, device), sq[1], _heads(where, "K", K, sk, dtype, device),
+    args = (cache.packed, plan.packed, plan.positions(where, positions, tokens, device), _measured(where, "Q", Q, sq, dtype, device), sq[1], _heads(where, "K", K, sk, dtype, device),
             _heads(where, "V", V, sk, dtype, device), _written(where, "Qo", Qo, sq, dtype, device), _whole(where, "places", places, torch.int64, (tokens,), device), tokens, plan.type)
-    _of_gpu(where, device)
+    if device < 0:
+        _no_gpu(where)
     status = lib().s24_kv_append(*args, _stream())
     if status != 0:
         raise S24Error(status, where)

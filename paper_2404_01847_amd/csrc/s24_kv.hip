@@ -307,6 +307,8 @@ template <int LANES> __device__ __forceinline__ float sixteen_numbers(const floa
     return step;
 }
 // One launch: waves that write V as above, and waves that have the rows of the queries and keys of a token.
+// Bound by memory: 13868 tokens of 64 + 8 heads of 128 with norms into 8 bits take 103 us, 5.3 TB/s of 546 MB (vector instructions are issued in 52 % of the cycles, a plain copy reaches
+// 6.5); 16 tokens 4.1, which is the launch.
 template <typename T, int BITS, int LANES, bool NEIGHBOURS>
 __global__ __launch_bounds__(256) void kv_append_kernel(const AppendArgs a)
 {

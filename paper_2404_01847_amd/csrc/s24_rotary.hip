@@ -13,6 +13,10 @@ struct ForwardArgs {
     int shares;
     bool back;
 };
+// Bound by memory: 8192 tokens of 64 + 8 heads of 128 with norms take 48 us, 6.3 TB/s of what they read and write (a plain copy reaches 6.5), with vector instructions issued in 51 % of the
+// cycles; 8 x 1024 tokens of 12 + 12 heads of 64 without 13 (4.0, two calls on the same tensors).  729 tokens take 4, which is the launch.  Rows that the attention reads next are
+// stored plainly: past the caches the kernel alone gains, but this and the attention of 8192 tokens of 64 heads on 8 together take 1134 us and not 1088.  Gradients, which a large
+// product reads much later, go past them.
 template <typename T, int LANES, bool NEIGHBOURS>
 __global__ __launch_bounds__(256) void rotary_kernel(const ForwardArgs a)
 {
@@ -33,6 +37,9 @@ __global__ __launch_bounds__(256) void rotary_kernel(const ForwardArgs a)
 
 // Backward where something is normalised.  A wave has the queries or the keys alone: a stretch of their groups of rows, token by token, over which it sums dw in registers; a
 // workgroup's sums go to memory, for another launch to add in order.
+// Bound by memory: 8192 tokens of 64 + 8 heads of 128 take 91 us, 5.0 TB/s (adding two tensors of that size to a third, by an elementwise kernel that does nothing else, 5.8), with vector
+// instructions issued in 50 % of the cycles at three waves a SIMD: dw keeps 16 sums in each lane, so there are registers for four.  A second group of rows ahead of the arithmetic, two
+// groups at once, and seven or eight waves with what they spill, were slower.
 struct BackwardArgs {
     Turn t;
     Strided dzq, dzk, xq, xk, dxq, dxk;
