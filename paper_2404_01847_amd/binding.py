@@ -719,9 +719,7 @@ def attn_chunk(cache, Q, cu, table, lengths, O, workspace, scale=None, causal=Tr
     args = (cache.packed, _measured(where, "Q", Q, shape, dtype, device), shape[1], _whole(where, "cu", cu, torch.int32, (sequences + 1,), device),
             _whole(where, "table", table, torch.int32, n, device), width, _whole(where, "lengths", lengths, torch.int32, (sequences,), device), sequences, shape[0],
             d ** -0.5 if scale is None else scale, bool(causal), _heads(where, "O", O, shape, dtype, device), *_work(where, workspace, device), _DTYPES[dtype])
-    if device < 0:
-        _no_gpu(where)
-    status = lib().s24_attn_chunk(*args, _stream())
+    status = lib().s24_attn_chunk(*args, _stream_of(where, device))
     if status != 0:
         raise S24Error(status, where)
     return O
@@ -759,8 +757,14 @@ class RotaryPlan:
         return positions.data_ptr()
 
 
-def _no_gpu(where):
-    raise ValueError(f"{where}: the tensors must lie on a GPU")
+def _stream_of(where, device):
+    """_stream, for tensors of a device that has to be the current one: a stream's kernels run on its own device."""
+    if device < 0:
+        raise ValueError(f"{where}: the tensors must lie on a GPU")
+    now = torch._C._cuda_getDevice()
+    if device != now:
+        raise ValueError(f"{where}: the tensors lie on device {device}, the current one is {now}")
+    return torch._C._cuda_getCurrentRawStream(now)
 
 
 class OwnHeads:
@@ -791,9 +795,7 @@ def rotary_fwd(plan, Q, K, positions, Qo, Ko):
     tokens = sq[0]
     args = (plan.packed, plan.positions(where, positions, tokens, device), _measured(where, "Q", Q, sq, dtype, device), _measured(where, "K", K, sk, dtype, device),
             _written(where, "Qo", Qo, sq, dtype, device), _written(where, "Ko", Ko, sk, dtype, device), tokens, sq[1], sk[1], d, plan.type)
-    if device < 0:
-        _no_gpu(where)
-    status = lib().s24_rotary_fwd(*args, _stream())
+    status = lib().s24_rotary_fwd(*args, _stream_of(where, device))
     if status != 0:
         raise S24Error(status, where)
     return Qo, Ko
@@ -823,9 +825,7 @@ def rotary_bwd(plan, dQo, dKo, Q, K, positions, dQ, dK, dwq=None, dwk=None, beta
             k, gk = _heads(where, "K", K, sk, dtype, device), _whole(where, "dwk", dwk, torch.float32, (d,), device)
     args = (plan.packed, plan.positions(where, positions, tokens, device), _measured(where, "dQo", dQo, sq, dtype, device), _measured(where, "dKo", dKo, sk, dtype, device), q, k,
             _heads(where, "dQ", dQ, sq, dtype, device), _heads(where, "dK", dK, sk, dtype, device), gq, gk, beta, tokens, sq[1], sk[1], d, *_work(where, workspace, device), plan.type)
-    if device < 0:
-        _no_gpu(where)
-    status = lib().s24_rotary_bwd(*args, _stream())
+    status = lib().s24_rotary_bwd(*args, _stream_of(where, device))
     if status != 0:
         raise S24Error(status, where)
     return dQ, dK
@@ -843,9 +843,7 @@ def kv_append(cache, plan, Q, K, V, positions, places, Qo):
     sk = (tokens, cache.hkv, cache.d)
     args = (cache.packed, plan.packed, plan.positions(where, positions, tokens, device), _measured(where, "Q", Q, sq, dtype, device), sq[1], _heads(where, "K", K, sk, dtype, device),
             _heads(where, "V", V, sk, dtype, device), _written(where, "Qo", Qo, sq, dtype, device), _whole(where, "places", places, torch.int64, (tokens,), device), tokens, plan.type)
-    if device < 0:
-        _no_gpu(where)
-    status = lib().s24_kv_append(*args, _stream())
+    status = lib().s24_kv_append(*args, _stream_of(where, device))
     if status != 0:
         raise S24Error(status, where)
     return Qo

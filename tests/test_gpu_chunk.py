@@ -248,6 +248,17 @@ def test_nothing_new():
 
 
 @pytest.mark.parametrize("bits", [16, 8])
+def test_no_pages_to_see(bits):
+    """A table without columns, and a cache without pages: zeros, whatever the lengths say."""
+    from paper_2404_01847_amd.attention import PagedKV
+    Q = normal((9, 4, 64), BF16, 1)
+    for cache, table in ((PagedKV(4, 16, 2, 64, bits=bits), torch.zeros((2, 0), dtype=torch.int32, device="cuda")), (PagedKV(0, 16, 2, 64, bits=bits), torch.zeros((2, 300), dtype=torch.int32, device="cuda"))):
+        O = torch.full_like(Q, math.nan)
+        cache.attend_chunk(Q, gpu_i32([0, 4, 9]), table, gpu_i32([100, 5]), O)
+        assert not O.any()
+
+
+@pytest.mark.parametrize("bits", [16, 8])
 def test_tables_offsets_and_lengths_that_hold_anything_stay_in_the_operands(bits):
     from test_gpu_attention_guards import Guarded
     import paper_2404_01847_amd as s24

@@ -177,3 +177,14 @@ def test_the_binding_refuses_what_the_calls_cannot_see(lib):
                  lambda: s24.attn_chunk(c.buffers, scalar, cu, table, cu[:2], Q, None), lambda: s24.attn_chunk(c.buffers, Q, cu, table[0], cu[:2], Q, None)):
         with pytest.raises(ValueError, match="must have shape"):
             call()
+
+
+def test_tensors_of_another_device_than_the_current_one_are_refused(monkeypatch):
+    from paper_2404_01847_amd import binding
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 40 + device, raising=False)
+    assert binding._stream_of("call", 0) == 40
+    with pytest.raises(ValueError, match="device 1, the current one is 0"):
+        binding._stream_of("call", 1)
+    with pytest.raises(ValueError, match="must lie on a GPU"):
+        binding._stream_of("call", -1)
