@@ -791,7 +791,7 @@ template <typename T, int BITS> static void chunk(const ChunkArgs &a, dim3 grid,
     case 112: chunk_kernel<T, 128, 128, BITS, 112><<<grid, block, 0, st>>>(a); break;
     default: chunk_kernel<T, 128, 128, BITS, 128><<<grid, block, 0, st>>>(a); break;
     }
-    chunk_join_kernel<T><<<join, block, 0, st>>>(a);
+    if ((a.width << a.c.shift) > (3 * kLeastSteps / 2 - 1) * kChunkKeys) chunk_join_kernel<T><<<join, block, 0, st>>>(a);   // (shorter ones are one part)
 }
 }  // namespace s24_kv
 
