@@ -36,6 +36,7 @@ __device__ __forceinline__ int key_tiles(const ChunkArgs &a, int i) { return (ke
 // round, 242 in two; with 32 heads on 2, after 8000, 184 and 153; where the pieces come out even, 512 tokens after 16000, 140 and 158).
 constexpr int kFewRows = 32;      // of a sequence
 constexpr int kLeastSteps = 8;    // of a part
+constexpr int kCutSteps = kLeastSteps + kLeastSteps / 2;   // of the shortest sequence in two parts
 constexpr int kRound = 8;         // steps that a second round costs
 __device__ __forceinline__ bool is_few(const ChunkArgs &a, int i) { return (int64_t)span(a.cu, i, a.tokens).count * a.group <= kFewRows; }
 __device__ __forceinline__ int lanes_sum(int x) { return __builtin_amdgcn_readlane(running_sum(x), 63); }
@@ -97,7 +98,9 @@ struct Lists {
             const List x = in_turn(i);
             steps += (int64_t)x.tiles * x.keys, tiles += x.tiles, longest = x.tiles > 0 ? max(longest, x.keys) : longest;
         }
-        longest = max(lanes_max(longest), 1), tiles = lanes_sum(tiles);
+        longest = max(lanes_max(longest), 1);
+        if (longest < kCutSteps) return longest;
+        tiles = lanes_sum(tiles);
         const int high = lanes_sum((int)min(steps >> 12, (int64_t)1 << 24)), low = lanes_sum((int)(steps & 4095));
         // (More steps than the host has seen to have offsets that do not ascend: then nothing is cut.)
         if (high > 1 << 18 || tiles > a.pieces) return longest;
@@ -760,15 +763,18 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(const ChunkArgs a)
 }
 
 // ------------------------------------------------------------------ host
-// Tiles of rows of a key-value head at most, and pieces that they are cut into; 0: none is, where there are so many that the device is full to the end anyway
+// Tiles of rows of a key-value head at most, and pieces that they are cut into; 0: none is, where there are so many that the device is full to the end anyway, or the sequences are short
 static int64_t chunk_tiles(const s24_kv_cache *c, int64_t tokens, int64_t sequences, int64_t hq)
 {
     return tokens * (hq / c->hkv) / kChunkRows + (tokens < sequences ? tokens : sequences);
 }
 static int64_t chunk_pieces(const s24_kv_cache *c, int64_t width, int64_t tokens, int64_t sequences, int64_t hq)
 {
-    const int64_t held = 2 * (int64_t)s24_cu_count(), steps = (width * c->page + kChunkKeys - 1) / kChunkKeys, tiles = chunk_tiles(c, tokens, sequences, hq);
-    if (tokens * (hq / c->hkv) / kChunkRows * c->hkv >= 2 * held || steps <= kLeastSteps || tiles * steps > INT32_MAX / 2) return 0;   // (steps are counted in an int)
+    const int64_t held = 2 * (int64_t)s24_cu_count(), steps = (width * c->page + kChunkKeys - 1) / kChunkKeys, tiles = chunk_tiles(c, tokens, sequences, hq), rows = tokens * (hq / c->hkv);
+    if (rows / kChunkRows * c->hkv >= 2 * held || tiles * steps > INT32_MAX / 2) return 0;   // (steps are counted in an int)
+    // None is cut: the kernel that has a way for few rows, if most have few and more than two tiles of positions.  (16 sequences of 5 tokens after up to 500, 8 heads on 2 of 128 in 8 bits, 14 us
+    // so and 20 in whole tiles; 55 of 2 tokens after none, 12 heads, 15 and 13.)
+    if (steps < kCutSteps) return steps > 2 && rows <= kFewRows * sequences ? tiles : 0;
     const int64_t of_head = 2 * (held / c->hkv), worth = tiles * (1 + steps / kLeastSteps);   // no more than have so many steps each
     return of_head < worth ? of_head : worth;
 }
@@ -791,7 +797,7 @@ template <typename T, int BITS> static void chunk(const ChunkArgs &a, dim3 grid,
     case 112: chunk_kernel<T, 128, 128, BITS, 112><<<grid, block, 0, st>>>(a); break;
     default: chunk_kernel<T, 128, 128, BITS, 128><<<grid, block, 0, st>>>(a); break;
     }
-    if ((a.width << a.c.shift) > (3 * kLeastSteps / 2 - 1) * kChunkKeys) chunk_join_kernel<T><<<join, block, 0, st>>>(a);   // (shorter ones are one part)
+    if ((a.width << a.c.shift) > (kCutSteps - 1) * kChunkKeys) chunk_join_kernel<T><<<join, block, 0, st>>>(a);
 }
 }  // namespace s24_kv
 
@@ -800,6 +806,7 @@ using namespace s24_kv;
 extern "C" int64_t s24_attn_chunk_workspace(const s24_kv_cache *cache, int64_t width, int64_t tokens, int64_t sequences, int64_t hq)
 {
     if (cache == nullptr || cache->hkv <= 0 || cache->d <= 0 || cache->page <= 0 || width < 0 || tokens < 0 || sequences < 0 || hq <= 0 || hq % cache->hkv != 0) return 0;
+    if (width * cache->page <= (kCutSteps - 1) * kChunkKeys) return 0;   // none is cut
     return chunk_pieces(cache, width, tokens, sequences, hq) * cache->hkv * kChunkRows * ((int64_t)sizeof(float2) + cache->d * 4);
 }
 

@@ -109,6 +109,17 @@ def test_many_sequences(count, bits):
 
 
 @pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("new,lens", [([5] * 16, list(range(300, 460, 10))), ([1, 2, 33, 1, 0, 4], [700, 64, 500, 129, 300, 192]), ([2] * 90, [140 + 3 * i for i in range(90)]), ([7, 1], [703, 704]), ([3], [130])])
+def test_short_sequences_of_few_rows(new, lens, bits):
+    """None is cut, and there is no workspace."""
+    import paper_2404_01847_amd as s24
+    for heads, d, page in (((4, 2), 64, 64), ((8, 4), 112, 16)):
+        chunk(new, lens, *heads, d, BF16, bits, page, seed=len(new))
+        cache = filled(None, [16], page, heads[1], d, BF16, bits)[0]
+        assert s24.attn_chunk_workspace(cache.buffers, 704 // page, sum(new), len(new), heads[0]) == 0
+
+
+@pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("short,long,positions,heads", [(90, 10, 20000, 4), (60, 6, 5000, 7), (200, 50, 1200, 2), (249, 1, 30000, 2), (100, 27, 3000, 4), (300, 2, 10000, 1)])
 def test_many_short_sequences_beside_long_ones(short, long, positions, heads, bits):
     """More sequences than lanes, most of them of one step, a few cut into parts."""
