@@ -414,7 +414,7 @@ int s24_attn_decode(const s24_kv_cache *cache, const s24_heads *Q, int64_t hq, c
  * lengths[i] (device) positions, their own included.  Query t of lq sees the positions j <= t + lengths[i] - lq, or all of them where not `causal`; zeros for a query that sees none.
  * Any number of new tokens of each sequence, one too (s24_attn_decode is the faster call where all have one).  Lengths beyond width*page are cut; width*page up to 2^30, and
  * times hq / hkv below 2^36 (S24_ERR_SHAPE).  Precision, and what NaN does, are those of s24_attn_fwd and in an 8-bit cache those of s24_attn_decode.
- *   workspace  device, s24_attn_chunk_workspace(cache, width, tokens, sequences, hq) bytes (0 for many tokens: then NULL will do), 16-byte aligned; holds nothing between calls */
+ *   workspace  device, s24_attn_chunk_workspace(cache, width, tokens, sequences, hq) bytes (0 for many tokens, and for tables of up to 704 positions: then NULL will do), 16-byte aligned; holds nothing between calls */
 int64_t s24_attn_chunk_workspace(const s24_kv_cache *cache, int64_t width, int64_t tokens, int64_t sequences, int64_t hq);
 int s24_attn_chunk(const s24_kv_cache *cache, const s24_heads *Q, int64_t hq, const int32_t *cu, const int32_t *table, int64_t width, const int32_t *lengths,
                    int64_t sequences, int64_t tokens, float scale, int causal, const s24_heads *O, void *workspace, int64_t workspace_bytes, s24_dtype dt, void *stream);

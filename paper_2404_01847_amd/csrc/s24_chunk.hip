@@ -678,8 +678,8 @@ template <typename T, int D, int E, int BITS, int HEAD> __device__ __forceinline
     }
 }
 
-// What bounds it: for many rows matrix instructions and the vector instructions of the softmax, in turn more than at once: 2 x 4096 tokens of 32 heads of 128 285 us (0.97 PFLOP/s of
-// what they need, 45 and 47 % of the cycles), the same as the forward pass over packed rows takes; in 8 bits 4 chunks of 400 to 1024 tokens after up to 30000, 64 heads on 8, 2680 to 2740
+// What bounds it: for many rows matrix instructions and the vector instructions of the softmax, in turn more than at once: 2 x 4096 tokens of 32 heads of 128 285 to 297 us (0.95 PFLOP/s of
+// what they need, 45 and 47 % of the cycles), the same as the forward pass over packed rows takes; in 8 bits 4 chunks of 400 to 1024 tokens after up to 30000, 64 heads on 8, 2680 to 2760
 // (0.9; 37 and 60 %: the whole numbers become operands once for each tile of rows).  To look for the largest score only where weights have grown past the reference saved
 // instructions and lost time.
 template <typename T, int D, int E, int BITS, int HEAD>
