@@ -75,6 +75,12 @@ def test_grouped_heads(hq, hkv, bits):
 
 
 @pytest.mark.parametrize("bits", [16, 8])
+def test_more_heads_than_the_device_holds_workgroups(bits):
+    chunk([3, 40], [130, 900], 600, 600, 16, BF16, bits, 16)
+    chunk([3, 1], [300, 500], 600, 600, 16, BF16, bits, 16)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("d", [16, 32, 48, 80, 96, 112])
 def test_head_sizes_between(d, bits):
     for dtype in (BF16, F16):
