@@ -35,7 +35,9 @@ __device__ __forceinline__ int key_tiles(const ChunkArgs &a, int i) { return (ke
 // steps, and eight steps, they are cut into twice as many pieces, of which a compute unit takes the next when it is done with one (the same batch after up to 12000: 310 us in one
 // round, 242 in two; with 32 heads on 2, after 8000, 184 and 153; where the pieces come out even, 512 tokens after 16000, 140 and 158).
 constexpr int kFewRows = 32;      // of a sequence
-constexpr int kLeastSteps = 8;    // of a part
+// Least steps of a part, and where the longest sequence has at least so many.  (One sequence of 16000 positions, 4 heads on 1 of 128: 20.5 us with eight, 18.4 with six; 58 of up to 652, 16 heads
+// on 8 of 64, are better off in one part: 20 us and 22.)
+constexpr int kLeastSteps = 8, kLeastOfLong = 6, kLong = 32;
 constexpr int kCutSteps = kLeastSteps + kLeastSteps / 2;   // of the shortest sequence in two parts
 constexpr int kRound = 8;         // steps that a second round costs
 __device__ __forceinline__ bool is_few(const ChunkArgs &a, int i) { return (int64_t)span(a.cu, i, a.tokens).count * a.group <= kFewRows; }
@@ -78,7 +80,7 @@ struct Lists {
     // Least steps of a part that make no more than so many pieces
     __device__ __forceinline__ int least_steps(int pieces, int tiles, int all, int longest) const
     {
-        const int least = min(kLeastSteps, longest);
+        const int least = longest >= kLong ? kLeastOfLong : min(kLeastSteps, longest);
         // (A tile of x times as many steps has no more than x parts besides its first: all of them at most as many as pieces are left.)
         if (a.sequences > 64) return tiles == pieces ? longest : max(all / (pieces - tiles) + 1, least);
         int lo = max(all / pieces, least), hi = max(longest, lo);   // `hi` makes few enough pieces
@@ -775,7 +777,7 @@ static int64_t chunk_pieces(const s24_kv_cache *c, int64_t width, int64_t tokens
     // None is cut: the kernel that has a way for few rows, if most have few and more than two tiles of positions.  (16 sequences of 5 tokens after up to 500, 8 heads on 2 of 128 in 8 bits, 14 us
     // so and 20 in whole tiles; 55 of 2 tokens after none, 12 heads, 15 and 13.)
     if (steps < kCutSteps) return steps > 2 && rows <= kFewRows * sequences ? tiles : 0;
-    const int64_t of_head = 2 * (held / c->hkv), worth = tiles * (1 + steps / kLeastSteps);   // no more than have so many steps each
+    const int64_t of_head = 2 * (held / c->hkv), worth = tiles * (1 + steps / (steps >= kLong ? kLeastOfLong : kLeastSteps));   // no more than have so many steps each
     return of_head < worth ? of_head : worth;
 }
 template <typename T, int BITS> static void chunk(const ChunkArgs &a, dim3 grid, dim3 join, hipStream_t st)
