@@ -91,7 +91,7 @@ __global__ __launch_bounds__(256, 4) void rotary_bwd_kernel(const BackwardArgs a
         if (w != nullptr) {
             float y[16];
             P::widen(now_x, y);
-            const float r = part.factor(a.t, y);
+            const float r = head < heads ? part.factor(a.t, y) : 0.0f;   // (lanes without a row have zeros, of which the root has no value where eps is 0)
             float mean = 0.0f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
