@@ -426,7 +426,7 @@ int s24_attn_chunk(const s24_kv_cache *cache, const s24_heads *Q, int64_t hq, co
  * or (2p, 2p + 1) where `interleaved`.  A token has `axes` positions, of which pair p turns by number axis[p] (of an image or a video: time, height and width).
  * All arithmetic is fp32 and rounded once; a turn is reduced exactly, so that angles of far positions are as good as those of near ones.  mean(x^2) + eps has to be a
  * normal number of fp32; eps = 0 gives NaN for a head of zeros.  S24_BF16 and S24_F16; S24_F32 returns S24_ERR_UNSUPPORTED.
- *   frequencies  device fp64 [rotated / 2]
+ *   frequencies  device fp64 [rotated / 2]; pairs of one that is NaN or infinite become NaN
  *   axis         device int32 [rotated / 2] of 0 .. axes - 1 (others are cut to the last), or NULL: all turn by the first
  *   wq, wk       device [d] values of the calls' dtype, 16-byte aligned: weights of the queries' and of the keys' norm; NULL: not normalised
  *   rotated      a multiple of 16 up to d; 0: nothing is turned (frequencies and positions may be NULL)

@@ -67,6 +67,7 @@ template <typename T, int LANES, bool NEIGHBOURS> struct Part {
     float cosine[8], sine[8];
     // The pair that the lane finds the angle of: its frequency as a fraction of a turn, high + low / 2^32 in 2^-32, and where its axis has the positions
     uint32_t high, low;
+    bool none;         // it has no value: neither has the pair
     const int32_t *at;
     lds_angles *shared;
     __device__ __forceinline__ Part(const Turn &t, int lane, lds_angles *angles)
@@ -75,11 +76,12 @@ template <typename T, int LANES, bool NEIGHBOURS> struct Part {
         in = 16 * j < t.d, turned = 16 * j < t.rotated;
         const bool apart = turned && !NEIGHBOURS;
         a = apart ? 8 * j : 16 * j, b = apart ? (t.rotated >> 1) + 8 * j : 16 * j + 8;
-        high = low = 0, at = t.positions;
+        high = low = 0, none = false, at = t.positions;
         if (2 * lane >= t.rotated) return;
         if (t.axis != nullptr) at += (int64_t)min((uint32_t)t.axis[lane], (uint32_t)t.axes - 1) * t.tokens;
-        const double turns = t.frequencies[lane] * 0.15915494309189535, steps = (turns - rint(turns)) * 0x1p32, whole = fmin(floor(steps), 2147483647.0);
+        const double frequency = t.frequencies[lane], turns = frequency * 0.15915494309189535, steps = (turns - rint(turns)) * 0x1p32, whole = fmin(floor(steps), 2147483647.0);
         high = (uint32_t)(int32_t)whole, low = (uint32_t)fmin((steps - whole) * 0x1p32, 4294967295.0);
+        none = !(fabs(frequency) < (double)INFINITY);
     }
     // The angles of a token: each lane has one, and its row's eight come from the others'.  They are reduced without an error that grows with the position: of the
     // frequency's fraction of a turn in 64 bits times the position whole turns fall out of the word.
@@ -89,6 +91,7 @@ template <typename T, int LANES, bool NEIGHBOURS> struct Part {
         const uint32_t n = (uint32_t)position;
         float c, s;
         turn_of(n * high + __umulhi(n, low) - (position < 0 ? low : 0), c, s);
+        if (none) c = s = NAN;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         shared->cosine[lane] = c, shared->sine[lane] = back ? -s : s;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

@@ -1,8 +1,11 @@
 """Norms and rotations where a quantity of the formula has no finite value, on the GPU against 64 bits on the CPU (rotary_reference.py, which derives the bounds)."""
+import math
+
 import pytest
 import torch
 
-from test_gpu_rotary import Case
+from paper_2404_01847_amd.attention import Rotary
+from test_gpu_rotary import Case, empty_cache, frequencies
 
 pytestmark = pytest.mark.gpu
 BF16, F16 = torch.bfloat16, torch.float16
@@ -28,3 +31,39 @@ def test_a_head_of_zeros_without_eps_is_the_only_one_without_a_value(d):
     dQ, dK = c.layer.backward(c.dQ, c.dK, c.Q, c.K, c.positions, out=(torch.empty_like(c.dQ), torch.empty_like(c.dK)))
     assert bool(dQ[5, 3].isnan().all()) and dQ.isnan().any(2).nonzero().tolist() == [[5, 3]] and dK.isfinite().all()
     assert bool(c.layer.dwq.isnan().all()) and c.layer.dwk.isfinite().all()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+def test_frequencies_without_a_value_turn_their_pairs_into_nan(d, interleaved):
+    """NaN and infinities: their pairs have no value whatever the position, forward, backward and on the way into the cache; other pairs keep their bits."""
+    c = Case(40, 4, 2, d, BF16, norms=(False, False), interleaved=interleaved)
+    c.positions[0, :3] = torch.tensor([0, 1, -1], dtype=torch.int32)
+    outs = lambda: (torch.empty_like(c.dQ), torch.empty_like(c.dK))
+    want = [x.clone() for x in c.layer.forward(c.Q, c.K, c.positions)] + list(c.layer.backward(c.dQ, c.dK, None, None, c.positions, out=outs()))
+    pairs = torch.tensor([0, 5, d // 2 - 1])
+    f = frequencies(d).cuda()
+    f[pairs] = torch.tensor([math.nan, math.inf, -math.inf], dtype=torch.float64, device="cuda")
+    layer = Rotary(4, 2, d, 40, f, interleaved=interleaved)
+    got = [x.clone() for x in layer.forward(c.Q, c.K, c.positions)] + list(layer.backward(c.dQ, c.dK, None, None, c.positions, out=outs()))
+    lost = torch.zeros(d, dtype=torch.bool)
+    lost[torch.cat([2 * pairs, 2 * pairs + 1]) if interleaved else torch.cat([pairs, pairs + d // 2])] = True
+    for a, b in zip(got, want):
+        assert bool(a[..., lost].isnan().all()) and torch.equal(a[..., ~lost], b[..., ~lost])
+    cache = empty_cache(3, 16, 2, d, BF16, 8)
+    q = cache.append(layer, c.Q, c.K, c.V, c.positions, torch.arange(40, device="cuda"))
+    assert torch.equal(q.isnan(), got[0].isnan()) and bool(cache.k_step.transpose(1, 2).reshape(48, 2)[:40].isnan().all())
+
+
+def test_a_frequency_without_a_value_reaches_its_axis_of_every_token_and_the_norms_gradients():
+    c = Case(30, 4, 2, 64, F16, axes=2, axis=(torch.arange(32) % 2).to(torch.int32))
+    f = frequencies(64).cuda()
+    f[7] = math.nan
+    layer = Rotary(4, 2, 64, 30, f, *c.w, axis=c.axis.cuda(), axes=2, dtype=F16)
+    z, k = layer.forward(c.Q, c.K, c.positions)
+    for x in (z, k):
+        assert x.isnan().any((0, 1)).nonzero()[:, 0].tolist() == [7, 39] and bool(x[..., [7, 39]].isnan().all())
+    dQ, dK = layer.backward(c.dQ, c.dK, c.Q, c.K, c.positions, out=(torch.empty_like(c.dQ), torch.empty_like(c.dK)))
+    assert bool(dQ.isnan().all()) and bool(dK.isnan().all())       # the mean over a head has no value
+    for dw in (layer.dwq, layer.dwk):
+        assert dw.isnan().nonzero()[:, 0].tolist() == [7, 39]
