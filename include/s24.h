@@ -424,7 +424,8 @@ int s24_attn_chunk(const s24_kv_cache *cache, const s24_heads *Q, int64_t hq, co
  * A head x of d values becomes z:  y_i = x_i w_i / sqrt(mean(x^2) + eps), or y = x where it is not normalised;  the pair (y_a, y_b) number p is turned by the angle
  * position * frequencies[p] (in radians):  z_a = y_a cos - y_b sin,  z_b = y_b cos + y_a sin;  what lies past the first `rotated` values is not turned.  Pair p is (p, p + rotated / 2),
  * or (2p, 2p + 1) where `interleaved`.  A token has `axes` positions, of which pair p turns by number axis[p] (of an image or a video: time, height and width).
- * All arithmetic is fp32 and rounded once; a turn is reduced exactly, so that angles of far positions are as good as those of near ones.  mean(x^2) + eps has to be a
+ * All arithmetic is fp32 and rounded once; a frequency's fraction of a turn is held in 64 bits, of which the product with the position loses whole turns and nothing else: angles are
+ * within 2^-22 radians at every position, for frequencies up to 2^40 (beyond, the fraction itself loses places).  mean(x^2) + eps has to be a
  * normal number of fp32; eps = 0 gives NaN for a head of zeros.  S24_BF16 and S24_F16; S24_F32 returns S24_ERR_UNSUPPORTED.
  *   frequencies  device fp64 [rotated / 2]; pairs of one that is NaN or infinite become NaN
  *   axis         device int32 [rotated / 2] of 0 .. axes - 1 (others are cut to the last), or NULL: all turn by the first

@@ -32,6 +32,21 @@ __device__ __forceinline__ void turn_of(uint32_t phase, float &cosine, float &si
     sine = __uint_as_float(__float_as_uint(q) ^ (quarter & 2) << 30);
 }
 
+// Of x what is left of whole turns, as a word of 64 bits
+__device__ __forceinline__ uint64_t turn_word(double x)
+{
+    const double steps = (x - rint(x)) * 0x1p32, whole = fmin(floor(steps), 2147483647.0);
+    return ((uint64_t)(uint32_t)(int32_t)whole << 32) + (uint32_t)fmin((steps - whole) * 0x1p32, 4294967295.0);
+}
+// A frequency's fraction of a turn in 64 bits, for frequencies up to 2^40 within 3 of its last places: 1 / (2 pi) in two doubles, and what the product with the first
+// leaves.  (The product rounded to one double would be off by 2^-53 of the frequency, which the position multiplies: 100 radians a step are off by 2e-5 radians at position 2^31 so.)
+__device__ __forceinline__ uint64_t turn_fraction(double frequency)
+{
+#pragma clang fp contract(off)
+    const double turns = frequency * 0x1.45f306dc9c883p-3, left = fma(frequency, 0x1.45f306dc9c883p-3, -turns);
+    return turn_word(turns) + turn_word(fma(frequency, -9.839338337591243e-18, left));
+}
+
 // Sum over the lanes of a row
 template <int LANES> __device__ __forceinline__ float row_sum(float x)
 {
@@ -79,12 +94,13 @@ template <typename T, int LANES, bool NEIGHBOURS> struct Part {
         high = low = 0, none = false, at = t.positions;
         if (2 * lane >= t.rotated) return;
         if (t.axis != nullptr) at += (int64_t)min((uint32_t)t.axis[lane], (uint32_t)t.axes - 1) * t.tokens;
-        const double frequency = t.frequencies[lane], turns = frequency * 0.15915494309189535, steps = (turns - rint(turns)) * 0x1p32, whole = fmin(floor(steps), 2147483647.0);
-        high = (uint32_t)(int32_t)whole, low = (uint32_t)fmin((steps - whole) * 0x1p32, 4294967295.0);
+        const double frequency = t.frequencies[lane];
+        const uint64_t word = turn_fraction(frequency);
+        high = (uint32_t)(word >> 32), low = (uint32_t)word;
         none = !(fabs(frequency) < (double)INFINITY);
     }
-    // The angles of a token: each lane has one, and its row's eight come from the others'.  They are reduced without an error that grows with the position: of the
-    // frequency's fraction of a turn in 64 bits times the position whole turns fall out of the word.
+    // The angles of a token: each lane has one, and its row's eight come from the others'.  Of the frequency's fraction of a turn in 64
+    // bits times the position whole turns fall out of the word, and what the fraction is off by becomes 2^-31 of a turn at most.
     __device__ __forceinline__ void angles(const Turn &t, int32_t position, bool back, int lane)
     {
         if (t.rotated == 0) return;

@@ -1,5 +1,6 @@
 """Norms and rotations where a quantity of the formula has no finite value, on the GPU against 64 bits on the CPU (rotary_reference.py, which derives the bounds)."""
 import math
+from fractions import Fraction
 
 import pytest
 import torch
@@ -67,3 +68,31 @@ def test_a_frequency_without_a_value_reaches_its_axis_of_every_token_and_the_nor
     assert bool(dQ.isnan().all()) and bool(dK.isnan().all())       # the mean over a head has no value
     for dw in (layer.dwq, layer.dwk):
         assert dw.isnan().nonzero()[:, 0].tolist() == [7, 39]
+
+
+def exact_angles(positions, f):
+    """Angles within half a turn, from whole numbers and pi to 60 digits: [tokens][1][pairs]"""
+    pi = Fraction("3.14159265358979323846264338327950288419716939937510582097494")
+    out = torch.empty((positions.numel(), 1, f.numel()), dtype=torch.float64)
+    for j, x in enumerate(f.tolist()):
+        turns = Fraction(x) / (2 * pi)
+        for i, n in enumerate(positions.flatten().tolist()):
+            part = turns * n
+            out[i, 0, j] = float((part - round(part)) * 2 * pi)
+    return out
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("most", [1.0, 100.0, 1e5, 2.0 ** 40])
+def test_far_positions_turn_as_exactly_as_near_ones_at_any_frequency(most, interleaved):
+    """A fraction of a turn in 64 bits is off by less than 3 * 2^-64 for each step: 2^-28 radians at position 2^31, of the 2^-22 that the bound has for an angle."""
+    gen = torch.Generator().manual_seed(3)
+    far = [(1 << 31) - 1, -(1 << 31), (1 << 30) + 12345, 1 << 24, 100003, -77777, 1, 0]
+    at = torch.cat([torch.tensor(far), torch.randint(-(1 << 31), 1 << 31, (56,), generator=gen)]).to(torch.int32)[None]
+    f = most * torch.exp2(-12 * torch.rand(64, generator=gen, dtype=torch.float64)) * torch.where(torch.rand(64, generator=gen) < 0.5, -1.0, 1.0).double()
+    c = Case(64, 4, 2, 128, F16, norms=(False, False), interleaved=interleaved, views="whole")
+    c.positions.copy_(at)
+    c.layer = Rotary(4, 2, 128, 64, f.cuda(), interleaved=interleaved, dtype=F16)
+    c.at["angle"] = exact_angles(at, f)
+    c.what += f", frequencies up to {most}"
+    c.check()
