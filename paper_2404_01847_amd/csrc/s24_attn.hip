@@ -831,7 +831,7 @@ extern "C" int s24_attn_fwd(const s24_attn_shape *shape, const s24_heads *Q, con
     const int parts = forward_parts(shape);
     const int64_t groups = query_groups(shape, 128) * parts;
     const int64_t join = most_tiles(shape->tokens_q, shape->sequences, kJoinRows) * shape->hq;
-    S24_REQUIRE(groups <= kMostGroups && join <= kMostGroups, S24_ERR_SHAPE);
+    S24_REQUIRE(groups <= kMostGroups && (parts == 1 || join <= kMostGroups), S24_ERR_SHAPE);
     if (groups == 0) return S24_OK;
     Problem a = problem_of(shape);
     a.q = rows_of(Q), a.k = rows_of(K), a.v = rows_of(V), a.out = out_of(O), a.lse = lse;
@@ -848,19 +848,21 @@ template <typename T, int D, int E> static int backward(Problem a, bool joint, i
     const dim3 block(256);
     const int64_t hkv = a.hq / a.group, key_groups = most_tiles(a.tokens_k, a.sequences, 128) * hkv * a.by_key.parts;
     if (query_groups == 0 && key_groups == 0) return S24_OK;
-    if (joint && query_groups > 0) {
-        a.key_blocks = (unsigned)((key_groups + 7) / 8 * 8);   // dQ's workgroups meet the XCDs as they would in a launch of their own
-        const int64_t rows = (int64_t)a.tokens_q * a.hq, of_group = 2048 / D * kStatsRows;
-        attn_stats_kernel<T, D / 8><<<dim3((unsigned)((rows + of_group - 1) / of_group)), block, 0, st>>>(a);
+    const bool together = joint && query_groups > 0;
+    const int64_t rows = (int64_t)a.tokens_q * a.hq, of_group = 2048 / D * kStatsRows, stats = (rows + of_group - 1) / of_group, key_blocks = (key_groups + 7) / 8 * 8;
+    const int64_t dq_join = a.by_query.parts > 1 ? most_tiles(a.tokens_q, a.sequences, kJoinRows) * a.hq : 0, dkv_join = a.by_key.parts > 1 ? most_tiles(a.tokens_k, a.sequences, kJoinRows) * hkv : 0;
+    S24_REQUIRE((together ? key_blocks + query_groups <= kMostGroups && stats <= kMostGroups : query_groups <= kMostGroups && key_groups <= kMostGroups) && dq_join <= kMostGroups &&
+                dkv_join <= kMostGroups, S24_ERR_SHAPE);
+    if (together) {
+        a.key_blocks = (unsigned)key_blocks;   // dQ's workgroups meet the XCDs as they would in a launch of their own
+        attn_stats_kernel<T, D / 8><<<dim3((unsigned)stats), block, 0, st>>>(a);
         attn_bwd_kernel<T, D, E><<<dim3(a.key_blocks + (unsigned)query_groups), block, 0, st>>>(a);
     } else {
         if (query_groups > 0) attn_dq_kernel<T, D, E><<<dim3((unsigned)query_groups), block, 0, st>>>(a);
         if (key_groups > 0) attn_dkv_kernel<T, D, E><<<dim3((unsigned)key_groups), block, 0, st>>>(a);
     }
-    if (query_groups > 0 && a.by_query.parts > 1)
-        attn_dq_join_kernel<T><<<dim3((unsigned)(most_tiles(a.tokens_q, a.sequences, kJoinRows) * a.hq)), block, 0, st>>>(a);
-    if (key_groups > 0 && a.by_key.parts > 1)
-        attn_dkv_join_kernel<T><<<dim3((unsigned)(most_tiles(a.tokens_k, a.sequences, kJoinRows) * hkv)), block, 0, st>>>(a);
+    if (query_groups > 0 && dq_join > 0) attn_dq_join_kernel<T><<<dim3((unsigned)dq_join), block, 0, st>>>(a);
+    if (key_groups > 0 && dkv_join > 0) attn_dkv_join_kernel<T><<<dim3((unsigned)dkv_join), block, 0, st>>>(a);
     return s24_launch_status();
 }
 template <typename T> static int backward(const Problem &a, bool joint, int64_t query_groups, hipStream_t st)
@@ -888,9 +890,8 @@ extern "C" int s24_attn_bwd(const s24_attn_shape *shape, const s24_heads *Q, con
     S24_REQUIRE((lse != nullptr && workspace != nullptr) || shape->tokens_q == 0, S24_ERR_NULL);
     S24_REQUIRE(s24_aligned(lse, 4) && s24_aligned(workspace, 16), S24_ERR_ALIGN);
     S24_REQUIRE(workspace_bytes >= s24_attn_bwd_workspace(shape), S24_ERR_SHAPE);
-    // (a join has the most workgroups of all launches: parts are taken of few tiles only)
-    S24_REQUIRE(most_tiles(shape->tokens_q, shape->sequences, kJoinRows) * shape->hq <= kMostGroups / 2 &&
-                most_tiles(shape->tokens_k, shape->sequences, kJoinRows) * shape->hkv <= kMostGroups / 2, S24_ERR_SHAPE);
+    S24_REQUIRE(most_tiles(shape->tokens_q, shape->sequences, kJoinRows) * shape->hq <= INT32_MAX / 2 &&
+                most_tiles(shape->tokens_k, shape->sequences, kJoinRows) * shape->hkv <= INT32_MAX / 2, S24_ERR_SHAPE);   // (tiles are numbered in an int)
     Problem a = problem_of(shape);
     a.q = rows_of(Q), a.k = rows_of(K), a.v = rows_of(V), a.o = rows_of(O), a.dO = rows_of(dO);
     a.dq = out_of(dQ), a.dk = out_of(dK), a.dv = out_of(dV);

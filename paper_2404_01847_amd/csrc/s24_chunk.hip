@@ -780,6 +780,8 @@ static int64_t chunk_pieces(const s24_kv_cache *c, int64_t width, int64_t tokens
     const int64_t of_head = 2 * (held / c->hkv), worth = tiles * (1 + steps / (steps >= kLong ? kLeastOfLong : kLeastSteps));   // no more than have so many steps each
     return of_head < worth ? of_head : worth;
 }
+// Whether a second launch adds parts (a cache without pages has none, whatever its table's width)
+static bool joins(int64_t page, int64_t width, int64_t pieces) { return pieces > 0 && width * page > (kCutSteps - 1) * kChunkKeys; }
 template <typename T, int BITS> static void chunk(const ChunkArgs &a, dim3 grid, dim3 join, hipStream_t st)
 {
     const dim3 block(256);
@@ -799,7 +801,7 @@ template <typename T, int BITS> static void chunk(const ChunkArgs &a, dim3 grid,
     case 112: chunk_kernel<T, 128, 128, BITS, 112><<<grid, block, 0, st>>>(a); break;
     default: chunk_kernel<T, 128, 128, BITS, 128><<<grid, block, 0, st>>>(a); break;
     }
-    if ((a.width << a.c.shift) > (kCutSteps - 1) * kChunkKeys) chunk_join_kernel<T><<<join, block, 0, st>>>(a);
+    if (joins(a.c.page, a.width, a.pieces)) chunk_join_kernel<T><<<join, block, 0, st>>>(a);
 }
 }  // namespace s24_kv
 
@@ -834,7 +836,7 @@ extern "C" int s24_attn_chunk(const s24_kv_cache *cache, const s24_heads *Q, int
     int sum_rows = 1;
     while (sum_rows < 64 && tokens * hq > 1024 * sum_rows) sum_rows *= 2;
     const int64_t join = most_tiles(tokens * group, tokens < sequences ? tokens : sequences, sum_rows) * cache->hkv;
-    S24_REQUIRE(groups <= kMostGroups && join <= kMostGroups, S24_ERR_SHAPE);
+    S24_REQUIRE(groups <= kMostGroups && (!joins(cache->page, cache->pages > 0 ? width : 0, pieces) || join <= kMostGroups), S24_ERR_SHAPE);
     ChunkArgs a{cache_of(cache), {static_cast<uint16_t *>(Q->data), Q->token, Q->head}, {static_cast<uint16_t *>(O->data), O->token, O->head}, cu, table, lengths,
                 cache->pages > 0 ? width : 0, (int)sequences, (int)tokens, (int)hq, (int)group, causal != 0, (int)pieces, (int)(pieces < round ? pieces : round), sum_rows, scale};
     a.weights = static_cast<float2 *>(workspace);

@@ -864,7 +864,7 @@ extern "C" int s24_kv_write(const s24_kv_cache *cache, const s24_heads *K, const
     const int64_t waves = 2 * ((tokens + 15) / 16) * write_units(cache);   // of K and of V
     const bool runs = by_runs(cache, tokens);
     const int64_t groups = runs ? (waves + 3) / 4 : (tokens * cache->hkv + 3) / 4;
-    S24_REQUIRE((runs ? waves + 3 : groups) <= kMostGroups, S24_ERR_SHAPE);   // (the runs' kernel numbers its waves in an int)
+    S24_REQUIRE(groups <= kMostGroups, S24_ERR_SHAPE);   // (so waves are numbered in an int)
     const dim3 grid((unsigned)groups);
     if (cache->bits == 16) write<uint16_t, 16>(a, runs, grid, st);   // a copy, whatever the type
     else if (dt == S24_BF16) write<uint16_t, 8>(a, runs, grid, st);
@@ -905,7 +905,7 @@ extern "C" int s24_kv_append(const s24_kv_cache *cache, const s24_rotary *rotary
     const int64_t waves = a.runs ? ((tokens + 15) / 16) * write_units(cache) : tokens * cache->hkv;
     a.shares = s24_rotary_rows::shares_of_token(tokens, hq, cache->hkv, cache->d);
     const int64_t values = cache->pages > 0 ? (waves + 3) / 4 : 0, groups = values + (tokens * a.shares + 3) / 4;
-    S24_REQUIRE(waves + 3 <= kMostGroups && groups <= kMostGroups, S24_ERR_SHAPE);   // (the waves that write V are numbered in an int)
+    S24_REQUIRE(groups <= kMostGroups, S24_ERR_SHAPE);   // (so the waves that write V are numbered in an int)
     a.value_blocks = (int)values;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const dim3 grid((unsigned)groups);
@@ -943,6 +943,14 @@ extern "C" int64_t s24_attn_decode_workspace(const s24_kv_cache *cache, int64_t 
 }
 
 namespace s24_kv {
+// A wave adds the parts of a row where there are few of them.  (Four and one: 64 sequences of 512 positions, 64 heads on 8 of 128 in 8 bits, 27.6 and 23.9 us;
+// one of 4096 10.6 and 14.7.)
+static bool one_wave_joins(const DecodeArgs &a) { return a.shares <= 8 * (int64_t)a.sequences; }
+static int64_t join_groups(const DecodeArgs &a)
+{
+    const int64_t rows = (int64_t)a.sequences * a.hq;
+    return one_wave_joins(a) ? (rows + 3) / 4 : rows;
+}
 template <typename T, int BITS> static void decode(const DecodeArgs &a, dim3 grid, hipStream_t st)
 {
     const dim3 block(256);
@@ -957,11 +965,9 @@ template <typename T, int BITS> static void decode(const DecodeArgs &a, dim3 gri
     default: attn_decode_kernel<T, 128, BITS><<<grid, block, 0, st>>>(a); break;
     }
     if (a.whole) return;
-    // A wave adds the parts of a row where there are few of them.  (Four and one: 64 sequences of 512 positions, 64 heads on 8 of 128 in 8 bits, 27.6 and 23.9 us;
-    // one of 4096 10.6 and 14.7.)
-    const int64_t rows = (int64_t)a.sequences * a.hq;
-    if (a.shares <= 8 * (int64_t)a.sequences) attn_join_kernel<T, 1><<<dim3((unsigned)((rows + 3) / 4)), block, 0, st>>>(a);
-    else attn_join_kernel<T, 4><<<dim3((unsigned)rows), block, 0, st>>>(a);
+    const dim3 join((unsigned)join_groups(a));
+    if (one_wave_joins(a)) attn_join_kernel<T, 1><<<join, block, 0, st>>>(a);
+    else attn_join_kernel<T, 4><<<join, block, 0, st>>>(a);
 }
 }  // namespace s24_kv
 
@@ -989,8 +995,9 @@ extern "C" int s24_attn_decode(const s24_kv_cache *cache, const s24_heads *Q, in
     a.whole = a.width * cache->page <= (sequences >= fit ? 512 : 128);
     const int64_t shares = a.whole ? sequences : most < fit ? (most > 0 ? most : 1) : fit;
     const int64_t groups = (shares * heads + 3) / 4;
-    S24_REQUIRE(sequences * hq <= kMostGroups / 2, S24_ERR_SHAPE);
+    S24_REQUIRE(sequences * hq <= INT32_MAX / 2 && groups <= kMostGroups, S24_ERR_SHAPE);
     a.shares = (int)shares, a.scale = scale, a.part = static_cast<float *>(workspace);
+    S24_REQUIRE(a.whole || join_groups(a) <= kMostGroups, S24_ERR_SHAPE);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const dim3 grid((unsigned)groups);
     if (dt == S24_BF16) cache->bits == 16 ? decode<uint16_t, 16>(a, grid, st) : decode<uint16_t, 8>(a, grid, st);
