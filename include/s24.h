@@ -13,8 +13,8 @@
  *
  * Limits: every size is below 2^31, and the feature extents of the GEMM entry points (q, r, 2f) below 2^23: the
  * kernels address one tile's operand rows with 32-bit byte offsets from a per-tile base (S24_ERR_SHAPE beyond).
- * A launch holds less than 2^32 work items: calls of attention, rotation and the cache that would take more return S24_ERR_SHAPE (a wave of 64 to a token, as the rotation of one head
- * of 16 has it: 2^26 tokens).
+ * A launch holds less than 2^32 work items: calls that would take more, and are not cut into several, return S24_ERR_SHAPE (elementwise 2^35 values; the rotation of one head of 16,
+ * a wave to a token, 2^26 tokens).
  *
  * Errors: every entry point returns an s24_status.  Arguments are validated on
  * the host before anything is launched, so a failing call has no effect on

@@ -345,8 +345,8 @@ inline int check_rows(const s24_heads *v, int64_t tokens, int64_t heads, int64_t
 }
 // Workgroups for tiles of `rows` of packed sequences: no more tiles than this, however the tokens are shared out.
 inline int64_t most_tiles(int64_t tokens, int64_t sequences, int rows) { return tokens / rows + (tokens < sequences ? tokens : sequences); }
-// Workgroups of 256 that a launch takes: fewer than 2^32 work items (of more it silently runs the remainder)
-constexpr int64_t kMostGroups = 0xFFFFFF;
+// Workgroups of 256 that a launch takes
+constexpr int64_t kMostGroups = kMostItems / 256;
 
 // How the work of a launch is cut up.  A workgroup's steps follow each other, and when causal the last queries (the first keys) take twice the average: few
 // workgroups, or some with many steps, leave most of the device idle.  So what a tile sums over is cut into parts, whose sums go through memory in fp32

@@ -15,6 +15,8 @@ static inline bool s24_aligned(const void *p, size_t a) { return (reinterpret_ca
 static inline bool s24_valid_dtype(int dt) { return dt == S24_F32 || dt == S24_BF16 || dt == S24_F16; }
 static inline bool s24_valid_gate(int g) { return g == S24_GATE_SILU || g == S24_GATE_GELU_ERF; }
 static inline bool s24_valid_layout(int l) { return l == S24_ROW_MAJOR || l == S24_COL_MAJOR; }
+// Work items of a launch: fewer than 2^32.  (Of more the runtime silently runs the remainder.)
+constexpr int64_t kMostItems = 0xFFFFFFFF;
 static inline size_t s24_elem_size(int dt) { return dt == S24_F32 ? 4 : 2; }
 
 // Compute units of the current device, read once (256 on MI355X; that figure also stands in where no device

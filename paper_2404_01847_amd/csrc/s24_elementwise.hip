@@ -338,7 +338,7 @@ __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const T *__restrict__
 }
 
 inline unsigned blocks_for(int64_t n) { return (unsigned)((n + kThreads - 1) / kThreads); }
-constexpr int64_t kMaxThreads = (int64_t)0x7FFFFFFF * kThreads;
+constexpr int64_t kMaxThreads = kMostItems / kThreads * kThreads;   // of whole workgroups
 
 }  // namespace
 
@@ -381,6 +381,7 @@ int launch_glu_fwd(const void *G, const void *U, void *H, int64_t rows, int64_t 
                    hipStream_t st)
 {
     const int64_t n8 = rows * cols / 8;
+    S24_REQUIRE(n8 <= kMaxThreads, S24_ERR_SHAPE);
     const dim3 grid(blocks_for(n8)), block(kThreads);
     auto *g = static_cast<const T *>(G), *u = static_cast<const T *>(U);
     auto *h = static_cast<T *>(H);
@@ -395,6 +396,7 @@ int launch_glu_bwd(const void *dH, const void *G, const void *U, void *dG, void 
                    int64_t ld_z, int gate, hipStream_t st)
 {
     const int64_t n8 = rows * cols / 8;
+    S24_REQUIRE(n8 <= kMaxThreads, S24_ERR_SHAPE);
     const dim3 grid(blocks_for(n8)), block(kThreads);
     auto *d = static_cast<const T *>(dH), *g = static_cast<const T *>(G), *u = static_cast<const T *>(U);
     auto *dg = static_cast<T *>(dG), *du = static_cast<T *>(dU);
@@ -410,7 +412,7 @@ int launch_glu_fwd_t(const void *G, const void *U, void *H, int64_t rows, int64_
                      hipStream_t st)
 {
     const dim3 grid((unsigned)((cols + kTT - 1) / kTT), (unsigned)((rows + kTT - 1) / kTT)), block(kThreads);
-    S24_REQUIRE(grid.y <= 65535, S24_ERR_SHAPE);   // 4 M rows of the source: beyond any token count of one GPU
+    S24_REQUIRE(grid.y <= 65535 && (int64_t)grid.x * kThreads <= kMostItems, S24_ERR_SHAPE);   // 4 M rows of the source: beyond any token count of one GPU
     auto *g = static_cast<const T *>(G), *u = static_cast<const T *>(U);
     auto *h = static_cast<T *>(H);
     if (gate == S24_GATE_SILU)
@@ -424,7 +426,7 @@ int launch_glu_bwd_t(const void *dH, const void *G, const void *U, void *dG, voi
                      int64_t ld_z, int gate, hipStream_t st)
 {
     const dim3 grid((unsigned)((cols + kTT - 1) / kTT), (unsigned)((rows + kTT - 1) / kTT)), block(kThreads);
-    S24_REQUIRE(grid.y <= 65535, S24_ERR_SHAPE);   // 4 M rows of the source: beyond any token count of one GPU
+    S24_REQUIRE(grid.y <= 65535 && (int64_t)grid.x * kThreads <= kMostItems, S24_ERR_SHAPE);   // 4 M rows of the source: beyond any token count of one GPU
     auto *d = static_cast<const T *>(dH), *g = static_cast<const T *>(G), *u = static_cast<const T *>(U);
     auto *dg = static_cast<T *>(dG), *du = static_cast<T *>(dU);
     if (gate == S24_GATE_SILU)
@@ -440,7 +442,7 @@ int check_glu(int64_t p, int64_t f, int dt, int gate)
 {
     S24_REQUIRE(s24_valid_dtype(dt) && s24_valid_gate(gate), S24_ERR_DTYPE);
     S24_REQUIRE(p >= 0 && f >= 0 && f % 8 == 0, S24_ERR_SHAPE);
-    S24_REQUIRE(p * f / 8 <= kMaxThreads && f / 8 < (1ll << 31) && p < (1ll << 31), S24_ERR_SHAPE);
+    S24_REQUIRE(p < (1ll << 31) && f < (1ll << 31), S24_ERR_SHAPE);
     return S24_OK;
 }
 bool ld_ok(int layout, int64_t ld, int64_t p, int64_t n) { return ld % 8 == 0 && ld >= (layout == S24_COL_MAJOR ? p : n); }
@@ -532,6 +534,7 @@ extern "C" int s24_bias_grad(const void *dZ, s24_layout layout, int64_t ld, int6
     if (n == 0) return S24_OK;
     S24_REQUIRE(db != nullptr && (p == 0 || dZ != nullptr), S24_ERR_NULL);
     S24_REQUIRE(s24_aligned(dZ, 16) && s24_aligned(db, 4), S24_ERR_ALIGN);
+    S24_REQUIRE(layout == S24_ROW_MAJOR ? (n + 63) / 64 * kBiasThreads <= kMostItems : (n + 3) / 4 * kThreads <= kMostItems, S24_ERR_SHAPE);
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (layout == S24_ROW_MAJOR)
         S24_WITH_TYPE(dt, hipLaunchKernelGGL(bias_grad_rows_kernel<T>, dim3((unsigned)((n + 63) / 64)), dim3(kBiasThreads), 0, st,

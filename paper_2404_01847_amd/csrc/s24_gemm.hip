@@ -1538,6 +1538,14 @@ __global__ __launch_bounds__(kThreads) void fill_zero_kernel(float *__restrict__
     const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (i < n) p[i] = 0.0f;
 }
+void fill_zero(float *p, int64_t n, hipStream_t st)
+{
+    constexpr int64_t LAUNCH = 1ll << 31;
+    for (int64_t begin = 0; begin < n; begin += LAUNCH) {
+        const int64_t count = std::min(n - begin, LAUNCH);
+        hipLaunchKernelGGL(fill_zero_kernel, dim3((unsigned)((count + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, p + begin, count);
+    }
+}
 
 inline unsigned ceil_div(int64_t a, int64_t b) { return (unsigned)((a + b - 1) / b); }
 
@@ -2039,7 +2047,7 @@ int run_dense_dw(const void *dY, const void *X, float *dW, int64_t p, int64_t q,
     const bool accum = beta != 0.0f;
     bool decay_pending = W != nullptr;
     if (p == 0) {  // empty contraction: dW = beta * dW (the GEMM kernels need at least one token)
-        if (!accum) hipLaunchKernelGGL(fill_zero_kernel, dim3(ceil_div(q * r, kThreads)), dim3(kThreads), 0, st, dW, q * r);
+        if (!accum) fill_zero(dW, q * r, st);
     } else if (dt != S24_F32) {
         auto *a = static_cast<const uint16_t *>(dY), *b = static_cast<const uint16_t *>(X);
         const bool fuse = decay_pending && wdt == dt;   // the epilogue reads W in the operands' own 16-bit type
@@ -2409,7 +2417,7 @@ extern "C" int s24_spmm_dw(const void *vals, const uint16_t *meta, const void *X
     const bool accum = beta != 0.0f;
     bool decay_pending = W != nullptr;
     if (p == 0) {
-        if (!accum) hipLaunchKernelGGL(fill_zero_kernel, dim3(ceil_div(q * r, kThreads)), dim3(kThreads), 0, st, dW, q * r);
+        if (!accum) fill_zero(dW, q * r, st);
     } else {
         S24_REQUIRE(meta != nullptr, S24_ERR_NULL);
         S24_REQUIRE(s24_aligned(meta, 4), S24_ERR_ALIGN);

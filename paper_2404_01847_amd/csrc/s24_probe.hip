@@ -108,7 +108,7 @@ extern "C" int s24_probe_copy(const void *src, void *dst, int64_t bytes, void *s
     S24_REQUIRE(s24_aligned(src, 16) && s24_aligned(dst, 16), S24_ERR_ALIGN);
     const int64_t n16 = bytes / 16;
     const int64_t grid = (n16 + 255) / 256;
-    S24_REQUIRE(grid < (1ll << 31), S24_ERR_SHAPE);
+    S24_REQUIRE(grid * 256 <= kMostItems, S24_ERR_SHAPE);
     hipLaunchKernelGGL(copy_kernel, dim3((unsigned)grid), dim3(256), 0, static_cast<hipStream_t>(stream),
                        static_cast<const u32x4 *>(src), static_cast<u32x4 *>(dst), n16);
     return s24_launch_status();

@@ -57,3 +57,14 @@ def test_attention_of_more_rows_than_a_launch_could_join():
         ref, bound = packed(Q[rows], K[rows], V[rows], [0, n], [0, n], d ** -0.5, True, dO[rows])
         for name, x in zip(("O", "dQ", "dK", "dV"), (O, *grads)):
             assert_within(x[rows], ref[name], bound[name], f"{name} of sequence {i}")
+
+
+def test_a_weight_gradient_of_no_tokens_with_more_values_than_a_launch_has_work_items():
+    """Cleared, all of it."""
+    import paper_2404_01847_amd as s24
+    q, r = 65536 + 64, 65536
+    dW = torch.full((r, q), math.nan, device="cuda")
+    assert dW.numel() > 1 << 32
+    some = torch.empty(1024, dtype=BF16, device="cuda").data_ptr()       # (an empty tensor has no address)
+    assert s24.lib().s24_dense_dw(some, some, dW.data_ptr(), 0, q, r, 0.0, s24.BF16, None) == 0
+    assert not bool(dW.any())

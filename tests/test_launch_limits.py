@@ -43,3 +43,22 @@ def test_packed_sequences(lib):
 def test_chunks(lib):
     big = rows(64, token=1024, head=16)
     assert lib.s24_attn_chunk(cache(hkv=64, d=16), big, 64, P, P, 4, P, 1, 1 << 25, 0.125, 1, big, P, 1 << 50, BF16, None) == SHAPE
+
+
+def test_elementwise(lib):
+    """Eight values to a work item; of bias gradients 64 features (4 of contiguous tokens) to a workgroup."""
+    BF = BF16
+    p, f = 1 << 15, 1 << 20                                               # p f / 8 = 2^32
+    assert lib.s24_masked_decay_grad(P, P, BF, P, 1e-4, p, f, None) == SHAPE
+    assert lib.s24_act_fwd(P, P, p * f, 0, BF, None) == SHAPE
+    assert lib.s24_act_bwd(P, P, P, p * f, 0, BF, None) == SHAPE
+    assert lib.s24_swiglu_fwd(P, P, P, p, f, 2 * f, BF, None) == SHAPE
+    assert lib.s24_swiglu_bwd(P, P, P, P, P, p, f, 2 * f, BF, None) == SHAPE
+    for layout in (0, 1):                                                 # both row-major, both column-major
+        ld_z, ld_h = (2 * f, f) if layout == 0 else (p, p)
+        assert lib.s24_glu_fwd(P, layout, ld_z, P, layout, ld_h, p, f, 0, BF, None) == SHAPE
+        assert lib.s24_glu_bwd(P, layout, ld_h, P, layout, ld_z, P, p, f, 0, BF, None) == SHAPE
+    n = 1 << 28
+    assert lib.s24_bias_grad(P, 0, n, 8, n, P, 0.0, BF, None) == SHAPE
+    assert lib.s24_bias_grad(P, 1, 8, 8, n // 4, P, 0.0, BF, None) == SHAPE
+    assert lib.s24_probe_copy(P, P, 1 << 36, None) == SHAPE
