@@ -1705,6 +1705,7 @@ int launch_spmm(const void *B, const void *Av, const uint16_t *Am, void *Out, in
     }
     const int tiles_m = (int)ceil_div(M, tile.bm()), tiles_n = (int)ceil_div(N, tile.bn());
     const dim3 grid(((tiles_m * tiles_n + 7) / 8) * 8), block(tile.threads());
+    S24_REQUIRE((int64_t)grid.x * block.x <= kMostItems, S24_ERR_SHAPE);
 #define S24_LAUNCH_NT(ACC, BIASED, MI, WN)                                                                                             \
     hipLaunchKernelGGL((big::spmm_nt_big_kernel<T, ACC, false, false, S24_GATE_SILU, BIASED, 0, S24_ACT_RELU, MI, WN>), grid, block, 0, \
                        st, b, av, Am, o, (int)N, (int)K, (int)M, tiles_m, tiles_n, tile.kind == NtTile::Large ? g_clock_probe : nullptr, \
@@ -1775,6 +1776,7 @@ extern "C" int s24_spmm_fwd_glu(const void *X, const void *vals, const uint16_t 
     if (dt != S24_F32 && tile.kind != NtTile::Small) {   // 128 gate and 128 up features per tile
         const int tiles_m = (int)ceil_div(f, 128), tiles_n = (int)ceil_div(p, tile.bn());
         const dim3 grid(((tiles_m * tiles_n + 7) / 8) * 8), block(tile.threads());
+        S24_REQUIRE((int64_t)grid.x * block.x <= kMostItems, S24_ERR_SHAPE);
         auto *x = static_cast<const uint16_t *>(X), *av = static_cast<const uint16_t *>(vals), *d = static_cast<const uint16_t *>(bias);
         auto *gu = static_cast<uint16_t *>(GU), *h = static_cast<uint16_t *>(H);
 #define S24_LAUNCH_FWD_GLU(G, WN)                                                                                                    \
@@ -1818,6 +1820,7 @@ extern "C" int s24_spmm_bwd_dx_glu(const void *dY, const void *valsT, const uint
     // only the large-tile 16-bit kernel carries this epilogue; other shapes take s24_spmm_bwd_dx + s24_glu_bwd
     S24_REQUIRE(dt != S24_F32 && gated_bwd_fits(p, f), S24_ERR_UNSUPPORTED);
     const dim3 grid(((tiles_m * tiles_n + 7) / 8) * 8), block(big::THREADS);
+    S24_REQUIRE((int64_t)grid.x * block.x <= kMostItems, S24_ERR_SHAPE);
     hipStream_t st = static_cast<hipStream_t>(stream);
     auto *dy = static_cast<const uint16_t *>(dY), *av = static_cast<const uint16_t *>(valsT), *gu = static_cast<const uint16_t *>(GU);
     auto *o = static_cast<uint16_t *>(dGU);
@@ -1856,6 +1859,7 @@ extern "C" int s24_spmm_fwd_act(const void *X, const void *vals, const uint16_t 
         const int tiles_m = (int)ceil_div(r, tile.bm()), tiles_n = (int)ceil_div(p, tile.bn());
         S24_REQUIRE((int64_t)tiles_m * tiles_n < (1ll << 30), S24_ERR_SHAPE);
         const dim3 grid(((tiles_m * tiles_n + 7) / 8) * 8), block(tile.threads());
+        S24_REQUIRE((int64_t)grid.x * block.x <= kMostItems, S24_ERR_SHAPE);
         auto *x = static_cast<const uint16_t *>(X), *av = static_cast<const uint16_t *>(vals), *d = static_cast<const uint16_t *>(bias);
         auto *z = static_cast<uint16_t *>(Z), *h = static_cast<uint16_t *>(H);
 #define S24_LAUNCH_FWD_ACT(A, BIASED, MI, WN)                                                                                           \
@@ -1893,6 +1897,7 @@ extern "C" int s24_spmm_bwd_dx_act(const void *dY, const void *valsT, const uint
     const int tiles_m = (int)ceil_div(f, tile.bm()), tiles_n = (int)ceil_div(p, tile.bn());
     S24_REQUIRE((int64_t)tiles_m * tiles_n < (1ll << 30), S24_ERR_SHAPE);
     const dim3 grid(((tiles_m * tiles_n + 7) / 8) * 8), block(tile.threads());
+    S24_REQUIRE((int64_t)grid.x * block.x <= kMostItems, S24_ERR_SHAPE);
     hipStream_t st = static_cast<hipStream_t>(stream);
     auto *dy = static_cast<const uint16_t *>(dY), *av = static_cast<const uint16_t *>(valsT), *z = static_cast<const uint16_t *>(Z);
     auto *o = static_cast<uint16_t *>(dZ);
@@ -1925,6 +1930,7 @@ extern "C" int s24_dense_gemm(const void *X, const void *W, void *Y, int64_t p, 
     const NtTile tile = dense_tile(r, p);
     const int tiles_m = (int)ceil_div(r, tile.bm()), tiles_n = (int)ceil_div(p, tile.bn());
     const dim3 grid(((tiles_m * tiles_n + 7) / 8) * 8), block(tile.threads());
+    S24_REQUIRE((int64_t)grid.x * block.x <= kMostItems, S24_ERR_SHAPE);
 #define S24_LAUNCH_DENSE(MI, WN)                                                                                              \
     hipLaunchKernelGGL((bignt::dense_nt_big_kernel<T, MI, WN>), grid, block, 0, st, x, w, y, (int)p, (int)q, (int)r, tiles_m, \
                        tiles_n, tile.kind == NtTile::Large ? g_clock_probe : nullptr)
@@ -2426,6 +2432,7 @@ extern "C" int s24_spmm_dw(const void *vals, const uint16_t *meta, const void *X
             S24_REQUIRE((int64_t)ceil_div(r, 128) * ceil_div(q, 128) < (1ll << 30), S24_ERR_SHAPE);
             const int tiles_m = (int)ceil_div(r, tile.bm()), tiles_n = (int)ceil_div(q, tile.bn());
             const dim3 grid(((tiles_m * tiles_n + 7) / 8) * 8), block(tile.threads());
+            S24_REQUIRE((int64_t)grid.x * block.x <= kMostItems, S24_ERR_SHAPE);
             auto *av = static_cast<const uint16_t *>(vals), *x = static_cast<const uint16_t *>(X);
             const bool fuse = decay_pending && wdt == dt;
             auto *w = static_cast<const uint16_t *>(fuse ? W : nullptr);

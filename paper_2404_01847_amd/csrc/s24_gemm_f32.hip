@@ -405,7 +405,7 @@ int launch_nt(const S24F32Nt &g, hipStream_t st)
 {
     const int64_t F = EPI == S24_F32_GLU ? g.M / 2 : g.M;
     const int64_t tiles_m = ceil_div(F, EPI == S24_F32_GLU ? 32 : 32 * T), tiles = tiles_m * ceil_div(g.N, 32 * T);
-    S24_REQUIRE(tiles < (1ll << 31), S24_ERR_SHAPE);
+    S24_REQUIRE(tiles * 64 * KS <= kMostItems, S24_ERR_SHAPE);
     hipLaunchKernelGGL((f32_nt_kernel<SPARSE, ACCUM, EPI, ACT, T, KS>), dim3((unsigned)tiles), dim3(64 * KS), 0, st, s24_pack(g.B, g.Av), s24_pack(g.Am, (int)g.N, (int)g.K),
                        s24_pack((int)g.M, (int)F, (int)tiles_m, 0), (NtEnds{g.Out, g.H, g.bias}));
     return s24_launch_status();
@@ -433,6 +433,7 @@ template <bool SPARSE, bool ACCUM, int EPI, int ACT> int choose_nt(const S24F32N
 
 template <bool SPARSE, int T, int KS, int D = 1> int launch_tn(TnArgs &a, int64_t tiles, bool accum, hipStream_t st)
 {
+    S24_REQUIRE(tiles * 64 * KS <= kMostItems, S24_ERR_SHAPE);
     const dim3 grid((unsigned)tiles), block(64 * KS);
     if (accum) hipLaunchKernelGGL((f32_tn_kernel<SPARSE, true, T, KS, D>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((f32_tn_kernel<SPARSE, false, T, KS, D>), grid, block, 0, st, a);

@@ -62,3 +62,12 @@ def test_elementwise(lib):
     assert lib.s24_bias_grad(P, 0, n, 8, n, P, 0.0, BF, None) == SHAPE
     assert lib.s24_bias_grad(P, 1, 8, 8, n // 4, P, 0.0, BF, None) == SHAPE
     assert lib.s24_probe_copy(P, P, 1 << 36, None) == SHAPE
+
+
+def test_products(lib):
+    """Of so many tokens that the tiles of 64 (16 bits: 128) of them are 2^24 workgroups of 256."""
+    p = (1 << 31) - 64
+    for dt in (1, 2, 0):
+        assert lib.s24_dense_gemm(P, P, P, p, 64, 64, dt, None) == SHAPE
+        assert lib.s24_spmm_fwd(P, P, P, P, p, 64, 64, dt, None) == SHAPE
+        assert lib.s24_spmm_bwd_dx(P, P, P, P, p, 64, 64, 0.0, dt, None) == SHAPE
