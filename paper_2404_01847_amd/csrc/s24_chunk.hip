@@ -17,7 +17,7 @@ struct ChunkArgs {
     Strided q, o;
     const int *cu, *table, *lengths;
     int64_t width;
-    int sequences, tokens, hq, group, causal;
+    int sequences, tokens, group, causal;
     int pieces, round; // that the tiles of a key-value head are cut into at most, 0: none is cut; as many of them as the device holds workgroups
     int sum_rows;      // that a workgroup adds the parts of
     float scale;
@@ -30,8 +30,8 @@ __device__ __forceinline__ int row_tiles(const ChunkArgs &a, int i) { return (in
 __device__ __forceinline__ int key_tiles(const ChunkArgs &a, int i) { return (keys_of(a, i).count + kChunkKeys - 1) / kChunkKeys; }
 // Where tiles of rows are few, the positions that they go over are cut into parts, those of a sequence of one size, which leave their sums for another kernel to add; a tile in one part
 // is finished where it is.  A part has about `each` steps (tiles of positions): as few as make no more pieces than the device holds workgroups, two to a compute unit.  (12
-// sequences of 2 to 512 tokens after up to 4000, 32 heads on 8 of 128, 43 tiles of 35 to 62 steps: uncut 142 us, so 117.  Steps dealt out evenly, whatever tiles they belong to,
-// 157: a piece costs 5 to 10 us besides its steps.)  Where the tiles do not go evenly into them, so that the last piece would end more than a quarter later than an even share of all
+// sequences of 2 to 512 tokens after up to 4000, 32 heads on 8 of 128, 43 tiles of 35 to 62 steps: uncut 142 us, so 112 to 115.  Steps dealt out evenly, whatever tiles they belong
+// to, 157: a piece costs 5 to 10 us besides its steps.)  Where the tiles do not go evenly into them, so that the last piece would end more than a quarter later than an even share of all
 // steps, and eight steps, they are cut into twice as many pieces, of which a compute unit takes the next when it is done with one (the same batch after up to 12000: 310 us in one
 // round, 242 in two; with 32 heads on 2, after 8000, 184 and 153; where the pieces come out even, 512 tokens after 16000, 140 and 158).
 constexpr int kFewRows = 32;      // of a sequence
@@ -62,17 +62,17 @@ __device__ __forceinline__ Parts parts_in(int keys, int each)
     return {count, (keys + count - 1) / count};
 }
 // The sequences as the cutting sees them.  Up to 64 of them are looked at once, a lane each.
-struct List { int tiles, keys, few; };   // of rows, of positions
-struct Lists {
+struct Extent { int tiles, keys, few; };   // of rows, of positions
+struct Cutting {
     const ChunkArgs &a;
     int lane;
-    List mine;
-    __device__ __forceinline__ Lists(const ChunkArgs &args, int of_lane) : a(args), lane(of_lane) { mine = lane < a.sequences ? look(lane) : List{0, 0, 0}; }
-    __device__ __forceinline__ List look(int i) const { return {row_tiles(a, i), key_tiles(a, i), is_few(a, i)}; }
+    Extent mine;
+    __device__ __forceinline__ Cutting(const ChunkArgs &args, int of_lane) : a(args), lane(of_lane) { mine = lane < a.sequences ? look(lane) : Extent{0, 0, 0}; }
+    __device__ __forceinline__ Extent look(int i) const { return {row_tiles(a, i), key_tiles(a, i), is_few(a, i)}; }
     // That of sequence i, by the lane that has it in turn
-    __device__ __forceinline__ List in_turn(int i) const { return a.sequences <= 64 ? mine : look(i); }
+    __device__ __forceinline__ Extent in_turn(int i) const { return a.sequences <= 64 ? mine : look(i); }
     // That of a sequence which is the same for all lanes
-    __device__ __forceinline__ List of(int i) const
+    __device__ __forceinline__ Extent of(int i) const
     {
         if (a.sequences > 64) return look(i);
         return {__builtin_amdgcn_readlane(mine.tiles, i), __builtin_amdgcn_readlane(mine.keys, i), __builtin_amdgcn_readlane(mine.few, i)};
@@ -97,7 +97,7 @@ struct Lists {
         int64_t steps = 0;
         int longest = 0, tiles = 0;
         for (int i = lane; i < a.sequences; i += 64) {
-            const List x = in_turn(i);
+            const Extent x = in_turn(i);
             steps += (int64_t)x.tiles * x.keys, tiles += x.tiles, longest = x.tiles > 0 ? max(longest, x.keys) : longest;
         }
         longest = max(lanes_max(longest), 1);
@@ -118,7 +118,7 @@ struct Lists {
     {
         int before = 0;
         for (int i = lane; i < sequence; i += 64) {
-            const List x = in_turn(i);
+            const Extent x = in_turn(i);
             const int count = parts_in(x.keys, each).count;
             before += count > 1 ? x.tiles * count : 0;
         }
@@ -131,24 +131,24 @@ struct Piece { int sequence, tile, begin, end, slot; };
 // run at the same time read the same positions.
 __device__ __forceinline__ bool find_part(const ChunkArgs &a, int t, int lane, Piece &piece)
 {
-    const Lists lists(a, lane);
-    const int each = lists.each(), most = (int)((a.width << a.c.shift) / kChunkKeys) + 2;
+    const Cutting cutting(a, lane);
+    const int each = cutting.each(), most = (int)((a.width << a.c.shift) / kChunkKeys) + 2;
     int wide = 0, sequence, at;
     for (int i = lane; i < a.sequences; i += 64) {
-        const List x = lists.in_turn(i);
+        const Extent x = cutting.in_turn(i);
         wide += x.few ? 0 : x.tiles * parts_in(x.keys, each).count;
     }
     wide = lanes_sum(wide);
     const bool few = t >= wide;
     auto of = [&](int i) {
-        const List x = lists.in_turn(i);
+        const Extent x = cutting.in_turn(i);
         const Parts p = parts_in(x.keys, each);
         return x.few == few ? Lengths{x.tiles * p.count, INT32_MAX, max(p.steps, 1)} : Lengths{0, 0, 0};
     };
     if (!find_by_length(true, a.sequences, few ? t - wide : t, most, lane, sequence, at, of)) return false;
-    const List x = lists.of(sequence);
+    const Extent x = cutting.of(sequence);
     const Parts p = parts_in(x.keys, each);
-    const int part = at / max(x.tiles, 1), slot = p.count == 1 ? -1 : lists.slots_before(each, sequence) + at;
+    const int part = at / max(x.tiles, 1), slot = p.count == 1 ? -1 : cutting.slots_before(each, sequence) + at;
     piece = {sequence, x.tiles - 1 - (at - part * x.tiles), part * p.steps, min(x.keys, (part + 1) * p.steps), slot};
     return at >= 0 && part < p.count && slot < a.pieces;   // (as they are, where the offsets ascend)
 }
@@ -466,7 +466,7 @@ __device__ __forceinline__ void few_rows(const ChunkArgs &a, const Queries &s_, 
                 }
                 if (BITS == 8) s[i][j] *= sv[i];
             }
-            p[j] = operand<M>(s[0][j], s[1][j]);
+            p[j] = operand<M>(s[0][j], s[1][j]);   // rounded to the operands' 16 bits, as the packed forward pass has it: 2^-8 (2^-11) of a weight
         }
 #pragma unroll
         for (int n = 0; n < d / 16; ++n) {
@@ -711,10 +711,10 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(const ChunkArgs a)
     const int block = blockIdx.x / a.c.hkv, kv = blockIdx.x - block * a.c.hkv, lane = threadIdx.x & 63;
     int sequence, index, unused;
     if (!find_item(a.sequences, block, lane, sequence, index, unused, [&](int i) { return (int)(((int64_t)span(a.cu, i, a.tokens).count * a.group + a.sum_rows - 1) / a.sum_rows); })) return;
-    const Lists lists(a, lane);
-    const int each = lists.each(), n = lists.of(sequence).tiles, parts = parts_in(lists.of(sequence).keys, each).count;
+    const Cutting cutting(a, lane);
+    const int each = cutting.each(), n = cutting.of(sequence).tiles, parts = parts_in(cutting.of(sequence).keys, each).count;
     if (parts == 1) return;
-    const int before = lists.slots_before(each, sequence);
+    const int before = cutting.slots_before(each, sequence);
     if (before + n * parts > a.pieces) return;
     const Span s = span(a.cu, sequence, a.tokens);
     const int row0 = index * a.sum_rows, rows = min(a.sum_rows, s.count * a.group - row0), tile = row0 / kChunkRows, d = a.c.d;
@@ -765,7 +765,10 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(const ChunkArgs a)
 }
 
 // ------------------------------------------------------------------ host
-// Tiles of rows of a key-value head at most, and pieces that they are cut into; 0: none is, where there are so many that the device is full to the end anyway, or the sequences are short
+// Tiles of rows of a key-value head at most, and pieces that they are cut into; 0: none is, where the sequences are short, or the rows make four whole tiles for each compute unit.  Those keep the device
+// full to the end if the sequences are of like length; one that is much longer than the others then goes on alone, a workgroup for each of its tiles.  (64 heads on 8 of 128: a prompt of 1800 tokens
+// beside one token after 128000 takes 313 us, of 2048 4100, the two by themselves 91 and 93; after 30000 135 and 792.  700 sequences of 6 tokens after 1000, 32 heads on 8, lose nothing: 0.77 us for
+// each in whole tiles, 0.86 of 682 by the way for few rows.)
 static int64_t chunk_tiles(const s24_kv_cache *c, int64_t tokens, int64_t sequences, int64_t hq)
 {
     return tokens * (hq / c->hkv) / kChunkRows + (tokens < sequences ? tokens : sequences);
@@ -838,7 +841,7 @@ extern "C" int s24_attn_chunk(const s24_kv_cache *cache, const s24_heads *Q, int
     const int64_t join = most_tiles(tokens * group, tokens < sequences ? tokens : sequences, sum_rows) * cache->hkv;
     S24_REQUIRE(groups <= kMostGroups && (!joins(cache->page, cache->pages > 0 ? width : 0, pieces) || join <= kMostGroups), S24_ERR_SHAPE);
     ChunkArgs a{cache_of(cache), {static_cast<uint16_t *>(Q->data), Q->token, Q->head}, {static_cast<uint16_t *>(O->data), O->token, O->head}, cu, table, lengths,
-                cache->pages > 0 ? width : 0, (int)sequences, (int)tokens, (int)hq, (int)group, causal != 0, (int)pieces, (int)(pieces < round ? pieces : round), sum_rows, scale};
+                cache->pages > 0 ? width : 0, (int)sequences, (int)tokens, (int)group, causal != 0, (int)pieces, (int)(pieces < round ? pieces : round), sum_rows, scale};
     a.weights = static_cast<float2 *>(workspace);
     a.sums = reinterpret_cast<float *>(static_cast<char *>(workspace) + pieces * cache->hkv * kChunkRows * sizeof(float2));
     const hipStream_t st = static_cast<hipStream_t>(stream);
